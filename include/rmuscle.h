@@ -296,6 +296,98 @@ rm_status rm_context_ffn_packed(const rm_ffn_shape *s, const void *packed, int32
                                 const int32_t *rows, const int32_t *count, int32_t max_rows, float *y, void *ws,
                                 size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Attention side of the layers (the method keeps attention dense, section 4.1; these are the calls between two FFN
+ * layers of the action expert and of the VLM).  Forward only.
+ * ---------------------------------------------------------------------------------------------------------- */
+
+/* Where the head vectors of a tensor lie: element c of head h of token t of sample b is element
+ * b * batch + t * token + h * head + c of data (dtype: the call's).  The elements of a head are consecutive; data and
+ * every stride in bytes are multiples of 16 (the stride of an axis of size 1 is not used), strides are not negative
+ * and the token stride of keys and values is below 16 MiB.  Inputs may overlap each other and may have stride 0 (one
+ * head or sample seen by all); an output's elements must be distinct and its extent must not overlap an input's. */
+typedef struct rm_heads {
+    void *data;
+    int64_t batch, token, head;
+} rm_heads;
+
+/* n_q_heads: a multiple of n_kv_heads; query head h uses key head h / (n_q_heads / n_kv_heads).
+ * head_dim: a multiple of 8, at most 256.  dtype: an rm_dtype, of queries, keys, values and output.
+ * scale: finite; scores are scale * <q, k>.  softcap: >= 0; not 0: scores become softcap * tanh(score / softcap).
+ * Scores, maxima, sums and the output are accumulated in float32; with RM_BF16 the softmax's weights are rounded to
+ * bf16 before their product with the values (as the values are), their sum is not. */
+typedef struct rm_attn_shape {
+    int32_t n_q_heads, n_kv_heads, head_dim, dtype;
+    float scale, softcap;
+} rm_attn_shape;
+
+/* Queries and keys of every head normalized and rotated by their position, keys and values written to rows of a
+ * cache, in one pass.  For token n, head vector x in R^D (D = head_dim):
+ *     u = gain ? x / sqrt(mean(x^2) + eps) * gain : x             (gain_q for queries, gain_k for keys, float32 [D])
+ *     (u_i, u_j) -> (u_i cos a - u_j sin a, u_j cos a + u_i sin a),  a = pos[n] * inv_freq[i],  i < rot / 2
+ * with j = i + rot / 2, or with pairs != 0 the elements 2 i and 2 i + 1; elements from rot on are not rotated.
+ *     q_out[n] = u of q[n];  k_out[slot[n]] = u of k[n];  v_out[slot[n]] = v[n]
+ *   in_dtype, out_dtype: of q, k, v and of the outputs.  q, k, v, q_out, k_out, v_out: their batch stride is not used;
+ *             q and q_out hold n_tok tokens, k and v too, k_out and v_out `rows` rows.  v.data NULL: no values.
+ *   pos:      int32 [n_tok], any value.  inv_freq: float32 [rot / 2] (may be NULL with rot = 0).
+ *   slot:     int32 [n_tok] row of each token in k_out and v_out; a slot outside [0, rows) drops the token's key and
+ *             value; NULL: row n (rows >= n_tok).  Slots are distinct: tokens that share one leave an unspecified
+ *             mix of theirs in it.  Other rows keep what they hold.
+ * head_dim a multiple of 8, at most 256; rot a multiple of 4 in [0, head_dim].  Angles are reduced in 64 bits,
+ * everything else is float32.  n_tok >= 0.  Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN. */
+rm_status rm_qk_norm_rope(int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t in_dtype,
+                          int32_t out_dtype, const rm_heads *q, const rm_heads *k, const rm_heads *v,
+                          const rm_heads *q_out, const rm_heads *k_out, const rm_heads *v_out, int32_t rows,
+                          const int32_t *pos, const int32_t *slot, const float *inv_freq, int32_t rot, int32_t pairs,
+                          const float *gain_q, const float *gain_k, float eps, void *stream);
+
+/* The masks that rm_span_attention takes: one interval [lo, hi) of keys per query row.  Row i of sample b is at
+ * position p = q_start[b] + i (q_start NULL: 0) of N keys, of which kv_len[b] (NULL: N; clamped to [0, N]) are in use:
+ *     hi = kv_len[b], with causal: min(kv_len[b], max(p + 1, prefix_len[b]))   (prefix_len NULL: 0; causal only)
+ *     lo = 0, with window > 0: max(0, p - window + 1)
+ *     with doc: both cut to the run of equal ids doc[b][.] that holds p; a row of a negative id sees nothing.
+ * With causal or doc a row at a position outside [0, kv_len[b]) sees nothing.  A row that sees nothing gets (0, 0).
+ *   q_start, kv_len, prefix_len: int32 [B] or NULL.  doc: int32 [B][N] or NULL.  span: int32 [B][T][2], out.
+ * B, T, N >= 1, N < 2^30, window >= 0. */
+rm_status rm_attn_spans(int32_t B, int32_t T, int32_t N, int32_t causal, int32_t window, const int32_t *q_start,
+                        const int32_t *kv_len, const int32_t *prefix_len, const int32_t *doc, int32_t *span,
+                        void *stream);
+
+/* Attention of query rows over one interval of their sample's keys each:
+ *     s_j = cap(scale * <q[b,i,h], k[b,j,h']>) - slopes[h] * |q_start[b] + i - j|,   lo[b,i] <= j < hi[b,i]
+ *     out[b,i,h] = sum_j softmax(s)_j v[b,j,h']            (no key, or no score above -infinity: 0)
+ * Keys outside a row's interval do not affect it, whatever they hold (NaN and infinities too).
+ *   q, out: [B][T][n_q_heads][head_dim]; k, v: [B][N][n_kv_heads][head_dim]; T >= 1, 0 <= N < 2^30.
+ *   span:    int32 [B][T][2], 8-byte aligned, clamped to [0, N] (rm_attn_spans makes it), or NULL: every row sees all.
+ *   slopes:  float32 [n_q_heads] or NULL: no bias.  q_start: int32 [B] or NULL (0); read with slopes only.
+ *   ws, ws_bytes: at least rm_span_attention_workspace_size bytes (which may be 0: ws may then be NULL), 256-byte
+ *            aligned; scratch as for rm_workspace_size.
+ * A single token's step is the same call with T = 1. */
+rm_status rm_span_attention_workspace_size(const rm_attn_shape *s, int32_t B, int32_t T, int32_t N, size_t *bytes);
+rm_status rm_span_attention(const rm_attn_shape *s, int32_t B, int32_t T, int32_t N, const rm_heads *q,
+                            const rm_heads *k, const rm_heads *v, const rm_heads *out, const int32_t *span,
+                            const float *slopes, const int32_t *q_start, void *ws, size_t ws_bytes, void *stream);
+
+/* Attention of a batch whose samples share a long prefix: samples g * per_group .. of group g attend to the group's
+ * prefix keys, which are read once for all of them, and to their own.  The action expert's samples of one
+ * observation are such a batch, and so are single tokens behind a shared prompt (T = 1).  For sample b of group
+ * g = b / per_group, row t sees
+ *     prefix keys j < prefix_len[g]  (NULL: P; clamped to [0, P])  and
+ *     own keys j < own_len[b]        (NULL: S; clamped to [0, S]), with causal only j <= own_len[b] - T + t
+ * (the rows are the last T of the sample's own positions), scores capped as the shape says, one softmax over both;
+ * a row that sees no key gives 0.  Keys that a row does not see do not affect it.
+ *   q, out: [n_groups * per_group][T][n_q_heads][head_dim]; k_prefix, v_prefix: [n_groups][P][n_kv_heads][head_dim];
+ *   k_own, v_own: [n_groups * per_group][S][n_kv_heads][head_dim]; P, S >= 0 and below 2^30 (their keys and values are
+ *   not read when 0 and may be NULL).
+ * Workspace as for rm_span_attention. */
+rm_status rm_prefix_attention_workspace_size(const rm_attn_shape *s, int32_t n_groups, int32_t per_group, int32_t T,
+                                             int32_t P, int32_t S, size_t *bytes);
+rm_status rm_prefix_attention(const rm_attn_shape *s, int32_t n_groups, int32_t per_group, int32_t T, int32_t P,
+                              int32_t S, const rm_heads *q, const rm_heads *k_prefix, const rm_heads *v_prefix,
+                              const int32_t *prefix_len, const rm_heads *k_own, const rm_heads *v_own,
+                              const int32_t *own_len, int32_t causal, const rm_heads *out, void *ws, size_t ws_bytes,
+                              void *stream);
+
 /* Down-projection row norms ||W_down[n]||_2 of one layer (the weight factor of Eq. 1, section 3.4), float32.
  *   w_down: [d_ff][d] in wdtype (the layout of rm_ffn_layer_weights.w_down), 16-byte aligned; d a multiple of 32.
  *   norms:  float32 [d_ff] out.

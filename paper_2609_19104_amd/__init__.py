@@ -10,6 +10,8 @@ Layouts (see include/rmuscle.h for the full contract):
   x, y  float32 [B][T][d];  weights [d_ff][d] float32 or bfloat16, row n = neuron n (w_down neuron-major)
   idx   int32 [B][d_ff] per layer ([L][B][d_ff] for a stack), count int32 [B] ([L][B])
   Eq. 4 anchor state: y_anchor float32 [L][B][T][d], h_anchor float32 [L][B][max_count][T]
+  attention: q, out [B][T][n_q_heads][D], k, v [B][N][n_kv_heads][D], float32 or bfloat16, any strides whose last
+  is 1; span int32 [B][T][2]
 """
 from __future__ import annotations
 
@@ -50,6 +52,8 @@ EXPORTED = ("rm_mask_compact", "rm_workspace_size", "rm_sparse_ffn_layer", "rm_s
             "rm_delta_ffn_stack", "rm_gather_stack_rows", "rm_context_select", "rm_context_workspace_size",
             "rm_context_ffn", "rm_context_pack_size", "rm_context_pack", "rm_context_ffn_packed", "rm_neuron_norms",
             "rm_group_masks",
+            "rm_qk_norm_rope", "rm_attn_spans", "rm_span_attention_workspace_size", "rm_span_attention",
+            "rm_prefix_attention_workspace_size", "rm_prefix_attention",
             "rm_profile_kernel_events", "rm_layer_kernels", "rm_stream_read",
             "rm_status_string", "rm_last_error")
 
@@ -74,6 +78,16 @@ class LayerWeights(ctypes.Structure):
                 ("norm_g", ctypes.c_void_p), ("out_gate", ctypes.c_void_p)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64),
+                ("head", ctypes.c_int64)]
+
+
+class AttnShape(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("softcap", ctypes.c_float)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -92,6 +106,7 @@ def load_library() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIB_PATH)
     i32, vp, sz = ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t
     sp, wp = ctypes.POINTER(FfnShape), ctypes.POINTER(LayerWeights)
+    hp, ap, f32 = ctypes.POINTER(Heads), ctypes.POINTER(AttnShape), ctypes.c_float
     sigs = {
         "rm_mask_compact": [vp, i32, i32, vp, vp, vp],
         "rm_workspace_size": [sp, i32, i32, i32, ctypes.POINTER(sz)],
@@ -112,6 +127,13 @@ def load_library() -> ctypes.CDLL:
         "rm_context_ffn_packed": [sp, vp, i32, vp, vp, vp, i32, vp, vp, sz, vp],
         "rm_neuron_norms": [vp, i32, i32, i32, vp, vp],
         "rm_group_masks": [vp, i32, i32, i32, i32, vp, i32, vp, vp, vp],
+        "rm_qk_norm_rope": [i32, i32, i32, i32, i32, i32, hp, hp, hp, hp, hp, hp, i32, vp, vp, vp, i32, i32, vp, vp,
+                            f32, vp],
+        "rm_attn_spans": [i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp],
+        "rm_span_attention_workspace_size": [ap, i32, i32, i32, ctypes.POINTER(sz)],
+        "rm_span_attention": [ap, i32, i32, i32, hp, hp, hp, hp, vp, vp, vp, vp, sz, vp],
+        "rm_prefix_attention_workspace_size": [ap, i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
+        "rm_prefix_attention": [ap, i32, i32, i32, i32, i32, hp, hp, hp, vp, hp, hp, vp, i32, hp, vp, sz, vp],
         "rm_profile_kernel_events": [i32, vp, vp],
         "rm_layer_kernels": [sp, i32, i32, i32, ctypes.POINTER(ctypes.c_uint32)],
         "rm_stream_read": [vp, sz, i32, vp, vp],
@@ -543,6 +565,180 @@ def rm_group_masks(h: torch.Tensor, norms: torch.Tensor, k: int, scores: torch.T
         raise ValueError("norms must be [L][d_ff], scores [S][L][d_ff] and mask [L][d_ff]")
     _check(load_library().rm_group_masks(h.data_ptr(), S, L, d_ff, T, norms.data_ptr(), int(k), scores.data_ptr(),
                                          mask.data_ptr(), _stream(stream)))
+
+
+_ATTN_DTYPES = {torch.float32: RM_F32, torch.bfloat16: RM_BF16}
+
+
+def _heads(name: str, t: torch.Tensor, dtype, device, ndim: int) -> Heads:
+    """Strides and pointer of a tensor of head vectors ([B][T][H][D], or [T][H][D] without a batch axis)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == ndim and t.device == device):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if t.device != device or not t.is_cuda:
+            raise ValueError(f"{name} must be on a HIP device, the same as the other tensors, got {t.device}")
+        if t.dtype != dtype:
+            raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+        raise ValueError(f"{name} must have {ndim} dims, got {tuple(t.shape)}")
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] != 1:
+        raise ValueError(f"{name}: the elements of a head must be consecutive")
+    return Heads(t.data_ptr(), st[0] if ndim == 4 else 0, st[-3], st[-2])
+
+
+def _int32(name: str, t: Optional[torch.Tensor], device, shape) -> Optional[int]:
+    if t is None:
+        return None
+    _need_cuda(name, t, (torch.int32,))
+    if tuple(t.shape) != shape or t.device != device:
+        raise ValueError(f"{name} must be int32 {list(shape)} on {device}, got {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _float32(name: str, t: Optional[torch.Tensor], device, n: int) -> Optional[int]:
+    if t is None:
+        return None
+    _need_cuda(name, t, (torch.float32,), 1)
+    if t.shape[0] != n or t.device != device:
+        raise ValueError(f"{name} must be float32 [{n}] on {device}, got {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _attn_device(t: torch.Tensor, stream):
+    """The tensors' device; without a stream given it has to be the current one, whose stream the call runs on."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("tensors must be on a HIP device")
+    if stream is None and t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors are on {t.device}, which is not the current device: select it or give a stream of it")
+    return t.device
+
+
+def _attn_shape(q: torch.Tensor, n_kv_heads: int, scale: Optional[float], softcap: float) -> AttnShape:
+    if q.dtype not in _ATTN_DTYPES:
+        raise ValueError(f"queries must be float32 or bfloat16, got {q.dtype}")
+    D = q.shape[-1]
+    return AttnShape(q.shape[-2], n_kv_heads, D, _ATTN_DTYPES[q.dtype],
+                     D ** -0.5 if scale is None and D > 0 else scale, softcap)
+
+
+def _attn_ws(ws: Optional[torch.Tensor], device) -> Tuple[Optional[int], int]:
+    if ws is None:
+        return None, 0
+    _need_cuda("ws", ws, (torch.uint8,))
+    if ws.device != device:
+        raise ValueError(f"ws must be on {device}, got {ws.device}")
+    return ws.data_ptr(), ws.numel()
+
+
+def rm_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], q_out: torch.Tensor,
+                    k_out: torch.Tensor, v_out: Optional[torch.Tensor], pos: torch.Tensor,
+                    inv_freq: Optional[torch.Tensor], gain_q: Optional[torch.Tensor] = None,
+                    gain_k: Optional[torch.Tensor] = None, slot: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    pairs: bool = False, stream=None) -> None:
+    """q [N][Hq][D], k and v [N][Hk][D] (views of one projection's rows will do): queries normalized and rotated into
+    q_out [N][Hq][D], keys into rows slot[n] (None: n) of k_out [rows][Hk][D], values copied into those of v_out."""
+    dev = _attn_device(q, stream)
+    if q.dtype not in _ATTN_DTYPES or not isinstance(q_out, torch.Tensor) or q_out.dtype not in _ATTN_DTYPES:
+        raise ValueError("queries and outputs must be float32 or bfloat16")
+    hq, hk = _heads("q", q, q.dtype, dev, 3), _heads("k", k, q.dtype, dev, 3)
+    hqo, hko = _heads("q_out", q_out, q_out.dtype, dev, 3), _heads("k_out", k_out, q_out.dtype, dev, 3)
+    N, Hq, D = q.shape
+    Hk, rows = k.shape[1], k_out.shape[0]
+    if k.shape != (N, Hk, D) or q_out.shape != q.shape or k_out.shape != (rows, Hk, D):
+        raise ValueError("q and q_out must be [N][Hq][D], k [N][Hk][D] and k_out [rows][Hk][D]")
+    if (v is None) != (v_out is None):
+        raise ValueError("v and v_out go together")
+    hv, hvo = Heads(), Heads()
+    if v is not None:
+        hv, hvo = _heads("v", v, q.dtype, dev, 3), _heads("v_out", v_out, q_out.dtype, dev, 3)
+        if v.shape != k.shape or v_out.shape != k_out.shape:
+            raise ValueError("v must have k's shape and v_out k_out's")
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    _check(load_library().rm_qk_norm_rope(
+        N, Hq, Hk, D, _ATTN_DTYPES[q.dtype], _ATTN_DTYPES[q_out.dtype], hq, hk, hv, hqo, hko, hvo, rows,
+        _int32("pos", pos, dev, (N,)), _int32("slot", slot, dev, (N,)),
+        _float32("inv_freq", inv_freq, dev, rot // 2), rot, int(pairs), _float32("gain_q", gain_q, dev, D),
+        _float32("gain_k", gain_k, dev, D), eps, _stream(stream)))
+
+
+def rm_attn_spans(span: torch.Tensor, N: int, causal: bool = True, window: int = 0,
+                  q_start: Optional[torch.Tensor] = None, kv_len: Optional[torch.Tensor] = None,
+                  prefix_len: Optional[torch.Tensor] = None, doc: Optional[torch.Tensor] = None, stream=None) -> None:
+    """span int32 [B][T][2]: the interval of the N keys that each query row sees (see the header for the rules);
+    q_start, kv_len, prefix_len int32 [B], doc int32 [B][N]."""
+    dev = _attn_device(span, stream)
+    _need_cuda("span", span, (torch.int32,), 3)
+    B, T, two = span.shape
+    if two != 2:
+        raise ValueError("span must be [B][T][2]")
+    _check(load_library().rm_attn_spans(B, T, int(N), int(causal), int(window), _int32("q_start", q_start, dev, (B,)),
+                                        _int32("kv_len", kv_len, dev, (B,)),
+                                        _int32("prefix_len", prefix_len, dev, (B,)), _int32("doc", doc, dev, (B, N)),
+                                        span.data_ptr(), _stream(stream)))
+
+
+def span_attention_workspace(q: torch.Tensor, k: torch.Tensor) -> torch.Tensor:
+    """A workspace tensor (uint8) of the size rm_span_attention_workspace_size asks for (it may be 0)."""
+    out = ctypes.c_size_t(0)
+    _check(load_library().rm_span_attention_workspace_size(_attn_shape(q, k.shape[2], None, 0.0), q.shape[0],
+                                                           q.shape[1], k.shape[1], ctypes.byref(out)))
+    return torch.empty(int(out.value), dtype=torch.uint8, device=q.device)
+
+
+def rm_span_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                      ws: Optional[torch.Tensor], span: Optional[torch.Tensor] = None,
+                      slopes: Optional[torch.Tensor] = None, q_start: Optional[torch.Tensor] = None,
+                      scale: Optional[float] = None, softcap: float = 0.0, stream=None) -> None:
+    """out = softmax(cap(scale q k^T) - slopes |q_start + i - j|) v over each row's interval of keys (span None: all);
+    scale None: 1 / sqrt(D)."""
+    dev = _attn_device(q, stream)
+    hq, hk = _heads("q", q, q.dtype, dev, 4), _heads("k", k, q.dtype, dev, 4)
+    hv, ho = _heads("v", v, q.dtype, dev, 4), _heads("out", out, q.dtype, dev, 4)
+    B, T, Hq, D = q.shape
+    N, Hk = k.shape[1], k.shape[2]
+    if k.shape != (B, N, Hk, D) or v.shape != k.shape or out.shape != q.shape:
+        raise ValueError("q and out must be [B][T][Hq][D], k and v [B][N][Hk][D]")
+    wp, wn = _attn_ws(ws, dev)
+    _check(load_library().rm_span_attention(
+        _attn_shape(q, Hk, scale, softcap), B, T, N, hq, hk, hv, ho, _int32("span", span, dev, (B, T, 2)),
+        _float32("slopes", slopes, dev, Hq), _int32("q_start", q_start, dev, (B,)), wp, wn, _stream(stream)))
+
+
+def prefix_attention_workspace(q: torch.Tensor, k_prefix: torch.Tensor, k_own: torch.Tensor) -> torch.Tensor:
+    """A workspace tensor (uint8) of the size rm_prefix_attention_workspace_size asks for (it may be 0)."""
+    out = ctypes.c_size_t(0)
+    groups = k_prefix.shape[0]
+    if groups <= 0 or q.shape[0] % groups != 0:
+        raise ValueError("the samples must divide into the prefixes' groups")
+    _check(load_library().rm_prefix_attention_workspace_size(_attn_shape(q, k_own.shape[2], None, 0.0), groups,
+                                                             q.shape[0] // groups, q.shape[1], k_prefix.shape[1],
+                                                             k_own.shape[1], ctypes.byref(out)))
+    return torch.empty(int(out.value), dtype=torch.uint8, device=q.device)
+
+
+def rm_prefix_attention(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tensor, k_own: torch.Tensor,
+                        v_own: torch.Tensor, out: torch.Tensor, ws: Optional[torch.Tensor],
+                        prefix_len: Optional[torch.Tensor] = None, own_len: Optional[torch.Tensor] = None,
+                        causal: bool = False, scale: Optional[float] = None, softcap: float = 0.0, stream=None) -> None:
+    """Samples q [groups * per_group][T][Hq][D] over their group's prefix keys k_prefix [groups][P][Hk][D] and their own
+    k_own [groups * per_group][S][Hk][D], one softmax over both; scale None: 1 / sqrt(D)."""
+    dev = _attn_device(q, stream)
+    hq, ho = _heads("q", q, q.dtype, dev, 4), _heads("out", out, q.dtype, dev, 4)
+    hkp, hvp = _heads("k_prefix", k_prefix, q.dtype, dev, 4), _heads("v_prefix", v_prefix, q.dtype, dev, 4)
+    hko, hvo = _heads("k_own", k_own, q.dtype, dev, 4), _heads("v_own", v_own, q.dtype, dev, 4)
+    B, T, Hq, D = q.shape
+    groups, P, Hk, _ = k_prefix.shape
+    S = k_own.shape[1]
+    if groups <= 0 or B % groups != 0:
+        raise ValueError("the samples must divide into the prefixes' groups")
+    if (k_prefix.shape != (groups, P, Hk, D) or v_prefix.shape != k_prefix.shape or k_own.shape != (B, S, Hk, D)
+            or v_own.shape != k_own.shape or out.shape != q.shape):
+        raise ValueError("q and out must be [B][T][Hq][D], the prefix [groups][P][Hk][D] and the own keys [B][S][Hk][D]")
+    wp, wn = _attn_ws(ws, dev)
+    _check(load_library().rm_prefix_attention(
+        _attn_shape(q, Hk, scale, softcap), groups, B // groups, T, P, S, hq, hkp, hvp,
+        _int32("prefix_len", prefix_len, dev, (groups,)), hko, hvo, _int32("own_len", own_len, dev, (B,)),
+        int(causal), ho, wp, wn, _stream(stream)))
 
 
 def rm_profile_kernel_events(kernel: int, ev_begin: Optional[int], ev_end: Optional[int]) -> None:

@@ -305,6 +305,16 @@ bool device_has_256_cus() {
 
 namespace rm {
 
+rm_status api_fail(rm_status st, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
+    va_end(ap);
+    return st;
+}
+
+rm_status api_ok() { return ok(); }
+
 rm_status make_plan(const rm_ffn_shape *s, int B, int T, int max_count, Plan *p, unsigned form) {
     Plan q;
     q.d = s->d;

@@ -1,0 +1,48 @@
+// Launch plan and kernel arguments of the attention calls, shared by the host code and the kernels.
+#pragma once
+
+#include <type_traits>
+
+#include "rm_internal.h"
+
+namespace rm_attn {
+
+// One source of keys and values (strides in bytes).
+struct Src {
+    const char *k = nullptr, *v = nullptr;
+    int64_t k_b = 0, k_n = 0, k_h = 0, v_b = 0, v_n = 0, v_h = 0;
+};
+
+struct Args {
+    const char *q = nullptr;
+    int64_t q_b = 0, q_t = 0, q_h = 0;  // bytes
+    char *o = nullptr;
+    int64_t o_b = 0, o_t = 0, o_h = 0;
+    Src s0;                         // keys shared by a group's samples ([U] groups), seen by every row
+    Src s1;                         // each sample's own keys
+    const int32_t *len0 = nullptr;  // [U] or null: n0
+    const int32_t *len1 = nullptr;  // [U per] or null: n1
+    int n0 = 0, n1 = 0;
+    const int32_t *span = nullptr;  // [U][T][2] own keys that a row sees (per = 1), or null
+    const float *slopes = nullptr;  // [Hq] or null
+    const int32_t *q_start = nullptr;
+    int D = 0, Hk = 0, G = 0, T = 0, per = 0, U = 0, causal = 0;
+    int R = 0;                      // rows of a group and key head: per T G
+    int n_tiles = 0, splits = 1;    // row blocks, and workgroups that divide one's keys
+    float scale = 0.0f, cap = 0.0f; // scores times scale in powers of two; with a cap: scale = score scale / cap, cap in powers of two
+    float *part_o = nullptr, *part_ml = nullptr;  // [splits][U Hk][R][D] and [..][2], with splits > 1
+};
+
+struct Plan {
+    int dh = 0;         // the kernel's head width (64, 128, 256)
+    int kw = 1;         // key waves: 1 or several
+    int rows = 0;       // rows of a workgroup
+    int n_tiles = 0, splits = 1;
+    size_t off_ml = 0, total = 0;
+};
+
+hipError_t launch_bf16(const Plan &p, const Args &a, hipStream_t st);
+hipError_t launch_f32(const Plan &p, const Args &a, hipStream_t st);
+hipError_t launch_combine(bool bf16, const Args &a, hipStream_t st);
+
+}  // namespace rm_attn

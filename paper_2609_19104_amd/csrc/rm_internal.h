@@ -12,6 +12,10 @@
 
 namespace rm {
 
+// Sets the thread's error text and returns the status (rm_api.hip holds the text); success clears it.
+rm_status api_fail(rm_status st, const char *fmt, ...);
+rm_status api_ok();
+
 // ---------------------------------------------------------------------------------------------------------
 // Launch plan and workspace layout.  One plan is derived on the host from (shape, B, T, max_count); the same
 // function sizes the workspace and every launch, so they always agree.

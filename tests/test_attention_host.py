@@ -1,0 +1,185 @@
+"""Host-side refusals of the attention-side calls: every argument is checked before anything is enqueued (no GPU)."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+import paper_2609_19104_amd as rm
+
+MB = 1 << 20
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(rm.LIB_PATH):
+        pytest.skip("librmuscle.so not built")
+    return rm.load_library()
+
+
+def H(at, batch, token, head):
+    return rm.Heads(at, batch, token, head)
+
+
+def _span(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), B=2, T=4, N=100, q=None, k=None, v=None, out=None, span=None, slopes=None,
+          q_start=None, ws=None, ws_bytes=0):
+    q = q or H(1 * MB, T * 512, 512, 64)
+    k = k or H(2 * MB, N * 128, 128, 64)
+    v = v or H(3 * MB, N * 128, 128, 64)
+    out = out or H(4 * MB, T * 512, 512, 64)
+    return lib.rm_span_attention(rm.AttnShape(*shape), B, T, N, q, k, v, out, span, slopes, q_start, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,expected", [
+    (dict(shape=(8, 3, 64, 1, 0.1, 0.0)), rm.RM_ERR_SHAPE),
+    (dict(shape=(0, 0, 64, 1, 0.1, 0.0)), rm.RM_ERR_SHAPE),
+    (dict(shape=(8, 2, 60, 1, 0.1, 0.0)), rm.RM_ERR_SHAPE),
+    (dict(shape=(8, 2, 264, 1, 0.1, 0.0)), rm.RM_ERR_SHAPE),
+    (dict(shape=(8, 2, 64, 5, 0.1, 0.0)), rm.RM_ERR_DTYPE),
+    (dict(shape=(8, 2, 64, 1, float("nan"), 0.0)), rm.RM_ERR_INVALID_ARG),
+    (dict(shape=(8, 2, 64, 1, float("inf"), 0.0)), rm.RM_ERR_INVALID_ARG),
+    (dict(shape=(8, 2, 64, 1, 0.1, -1.0)), rm.RM_ERR_INVALID_ARG),
+    (dict(shape=(8, 2, 64, 1, 0.1, float("inf"))), rm.RM_ERR_INVALID_ARG),
+    (dict(B=0), rm.RM_ERR_INVALID_ARG),
+    (dict(T=0), rm.RM_ERR_INVALID_ARG),
+    (dict(N=-1), rm.RM_ERR_SHAPE),
+    (dict(N=1 << 30), rm.RM_ERR_SHAPE),
+    (dict(T=1 << 30), rm.RM_ERR_SHAPE),
+    (dict(q=H(None, 2048, 512, 64)), rm.RM_ERR_INVALID_ARG),
+    (dict(q=H(MB + 8, 2048, 512, 64)), rm.RM_ERR_ALIGN),
+    (dict(k=H(2 * MB, 12800, 132, 64)), rm.RM_ERR_ALIGN),
+    (dict(k=H(2 * MB, 12800, -128, 64)), rm.RM_ERR_SHAPE),
+    (dict(k=H(2 * MB, 1 << 62, 128, 64)), rm.RM_ERR_SHAPE),
+    (dict(v=H(2 * MB, 0, 8 * MB, 64)), rm.RM_ERR_SHAPE),            # 16 MiB from key to key
+    (dict(out=H(4 * MB, 2048, 512, 0)), rm.RM_ERR_SHAPE),           # heads on top of each other
+    (dict(out=H(4 * MB, 2048, 256, 64)), rm.RM_ERR_SHAPE),          # tokens into each other
+    (dict(out=H(1 * MB + 1024, 2048, 512, 64)), rm.RM_ERR_INVALID_ARG),  # over q
+    (dict(out=H(3 * MB, 2048, 512, 64)), rm.RM_ERR_INVALID_ARG),    # over v
+    (dict(span=4 * MB), rm.RM_ERR_INVALID_ARG),                     # out over the spans
+    (dict(span=5 * MB + 4), rm.RM_ERR_ALIGN),
+    (dict(slopes=5 * MB + 2), rm.RM_ERR_ALIGN),
+    (dict(slopes=4 * MB), rm.RM_ERR_INVALID_ARG),
+    (dict(slopes=5 * MB, q_start=4 * MB), rm.RM_ERR_INVALID_ARG),
+    (dict(N=100000, k=H(64 * MB, 0, 128, 64), v=H(128 * MB, 0, 128, 64)), rm.RM_ERR_INVALID_ARG),  # needs a workspace
+    (dict(N=100000, k=H(64 * MB, 0, 128, 64), v=H(128 * MB, 0, 128, 64), ws=256 * MB, ws_bytes=100), rm.RM_ERR_WORKSPACE),
+    (dict(N=100000, k=H(64 * MB, 0, 128, 64), v=H(128 * MB, 0, 128, 64), ws=256 * MB + 16, ws_bytes=1 << 30),
+     rm.RM_ERR_ALIGN),
+    (dict(N=100000, k=H(64 * MB, 0, 128, 64), v=H(128 * MB, 0, 128, 64), ws=4 * MB, ws_bytes=1 << 30),
+     rm.RM_ERR_INVALID_ARG),                                        # workspace over out
+    (dict(N=100000, k=H(64 * MB, 0, 128, 64), v=H(128 * MB, 0, 128, 64), ws=64 * MB, ws_bytes=1 << 30),
+     rm.RM_ERR_INVALID_ARG),                                        # workspace over k
+])
+def test_span_attention_refuses(lib, kw, expected):
+    assert _span(lib, **kw) == expected
+    assert rm.last_error() != ""
+
+
+def _prefix(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), G=2, per=3, T=4, P=100, S=20, q=None, kp=None, vp=None, plen=None,
+            ko=None, vo=None, olen=None, out=None, ws=None, ws_bytes=0):
+    q = q or H(1 * MB, T * 512, 512, 64)
+    kp, vp = kp or H(2 * MB, P * 128, 128, 64), vp or H(3 * MB, P * 128, 128, 64)
+    ko, vo = ko or H(5 * MB, S * 128, 128, 64), vo or H(6 * MB, S * 128, 128, 64)
+    out = out or H(4 * MB, T * 512, 512, 64)
+    return lib.rm_prefix_attention(rm.AttnShape(*shape), G, per, T, P, S, q, kp, vp, plen, ko, vo, olen, 0, out, ws,
+                                   ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,expected", [
+    (dict(shape=(8, 2, 64, 2, 0.1, 0.0)), rm.RM_ERR_DTYPE),
+    (dict(G=0), rm.RM_ERR_INVALID_ARG),
+    (dict(per=0), rm.RM_ERR_INVALID_ARG),
+    (dict(P=-1), rm.RM_ERR_SHAPE),
+    (dict(S=1 << 30), rm.RM_ERR_SHAPE),
+    (dict(per=1 << 20, T=1 << 10), rm.RM_ERR_SHAPE),
+    (dict(kp=H(None, 0, 128, 64)), rm.RM_ERR_INVALID_ARG),
+    (dict(vo=H(6 * MB + 4, 0, 128, 64)), rm.RM_ERR_ALIGN),
+    (dict(plen=7 * MB + 1), rm.RM_ERR_ALIGN),
+    (dict(olen=4 * MB), rm.RM_ERR_INVALID_ARG),                     # out over the lengths
+    (dict(out=H(5 * MB, 2048, 512, 64)), rm.RM_ERR_INVALID_ARG),    # over the own keys
+    (dict(P=100000, kp=H(64 * MB, 0, 128, 64), vp=H(128 * MB, 0, 128, 64)), rm.RM_ERR_INVALID_ARG),  # no workspace
+])
+def test_prefix_attention_refuses(lib, kw, expected):
+    assert _prefix(lib, **kw) == expected
+    assert rm.last_error() != ""
+
+
+def test_workspace_sizes(lib):
+    n = ctypes.c_size_t(1)
+    s = rm.AttnShape(8, 2, 64, 1, 0.125, 0.0)
+    assert lib.rm_span_attention_workspace_size(s, 1, 4096, 4096, ctypes.byref(n)) == rm.RM_OK and n.value == 0
+    assert lib.rm_span_attention_workspace_size(s, 1, 1, 65536, ctypes.byref(n)) == rm.RM_OK and n.value > 0
+    assert n.value % 256 == 0
+    assert lib.rm_span_attention_workspace_size(s, 1, 1, 65536, None) == rm.RM_ERR_INVALID_ARG
+    assert lib.rm_span_attention_workspace_size(None, 1, 1, 65536, ctypes.byref(n)) == rm.RM_ERR_INVALID_ARG
+    assert lib.rm_prefix_attention_workspace_size(s, 1, 1, 1, 65536, 0, ctypes.byref(n)) == rm.RM_OK and n.value > 0
+    assert lib.rm_prefix_attention_workspace_size(s, 0, 1, 1, 65536, 0, ctypes.byref(n)) == rm.RM_ERR_INVALID_ARG
+
+
+def _rope(lib, *, N=5, Hq=4, Hk=2, D=64, ind=1, outd=1, q=None, k=None, v=None, qo=None, ko=None, vo=None, rows=9,
+          pos=7 * MB, slot=8 * MB, f=9 * MB, rot=64, gq=None, gk=None, eps=1e-6):
+    q, k = q or H(1 * MB, 0, 256, 64), k or H(2 * MB, 0, 128, 64)
+    v, qo = v or H(3 * MB, 0, 128, 64), qo or H(4 * MB, 0, 256, 64)
+    ko, vo = ko or H(5 * MB, 0, 128, 64), vo or H(6 * MB, 0, 128, 64)
+    return lib.rm_qk_norm_rope(N, Hq, Hk, D, ind, outd, q, k, v, qo, ko, vo, rows, pos, slot, f, rot, 0, gq, gk, eps,
+                               None)
+
+
+@pytest.mark.parametrize("kw,expected", [
+    (dict(N=-1), rm.RM_ERR_INVALID_ARG),
+    (dict(Hq=0), rm.RM_ERR_INVALID_ARG),
+    (dict(rows=-1), rm.RM_ERR_INVALID_ARG),
+    (dict(D=36), rm.RM_ERR_SHAPE),
+    (dict(D=512, rot=0), rm.RM_ERR_SHAPE),
+    (dict(rot=66), rm.RM_ERR_SHAPE),
+    (dict(rot=68), rm.RM_ERR_SHAPE),
+    (dict(rot=-4), rm.RM_ERR_SHAPE),
+    (dict(ind=3), rm.RM_ERR_DTYPE),
+    (dict(outd=-1), rm.RM_ERR_DTYPE),
+    (dict(eps=-1.0), rm.RM_ERR_INVALID_ARG),
+    (dict(eps=float("nan")), rm.RM_ERR_INVALID_ARG),
+    (dict(slot=None, rows=4), rm.RM_ERR_SHAPE),
+    (dict(N=1 << 29), rm.RM_ERR_SHAPE),
+    (dict(pos=None), rm.RM_ERR_INVALID_ARG),
+    (dict(f=None), rm.RM_ERR_INVALID_ARG),
+    (dict(pos=7 * MB + 2), rm.RM_ERR_ALIGN),
+    (dict(gk=7 * MB + 2), rm.RM_ERR_ALIGN),
+    (dict(q=H(MB + 2, 0, 256, 64)), rm.RM_ERR_ALIGN),
+    (dict(q=H(MB, 0, 257, 64)), rm.RM_ERR_ALIGN),
+    (dict(qo=H(1 * MB, 0, 256, 64)), rm.RM_ERR_INVALID_ARG),        # over q
+    (dict(vo=H(5 * MB + 256, 0, 128, 64)), rm.RM_ERR_INVALID_ARG),  # over k_out
+    (dict(ko=H(7 * MB, 0, 128, 64)), rm.RM_ERR_INVALID_ARG),        # over pos
+    (dict(ko=H(5 * MB, 0, 64, 64)), rm.RM_ERR_SHAPE),               # rows into each other
+    (dict(vo=H(None, 0, 128, 64)), rm.RM_ERR_INVALID_ARG),
+])
+def test_qk_norm_rope_refuses(lib, kw, expected):
+    assert _rope(lib, **kw) == expected
+    assert rm.last_error() != ""
+
+
+@pytest.mark.parametrize("args,expected", [
+    ((0, 4, 4, 1, 0, None, None, None, None, MB), rm.RM_ERR_INVALID_ARG),
+    ((1, 0, 4, 1, 0, None, None, None, None, MB), rm.RM_ERR_INVALID_ARG),
+    ((1, 4, 0, 1, 0, None, None, None, None, MB), rm.RM_ERR_INVALID_ARG),
+    ((1, 4, 1 << 30, 1, 0, None, None, None, None, MB), rm.RM_ERR_SHAPE),
+    ((1, 4, 4, 1, -1, None, None, None, None, MB), rm.RM_ERR_INVALID_ARG),
+    ((1, 4, 4, 0, 0, None, None, 2 * MB, None, MB), rm.RM_ERR_INVALID_ARG),  # prefix lengths without causal
+    ((1, 4, 4, 1, 0, None, None, None, None, None), rm.RM_ERR_INVALID_ARG),
+    ((1, 4, 4, 1, 0, None, None, None, None, MB + 4), rm.RM_ERR_ALIGN),
+    ((1, 4, 4, 1, 0, 2 * MB + 1, None, None, None, MB), rm.RM_ERR_ALIGN),
+    ((1, 4, 4, 1, 0, None, None, None, MB + 16, MB), rm.RM_ERR_INVALID_ARG),  # span over doc
+])
+def test_attn_spans_refuses(lib, args, expected):
+    assert lib.rm_attn_spans(*args, None) == expected
+    assert rm.last_error() != ""
+
+
+def test_binding_refuses_cpu_tensors():
+    x = torch.zeros(1, 4, 2, 8)
+    with pytest.raises(ValueError):
+        rm.rm_span_attention(x, x, x, torch.zeros_like(x), None)
+    with pytest.raises(ValueError):
+        rm.rm_prefix_attention(x, x, x, x, x, torch.zeros_like(x), None)
+    with pytest.raises(ValueError):
+        rm.rm_qk_norm_rope(x[0], x[0], None, x[0], x[0], None, torch.zeros(4, dtype=torch.int32), None)
+    with pytest.raises(ValueError):
+        rm.rm_attn_spans(torch.zeros((1, 4, 2), dtype=torch.int32), 4)
