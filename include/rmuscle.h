@@ -313,7 +313,7 @@ typedef struct rm_heads {
 
 /* n_q_heads: a multiple of n_kv_heads; query head h uses key head h / (n_q_heads / n_kv_heads).
  * head_dim: a multiple of 8, at most 256.  dtype: an rm_dtype, of queries, keys, values and output.
- * scale: finite; scores are scale * <q, k>.  softcap: >= 0; not 0: scores become softcap * tanh(score / softcap).
+ * scale: finite and positive; scores are scale * <q, k>.  softcap: >= 0; not 0: scores become softcap * tanh(score / softcap).
  * Scores, maxima, sums and the output are accumulated in float32; with RM_BF16 the softmax's weights are rounded to
  * bf16 before their product with the values (as the values are), their sum is not. */
 typedef struct rm_attn_shape {

@@ -75,7 +75,8 @@ rm_status check_attn_shape(const rm_attn_shape *s) {
     if (s->head_dim <= 0 || s->head_dim % 8 != 0 || s->head_dim > 256)
         return api_fail(RM_ERR_SHAPE, "head_dim=%d must be a multiple of 8 in [8, 256]", s->head_dim);
     if (s->dtype != RM_F32 && s->dtype != RM_BF16) return api_fail(RM_ERR_DTYPE, "unknown dtype %d", s->dtype);
-    if (!std::isfinite(s->scale)) return api_fail(RM_ERR_INVALID_ARG, "scale must be finite");
+    if (!(s->scale > 0.0f) || !std::isfinite(s->scale))
+        return api_fail(RM_ERR_INVALID_ARG, "scale must be finite and positive");
     if (!(s->softcap >= 0.0f) || !std::isfinite(s->softcap))
         return api_fail(RM_ERR_INVALID_ARG, "softcap must be finite and not negative");
     return RM_OK;

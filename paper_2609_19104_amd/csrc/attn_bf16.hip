@@ -12,12 +12,12 @@ static hipError_t go(const Args &a, hipStream_t st) {
 
 hipError_t launch_bf16(const Plan &p, const Args &a, hipStream_t st) {
     if (p.kw > 1) {
-        if (p.dh == 64) return go<64, 1, 4, 1, 128, 1>(a, st);
-        if (p.dh == 128) return go<128, 1, 4, 1, 128, 1>(a, st);
+        if (p.dh == 64) return go<64, 1, 4, 1, 128, 2>(a, st);
+        if (p.dh == 128) return go<128, 1, 4, 1, 128, 2>(a, st);
         return go<256, 1, 4, 1, 128, 1>(a, st);
     }
-    if (p.dh == 64) return go<64, 4, 1, 1, 64, 1>(a, st);
-    if (p.dh == 128) return go<128, 4, 1, 1, 64, 1>(a, st);
+    if (p.dh == 64) return go<64, 4, 1, 1, 64, 2>(a, st);
+    if (p.dh == 128) return go<128, 4, 1, 1, 64, 2>(a, st);
     return go<256, 4, 1, 1, 64, 1>(a, st);
 }
 

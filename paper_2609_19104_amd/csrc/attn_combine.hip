@@ -6,37 +6,44 @@ namespace rm_attn {
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 // LPR lanes per row, 4 columns a lane (D <= 4 LPR).  Slices are added in order, so the sums are the same on every
-// call.  A slice without keys for the row has m = -inf; its sums are not read.
+// call.  A slice without keys for the row has m = -inf and sums of 0.
 template <bool BF, int LPR>
 __global__ __launch_bounds__(256) void combine_kernel(Args a) {
     const int64_t rows = static_cast<int64_t>(a.U) * a.Hk * a.R;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / LPR) + threadIdx.x / LPR;
-    const int c = (threadIdx.x % LPR) * 4;
-    if (row >= rows || c >= a.D) return;
+    const int col = (threadIdx.x % LPR) * 4, c = min(col, a.D - 4);
+    if (row >= rows) return;  // all of the row's lanes
+    // The slices' maxima and sums, one slice a lane: their common maximum, and each slice's factor.
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + row;
     const float *po = a.part_o + row * a.D + c;
+    const int lane = threadIdx.x % LPR;
     float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * rows].x);
+    for (int s = lane; s < a.splits; s += LPR) top = fmaxf(top, ml[s * rows].x);
+    for (int o = LPR / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     const float ref = top == -INFINITY ? 0.0f : top;
     float l = 0.0f;
     rm_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s0 = 0; s0 < a.splits; s0 += 4) {
-        float2 w[4];
-        rm_f32x4 v[4];
+    for (int s0 = 0; s0 < a.splits; s0 += LPR) {
+        const float2 mine = s0 + lane < a.splits ? ml[(s0 + lane) * rows] : make_float2(-INFINITY, 0.0f);
+        const float f = __builtin_amdgcn_exp2f(mine.x - ref);  // 0 for a slice without keys
+        const int n = min(a.splits - s0, LPR);
+        for (int i0 = 0; i0 < n; i0 += 8) {
+            rm_f32x4 v[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int s = min(s0 + i, a.splits - 1);
-            w[i] = ml[s * rows];
-            v[i] = *reinterpret_cast<const rm_f32x4 *>(po + s * rows * a.D);
-        }
+            for (int i = 0; i < 8; ++i)
+                v[i] = *reinterpret_cast<const rm_f32x4 *>(po + min(s0 + i0 + i, a.splits - 1) * rows * a.D);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (s0 + i >= a.splits || (w[i].x == -INFINITY && w[i].y == 0.0f)) continue;
-            const float f = __builtin_amdgcn_exp2f(w[i].x - ref);
-            l += w[i].y * f;
-            o += v[i] * f;
+            for (int i = 0; i < 8; ++i) {
+                const int from = (i0 + i) % LPR;
+                const float fi = __shfl(f, from, LPR), li = __shfl(mine.y, from, LPR);
+                if (i0 + i < n) {
+                    l += li * fi;
+                    o += v[i] * fi;
+                }
+            }
         }
     }
+    if (col >= a.D) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int ng = static_cast<int>(row / a.R), r = static_cast<int>(row - static_cast<int64_t>(ng) * a.R);
     const int u = ng / a.Hk, hk = ng - u * a.Hk;

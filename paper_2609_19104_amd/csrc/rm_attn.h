@@ -32,17 +32,35 @@ constexpr float kRaise = 8.0f;
 
 static __device__ uint4 zero16;  // what rows and columns outside a tile are staged from
 
-// rm_dma::dma16 with a 64-bit base in scalar registers and a 32-bit byte offset per lane.
-__device__ __forceinline__ void dma16_base(const void *base, uint32_t off, uint32_t lds) {
+// rm_dma::dma16 for two loads, STEP bytes apart in LDS, each lane at its 32-bit offset from a base in scalar registers.
+template <int STEP>
+__device__ __forceinline__ void dma16_pair(const void *base, uint32_t off0, uint32_t off1, uint32_t lds) {
     uint32_t keep;
     asm volatile(
-        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
+        "s_add_u32 m0, m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
         : "=&s"(keep)
-        : "v"(off), "s"(base), "s"(lds)
-        : "memory");
+        : "v"(off0), "v"(off1), "s"(base), "s"(lds), "n"(STEP)
+        : "memory", "scc");
+}
+
+// A value that is the same in every lane, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
+    return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+__device__ __forceinline__ const char *uniform(const char *p) {
+    return reinterpret_cast<const char *>(uniform(reinterpret_cast<int64_t>(p)));
 }
 
 __device__ __forceinline__ float xor32_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
+
+// a * b rounded, not part of a fused multiply-add.
+__device__ __forceinline__ float scaled(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
 
 __device__ __forceinline__ int wave_min(int v) {
     for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o));
@@ -73,6 +91,19 @@ __device__ __forceinline__ rm_bf16x8 read_v_rows(const uint8_t *p) {
     return __builtin_bit_cast(rm_bf16x8, v);
 }
 
+// Scheduling of a block of N steps of R LDS reads and M matrix-core instructions each: the reads run AHEAD steps ahead.
+template <int N, int AHEAD, int M, int R>
+__device__ __forceinline__ void pipeline() {
+    constexpr int A = AHEAD < N ? AHEAD : N;
+    __builtin_amdgcn_sched_group_barrier(0x100, A * R, 0);
+#pragma unroll
+    for (int i = 0; i < N - A; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, A * M, 0);
+}
+
 // One tile's place: keys [kb, min(kb + KT, end)) of segment seg (-1: the group's shared keys, else a sample).
 struct Tile {
     const char *k, *v;
@@ -88,6 +119,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     constexpr int KPW = KT / KW, NS = KPW / 32;
     constexpr int DB = DH / 32;               // output blocks of 32 columns
     constexpr int QF = BF ? DH / 16 : DH / 8; // fragments of a query row block
+    constexpr int AHEAD = 4;                  // LDS reads run this many matrix-core steps ahead
     static_assert(CPR >= 8 && CPR <= 64 && NI >= 1 && NI * RPI * W == KT && NS >= 1, "tile shape");
     constexpr int TILEB = KT * ROWB;
     // O of every wave passes through LDS when the key waves are joined.
@@ -190,7 +222,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         b_hi = wave_max(end);
         if (b_lo > b_hi) b_lo = b_hi;
     }
-    auto seg_keys = [&](int sg, int &lo, int &end) {
+    auto seg_keys = [&](int sg, int &lo, int &end) __attribute__((always_inline)) {
         lo = 0;
         if (sg < 0) {
             end = n0;
@@ -203,7 +235,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                 end = __builtin_amdgcn_readfirstlane(min(max(a.len1[static_cast<int64_t>(u) * a.per + sg], 0), a.n1));
         }
     };
-    auto seg_base = [&](Tile &t) {
+    auto seg_base = [&](Tile &t) __attribute__((always_inline)) {
         const Src &s = t.seg < 0 ? a.s0 : a.s1;
         const int64_t b = t.seg < 0 ? u : static_cast<int64_t>(u) * a.per + t.seg;
         t.kn = s.k_n;
@@ -217,27 +249,26 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         seg_keys(sg, lo, end);
         total += (end - lo + KT - 1) / KT;
     }
-    int64_t n_left;  // tiles of this slice
-    Tile cur;
-    {
-        const int64_t first = total * split / a.splits;
-        n_left = total * (split + 1) / a.splits - first;
+    const int64_t first = total * split / a.splits, n_tiles = total * (split + 1) / a.splits - first;
+    auto first_tile = [&](Tile &t) __attribute__((always_inline)) {
         int64_t skip = first;
-        cur.seg = -1;
-        cur.kb = cur.end = 0;
+        t.seg = -1;
+        t.kb = t.end = 0;
         for (int sg = -1; sg <= s_last; sg = sg < 0 ? s_first : sg + 1) {
             int lo, end;
             seg_keys(sg, lo, end);
             const int n = (end - lo + KT - 1) / KT;
-            cur.seg = sg;
-            cur.kb = lo + static_cast<int>(min(skip, static_cast<int64_t>(n))) * KT;
-            cur.end = end;
+            t.seg = sg;
+            t.kb = lo + static_cast<int>(min(skip, static_cast<int64_t>(n))) * KT;
+            t.end = end;
             if (skip < n) break;
             skip -= n;
         }
-        seg_base(cur);
-    }
-    auto advance = [&](Tile &t) {  // only called when another tile follows
+        seg_base(t);
+    };
+    Tile cur;
+    first_tile(cur);
+    auto advance = [&](Tile &t) __attribute__((always_inline)) {  // only called when another tile follows
         t.kb += KT;
         if (t.kb < t.end) {
             t.k += KT * t.kn;
@@ -262,26 +293,40 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     };
     const uint32_t lds_k = rm_dma::lds_addr(lds), lds_v = lds_k + TILEB;
     const bool whole_head = a.D == DH;
-    auto stage = [&](const Tile &t, bool values) {
-        const char *base = values ? t.v : t.k;
-        const int64_t sn = values ? t.vn : t.kn;
+    // The swizzle of a wave's load instructions repeats every PER of them.
+    constexpr int PERK = W * RPI >= 16 ? 1 : 16 / (W * RPI), PERV = BF || W * RPI >= 8 ? 1 : 8 / (W * RPI);
+    static_assert(NI % 2 == 0 && NI % PERK == 0 && NI % PERV == 0, "load instructions");
+    auto stage = [&](const Tile &t, bool values) __attribute__((always_inline)) {
+        const int64_t sn = uniform(values ? t.vn : t.kn);
+        const char *base = uniform(values ? t.v : t.k);
         const uint32_t to = (values ? lds_v : lds_k) + wave * 1024;
         if (whole_head && t.kb + KT <= t.end) {
+            // Row (n W + wave) RPI + lrow: token strides are below 2^24 bytes, so a tile's offsets fit in 32 bits.
+            const uint32_t row0 = (wave * RPI + lrow) * static_cast<uint32_t>(sn);
+            const uint32_t step = W * RPI * static_cast<uint32_t>(sn);
+            uint32_t chunk[PERK > PERV ? PERK : PERV];
 #pragma unroll
-            for (int n = 0; n < NI; ++n) {
-                const int row = (n * W + wave) * RPI;
-                const int chunk = pos ^ (values ? swz_v(row + lrow) : swz_k(row + lrow));
-                const uint32_t off = static_cast<uint32_t>(lrow) * static_cast<uint32_t>(sn) + chunk * 16;
-                dma16_base(base + row * sn, off, to + n * W * 1024);
+            for (int n = 0; n < (values ? PERV : PERK); ++n) {
+                const int row = (n * W + wave) * RPI + lrow;
+                chunk[n] = row0 + (pos ^ (values ? swz_v(row) : swz_k(row))) * 16;
             }
-        } else {  // rows past the end and columns past the head's are zeros
 #pragma unroll
-            for (int n = 0; n < NI; ++n) {
+            for (int n = 0; n < NI; n += 2)
+                dma16_pair<W * 1024>(base, chunk[n % (values ? PERV : PERK)] + n * step,
+                                     chunk[(n + 1) % (values ? PERV : PERK)] + (n + 1) * step,
+                                     __builtin_amdgcn_readfirstlane(to + n * W * 1024));
+        } else {  // rows past the end and columns past the head's are zeros
+            const int64_t zero = reinterpret_cast<int64_t>(&zero16);
+            const char *at = base + (wave * RPI + lrow) * sn;
+            const int left = t.end - t.kb;
+#pragma unroll 2
+            for (int n = 0; n < NI; ++n, at += W * RPI * sn) {
                 const int row = (n * W + wave) * RPI + lrow;
                 const int chunk = pos ^ (values ? swz_v(row) : swz_k(row));
-                const bool in = t.kb + row < t.end && chunk * 16 < a.D * ES;
-                const char *src = in ? base + row * sn + chunk * 16 : reinterpret_cast<const char *>(&zero16);
-                rm_dma::dma16(src, to + n * W * 1024);
+                // 0 or -1, without a branch
+                const int64_t in = static_cast<int64_t>((row - left) & (chunk * 16 - a.D * ES)) >> 63;
+                const int64_t src = zero + ((reinterpret_cast<int64_t>(at) + chunk * 16 - zero) & in);
+                rm_dma::dma16(reinterpret_cast<const char *>(src), __builtin_amdgcn_readfirstlane(to + n * W * 1024));
             }
         }
     };
@@ -289,7 +334,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     // ---------------------------------------------------------------- queries
     typedef typename std::conditional<BF, rm_bf16x8, rm_f32x4>::type QFrag;
     QFrag qf[QB][QF];
-    if (n_left > 0) stage(cur, false);
+    if (n_tiles > 0) stage(cur, false);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
@@ -323,251 +368,248 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     auto read_v = [](const uint8_t *p) { return read_v_rows<ROWB>(p); };
     rm_f32x16 o[QB][DB];
     float m[QB], l[QB];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        m[qb] = -INFINITY;
-        l[qb] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[qb][d] = rm_f32x16{};
-    }
+    // Scores with a cap or a bias are formed in powers of two; plain ones are scaled on the way into exp2.
+    const float sc = a.cap != 0.0f || a.slopes ? 1.0f : a.scale;
 
     // ---------------------------------------------------------------- tiles
-    for (; n_left > 0; --n_left) {
-        Tile nxt = cur;
-        if (n_left > 1) advance(nxt);
-        rm_dma::wait_barrier<0>();  // the keys are there, and every wave has read the last tile's values
-        stage(cur, true);
-
-        const int kbw = cur.kb + kw * KPW;
-        bool active = kbw < cur.end, mixed = kbw + KPW > cur.end;
-        if (cur.seg >= 0) {
-            active = active && cur.seg >= w_s0 && cur.seg <= w_s1 && kbw < w_maxhi && kbw + KPW > w_minlo;
-            mixed = mixed || w_s0 != w_s1 || kbw < w_maxlo || kbw + KPW > w_minhi;
+    // One pass over the slice's tiles, the first one's keys under way.  Returns whether a tile of keys that some rows
+    // see and others do not holds infinities or NaN among its values: 0 times those would spoil the rows that do not
+    // see them.  Such a workgroup (there is hardly ever one) makes a second pass with `clean`, which sets them to 0 in
+    // LDS, the other sums staying as they are bit for bit, and then adds them to the rows that see them.
+    auto pass = [&](const bool clean) __attribute__((always_inline)) -> bool {
+        uint32_t spoilt = 0;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            m[qb] = -INFINITY;
+            l[qb] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[qb][d] = rm_f32x16{};
         }
-        rm_f32x16 s[QB][NS];
-        if (active) {
+        for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
+            Tile nxt = cur;
+            if (n_left > 1) advance(nxt);
+            rm_dma::wait_barrier<0>();  // the keys are there, and every wave has read the last tile's values
+            stage(cur, true);
+
+            const int kbw = cur.kb + kw * KPW;
+            bool active = kbw < cur.end, mixed = kbw + KPW > cur.end, apart = false;
+            if (cur.seg >= 0) {
+                active = active && cur.seg >= w_s0 && cur.seg <= w_s1 && kbw < w_maxhi && kbw + KPW > w_minlo;
+                apart = w_s0 != w_s1 || kbw < w_maxlo || min(kbw + KPW, cur.end) > w_minhi;
+                mixed = mixed || apart;
+            }
+            auto interval = [&](int qb, int &lo, int &len) {  // the keys of this segment that the lane's row sees
+                lo = cur.seg < 0 ? 0 : r_lo[qb];
+                len = cur.seg < 0 ? n0 : (r_sample[qb] == cur.seg ? r_len[qb] : 0);
+            };
+            rm_f32x16 s[QB][NS];
+            if (active) {
 #pragma unroll
-            for (int ns = 0; ns < NS; ++ns) {
+                for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb) s[qb][ns] = rm_f32x16{};
+                    for (int ns = 0; ns < NS; ++ns) s[qb][ns] = rm_f32x16{};
+                // Key fragments AHEAD ahead of the products that take them.
+                QFrag kf[QF * NS];
+                auto read_k = [&](int x) {  // x = c NS + ns
+                    const int c = x / NS, ns = x % NS;
+                    return *reinterpret_cast<const QFrag *>(kb_ptr[c & 7] + ns * 32 * ROWB + (c >> 3) * 256);
+                };
 #pragma unroll
-                for (int c = 0; c < QF; ++c) {
-                    const uint8_t *p = kb_ptr[c & 7] + ns * 32 * ROWB + (c >> 3) * 256;
-                    const QFrag kf = *reinterpret_cast<const QFrag *>(p);
+                for (int x = 0; x < QF * NS; ++x) kf[x] = read_k(x);
+#pragma unroll
+                for (int x = 0; x < QF * NS; ++x)
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb) {
                         if constexpr (BF) {
-                            s[qb][ns] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[qb][c], s[qb][ns], 0, 0, 0);
+                            s[qb][x % NS] =
+                                __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], qf[qb][x / NS], s[qb][x % NS], 0, 0, 0);
                         } else {
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                s[qb][ns] =
-                                    __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i], qf[qb][c][i], s[qb][ns], 0, 0, 0);
+                                s[qb][x % NS] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[x][i], qf[qb][x / NS][i],
+                                                                                    s[qb][x % NS], 0, 0, 0);
                         }
                     }
-                }
-            }
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-                int lo = r_lo[qb], len = r_len[qb];
-                if (cur.seg < 0) {
-                    lo = 0;
-                    len = n0;
-                } else if (r_sample[qb] != cur.seg) {
-                    len = 0;
-                }
-                float top = -INFINITY;
-#pragma unroll
-                for (int ns = 0; ns < NS; ++ns) {
-                    const int k0 = kbw + 32 * ns + 4 * hi;
-                    rm_f32x16 &x = s[qb][ns];
-                    if (a.cap != 0.0f) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float z = x[i] * a.scale;  // score / cap
-                            float th;
-                            if constexpr (BF)
-                                th = 1.0f - 2.0f * __builtin_amdgcn_rcpf(
-                                                       __builtin_amdgcn_exp2f(z * (2.0f * kLog2e)) + 1.0f);
-                            else
-                                th = tanhf(z);
-                            x[i] = a.cap * th;
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x[i] *= a.scale;
-                    }
-                    if (a.slopes) {
-                        const int d0 = r_pos[qb] - k0;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            x[i] -= r_slope[qb] * fabsf(static_cast<float>(d0 - (8 * (i >> 2) + (i & 3))));
-                    }
-                    if (mixed) {
-                        const int d0 = k0 - lo;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            x[i] = static_cast<uint32_t>(d0 + 8 * (i >> 2) + (i & 3)) < static_cast<uint32_t>(len)
-                                       ? x[i]
-                                       : -INFINITY;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
-                }
-                top = xor32_max(top);
-                if (__any(top > m[qb] + kRaise || (m[qb] == -INFINITY && top > -INFINITY))) {
-                    const float mn = fmaxf(m[qb], top);
-                    const float f = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[qb] - mn);
-                    m[qb] = mn;
-                    l[qb] *= f;
-#pragma unroll
-                    for (int d = 0; d < DB; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[qb][d][i] *= f;
-                }
-                const float ref = m[qb] == -INFINITY ? 0.0f : m[qb];
-                float sum = 0.0f;
-#pragma unroll
-                for (int ns = 0; ns < NS; ++ns)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        s[qb][ns][i] = __builtin_amdgcn_exp2f(s[qb][ns][i] - ref);
-                        sum += s[qb][ns][i];
-                    }
-                l[qb] += sum;
-            }
-        }
-        rm_dma::wait_barrier<0>();  // the values are there, and every wave has read the keys
-        if (n_left > 1) stage(nxt, false);
-        if (active) {
-            // A key that some rows see and others do not may hold infinities or NaN: 0 times those would spoil the
-            // rows that do not see it.  The rare tile that has both goes the long way.
-            bool bad = false;
-            if (mixed) {
-                uint32_t any = 0;
-                if constexpr (BF) {
-#pragma unroll
-                    for (int ns = 0; ns < NS; ++ns)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-#pragma unroll
-                            for (int d = 0; d < DB; ++d) {
-                                const uint2 v = *reinterpret_cast<const uint2 *>(v_ptr[d % VP] + (d / VP) * 256 +
-                                                                                 (32 * ns + 8 * j) * ROWB);
-                                any |= nonfinite_bf16x2(v.x) | nonfinite_bf16x2(v.y);
-                            }
-                } else {
-#pragma unroll
-                    for (int ns = 0; ns < NS; ++ns)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-#pragma unroll
-                            for (int d = 0; d < DB; ++d)
-                                any |= nonfinite_f32(*reinterpret_cast<const float *>(
-                                    v_ptr[d % VP] + (d / VP) * 256 + (32 * ns + 8 * (i >> 2) + (i & 3)) * ROWB));
-                }
-                bad = __any(any != 0);
-            }
-            // o += V^T P^T; CLEAN leaves out V's infinities and NaN.
-            auto add_values = [&](auto clean) {
-                constexpr bool CLEAN = decltype(clean)::value;
-#pragma unroll
-                for (int ns = 0; ns < NS; ++ns) {
-                    if constexpr (BF) {
-#pragma unroll
-                        for (int st = 0; st < 2; ++st) {
-                            rm_bf16x8 p[QB];
-#pragma unroll
-                            for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) p[qb][i] = static_cast<__bf16>(s[qb][ns][8 * st + i]);
-#pragma unroll
-                            for (int d = 0; d < DB; ++d) {
-                                rm_bf16x8 vf = read_v(v_ptr[d % VP] + (d / VP) * 256 + (32 * ns + 16 * st) * ROWB);
-                                if constexpr (CLEAN) {
-#pragma unroll
-                                    for (int i = 0; i < 8; ++i)
-                                        vf[i] = fabsf(static_cast<float>(vf[i])) < INFINITY ? vf[i]
-                                                                                          : static_cast<__bf16>(0.0f);
-                                }
-#pragma unroll
-                                for (int qb = 0; qb < QB; ++qb)
-                                    o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[qb], o[qb][d], 0, 0, 0);
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-#pragma unroll
-                            for (int d = 0; d < DB; ++d) {
-                                float vf = *reinterpret_cast<const float *>(
-                                    v_ptr[d % VP] + (d / VP) * 256 + (32 * ns + 8 * (i >> 2) + (i & 3)) * ROWB);
-                                if constexpr (CLEAN) vf = fabsf(vf) < INFINITY ? vf : 0.0f;
-#pragma unroll
-                                for (int qb = 0; qb < QB; ++qb)
-                                    o[qb][d] =
-                                        __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[qb][ns][i], o[qb][d], 0, 0, 0);
-                            }
-                    }
-                }
-            };
-            if (!bad) {
-                add_values(std::false_type{});
-            } else {
-                add_values(std::true_type{});
-                // For each row and column, whether a key that the row sees holds +inf (or NaN), and -inf (or NaN):
-                // products of the 0/1 matrices of both, then the sums that the definition has.
+                pipeline<QF * NS, AHEAD, BF ? QB : 4 * QB, 1>();
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
-                    const int lo = cur.seg < 0 ? 0 : r_lo[qb];
-                    const int len = cur.seg < 0 ? n0 : (r_sample[qb] == cur.seg ? r_len[qb] : 0);
-                    auto sees = [&](int ns, int i) {
-                        const int k = kbw + 32 * ns + 4 * hi + 8 * (i >> 2) + (i & 3);
-                        return static_cast<uint32_t>(k - lo) < static_cast<uint32_t>(len) ? 1.0f : 0.0f;
-                    };
-                    auto plus = [](float x) { return !(fabsf(x) < INFINITY) && !(x < 0.0f) ? 1.0f : 0.0f; };
-                    auto minus = [](float x) { return !(fabsf(x) < INFINITY) && !(x > 0.0f) ? 1.0f : 0.0f; };
+                    if (a.cap != 0.0f) {
 #pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        rm_f32x16 np{}, nn{};
-#pragma unroll 1
-                        for (int ns = 0; ns < NS; ++ns) {
-                            const uint8_t *vp = v_ptr[d % VP] + (d / VP) * 256 + 32 * ns * ROWB;
-                            if constexpr (BF) {
+                        for (int ns = 0; ns < NS; ++ns)
 #pragma unroll
-                                for (int st = 0; st < 2; ++st) {
-                                    const rm_bf16x8 vf = read_v(vp + 16 * st * ROWB);
-                                    rm_bf16x8 vis, fp, fn;
-#pragma unroll
-                                    for (int i = 0; i < 8; ++i) {
-                                        vis[i] = static_cast<__bf16>(sees(ns, 8 * st + i));
-                                        fp[i] = static_cast<__bf16>(plus(static_cast<float>(vf[i])));
-                                        fn[i] = static_cast<__bf16>(minus(static_cast<float>(vf[i])));
-                                    }
-                                    np = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp, vis, np, 0, 0, 0);
-                                    nn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fn, vis, nn, 0, 0, 0);
-                                }
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    const float vf =
-                                        *reinterpret_cast<const float *>(vp + (8 * (i >> 2) + (i & 3)) * ROWB);
-                                    const float vis = sees(ns, i);
-                                    np = __builtin_amdgcn_mfma_f32_32x32x2f32(plus(vf), vis, np, 0, 0, 0);
-                                    nn = __builtin_amdgcn_mfma_f32_32x32x2f32(minus(vf), vis, nn, 0, 0, 0);
-                                }
+                            for (int i = 0; i < 16; ++i) {
+                                const float z = s[qb][ns][i] * a.scale;  // score / cap
+                                float th;
+                                if constexpr (BF)
+                                    th = 1.0f - 2.0f * __builtin_amdgcn_rcpf(
+                                                           __builtin_amdgcn_exp2f(z * (2.0f * kLog2e)) + 1.0f);
+                                else
+                                    th = tanhf(z);
+                                s[qb][ns][i] = a.cap * th;
                             }
+                    }
+                    if (a.slopes) {
+                        const float in = a.cap != 0.0f ? 1.0f : a.scale;
+#pragma unroll
+                        for (int ns = 0; ns < NS; ++ns) {
+                            const int d0 = r_pos[qb] - (kbw + 32 * ns + 4 * hi);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                s[qb][ns][i] = s[qb][ns][i] * in -
+                                               r_slope[qb] * fabsf(static_cast<float>(d0 - (8 * (i >> 2) + (i & 3))));
                         }
+                    }
+                    if (mixed) {
+                        int lo, len;
+                        interval(qb, lo, len);
+#pragma unroll
+                        for (int ns = 0; ns < NS; ++ns) {
+                            const int d0 = kbw + 32 * ns + 4 * hi - lo;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                s[qb][ns][i] =
+                                    static_cast<uint32_t>(d0 + 8 * (i >> 2) + (i & 3)) < static_cast<uint32_t>(len)
+                                        ? s[qb][ns][i]
+                                        : -INFINITY;
+                        }
+                    }
+                    float top = s[qb][0][0];
+#pragma unroll
+                    for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[qb][ns][i]);
+                    top = xor32_max(top) * sc;
+                    if (__any(top > m[qb] + kRaise || (m[qb] == -INFINITY && top > -INFINITY))) {
+                        const float mn = fmaxf(m[qb], top);
+                        const float f = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[qb] - mn);
+                        m[qb] = mn;
+                        l[qb] *= f;
+#pragma unroll
+                        for (int d = 0; d < DB; ++d)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[qb][d][i] *= f;
+                    }
+                    const float ref = m[qb] == -INFINITY ? 0.0f : m[qb];
+                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int ns = 0; ns < NS; ++ns)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            o[qb][d][i] += np[i] > 0.0f ? INFINITY : 0.0f;
-                            o[qb][d][i] += nn[i] > 0.0f ? -INFINITY : 0.0f;
+                            // (float32 rounds the score first, as the maximum was: the largest weight is 1 exactly)
+                            const float x = BF ? fmaf(s[qb][ns][i], sc, -ref) : scaled(s[qb][ns][i], sc) - ref;
+                            s[qb][ns][i] = __builtin_amdgcn_exp2f(x);
+                            sum[i & 3] += s[qb][ns][i];
+                        }
+                    l[qb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                }
+            }
+            rm_dma::wait_barrier<0>();  // the values are there, and every wave has read the keys
+            if (clean && cur.seg >= 0) {
+                for (int i = tid; i < TILEB / 16; i += 64 * W) {
+                    rm_u32x4 *at = reinterpret_cast<rm_u32x4 *>(lds + TILEB) + i;
+                    rm_u32x4 v = *at;
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (BF) {
+                            const uint32_t bad = nonfinite_bf16x2(v[e]);
+                            v[e] &= (bad & 0x8000u ? 0u : 0xffffu) | (bad >> 31 ? 0u : 0xffff0000u);
+                        } else {
+                            v[e] = nonfinite_f32(__uint_as_float(v[e])) ? 0u : v[e];
+                        }
+                    }
+                    *at = v;
+                }
+                rm_dma::wait_barrier<0>();
+            }
+            if (n_left > 1) stage(nxt, false);
+            if (active) {
+                if (apart && !clean) {
+#pragma unroll 1
+                    for (int r = 0; r < KPW; r += BF ? 8 : 1) {  // the wave's values, each lane some of them
+                        if (!BF && (r & 4)) continue;            // (float32: rows r and r + 4 in the two halves)
+#pragma unroll
+                        for (int d = 0; d < DB; ++d) {
+                            const uint8_t *vp = v_ptr[d % VP] + (d / VP) * 256 + r * ROWB;
+                            if constexpr (BF) {
+                                const uint2 v = *reinterpret_cast<const uint2 *>(vp);
+                                spoilt |= nonfinite_bf16x2(v.x) | nonfinite_bf16x2(v.y);
+                            } else {
+                                spoilt |= nonfinite_f32(*reinterpret_cast<const float *>(vp));
+                            }
+                        }
+                    }
+                }
+                if constexpr (BF) {
+                    rm_bf16x8 p[QB][2 * NS];
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                        for (int st = 0; st < 2 * NS; ++st)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                p[qb][st][i] = static_cast<__bf16>(s[qb][st / 2][8 * (st % 2) + i]);
+#pragma unroll
+                    for (int x = 0; x < 2 * NS * DB; ++x) {
+                        const int st = x / DB, d = x % DB;
+                        const rm_bf16x8 vf = read_v(v_ptr[d % VP] + (d / VP) * 256 + 16 * st * ROWB);
+#pragma unroll
+                        for (int qb = 0; qb < QB; ++qb)
+                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[qb][st], o[qb][d], 0, 0, 0);
+                    }
+                    pipeline<2 * NS * DB, AHEAD, QB, 2>();
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 16 * NS * DB; ++x) {
+                        const int ns = x / (16 * DB), i = x / DB % 16, d = x % DB;
+                        const float vf = *reinterpret_cast<const float *>(
+                            v_ptr[d % VP] + (d / VP) * 256 + (32 * ns + 8 * (i >> 2) + (i & 3)) * ROWB);
+#pragma unroll
+                        for (int qb = 0; qb < QB; ++qb)
+                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[qb][ns][i], o[qb][d], 0, 0, 0);
+                    }
+                    pipeline<16 * NS * DB, AHEAD, QB, 1>();
+                }
+            }
+            cur = nxt;
+        }
+        return spoilt != 0;
+    };
+    bool clean = false;
+    while (__builtin_amdgcn_readfirstlane(__syncthreads_or(pass(clean)))) {  // a pass with `clean` returns false
+        clean = true;
+        first_tile(cur);
+        stage(cur, false);
+    }
+    if (__builtin_expect(clean, false)) {  // the infinities and NaN that the second pass left out
+        first_tile(cur);
+        for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
+            const int k0 = cur.kb + kw * KPW, k1 = min(k0 + KPW, cur.end);
+            for (int k = k0; cur.seg >= 0 && k < k1; ++k) {
+                const char *row = cur.v + (k - cur.kb) * cur.vn;
+                for (int c0 = 0; c0 < a.D; c0 += 64) {
+                    float x = 0.0f;
+                    if (c0 + lane < a.D) {
+                        if constexpr (BF) x = rm_bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(row)[c0 + lane]);
+                        else x = reinterpret_cast<const float *>(row)[c0 + lane];
+                    }
+                    for (uint64_t bad = __ballot(!(fabsf(x) < INFINITY)); bad != 0; bad &= bad - 1) {
+                        const int from = __ffsll(static_cast<unsigned long long>(bad)) - 1;
+                        const float add = __shfl(x, from);
+#pragma unroll
+                        for (int qb = 0; qb < QB; ++qb) {
+                            const bool sees = r_sample[qb] == cur.seg &&
+                                              static_cast<uint32_t>(k - r_lo[qb]) < static_cast<uint32_t>(r_len[qb]);
+                            const int at = sees ? c0 + from - 4 * hi : -1;
+#pragma unroll
+                            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i)
+                                    o[qb][d][i] += at == 32 * d + 8 * (i >> 2) + (i & 3) ? add : 0.0f;
                         }
                     }
                 }
             }
+            if (n_left > 1) advance(cur);
         }
-        cur = nxt;
     }
 
     // ---------------------------------------------------------------- join and write
@@ -576,7 +618,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     float *join = reinterpret_cast<float *>(lds);
     if constexpr (KW > 1) {
         float *ml = join + W * QB * 32 * DH;  // [wave][qb][2][32]
-        rm_dma::wait_barrier<0>();            // every wave has read the last tile
+        rm_dma::wait_barrier<0>();            // every wave has read the last tile (of a second pass)
         if (hi == 0) {
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
