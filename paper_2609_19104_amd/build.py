@@ -27,6 +27,10 @@ HIPCC_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
 
+# The attention kernels' accumulators stay in the registers that ordinary instructions take: the softmax reads and rescales
+# them, and in accumulation registers each such use is a move there and back.
+EXTRA_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for name in ("attn_bf16.hip", "attn_f32.hip")}
+
 
 def hipcc() -> str:
     for cand in (os.environ.get("HIPCC"), shutil.which("hipcc"), "/opt/rocm/bin/hipcc"):
@@ -41,7 +45,7 @@ def sources():
 
 def _compile(src: str, verbose: bool) -> str:
     obj = os.path.join(BUILD_DIR, os.path.basename(src)[:-4] + ".o")
-    cmd = [hipcc(), *HIPCC_FLAGS, f"-I{INCLUDE}", f"-I{CSRC}", "-c", src, "-o", obj]
+    cmd = [hipcc(), *HIPCC_FLAGS, *EXTRA_FLAGS.get(os.path.basename(src), ()), f"-I{INCLUDE}", f"-I{CSRC}", "-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     # The host pass does not know the device-only target feature and says so; that line is not a problem.
     noise = "'-packed-fp32-ops' is not a recognized feature"

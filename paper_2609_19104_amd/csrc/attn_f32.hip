@@ -3,22 +3,22 @@
 
 namespace rm_attn {
 
-template <int DH, int RW, int KW, int QB, int KT, int WPE>
+template <int DH, int RW, int KW, int QB, int KT, int NBUF, int WPE>
 static hipError_t go(const Args &a, hipStream_t st) {
-    attn_kernel<false, DH, RW, KW, QB, KT, WPE>
+    attn_kernel<false, DH, RW, KW, QB, KT, NBUF, WPE>
         <<<dim3(static_cast<unsigned>(a.n_tiles) * a.splits * a.U * a.Hk), 64 * RW * KW, 0, st>>>(a);
     return hipGetLastError();
 }
 
 hipError_t launch_f32(const Plan &p, const Args &a, hipStream_t st) {
     if (p.kw > 1) {
-        if (p.dh == 64) return go<64, 1, 4, 1, 128, 2>(a, st);
-        if (p.dh == 128) return go<128, 1, 4, 1, 128, 1>(a, st);
-        return go<256, 2, 2, 1, 64, 1>(a, st);
+        if (p.dh == 64) return go<64, 1, 4, 1, 128, 1, 2>(a, st);
+        if (p.dh == 128) return go<128, 1, 4, 1, 128, 1, 1>(a, st);
+        return go<256, 2, 2, 1, 64, 1, 1>(a, st);
     }
-    if (p.dh == 64) return go<64, 4, 1, 1, 64, 2>(a, st);
-    if (p.dh == 128) return go<128, 4, 1, 1, 64, 2>(a, st);
-    return go<256, 4, 1, 1, 64, 1>(a, st);
+    if (p.dh == 64) return go<64, 4, 1, 1, 64, 2, 2>(a, st);
+    if (p.dh == 128) return go<128, 4, 1, 1, 64, 1, 2>(a, st);
+    return go<256, 4, 1, 1, 64, 1, 1>(a, st);
 }
 
 }  // namespace rm_attn

@@ -111,20 +111,20 @@ struct Tile {
     int kb, end, seg;
 };
 
-template <bool BF, int DH, int RW, int KW, int QB, int KT, int WPE>
+template <bool BF, int DH, int RW, int KW, int QB, int KT, int NBUF, int WPE>
 __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     constexpr int W = RW * KW, ES = BF ? 2 : 4, ROWB = DH * ES, CPR = ROWB / 16;
     constexpr int RPI = 64 / CPR;             // tile rows per load instruction of a wave (1 KB)
-    constexpr int NI = KT / RPI / W;          // load instructions per wave and matrix
-    constexpr int KPW = KT / KW, NS = KPW / 32;
+    constexpr int KPW = KT / KW, NS = KPW / 32;  // keys of a tile that a wave takes
+    constexpr int NI = KPW / RPI / RW;        // load instructions per wave and matrix
     constexpr int DB = DH / 32;               // output blocks of 32 columns
     constexpr int QF = BF ? DH / 16 : DH / 8; // fragments of a query row block
     constexpr int AHEAD = 4;                  // LDS reads run this many matrix-core steps ahead
-    static_assert(CPR >= 8 && CPR <= 64 && NI >= 1 && NI * RPI * W == KT && NS >= 1, "tile shape");
-    constexpr int TILEB = KT * ROWB;
+    static_assert(CPR >= 8 && CPR <= 64 && NI >= 1 && NI * RPI * RW == KPW && NS * 32 == KPW, "tile shape");
+    constexpr int TILEB = KPW * ROWB, KWB = 2 * NBUF * TILEB;  // one matrix's keys, and all buffers of a key wave
     // O of every wave passes through LDS when the key waves are joined.
     constexpr int JOINB = KW > 1 ? W * QB * 32 * DH * 4 + W * QB * 32 * 8 : 0;
-    constexpr int LDSB = 2 * TILEB > JOINB ? 2 * TILEB : JOINB;
+    constexpr int LDSB = KW * KWB > JOINB ? KW * KWB : JOINB;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[LDSB];
 
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, hi = lane >> 5;
@@ -291,50 +291,66 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         else
             return 8 * ((row >> 2) & 1);
     };
-    const uint32_t lds_k = rm_dma::lds_addr(lds), lds_v = lds_k + TILEB;
+    // A key wave's buffers: NBUF times its keys of a tile, then its values.  The RW waves that share them fill them.
+    uint8_t *const lds_w = lds + kw * KWB;
+    const uint32_t lds_at = rm_dma::lds_addr(lds_w);
     const bool whole_head = a.D == DH;
     // The swizzle of a wave's load instructions repeats every PER of them.
-    constexpr int PERK = W * RPI >= 16 ? 1 : 16 / (W * RPI), PERV = BF || W * RPI >= 8 ? 1 : 8 / (W * RPI);
+    constexpr int PERK = RW * RPI >= 16 ? 1 : 16 / (RW * RPI);
+    constexpr int PERV = BF ? (RW * RPI >= 4 ? 1 : 4 / (RW * RPI)) : (RW * RPI >= 8 ? 1 : 8 / (RW * RPI));
     static_assert(NI % 2 == 0 && NI % PERK == 0 && NI % PERV == 0, "load instructions");
-    auto stage = [&](const Tile &t, bool values) __attribute__((always_inline)) {
+    auto stage = [&](const Tile &t, int buf, bool values) __attribute__((always_inline)) {
         const int64_t sn = uniform(values ? t.vn : t.kn);
-        const char *base = uniform(values ? t.v : t.k);
-        const uint32_t to = (values ? lds_v : lds_k) + wave * 1024;
-        if (whole_head && t.kb + KT <= t.end) {
-            // Row (n W + wave) RPI + lrow: token strides are below 2^24 bytes, so a tile's offsets fit in 32 bits.
-            const uint32_t row0 = (wave * RPI + lrow) * static_cast<uint32_t>(sn);
-            const uint32_t step = W * RPI * static_cast<uint32_t>(sn);
+        const char *base = uniform(values ? t.v : t.k) + kw * KPW * sn;
+        const uint32_t to = lds_at + (buf * 2 + (values ? 1 : 0)) * TILEB + rw * 1024;
+        const int left = t.end - t.kb - kw * KPW;  // keys from the wave's first to the end
+        if (whole_head && left >= KPW) {
+            // Row (n RW + rw) RPI + lrow: token strides are below 2^24 bytes, so a tile's offsets fit in 32 bits.
+            const uint32_t row0 = (rw * RPI + lrow) * static_cast<uint32_t>(sn);
+            const uint32_t step = RW * RPI * static_cast<uint32_t>(sn);
             uint32_t chunk[PERK > PERV ? PERK : PERV];
 #pragma unroll
             for (int n = 0; n < (values ? PERV : PERK); ++n) {
-                const int row = (n * W + wave) * RPI + lrow;
+                const int row = (n * RW + rw) * RPI + lrow;
                 chunk[n] = row0 + (pos ^ (values ? swz_v(row) : swz_k(row))) * 16;
             }
 #pragma unroll
             for (int n = 0; n < NI; n += 2)
-                dma16_pair<W * 1024>(base, chunk[n % (values ? PERV : PERK)] + n * step,
-                                     chunk[(n + 1) % (values ? PERV : PERK)] + (n + 1) * step,
-                                     __builtin_amdgcn_readfirstlane(to + n * W * 1024));
+                dma16_pair<RW * 1024>(base, chunk[n % (values ? PERV : PERK)] + n * step,
+                                      chunk[(n + 1) % (values ? PERV : PERK)] + (n + 1) * step,
+                                      __builtin_amdgcn_readfirstlane(to + n * RW * 1024));
         } else {  // rows past the end and columns past the head's are zeros
             const int64_t zero = reinterpret_cast<int64_t>(&zero16);
-            const char *at = base + (wave * RPI + lrow) * sn;
-            const int left = t.end - t.kb;
+            const char *at = base + (rw * RPI + lrow) * sn;
 #pragma unroll 2
-            for (int n = 0; n < NI; ++n, at += W * RPI * sn) {
-                const int row = (n * W + wave) * RPI + lrow;
+            for (int n = 0; n < NI; ++n, at += RW * RPI * sn) {
+                const int row = (n * RW + rw) * RPI + lrow;
                 const int chunk = pos ^ (values ? swz_v(row) : swz_k(row));
                 // 0 or -1, without a branch
                 const int64_t in = static_cast<int64_t>((row - left) & (chunk * 16 - a.D * ES)) >> 63;
                 const int64_t src = zero + ((reinterpret_cast<int64_t>(at) + chunk * 16 - zero) & in);
-                rm_dma::dma16(reinterpret_cast<const char *>(src), __builtin_amdgcn_readfirstlane(to + n * W * 1024));
+                rm_dma::dma16(reinterpret_cast<const char *>(src), __builtin_amdgcn_readfirstlane(to + n * RW * 1024));
             }
         }
     };
+    // Waits until all but this wave's last `N` loads are there and its LDS reads are done; where several waves share
+    // the buffers, until that holds for all of them.
+    auto sync = [&](auto n) __attribute__((always_inline)) {
+        constexpr int N = decltype(n)::value;
+        if constexpr (RW > 1) rm_dma::wait_barrier<N>();
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    };
+    typedef std::integral_constant<int, 0> None;
+    typedef std::integral_constant<int, NI> OneMatrix;
+    typedef std::integral_constant<int, 63> Any;  // reads only
 
     // ---------------------------------------------------------------- queries
     typedef typename std::conditional<BF, rm_bf16x8, rm_f32x4>::type QFrag;
     QFrag qf[QB][QF];
-    if (n_tiles > 0) stage(cur, false);
+    if (n_tiles > 0) {
+        stage(cur, 0, false);
+        stage(cur, 0, true);
+    }
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
@@ -346,23 +362,23 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         }
 
     // ---------------------------------------------------------------- fragment addresses (bytes in LDS)
-    const uint8_t *kb_ptr[8];  // keys: chunk 2 c + hi of row kw KPW + 32 ns + col, by c mod 8 (the rest are offsets)
+    const uint8_t *kb_ptr[8];  // keys: chunk 2 c + hi of row 32 ns + col, by c mod 8 (the rest are offsets)
     {
-        const int row = kw * KPW + col;
+        const int row = col;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) kb_ptr[c] = lds + row * ROWB + (((2 * c + hi) ^ swz_k(row)) & (CPR - 1)) * 16;
+        for (int c = 0; c < 8; ++c) kb_ptr[c] = lds_w + row * ROWB + (((2 * c + hi) ^ swz_k(row)) & (CPR - 1)) * 16;
     }
     constexpr int VP = BF ? (DB < 4 ? DB : 4) : 2;
     const uint8_t *v_ptr[VP];
     if constexpr (BF) {
-        const int i = (lane & 15) >> 2, row = kw * KPW + 4 * hi + i;
+        const int i = (lane & 15) >> 2, row = 4 * hi + i;
         const int inner = 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
 #pragma unroll
-        for (int d = 0; d < VP; ++d) v_ptr[d] = lds + TILEB + row * ROWB + ((d * 64) ^ (swz_v(i) * 16)) + inner;
+        for (int d = 0; d < VP; ++d) v_ptr[d] = lds_w + TILEB + row * ROWB + ((d * 64) ^ (swz_v(i) * 16)) + inner;
     } else {
-        const int row = kw * KPW + 4 * hi;
+        const int row = 4 * hi;
 #pragma unroll
-        for (int d = 0; d < VP; ++d) v_ptr[d] = lds + TILEB + row * ROWB + ((d * 128) ^ (hi * 128)) + col * 4;
+        for (int d = 0; d < VP; ++d) v_ptr[d] = lds_w + TILEB + row * ROWB + ((d * 128) ^ (hi * 128)) + col * 4;
     }
 
     auto read_v = [](const uint8_t *p) { return read_v_rows<ROWB>(p); };
@@ -385,11 +401,21 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[qb][d] = rm_f32x16{};
         }
+        int buf = 0;
         for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
             Tile nxt = cur;
             if (n_left > 1) advance(nxt);
-            rm_dma::wait_barrier<0>();  // the keys are there, and every wave has read the last tile's values
-            stage(cur, true);
+            const int at = NBUF == 2 ? buf * 2 * TILEB : 0;  // this tile's buffers
+            if constexpr (NBUF == 2) {  // keys and values a tile ahead
+                sync(None{});
+                if (n_left > 1) {
+                    stage(nxt, buf ^ 1, false);
+                    stage(nxt, buf ^ 1, true);
+                }
+                buf ^= 1;
+            } else {  // the tile's keys; its values are under way
+                sync(OneMatrix{});
+            }
 
             const int kbw = cur.kb + kw * KPW;
             bool active = kbw < cur.end, mixed = kbw + KPW > cur.end, apart = false;
@@ -412,7 +438,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                 QFrag kf[QF * NS];
                 auto read_k = [&](int x) {  // x = c NS + ns
                     const int c = x / NS, ns = x % NS;
-                    return *reinterpret_cast<const QFrag *>(kb_ptr[c & 7] + ns * 32 * ROWB + (c >> 3) * 256);
+                    return *reinterpret_cast<const QFrag *>(kb_ptr[c & 7] + at + ns * 32 * ROWB + (c >> 3) * 256);
                 };
 #pragma unroll
                 for (int x = 0; x < QF * NS; ++x) kf[x] = read_k(x);
@@ -431,6 +457,12 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                         }
                     }
                 pipeline<QF * NS, AHEAD, BF ? QB : 4 * QB, 1>();
+            }
+            if constexpr (NBUF == 1) {  // every wave has read the keys: the next ones'
+                sync(Any{});
+                if (n_left > 1) stage(nxt, 0, false);
+            }
+            if (active) {
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
                     if (a.cap != 0.0f) {
@@ -479,15 +511,20 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[qb][ns][i]);
                     top = xor32_max(top) * sc;
-                    if (__any(top > m[qb] + kRaise || (m[qb] == -INFINITY && top > -INFINITY))) {
-                        const float mn = fmaxf(m[qb], top);
-                        const float f = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[qb] - mn);
+                    // Raising the maximum of a row without sums so far (m = -inf) needs no rescaling.
+                    const bool raise = top > m[qb] + kRaise;  // (false for top = -inf)
+                    if (__any(raise)) {
+                        const float mn = raise ? top : m[qb];
+                        const bool any = __any(raise && m[qb] != -INFINITY);
+                        const float f = raise ? __builtin_amdgcn_exp2f(m[qb] - mn) : 1.0f;
                         m[qb] = mn;
-                        l[qb] *= f;
+                        if (any) {
+                            l[qb] *= f;
 #pragma unroll
-                        for (int d = 0; d < DB; ++d)
+                            for (int d = 0; d < DB; ++d)
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) o[qb][d][i] *= f;
+                                for (int i = 0; i < 16; ++i) o[qb][d][i] *= f;
+                        }
                     }
                     const float ref = m[qb] == -INFINITY ? 0.0f : m[qb];
                     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -503,11 +540,14 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                     l[qb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 }
             }
-            rm_dma::wait_barrier<0>();  // the values are there, and every wave has read the keys
+            if constexpr (NBUF == 1) {  // the values
+                if (n_left > 1) sync(OneMatrix{});
+                else sync(None{});
+            }
             if (clean && cur.seg >= 0) {
-                for (int i = tid; i < TILEB / 16; i += 64 * W) {
-                    rm_u32x4 *at = reinterpret_cast<rm_u32x4 *>(lds + TILEB) + i;
-                    rm_u32x4 v = *at;
+                for (int i = rw * 64 + lane; i < TILEB / 16; i += 64 * RW) {
+                    rm_u32x4 *p = reinterpret_cast<rm_u32x4 *>(lds_w + TILEB + at) + i;
+                    rm_u32x4 v = *p;
                     for (int e = 0; e < 4; ++e) {
                         if constexpr (BF) {
                             const uint32_t bad = nonfinite_bf16x2(v[e]);
@@ -516,11 +556,10 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                             v[e] = nonfinite_f32(__uint_as_float(v[e])) ? 0u : v[e];
                         }
                     }
-                    *at = v;
+                    *p = v;
                 }
-                rm_dma::wait_barrier<0>();
+                sync(Any{});
             }
-            if (n_left > 1) stage(nxt, false);
             if (active) {
                 if (apart && !clean) {
 #pragma unroll 1
@@ -528,7 +567,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                         if (!BF && (r & 4)) continue;            // (float32: rows r and r + 4 in the two halves)
 #pragma unroll
                         for (int d = 0; d < DB; ++d) {
-                            const uint8_t *vp = v_ptr[d % VP] + (d / VP) * 256 + r * ROWB;
+                            const uint8_t *vp = v_ptr[d % VP] + at + (d / VP) * 256 + r * ROWB;
                             if constexpr (BF) {
                                 const uint2 v = *reinterpret_cast<const uint2 *>(vp);
                                 spoilt |= nonfinite_bf16x2(v.x) | nonfinite_bf16x2(v.y);
@@ -550,7 +589,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
 #pragma unroll
                     for (int x = 0; x < 2 * NS * DB; ++x) {
                         const int st = x / DB, d = x % DB;
-                        const rm_bf16x8 vf = read_v(v_ptr[d % VP] + (d / VP) * 256 + 16 * st * ROWB);
+                        const rm_bf16x8 vf = read_v(v_ptr[d % VP] + at + (d / VP) * 256 + 16 * st * ROWB);
 #pragma unroll
                         for (int qb = 0; qb < QB; ++qb)
                             o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[qb][st], o[qb][d], 0, 0, 0);
@@ -561,13 +600,17 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                     for (int x = 0; x < 16 * NS * DB; ++x) {
                         const int ns = x / (16 * DB), i = x / DB % 16, d = x % DB;
                         const float vf = *reinterpret_cast<const float *>(
-                            v_ptr[d % VP] + (d / VP) * 256 + (32 * ns + 8 * (i >> 2) + (i & 3)) * ROWB);
+                            v_ptr[d % VP] + at + (d / VP) * 256 + (32 * ns + 8 * (i >> 2) + (i & 3)) * ROWB);
 #pragma unroll
                         for (int qb = 0; qb < QB; ++qb)
                             o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[qb][ns][i], o[qb][d], 0, 0, 0);
                     }
                     pipeline<16 * NS * DB, AHEAD, QB, 1>();
                 }
+            }
+            if constexpr (NBUF == 1) {  // every wave has read the values: the next ones'
+                sync(Any{});
+                if (n_left > 1) stage(nxt, 0, true);
             }
             cur = nxt;
         }
@@ -577,7 +620,8 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     while (__builtin_amdgcn_readfirstlane(__syncthreads_or(pass(clean)))) {  // a pass with `clean` returns false
         clean = true;
         first_tile(cur);
-        stage(cur, false);
+        stage(cur, 0, false);
+        stage(cur, 0, true);
     }
     if (__builtin_expect(clean, false)) {  // the infinities and NaN that the second pass left out
         first_tile(cur);
