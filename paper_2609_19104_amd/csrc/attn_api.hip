@@ -99,6 +99,7 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
         return api_fail(RM_ERR_SHAPE, "too many query rows");
     const int64_t rows = static_cast<int64_t>(R), ng = static_cast<int64_t>(groups);
     q.dh = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+    q.pad = D != q.dh;
     constexpr int64_t kCUs = 256;
     const bool key_waves = ceil_div(rows, 128) * ng < 2 * kCUs || rows <= 32;
     q.kw = key_waves ? 4 : 1;
@@ -140,6 +141,8 @@ rm_status attn_run(const rm_attn_shape *s, const rm_attn::Plan &p, rm_attn::Args
     } else {
         a.scale = s->scale * log2e;
     }
+    a.by_g = rm_attn::divisor(a.G);
+    a.by_t = rm_attn::divisor(a.T);
     a.n_tiles = p.n_tiles;
     a.splits = p.splits;
     if (p.total > 0) {

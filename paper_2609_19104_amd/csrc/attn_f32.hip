@@ -4,21 +4,22 @@
 namespace rm_attn {
 
 template <int DH, int RW, int KW, int QB, int KT, int NBUF, int WPE>
-static hipError_t go(const Args &a, hipStream_t st) {
-    attn_kernel<false, DH, RW, KW, QB, KT, NBUF, WPE>
-        <<<dim3(static_cast<unsigned>(a.n_tiles) * a.splits * a.U * a.Hk), 64 * RW * KW, 0, st>>>(a);
+static hipError_t go(const Plan &p, const Args &a, hipStream_t st) {
+    const dim3 grid(static_cast<unsigned>(a.n_tiles) * a.splits * a.U * a.Hk);
+    if (p.pad) attn_kernel<false, DH, true, RW, KW, QB, KT, NBUF, WPE><<<grid, 64 * RW * KW, 0, st>>>(a);
+    else attn_kernel<false, DH, false, RW, KW, QB, KT, NBUF, WPE><<<grid, 64 * RW * KW, 0, st>>>(a);
     return hipGetLastError();
 }
 
 hipError_t launch_f32(const Plan &p, const Args &a, hipStream_t st) {
     if (p.kw > 1) {
-        if (p.dh == 64) return go<64, 1, 4, 1, 128, 1, 2>(a, st);
-        if (p.dh == 128) return go<128, 1, 4, 1, 128, 1, 1>(a, st);
-        return go<256, 2, 2, 1, 64, 1, 1>(a, st);
+        if (p.dh == 64) return go<64, 1, 4, 1, 128, 1, 2>(p, a, st);
+        if (p.dh == 128) return go<128, 1, 4, 1, 128, 1, 1>(p, a, st);
+        return go<256, 2, 2, 1, 64, 1, 1>(p, a, st);
     }
-    if (p.dh == 64) return go<64, 4, 1, 1, 64, 2, 2>(a, st);
-    if (p.dh == 128) return go<128, 4, 1, 1, 64, 1, 2>(a, st);
-    return go<256, 4, 1, 1, 64, 1, 1>(a, st);
+    if (p.dh == 64) return go<64, 4, 1, 1, 64, 2, 2>(p, a, st);
+    if (p.dh == 128) return go<128, 4, 1, 1, 64, 1, 2>(p, a, st);
+    return go<256, 4, 1, 1, 64, 1, 1>(p, a, st);
 }
 
 }  // namespace rm_attn

@@ -2,23 +2,25 @@
 // attn_f32.hip): one pass over the keys with a running maximum and sum per query row.
 //
 // A workgroup takes 32 RW QB query rows (the tokens of one group times the query heads of one key head, so that a
-// key head's rows are read once for all its query heads) and walks tiles of KT keys that its waves stage in LDS
-// together, keys and values each in one buffer: while the scores of a tile are formed its values arrive, and while
-// they are summed the next tile's keys.  RW of the waves divide the rows and KW the keys of a tile; the KW partial
-// results are joined in LDS at the end.  With `splits` > 1 several workgroups divide a row block's tiles and leave
-// partial results in the workspace for the combine kernel.
+// key head's rows are read once for all its query heads) and walks tiles of KT keys.  RW of its waves divide the rows
+// and KW the keys of a tile; the waves that take the same keys load them straight into LDS buffers of their own, so
+// with RW = 1 no wave waits for another before the KW partial results are joined in LDS at the end.  With `splits` > 1
+// several workgroups divide a row block's tiles and leave partial results in the workspace for the combine kernel.
 //
 // Matrix-core layout (32x32 tiles): S^T = K Q^T, so a lane holds scores of one query row (column lane % 32) and
 // row statistics, spans and slopes are one register per lane; O^T = V^T P^T takes P straight from the score
 // registers: the 16 keys of a matrix-core step may come in any order as long as V's rows come in the same, and the
 // order the scores have (keys 16 s + 4 h + {0..3} and + 8 for lane half h) is the one V's fragments are read in.
+//
+// What bounds it: a compute unit loads 64 bytes a cycle into LDS and reads 128, and a matrix-core step of 32 cycles
+// takes one KB from LDS per wave.  The load instructions go out between the matrix-core steps, since a wave that
+// issues several in a row waits for the load unit (16 cycles an instruction and wave).
 #pragma once
 
 #include "rm_attn_plan.h"
 #include "rm_dma.h"
 
 typedef float rm_f32x16 __attribute__((ext_vector_type(16)));
-typedef float rm_f32x8 __attribute__((ext_vector_type(8)));
 typedef short rm_s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 rm_bf16x4 __attribute__((ext_vector_type(4)));
 
@@ -30,20 +32,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 // most tiles need no rescaling of the output registers.
 constexpr float kRaise = 8.0f;
 
-static __device__ uint4 zero16;  // what rows and columns outside a tile are staged from
-
-// rm_dma::dma16 for two loads, STEP bytes apart in LDS, each lane at its 32-bit offset from a base in scalar registers.
-template <int STEP>
-__device__ __forceinline__ void dma16_pair(const void *base, uint32_t off0, uint32_t off1, uint32_t lds) {
-    uint32_t keep;
-    asm volatile(
-        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
-        "s_add_u32 m0, m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
-        : "=&s"(keep)
-        : "v"(off0), "v"(off1), "s"(base), "s"(lds), "n"(STEP)
-        : "memory", "scc");
-}
-
 // A value that is the same in every lane, in scalar registers.
 __device__ __forceinline__ int64_t uniform(int64_t x) {
     const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x));
@@ -54,7 +42,34 @@ __device__ __forceinline__ const char *uniform(const char *p) {
     return reinterpret_cast<const char *>(uniform(reinterpret_cast<int64_t>(p)));
 }
 
-__device__ __forceinline__ float xor32_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
+// Two loads of 16 bytes per lane straight into LDS at lds + 16 lane and lds + STEP + 16 lane, each lane at its 32-bit
+// offset from a base in scalar registers; only the lanes of mask0 (mask1) take part.  M0 and EXEC are kept and put back.
+// No memory clobber: the buffers are read between the waits below only, which have one.
+template <int STEP>
+__device__ __forceinline__ void dma16_pair(const void *base, uint32_t off0, uint32_t off1, uint32_t lds, uint64_t mask0,
+                                           uint64_t mask1) {
+    uint32_t keep;
+    uint64_t exec;
+    mask0 = uniform(static_cast<int64_t>(mask0));
+    mask1 = uniform(static_cast<int64_t>(mask1));
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_and_saveexec_b64 %1, %7\n\tglobal_load_lds_dwordx4 %2, %4\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_and_b64 exec, %1, %8\n\tglobal_load_lds_dwordx4 %3, %4\n\t"
+        "s_mov_b64 exec, %1\n\ts_mov_b32 m0, %0"
+        : "=&s"(keep), "=&s"(exec)
+        : "v"(off0), "v"(off1), "s"(uniform(static_cast<const char *>(base))), "s"(lds), "n"(STEP), "s"(mask0), "s"(mask1)
+        : "scc");
+}
+
+// The other lane half's value joined with this one's.
+__device__ __forceinline__ float xor32_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float xor32_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
 // a * b rounded, not part of a fused multiply-add.
 __device__ __forceinline__ float scaled(float a, float b) {
@@ -62,14 +77,17 @@ __device__ __forceinline__ float scaled(float a, float b) {
     return a * b;
 }
 
-__device__ __forceinline__ int wave_min(int v) {
-    for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o));
-    return __builtin_amdgcn_readfirstlane(v);
-}
+// Maximum over the wave, in data-parallel steps along the rows of 16 lanes and then across them.
 __device__ __forceinline__ int wave_max(int v) {
-    for (int o = 32; o >= 1; o >>= 1) v = max(v, __shfl_xor(v, o));
-    return __builtin_amdgcn_readfirstlane(v);
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x111, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x112, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x114, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x118, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x142, 0xa, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(v, 63);
 }
+__device__ __forceinline__ int wave_min(int v) { return -wave_max(-v); }  // (no value here is INT_MIN)
 
 // Whether any of the values packed in v is infinite or NaN (all exponent bits set): the carry out of the exponent
 // field reaches the sign bit.
@@ -91,17 +109,9 @@ __device__ __forceinline__ rm_bf16x8 read_v_rows(const uint8_t *p) {
     return __builtin_bit_cast(rm_bf16x8, v);
 }
 
-// Scheduling of a block of N steps of R LDS reads and M matrix-core instructions each: the reads run AHEAD steps ahead.
-template <int N, int AHEAD, int M, int R>
-__device__ __forceinline__ void pipeline() {
-    constexpr int A = AHEAD < N ? AHEAD : N;
-    __builtin_amdgcn_sched_group_barrier(0x100, A * R, 0);
-#pragma unroll
-    for (int i = 0; i < N - A; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, A * M, 0);
+
+__device__ __forceinline__ int divide(int n, Divisor d) {  // n < 2^30
+    return d.mul == 0 ? n : static_cast<int>(__umulhi(static_cast<uint32_t>(n), d.mul) >> d.shift);
 }
 
 // One tile's place: keys [kb, min(kb + KT, end)) of segment seg (-1: the group's shared keys, else a sample).
@@ -111,16 +121,18 @@ struct Tile {
     int kb, end, seg;
 };
 
-template <bool BF, int DH, int RW, int KW, int QB, int KT, int NBUF, int WPE>
+// PAD: the head is narrower than the kernel's DH columns.
+template <bool BF, int DH, bool PAD, int RW, int KW, int QB, int KT, int NBUF, int WPE>
 __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     constexpr int W = RW * KW, ES = BF ? 2 : 4, ROWB = DH * ES, CPR = ROWB / 16;
-    constexpr int RPI = 64 / CPR;             // tile rows per load instruction of a wave (1 KB)
+    constexpr int RPI = 64 / CPR;                // rows per load instruction of a wave (1 KB)
     constexpr int KPW = KT / KW, NS = KPW / 32;  // keys of a tile that a wave takes
-    constexpr int NI = KPW / RPI / RW;        // load instructions per wave and matrix
-    constexpr int DB = DH / 32;               // output blocks of 32 columns
-    constexpr int QF = BF ? DH / 16 : DH / 8; // fragments of a query row block
-    constexpr int AHEAD = 4;                  // LDS reads run this many matrix-core steps ahead
-    static_assert(CPR >= 8 && CPR <= 64 && NI >= 1 && NI * RPI * RW == KPW && NS * 32 == KPW, "tile shape");
+    constexpr int NP = KPW / RPI / RW / 2;       // pairs of load instructions per wave and matrix
+    constexpr int STEP = RW * RPI;               // rows from one of a wave's load instructions to the next
+    constexpr int DB = DH / 32;                  // output blocks of 32 columns
+    constexpr int QF = BF ? DH / 16 : DH / 8;    // fragments of a query row block
+    constexpr int AHEAD = 4;                     // LDS reads run this many matrix-core steps ahead
+    static_assert(CPR >= 8 && CPR <= 64 && NP >= 1 && NP * 2 * STEP == KPW && NS * 32 == KPW, "tile shape");
     constexpr int TILEB = KPW * ROWB, KWB = 2 * NBUF * TILEB;  // one matrix's keys, and all buffers of a key wave
     // O of every wave passes through LDS when the key waves are joined.
     constexpr int JOINB = KW > 1 ? W * QB * 32 * DH * 4 + W * QB * 32 * 8 : 0;
@@ -150,78 +162,96 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     const int u = ng / a.Hk, hk = ng % a.Hk;
     const int rows_end = min(row0 + 32 * RW * QB, a.R);
 
-    // ---------------------------------------------------------------- rows
-    const int n0 = a.n0 == 0 ? 0 : (a.len0 ? min(max(a.len0[u], 0), a.n0) : a.n0);
-    int r_sample[QB], r_lo[QB], r_len[QB];
-    float r_slope[QB];
-    int r_pos[QB];
-    int w_maxlo = 0, w_minhi = 0x7fffffff, w_minlo = 0x7fffffff, w_maxhi = 0, w_s0 = 0x7fffffff, w_s1 = -1;
-    const char *qrow[QB];
-    char *orow[QB];
-    bool r_ok[QB];
+    // ---------------------------------------------------------------- queries
+    typedef typename std::conditional<BF, rm_bf16x8, rm_f32x4>::type QFrag;
+    QFrag qf[QB][QF];
+    int r_smp[QB], r_tok[QB], r_head[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const int r = row0 + (rw * QB + qb) * 32 + col;
-        r_ok[qb] = r < a.R;
-        const int rc = min(r, a.R - 1);
-        const int tok = rc / a.G, g = rc - tok * a.G;
-        const int smp = tok / a.T, t = tok - smp * a.T;
-        const int64_t b = static_cast<int64_t>(u) * a.per + smp;
-        const int h = hk * a.G + g;
-        qrow[qb] = a.q + b * a.q_b + t * a.q_t + h * a.q_h;
-        orow[qb] = a.o + b * a.o_b + t * a.o_t + h * a.o_h;
-        int lo = 0, end = a.n1;
-        if (a.span) {
-            const int2 sp = *reinterpret_cast<const int2 *>(a.span + 2 * (b * a.T + t));
-            lo = min(max(sp.x, 0), a.n1);
-            end = min(max(sp.y, 0), a.n1);
-        } else if (a.n1 > 0) {
-            if (a.len1) end = min(max(a.len1[b], 0), a.n1);
-            if (a.causal) end = min(max(end - a.T + t + 1, 0), end);
+        const int r = min(row0 + (rw * QB + qb) * 32 + col, a.R - 1);
+        const int tok = divide(r, a.by_g);
+        r_head[qb] = hk * a.G + r - tok * a.G;
+        r_smp[qb] = divide(tok, a.by_t);
+        r_tok[qb] = tok - r_smp[qb] * a.T;
+        const char *q = a.q + (static_cast<int64_t>(u) * a.per + r_smp[qb]) * a.q_b + r_tok[qb] * a.q_t +
+                        r_head[qb] * a.q_h;
+#pragma unroll
+        for (int c = 0; c < QF; ++c) {
+            const int byte = (2 * c + hi) * 16;
+            rm_u32x4 v = {0, 0, 0, 0};
+            if (!PAD || byte < a.D * ES) v = *reinterpret_cast<const rm_u32x4 *>(q + byte);
+            qf[qb][c] = __builtin_bit_cast(QFrag, v);
         }
-        r_sample[qb] = smp;
-        r_lo[qb] = lo;
-        r_len[qb] = max(end - lo, 0);
-        r_slope[qb] = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
-        r_pos[qb] = (a.slopes && a.q_start ? a.q_start[b] : 0) + t;
-        if (r_ok[qb]) {
-            if (r_len[qb] > 0) {
+    }
+
+    // ---------------------------------------------------------------- the keys that rows see
+    // Of the wave's rows: the first and last sample, and over the own keys that rows see the least and greatest begin
+    // and end (greatest begin INT_MAX or least end 0 where a row sees none: no tile is whole for it).
+    const int w_row = row0 + rw * QB * 32, w_last = min(w_row + QB * 32, a.R) - 1;
+    const int w_s0 = w_row < a.R ? divide(divide(w_row, a.by_g), a.by_t) : 0x7fffffff;
+    const int w_s1 = w_row < a.R ? divide(divide(w_last, a.by_g), a.by_t) : -1;
+    const int s_first = divide(divide(row0, a.by_g), a.by_t), s_last = divide(divide(rows_end - 1, a.by_g), a.by_t);
+    const int n0 = a.n0 == 0 ? 0 : (a.len0 ? min(max(a.len0[u], 0), a.n0) : a.n0);
+    auto own_len = [&](int smp) __attribute__((always_inline)) {
+        return a.n1 > 0 && a.len1 ? min(max(a.len1[static_cast<int64_t>(u) * a.per + smp], 0), a.n1) : a.n1;
+    };
+    auto causal_end = [&](int len, int t) __attribute__((always_inline)) { return min(max(len - a.T + t + 1, 0), len); };
+    int r_lo[QB], r_len[QB];
+    int w_maxlo = 0, w_minhi = 0x7fffffff, w_minlo = 0, w_maxhi = 0x7fffffff;
+    int b_lo = 0, b_hi = 0;  // with spans: the keys that any of the workgroup's rows sees
+    if (a.span) {
+        const int2 *span = reinterpret_cast<const int2 *>(a.span) + static_cast<int64_t>(u) * a.T;
+        w_maxlo = 0, w_minhi = 0x7fffffff, w_minlo = 0x7fffffff, w_maxhi = 0;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const int2 sp = span[r_tok[qb]];
+            const int lo = min(max(sp.x, 0), a.n1), end = min(max(sp.y, 0), a.n1);
+            r_lo[qb] = lo;
+            r_len[qb] = max(end - lo, 0);
+            if (lo < end) {
                 w_maxlo = max(w_maxlo, lo);
                 w_minhi = min(w_minhi, end);
                 w_minlo = min(w_minlo, lo);
                 w_maxhi = max(w_maxhi, end);
             } else {
-                w_maxlo = 0x7fffffff;  // no tile is whole for a row that sees nothing
+                w_maxlo = 0x7fffffff;
             }
-            w_s0 = min(w_s0, smp);
-            w_s1 = max(w_s1, smp);
+        }
+        w_maxlo = wave_max(w_maxlo);
+        w_minhi = wave_min(w_minhi);
+        w_minlo = wave_min(w_minlo);
+        w_maxhi = wave_max(w_maxhi);
+        b_lo = w_minlo;
+        b_hi = w_maxhi;
+        if constexpr (RW > 1) {  // the other waves' rows
+            int lo = 0x7fffffff, end = 0;
+            const int t0 = divide(row0, a.by_g), t1 = divide(rows_end - 1, a.by_g);
+            for (int t = t0 + lane; t <= t1; t += 64) {
+                const int2 sp = span[t];
+                const int x = min(max(sp.x, 0), a.n1), y = min(max(sp.y, 0), a.n1);
+                if (x < y) {
+                    lo = min(lo, x);
+                    end = max(end, y);
+                }
+            }
+            b_lo = wave_min(lo);
+            b_hi = wave_max(end);
+        }
+        b_lo = min(b_lo, b_hi);
+    } else {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const int len = own_len(r_smp[qb]);
+            r_lo[qb] = 0;
+            r_len[qb] = a.causal ? causal_end(len, r_tok[qb]) : len;
+        }
+        if (a.causal && w_s0 == w_s1) {  // (rows of several samples make every tile partial anyway)
+            const int len = __builtin_amdgcn_readfirstlane(own_len(w_s0));
+            w_minhi = causal_end(len, divide(w_row, a.by_g) - w_s0 * a.T);
         }
     }
-    w_maxlo = wave_max(w_maxlo);
-    w_minhi = wave_min(w_minhi);
-    w_minlo = wave_min(w_minlo);
-    w_maxhi = wave_max(w_maxhi);
-    w_s0 = wave_min(w_s0);
-    w_s1 = wave_max(w_s1);
 
     // ---------------------------------------------------------------- segments of keys
-    const int s_first = row0 / a.G / a.T, s_last = (rows_end - 1) / a.G / a.T;
-    int b_lo = 0, b_hi = 0;  // with spans: the keys that any of the workgroup's rows sees
-    if (a.span) {
-        int lo = 0x7fffffff, end = 0;
-        const int t0 = row0 / a.G, t1 = (rows_end - 1) / a.G;
-        for (int t = t0 + lane; t <= t1; t += 64) {
-            const int2 sp = *reinterpret_cast<const int2 *>(a.span + 2 * (static_cast<int64_t>(u) * a.T + t));
-            const int x = min(max(sp.x, 0), a.n1), y = min(max(sp.y, 0), a.n1);
-            if (x < y) {
-                lo = min(lo, x);
-                end = max(end, y);
-            }
-        }
-        b_lo = wave_min(lo);
-        b_hi = wave_max(end);
-        if (b_lo > b_hi) b_lo = b_hi;
-    }
     auto seg_keys = [&](int sg, int &lo, int &end) __attribute__((always_inline)) {
         lo = 0;
         if (sg < 0) {
@@ -230,9 +260,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             lo = b_lo;
             end = b_hi;
         } else {
-            end = a.n1;
-            if (a.n1 > 0 && a.len1)
-                end = __builtin_amdgcn_readfirstlane(min(max(a.len1[static_cast<int64_t>(u) * a.per + sg], 0), a.n1));
+            end = __builtin_amdgcn_readfirstlane(own_len(sg));
         }
     };
     auto seg_base = [&](Tile &t) __attribute__((always_inline)) {
@@ -249,7 +277,11 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         seg_keys(sg, lo, end);
         total += (end - lo + KT - 1) / KT;
     }
-    const int64_t first = total * split / a.splits, n_tiles = total * (split + 1) / a.splits - first;
+    int64_t first = 0, n_tiles = total;
+    if (a.splits > 1) {
+        first = total * split / a.splits;
+        n_tiles = total * (split + 1) / a.splits - first;
+    }
     auto first_tile = [&](Tile &t) __attribute__((always_inline)) {
         int64_t skip = first;
         t.seg = -1;
@@ -266,8 +298,6 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         }
         seg_base(t);
     };
-    Tile cur;
-    first_tile(cur);
     auto advance = [&](Tile &t) __attribute__((always_inline)) {  // only called when another tile follows
         t.kb += KT;
         if (t.kb < t.end) {
@@ -283,7 +313,12 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     };
 
     // ---------------------------------------------------------------- staging
-    const int lrow = lane / CPR, pos = lane % CPR;
+    // A key wave's buffers: NBUF times its keys of a tile, then its values; the RW waves that share them fill them.  A
+    // row's 16-byte chunk c lies at c ^ swz(row), so that the lanes of a fragment read, 16 rows at one chunk, take
+    // different banks.  The load instruction n of a wave brings rows n STEP + (rw RPI + lane / CPR); the two terms have no
+    // bits in common, so swz of the sum is swz of one ^ swz of the other.
+    uint8_t *const lds_w = lds + kw * KWB;
+    const uint32_t lds_at = rm_dma::lds_addr(lds_w) + rw * 1024;
     auto swz_k = [](int row) { return CPR == 8 ? (row >> 1) & 7 : row & 15; };
     auto swz_v = [](int row) {
         if constexpr (BF)
@@ -291,47 +326,33 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         else
             return 8 * ((row >> 2) & 1);
     };
-    // A key wave's buffers: NBUF times its keys of a tile, then its values.  The RW waves that share them fill them.
-    uint8_t *const lds_w = lds + kw * KWB;
-    const uint32_t lds_at = rm_dma::lds_addr(lds_w);
-    const bool whole_head = a.D == DH;
-    // The swizzle of a wave's load instructions repeats every PER of them.
-    constexpr int PERK = RW * RPI >= 16 ? 1 : 16 / (RW * RPI);
-    constexpr int PERV = BF ? (RW * RPI >= 4 ? 1 : 4 / (RW * RPI)) : (RW * RPI >= 8 ? 1 : 8 / (RW * RPI));
-    static_assert(NI % 2 == 0 && NI % PERK == 0 && NI % PERV == 0, "load instructions");
-    auto stage = [&](const Tile &t, int buf, bool values) __attribute__((always_inline)) {
-        const int64_t sn = uniform(values ? t.vn : t.kn);
-        const char *base = uniform(values ? t.v : t.k) + kw * KPW * sn;
-        const uint32_t to = lds_at + (buf * 2 + (values ? 1 : 0)) * TILEB + rw * 1024;
-        const int left = t.end - t.kb - kw * KPW;  // keys from the wave's first to the end
-        if (whole_head && left >= KPW) {
-            // Row (n RW + rw) RPI + lrow: token strides are below 2^24 bytes, so a tile's offsets fit in 32 bits.
-            const uint32_t row0 = (rw * RPI + lrow) * static_cast<uint32_t>(sn);
-            const uint32_t step = RW * RPI * static_cast<uint32_t>(sn);
-            uint32_t chunk[PERK > PERV ? PERK : PERV];
+    const int lrow = rw * RPI + lane / CPR;
+    const uint32_t chunk_k = (lane % CPR ^ swz_k(lrow)) * 16, chunk_v = (lane % CPR ^ swz_v(lrow)) * 16;
+    // Loads of pair p of a matrix of tile t into buffer buf.  Rows past the last key are that key again (their scores are
+    // masked); columns past the head's are zeros of the keys, set once, and any of the values.  Token strides are below
+    // 2^24 bytes, so a tile's offsets fit in 32 bits.
+    auto stage = [&](const Tile &t, int buf, bool values, int p, uint64_t mask) __attribute__((always_inline)) {
+        const uint32_t sn = static_cast<uint32_t>(values ? t.vn : t.kn);
+        const int last = t.end - 1 - t.kb;
+        int row = kw * KPW + lrow;
+        uint32_t chunk = values ? chunk_v : chunk_k;
+        asm volatile("" : "+v"(row), "+v"(chunk));  // (else every instruction's offset is kept in a register)
+        uint32_t off[2];
+        uint64_t m[2] = {mask, mask};
 #pragma unroll
-            for (int n = 0; n < (values ? PERV : PERK); ++n) {
-                const int row = (n * RW + rw) * RPI + lrow;
-                chunk[n] = row0 + (pos ^ (values ? swz_v(row) : swz_k(row))) * 16;
+        for (int i = 0; i < 2; ++i) {
+            const int n = 2 * p + i;
+            uint32_t c = chunk ^ static_cast<uint32_t>((values ? swz_v(n * STEP) : swz_k(n * STEP)) * 16);
+            if constexpr (PAD) {
+                if (values) c = min(c, static_cast<uint32_t>(a.D * ES - 16));
+                else m[i] &= __ballot(c < static_cast<uint32_t>(a.D * ES));
             }
-#pragma unroll
-            for (int n = 0; n < NI; n += 2)
-                dma16_pair<RW * 1024>(base, chunk[n % (values ? PERV : PERK)] + n * step,
-                                      chunk[(n + 1) % (values ? PERV : PERK)] + (n + 1) * step,
-                                      __builtin_amdgcn_readfirstlane(to + n * RW * 1024));
-        } else {  // rows past the end and columns past the head's are zeros
-            const int64_t zero = reinterpret_cast<int64_t>(&zero16);
-            const char *at = base + (rw * RPI + lrow) * sn;
-#pragma unroll 2
-            for (int n = 0; n < NI; ++n, at += RW * RPI * sn) {
-                const int row = (n * RW + rw) * RPI + lrow;
-                const int chunk = pos ^ (values ? swz_v(row) : swz_k(row));
-                // 0 or -1, without a branch
-                const int64_t in = static_cast<int64_t>((row - left) & (chunk * 16 - a.D * ES)) >> 63;
-                const int64_t src = zero + ((reinterpret_cast<int64_t>(at) + chunk * 16 - zero) & in);
-                rm_dma::dma16(reinterpret_cast<const char *>(src), __builtin_amdgcn_readfirstlane(to + n * RW * 1024));
-            }
+            off[i] = (static_cast<uint32_t>(min(row + n * STEP, last)) & 0xffffffu) * (sn & 0xffffffu) + c;
         }
+        dma16_pair<RW * 1024>(values ? t.v : t.k, off[0], off[1],
+                              __builtin_amdgcn_readfirstlane(lds_at + (buf * 2 + (values ? 1 : 0)) * TILEB +
+                                                             2 * p * RW * 1024),
+                              m[0], m[1]);
     };
     // Waits until all but this wave's last `N` loads are there and its LDS reads are done; where several waves share
     // the buffers, until that holds for all of them.
@@ -340,55 +361,61 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         if constexpr (RW > 1) rm_dma::wait_barrier<N>();
         else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
     };
+    // Loads in flight when a matrix is waited for: with two buffers the whole other matrix, with one the pairs of the next
+    // keys that go out during the softmax.
+    constexpr int NH = NBUF == 2 ? 0 : NP / 2;
     typedef std::integral_constant<int, 0> None;
-    typedef std::integral_constant<int, NI> OneMatrix;
+    typedef std::integral_constant<int, NBUF == 2 ? 2 * NP : 2 * NH> Others;
     typedef std::integral_constant<int, 63> Any;  // reads only
+    constexpr uint64_t kAll = ~0ull;
 
-    // ---------------------------------------------------------------- queries
-    typedef typename std::conditional<BF, rm_bf16x8, rm_f32x4>::type QFrag;
-    QFrag qf[QB][QF];
-    if (n_tiles > 0) {
-        stage(cur, 0, false);
-        stage(cur, 0, true);
-    }
+    Tile cur;
+    first_tile(cur);
+    auto start = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
+        for (int p = 0; p < NP; ++p) stage(cur, 0, false, p, kAll);
+        if constexpr (NBUF == 2) {
 #pragma unroll
-        for (int c = 0; c < QF; ++c) {
-            const int byte = (2 * c + hi) * 16;
-            rm_u32x4 v = {0, 0, 0, 0};
-            if (byte < a.D * ES) v = *reinterpret_cast<const rm_u32x4 *>(qrow[qb] + byte);
-            qf[qb][c] = __builtin_bit_cast(QFrag, v);
+            for (int p = 0; p < NP; ++p) stage(cur, 0, true, p, kAll);
         }
-
-    // ---------------------------------------------------------------- fragment addresses (bytes in LDS)
-    const uint8_t *kb_ptr[8];  // keys: chunk 2 c + hi of row 32 ns + col, by c mod 8 (the rest are offsets)
-    {
-        const int row = col;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) kb_ptr[c] = lds_w + row * ROWB + (((2 * c + hi) ^ swz_k(row)) & (CPR - 1)) * 16;
+    };
+    if constexpr (PAD) {
+        for (int b = 0; b < NBUF; ++b)
+            for (int i = rw * 64 + lane; i < TILEB / 16; i += 64 * RW)
+                *(reinterpret_cast<rm_u32x4 *>(lds_w + 2 * b * TILEB) + i) = rm_u32x4{0, 0, 0, 0};
+        sync(None{});
     }
+    if (n_tiles > 0) start();
+
+    // ---------------------------------------------------------------- fragment addresses
+    const uint8_t *kb_ptr[8];  // keys: chunk 2 c + hi of row 32 ns + col, by c mod 8 (the rest are offsets)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) kb_ptr[c] = lds_w + col * ROWB + (((2 * c + hi) ^ swz_k(col)) & (CPR - 1)) * 16;
     constexpr int VP = BF ? (DB < 4 ? DB : 4) : 2;
     const uint8_t *v_ptr[VP];
     if constexpr (BF) {
-        const int i = (lane & 15) >> 2, row = 4 * hi + i;
-        const int inner = 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+        const int i = (lane & 15) >> 2, inner = 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
 #pragma unroll
-        for (int d = 0; d < VP; ++d) v_ptr[d] = lds_w + TILEB + row * ROWB + ((d * 64) ^ (swz_v(i) * 16)) + inner;
+        for (int d = 0; d < VP; ++d)
+            v_ptr[d] = lds_w + TILEB + (4 * hi + i) * ROWB + ((d * 64) ^ (swz_v(i) * 16)) + inner;
     } else {
-        const int row = 4 * hi;
 #pragma unroll
-        for (int d = 0; d < VP; ++d) v_ptr[d] = lds_w + TILEB + row * ROWB + ((d * 128) ^ (hi * 128)) + col * 4;
+        for (int d = 0; d < VP; ++d) v_ptr[d] = lds_w + TILEB + 4 * hi * ROWB + ((d * 128) ^ (hi * 128)) + col * 4;
     }
 
-    auto read_v = [](const uint8_t *p) { return read_v_rows<ROWB>(p); };
     rm_f32x16 o[QB][DB];
-    float m[QB], l[QB];
+    float m[QB], l[QB], r_slope[QB];
+    int r_pos[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        r_slope[qb] = a.slopes ? a.slopes[r_head[qb]] * kLog2e : 0.0f;
+        r_pos[qb] = (a.slopes && a.q_start ? a.q_start[u] : 0) + r_tok[qb];  // (slopes: one sample a group)
+    }
     // Scores with a cap or a bias are formed in powers of two; plain ones are scaled on the way into exp2.
     const float sc = a.cap != 0.0f || a.slopes ? 1.0f : a.scale;
 
     // ---------------------------------------------------------------- tiles
-    // One pass over the slice's tiles, the first one's keys under way.  Returns whether a tile of keys that some rows
+    // One pass over the slice's tiles, the first one's loads under way.  Returns whether a tile of keys that some rows
     // see and others do not holds infinities or NaN among its values: 0 times those would spoil the rows that do not
     // see them.  Such a workgroup (there is hardly ever one) makes a second pass with `clean`, which sets them to 0 in
     // LDS, the other sums staying as they are bit for bit, and then adds them to the rows that see them.
@@ -404,46 +431,35 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         int buf = 0;
         for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
             Tile nxt = cur;
-            if (n_left > 1) advance(nxt);
-            const int at = NBUF == 2 ? buf * 2 * TILEB : 0;  // this tile's buffers
-            if constexpr (NBUF == 2) {  // keys and values a tile ahead
-                sync(None{});
-                if (n_left > 1) {
-                    stage(nxt, buf ^ 1, false);
-                    stage(nxt, buf ^ 1, true);
-                }
-                buf ^= 1;
-            } else {  // the tile's keys; its values are under way
-                sync(OneMatrix{});
-            }
+            const bool more = n_left > 1;
+            if (more) advance(nxt);
+            const uint64_t next = more ? kAll : 0;  // the lanes that load the next tile
+            const int at = NBUF == 2 ? buf * 2 * TILEB : 0;    // this tile's buffers
+            if constexpr (NBUF == 2) buf ^= 1;
+            sync(std::conditional_t<NBUF == 2, Others, None>{});  // the keys
 
             const int kbw = cur.kb + kw * KPW;
-            bool active = kbw < cur.end, mixed = kbw + KPW > cur.end, apart = false;
-            if (cur.seg >= 0) {
-                active = active && cur.seg >= w_s0 && cur.seg <= w_s1 && kbw < w_maxhi && kbw + KPW > w_minlo;
-                apart = w_s0 != w_s1 || kbw < w_maxlo || min(kbw + KPW, cur.end) > w_minhi;
-                mixed = mixed || apart;
-            }
-            auto interval = [&](int qb, int &lo, int &len) {  // the keys of this segment that the lane's row sees
-                lo = cur.seg < 0 ? 0 : r_lo[qb];
-                len = cur.seg < 0 ? n0 : (r_sample[qb] == cur.seg ? r_len[qb] : 0);
-            };
+            bool mixed = kbw + KPW > cur.end;  // keys that not all rows see
+            if (cur.seg >= 0)
+                mixed = mixed || cur.seg != w_s0 || cur.seg != w_s1 || kbw < w_maxlo || kbw + KPW > w_minhi;
+
             rm_f32x16 s[QB][NS];
-            if (active) {
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb)
+            for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-                    for (int ns = 0; ns < NS; ++ns) s[qb][ns] = rm_f32x16{};
-                // Key fragments AHEAD ahead of the products that take them.
-                QFrag kf[QF * NS];
-                auto read_k = [&](int x) {  // x = c NS + ns
+                for (int ns = 0; ns < NS; ++ns) s[qb][ns] = rm_f32x16{};
+            {  // S^T = K Q^T; with two buffers the next tile's keys go out meanwhile, with one this tile's values
+                constexpr int X = QF * NS;
+                QFrag kf[X];
+                auto read_k = [&](int x) __attribute__((always_inline)) {
                     const int c = x / NS, ns = x % NS;
-                    return *reinterpret_cast<const QFrag *>(kb_ptr[c & 7] + at + ns * 32 * ROWB + (c >> 3) * 256);
+                    kf[x] = *reinterpret_cast<const QFrag *>(kb_ptr[c & 7] + at + ns * 32 * ROWB + (c >> 3) * 256);
                 };
 #pragma unroll
-                for (int x = 0; x < QF * NS; ++x) kf[x] = read_k(x);
+                for (int x = 0; x < AHEAD; ++x) read_k(x);
 #pragma unroll
-                for (int x = 0; x < QF * NS; ++x)
+                for (int x = 0; x < X; ++x) {
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb) {
                         if constexpr (BF) {
@@ -456,95 +472,106 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                                                                                     s[qb][x % NS], 0, 0, 0);
                         }
                     }
-                pipeline<QF * NS, AHEAD, BF ? QB : 4 * QB, 1>();
+                    if (x + AHEAD < X) read_k(x + AHEAD);
+#pragma unroll
+                    for (int p = x * NP / X; p < (x + 1) * NP / X; ++p) {
+                        if constexpr (NBUF == 2) stage(nxt, buf, false, p, next);
+                        else stage(cur, 0, true, p, kAll);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if constexpr (NBUF == 1) {  // every wave has read the keys: the next ones'
-                sync(Any{});
-                if (n_left > 1) stage(nxt, 0, false);
-            }
-            if (active) {
+            if constexpr (NBUF == 1) sync(Any{});  // every wave has read the keys: the next ones may come
+            auto interval = [&](int qb, int &lo, int &len) {  // the keys of this segment that the lane's row sees
+                lo = cur.seg < 0 ? 0 : r_lo[qb];
+                len = cur.seg < 0 ? n0 : (r_smp[qb] == cur.seg ? r_len[qb] : 0);
+            };
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb) {
-                    if (a.cap != 0.0f) {
-#pragma unroll
-                        for (int ns = 0; ns < NS; ++ns)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const float z = s[qb][ns][i] * a.scale;  // score / cap
-                                float th;
-                                if constexpr (BF)
-                                    th = 1.0f - 2.0f * __builtin_amdgcn_rcpf(
-                                                           __builtin_amdgcn_exp2f(z * (2.0f * kLog2e)) + 1.0f);
-                                else
-                                    th = tanhf(z);
-                                s[qb][ns][i] = a.cap * th;
-                            }
-                    }
-                    if (a.slopes) {
-                        const float in = a.cap != 0.0f ? 1.0f : a.scale;
-#pragma unroll
-                        for (int ns = 0; ns < NS; ++ns) {
-                            const int d0 = r_pos[qb] - (kbw + 32 * ns + 4 * hi);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                s[qb][ns][i] = s[qb][ns][i] * in -
-                                               r_slope[qb] * fabsf(static_cast<float>(d0 - (8 * (i >> 2) + (i & 3))));
-                        }
-                    }
-                    if (mixed) {
-                        int lo, len;
-                        interval(qb, lo, len);
-#pragma unroll
-                        for (int ns = 0; ns < NS; ++ns) {
-                            const int d0 = kbw + 32 * ns + 4 * hi - lo;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                s[qb][ns][i] =
-                                    static_cast<uint32_t>(d0 + 8 * (i >> 2) + (i & 3)) < static_cast<uint32_t>(len)
-                                        ? s[qb][ns][i]
-                                        : -INFINITY;
-                        }
-                    }
-                    float top = s[qb][0][0];
-#pragma unroll
-                    for (int ns = 0; ns < NS; ++ns)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[qb][ns][i]);
-                    top = xor32_max(top) * sc;
-                    // Raising the maximum of a row without sums so far (m = -inf) needs no rescaling.
-                    const bool raise = top > m[qb] + kRaise;  // (false for top = -inf)
-                    if (__any(raise)) {
-                        const float mn = raise ? top : m[qb];
-                        const bool any = __any(raise && m[qb] != -INFINITY);
-                        const float f = raise ? __builtin_amdgcn_exp2f(m[qb] - mn) : 1.0f;
-                        m[qb] = mn;
-                        if (any) {
-                            l[qb] *= f;
-#pragma unroll
-                            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[qb][d][i] *= f;
-                        }
-                    }
-                    const float ref = m[qb] == -INFINITY ? 0.0f : m[qb];
-                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int qb = 0; qb < QB; ++qb) {
+                if (a.cap != 0.0f) {
 #pragma unroll
                     for (int ns = 0; ns < NS; ++ns)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            // (float32 rounds the score first, as the maximum was: the largest weight is 1 exactly)
-                            const float x = BF ? fmaf(s[qb][ns][i], sc, -ref) : scaled(s[qb][ns][i], sc) - ref;
-                            s[qb][ns][i] = __builtin_amdgcn_exp2f(x);
-                            sum[i & 3] += s[qb][ns][i];
+                            const float z = s[qb][ns][i] * a.scale;  // score / cap
+                            float th;
+                            if constexpr (BF)
+                                th = 1.0f - 2.0f * __builtin_amdgcn_rcpf(
+                                                       __builtin_amdgcn_exp2f(z * (2.0f * kLog2e)) + 1.0f);
+                            else
+                                th = tanhf(z);
+                            s[qb][ns][i] = a.cap * th;
                         }
-                    l[qb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 }
+                if (a.slopes) {
+                    const float in = a.cap != 0.0f ? 1.0f : a.scale;
+#pragma unroll
+                    for (int ns = 0; ns < NS; ++ns) {
+                        const int d0 = r_pos[qb] - (kbw + 32 * ns + 4 * hi);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            s[qb][ns][i] = s[qb][ns][i] * in -
+                                           r_slope[qb] * fabsf(static_cast<float>(d0 - (8 * (i >> 2) + (i & 3))));
+                    }
+                }
+                if (mixed) {
+                    int lo, len;
+                    interval(qb, lo, len);
+#pragma unroll
+                    for (int ns = 0; ns < NS; ++ns) {
+                        const int d0 = kbw + 32 * ns + 4 * hi - lo;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            s[qb][ns][i] =
+                                static_cast<uint32_t>(d0 + 8 * (i >> 2) + (i & 3)) < static_cast<uint32_t>(len)
+                                    ? s[qb][ns][i]
+                                    : -INFINITY;
+                    }
+                }
+                float top = s[qb][0][0];
+#pragma unroll
+                for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[qb][ns][i]);
+                top = xor32_max(top) * sc;
+                // Raising the maximum of a row without sums so far (m = -inf) needs no rescaling.
+                const bool raise = top > m[qb] + kRaise;  // (false for top = -inf)
+                if (__any(raise)) {
+                    const float mn = raise ? top : m[qb];
+                    const bool any = __any(raise && m[qb] != -INFINITY);
+                    const float f = raise ? __builtin_amdgcn_exp2f(m[qb] - mn) : 1.0f;
+                    m[qb] = mn;
+                    if (any) {
+                        l[qb] *= f;
+#pragma unroll
+                        for (int d = 0; d < DB; ++d)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[qb][d][i] *= f;
+                    }
+                }
+                const float ref = m[qb] == -INFINITY ? 0.0f : m[qb];
+                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                constexpr int X = 4 * NS;
+#pragma unroll
+                for (int x = 0; x < X; ++x) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float e = s[qb][x / 4][4 * (x % 4) + j];
+                        // (float32 rounds the score first, as the maximum was: the largest weight is 1 exactly)
+                        const float w = __builtin_amdgcn_exp2f(BF ? fmaf(e, sc, -ref) : scaled(e, sc) - ref);
+                        s[qb][x / 4][4 * (x % 4) + j] = w;
+                        sum[j] += w;
+                    }
+                    if (NBUF == 1 && qb == QB - 1) {
+#pragma unroll
+                        for (int p = x * NH / X; p < (x + 1) * NH / X; ++p) stage(nxt, 0, false, p, next);
+                    }
+                }
+                l[qb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             }
-            if constexpr (NBUF == 1) {  // the values
-                if (n_left > 1) sync(OneMatrix{});
-                else sync(None{});
-            }
-            if (clean && cur.seg >= 0) {
+            if (more) sync(Others{});  // the values
+            else sync(None{});
+            if (clean) {
                 for (int i = rw * 64 + lane; i < TILEB / 16; i += 64 * RW) {
                     rm_u32x4 *p = reinterpret_cast<rm_u32x4 *>(lds_w + TILEB + at) + i;
                     rm_u32x4 v = *p;
@@ -559,58 +586,68 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                     *p = v;
                 }
                 sync(Any{});
-            }
-            if (active) {
-                if (apart && !clean) {
+            } else if (mixed) {
 #pragma unroll 1
-                    for (int r = 0; r < KPW; r += BF ? 8 : 1) {  // the wave's values, each lane some of them
-                        if (!BF && (r & 4)) continue;            // (float32: rows r and r + 4 in the two halves)
+                for (int r = 0; r < KPW; r += BF ? 8 : 1) {  // the wave's values, each lane some of them
+                    if (!BF && (r & 4)) continue;            // (float32: rows r and r + 4 in the two halves)
 #pragma unroll
-                        for (int d = 0; d < DB; ++d) {
-                            const uint8_t *vp = v_ptr[d % VP] + at + (d / VP) * 256 + r * ROWB;
-                            if constexpr (BF) {
-                                const uint2 v = *reinterpret_cast<const uint2 *>(vp);
-                                spoilt |= nonfinite_bf16x2(v.x) | nonfinite_bf16x2(v.y);
-                            } else {
-                                spoilt |= nonfinite_f32(*reinterpret_cast<const float *>(vp));
-                            }
+                    for (int d = 0; d < DB; ++d) {
+                        const uint8_t *vp = v_ptr[d % VP] + at + (d / VP) * 256 + r * ROWB;
+                        if constexpr (BF) {
+                            const uint2 v = *reinterpret_cast<const uint2 *>(vp);
+                            spoilt |= nonfinite_bf16x2(v.x) | nonfinite_bf16x2(v.y);
+                        } else {
+                            spoilt |= nonfinite_f32(*reinterpret_cast<const float *>(vp));
                         }
                     }
                 }
-                if constexpr (BF) {
-                    rm_bf16x8 p[QB][2 * NS];
-#pragma unroll
-                    for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-                        for (int st = 0; st < 2 * NS; ++st)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                p[qb][st][i] = static_cast<__bf16>(s[qb][st / 2][8 * (st % 2) + i]);
-#pragma unroll
-                    for (int x = 0; x < 2 * NS * DB; ++x) {
-                        const int st = x / DB, d = x % DB;
-                        const rm_bf16x8 vf = read_v(v_ptr[d % VP] + at + (d / VP) * 256 + 16 * st * ROWB);
-#pragma unroll
-                        for (int qb = 0; qb < QB; ++qb)
-                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[qb][st], o[qb][d], 0, 0, 0);
-                    }
-                    pipeline<2 * NS * DB, AHEAD, QB, 2>();
-                } else {
-#pragma unroll
-                    for (int x = 0; x < 16 * NS * DB; ++x) {
-                        const int ns = x / (16 * DB), i = x / DB % 16, d = x % DB;
-                        const float vf = *reinterpret_cast<const float *>(
-                            v_ptr[d % VP] + at + (d / VP) * 256 + (32 * ns + 8 * (i >> 2) + (i & 3)) * ROWB);
-#pragma unroll
-                        for (int qb = 0; qb < QB; ++qb)
-                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[qb][ns][i], o[qb][d], 0, 0, 0);
-                    }
-                    pipeline<16 * NS * DB, AHEAD, QB, 1>();
-                }
             }
-            if constexpr (NBUF == 1) {  // every wave has read the values: the next ones'
-                sync(Any{});
-                if (n_left > 1) stage(nxt, 0, true);
+            {  // O^T += V^T P^T; with two buffers the next tile's values go out meanwhile, with one the rest of its keys
+                constexpr int X = (BF ? 2 : 16) * NS * DB, NQ = NBUF == 2 ? NP : NP - NH;
+                typedef typename std::conditional<BF, rm_bf16x8, float>::type VFrag;
+                VFrag vf[2 * AHEAD];
+                auto read_v = [&](int x) __attribute__((always_inline)) {
+                    const int st = x / DB, d = x % DB;
+                    if constexpr (BF)
+                        vf[x % (2 * AHEAD)] = read_v_rows<ROWB>(v_ptr[d % VP] + at + (d / VP) * 256 + 16 * st * ROWB);
+                    else
+                        vf[x % (2 * AHEAD)] = *reinterpret_cast<const float *>(
+                            v_ptr[d % VP] + at + (d / VP) * 256 + (32 * (st / 16) + 8 * (st % 16 >> 2) + (st & 3)) * ROWB);
+                };
+                VFrag p[QB];
+#pragma unroll
+                for (int x = 0; x < AHEAD; ++x) read_v(x);
+#pragma unroll
+                for (int x = 0; x < X; ++x) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const int st = x / DB, d = x % DB;
+                    if (d == 0) {
+#pragma unroll
+                        for (int qb = 0; qb < QB; ++qb) {
+                            if constexpr (BF) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i)
+                                    p[qb][i] = static_cast<__bf16>(s[qb][st / 2][8 * (st % 2) + i]);
+                            } else {
+                                p[qb] = s[qb][st / 16][st % 16];
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) {
+                        if constexpr (BF)
+                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x % (2 * AHEAD)], p[qb], o[qb][d], 0, 0, 0);
+                        else
+                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[x % (2 * AHEAD)], p[qb], o[qb][d], 0, 0, 0);
+                    }
+                    if (x + AHEAD < X) read_v(x + AHEAD);
+#pragma unroll
+                    for (int q = x * NQ / X; q < (x + 1) * NQ / X; ++q) {
+                        if constexpr (NBUF == 2) stage(nxt, buf, true, q, next);
+                        else stage(nxt, 0, false, NH + q, next);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
             cur = nxt;
         }
@@ -620,14 +657,13 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     while (__builtin_amdgcn_readfirstlane(__syncthreads_or(pass(clean)))) {  // a pass with `clean` returns false
         clean = true;
         first_tile(cur);
-        stage(cur, 0, false);
-        stage(cur, 0, true);
+        start();
     }
     if (__builtin_expect(clean, false)) {  // the infinities and NaN that the second pass left out
         first_tile(cur);
         for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
             const int k0 = cur.kb + kw * KPW, k1 = min(k0 + KPW, cur.end);
-            for (int k = k0; cur.seg >= 0 && k < k1; ++k) {
+            for (int k = k0; k < k1; ++k) {
                 const char *row = cur.v + (k - cur.kb) * cur.vn;
                 for (int c0 = 0; c0 < a.D; c0 += 64) {
                     float x = 0.0f;
@@ -640,8 +676,9 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                         const float add = __shfl(x, from);
 #pragma unroll
                         for (int qb = 0; qb < QB; ++qb) {
-                            const bool sees = r_sample[qb] == cur.seg &&
-                                              static_cast<uint32_t>(k - r_lo[qb]) < static_cast<uint32_t>(r_len[qb]);
+                            const bool sees =
+                                cur.seg < 0 || (r_smp[qb] == cur.seg &&
+                                                static_cast<uint32_t>(k - r_lo[qb]) < static_cast<uint32_t>(r_len[qb]));
                             const int at = sees ? c0 + from - 4 * hi : -1;
 #pragma unroll
                             for (int d = 0; d < DB; ++d)
@@ -658,38 +695,21 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
 
     // ---------------------------------------------------------------- join and write
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) l[qb] += __shfl_xor(l[qb], 32);
+    for (int qb = 0; qb < QB; ++qb) l[qb] = xor32_sum(l[qb]);
     float *join = reinterpret_cast<float *>(lds);
-    if constexpr (KW > 1) {
-        float *ml = join + W * QB * 32 * DH;  // [wave][qb][2][32]
-        rm_dma::wait_barrier<0>();            // every wave has read the last tile (of a second pass)
-        if (hi == 0) {
+    float *ml = join + W * QB * 32 * DH;  // [wave][qb][2][32]
+    if constexpr (KW > 1) {  // (every wave has read the last tile: the barrier after the pass)
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
+        for (int qb = 0; qb < QB; ++qb) {
+            if (hi == 0) {
                 ml[((wave * QB + qb) * 2 + 0) * 32 + col] = m[qb];
                 ml[((wave * QB + qb) * 2 + 1) * 32 + col] = l[qb];
             }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int k = 0; k < KW; ++k) top = fmaxf(top, ml[(((k * RW + rw) * QB + qb) * 2 + 0) * 32 + col]);
-            const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-            for (int k = 0; k < KW; ++k)
-                sum += ml[(((k * RW + rw) * QB + qb) * 2 + 1) * 32 + col] *
-                       __builtin_amdgcn_exp2f(ml[(((k * RW + rw) * QB + qb) * 2 + 0) * 32 + col] - ref);
-            const float f = __builtin_amdgcn_exp2f(m[qb] - ref);
-            m[qb] = top;
-            l[qb] = sum;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const rm_f32x4 v = {o[qb][d][4 * i] * f, o[qb][d][4 * i + 1] * f, o[qb][d][4 * i + 2] * f,
-                                        o[qb][d][4 * i + 3] * f};
+                    const rm_f32x4 v = {o[qb][d][4 * i], o[qb][d][4 * i + 1], o[qb][d][4 * i + 2], o[qb][d][4 * i + 3]};
                     *reinterpret_cast<rm_f32x4 *>(join + ((((wave * QB + qb) * DB + d) * 4 + i) * 64 + lane) * 4) = v;
                 }
         }
@@ -698,12 +718,31 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         const int r = row0 + (rw * QB + qb) * 32 + col;
+        float f[KW];  // the key waves' factors
+        if constexpr (KW > 1) {
+            float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                f[k] = ml[(((k * RW + rw) * QB + qb) * 2 + 0) * 32 + col];
+                top = fmaxf(top, f[k]);
+            }
+            const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                f[k] = __builtin_amdgcn_exp2f(f[k] - ref);
+                sum += ml[(((k * RW + rw) * QB + qb) * 2 + 1) * 32 + col] * f[k];
+            }
+            m[qb] = top;
+            l[qb] = sum;
+        }
         const float inv = a.splits > 1 ? 1.0f : (l[qb] == 0.0f ? 0.0f : 1.0f / l[qb]);
         const int64_t prow = (static_cast<int64_t>(split) * a.U * a.Hk + ng) * a.R + r;
-        if (a.splits > 1 && r_ok[qb] && hi == 0 && kw == 0) {
+        if (a.splits > 1 && r < a.R && hi == 0 && kw == 0) {
             a.part_ml[2 * prow] = m[qb];
             a.part_ml[2 * prow + 1] = l[qb];
         }
+        char *orow = a.o + (static_cast<int64_t>(u) * a.per + r_smp[qb]) * a.o_b + r_tok[qb] * a.o_t +
+                     r_head[qb] * a.o_h;
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
             if (KW > 1 && d % KW != kw) continue;
@@ -715,21 +754,22 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
 #pragma unroll
                     for (int k = 0; k < KW; ++k)
                         v += *reinterpret_cast<const rm_f32x4 *>(
-                            join + (((((k * RW + rw) * QB + qb) * DB + d) * 4 + i) * 64 + lane) * 4);
+                                 join + (((((k * RW + rw) * QB + qb) * DB + d) * 4 + i) * 64 + lane) * 4) *
+                             f[k];
                 } else {
                     v = rm_f32x4{o[qb][d][4 * i], o[qb][d][4 * i + 1], o[qb][d][4 * i + 2], o[qb][d][4 * i + 3]};
                 }
                 const int c = 32 * d + 8 * i + 4 * hi;
-                if (!r_ok[qb] || c >= a.D) continue;
+                if (r >= a.R || (PAD && c >= a.D)) continue;
                 if (a.splits > 1) {
                     *reinterpret_cast<rm_f32x4 *>(a.part_o + prow * a.D + c) = v;
                 } else if constexpr (BF) {
                     rm_bf16x4 w;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] = static_cast<__bf16>(v[e] * inv);
-                    *reinterpret_cast<rm_bf16x4 *>(orow[qb] + c * 2) = w;
+                    *reinterpret_cast<rm_bf16x4 *>(orow + c * 2) = w;
                 } else {
-                    *reinterpret_cast<rm_f32x4 *>(orow[qb] + c * 4) = v * inv;
+                    *reinterpret_cast<rm_f32x4 *>(orow + c * 4) = v * inv;
                 }
             }
         }

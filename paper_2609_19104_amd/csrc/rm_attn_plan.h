@@ -13,6 +13,21 @@ struct Src {
     int64_t k_b = 0, k_n = 0, k_h = 0, v_b = 0, v_n = 0, v_h = 0;
 };
 
+// n / d for 0 <= n < 2^30: the high half of n mul, shifted (mul = 0: d = 1).  mul = ceil(2^(32 + shift) / d) with
+// shift = max(0, ceil(log2 d) - 2) fits 32 bits and is off by less than d, which n < 2^30 keeps below one d-th.
+struct Divisor {
+    uint32_t mul = 0, shift = 0;
+};
+inline Divisor divisor(uint32_t d) {
+    Divisor r;
+    if (d <= 1) return r;
+    uint32_t log = 0;
+    while ((1ull << log) < d) ++log;
+    r.shift = log > 2 ? log - 2 : 0;
+    r.mul = static_cast<uint32_t>(((1ull << (32 + r.shift)) + d - 1) / d);
+    return r;
+}
+
 struct Args {
     const char *q = nullptr;
     int64_t q_b = 0, q_t = 0, q_h = 0;  // bytes
@@ -27,6 +42,7 @@ struct Args {
     const float *slopes = nullptr;  // [Hq] or null
     const int32_t *q_start = nullptr;
     int D = 0, Hk = 0, G = 0, T = 0, per = 0, U = 0, causal = 0;
+    Divisor by_g, by_t;             // G and T
     int R = 0;                      // rows of a group and key head: per T G
     int n_tiles = 0, splits = 1;    // row blocks, and workgroups that divide one's keys
     float scale = 0.0f, cap = 0.0f; // scores times scale in powers of two; with a cap: scale = score scale / cap, cap in powers of two
@@ -36,6 +52,7 @@ struct Args {
 struct Plan {
     int dh = 0;         // the kernel's head width (64, 128, 256)
     int kw = 1;         // key waves: 1 or several
+    bool pad = false;   // the head is narrower
     int rows = 0;       // rows of a workgroup
     int n_tiles = 0, splits = 1;
     size_t off_ml = 0, total = 0;

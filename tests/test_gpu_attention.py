@@ -318,6 +318,28 @@ def test_prefix_long_and_few_rows(dtype, D):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("causal", [False, True])
+def test_prefix_many_rows(dtype, D, causal):
+    """Enough rows for the kernel whose waves divide them, each wave with samples of its own; two samples hold NaN."""
+    g = gen(24, D)
+    G, per, T, P, S, H = 2, 75, 33, 70, 40, 16
+    q, kp, vp, ko, vo = make_prefix(g, G, per, T, P, S, H, H, D, dtype)
+    olen = torch.randint(0, S + 1, (G * per,), generator=g, dtype=torch.int32)
+    olen[0], olen[1], olen[-1] = S, 0, 1
+    plen = ints([P, 33])
+    ko[5], vo[80] = float("nan"), float("nan")
+    out = run_prefix(q, kp, vp, ko, vo, plen, olen.cuda(), causal)
+    for b in (0, 1, 2, 4, 6, 74, 75, 79, 81, 149):
+        i = b // per
+        for h in (0, H - 1):
+            a = [t[:, :, h:h + 1] for t in (q[b:b + 1], kp[i:i + 1], vp[i:i + 1], ko[b:b + 1], vo[b:b + 1])]
+            ref, mag, big = att.prefix_attention(*(f64(t) for t in a), np.float32(D ** -0.5), 0.0, [int(plen[i])],
+                                                 [int(olen[b])], causal)
+            check(out[b:b + 1, :, h:h + 1], ref, bound(ref, mag, big, dtype, D, P + S))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("T", [1, 20])
 def test_one_samples_nan_stays_its_own(dtype, T):
     g = gen(23, T)
