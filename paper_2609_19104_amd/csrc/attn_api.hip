@@ -107,10 +107,20 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     q.n_tiles = static_cast<int>(ceil_div(rows, q.rows));
     const int64_t wgs = q.n_tiles * ng;
     if (wgs >= (static_cast<int64_t>(1) << 31)) return api_fail(RM_ERR_SHAPE, "launch grid too large");
-    // Few row blocks and long keys: several workgroups divide the keys.
+    // Few row blocks: several workgroups divide the keys, as many as fill the compute units once (two workgroups to one,
+    // where their LDS allows it: heads up to 128 in bf16, 64 in float32), if the tiles that each of them then has less pay
+    // for the second launch and the partial results.  In us: a tile of 128 keys 0.4 (64 columns), 0.8 (128), 1.6 (256);
+    // the join 4 and its traffic at 4 TB/s.
     const int64_t tiles = ceil_div(n0, 128) + ceil_div(n1, 128);
+    const int64_t slots = kCUs * (q.dh * (bf ? 1 : 2) <= 128 ? 2 : 1);
+    const double tile_us = 0.4 * (q.dh / 64) * (bf ? 1 : 2), join_us = 4.0;
+    const double part_us = static_cast<double>(rows) * ng * D * 8 / 4e6;  // one slice's results written and read
     q.splits = 1;
-    if (wgs < kCUs) q.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(2 * kCUs / wgs, tiles / 4)));
+    double best = tiles * tile_us;
+    for (int64_t n = 2; n * wgs <= slots && n <= tiles; n += n < 16 ? 1 : n / 8) {
+        const double us = ceil_div(tiles, n) * tile_us + join_us + n * part_us;
+        if (us < best) best = us, q.splits = static_cast<int>(n);
+    }
     if (q.splits > 1) {
         const size_t n = static_cast<size_t>(q.splits) * ng * rows;
         q.off_ml = align_up(n * D * 4, 256);

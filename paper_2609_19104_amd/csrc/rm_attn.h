@@ -143,18 +143,18 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rw = wave % RW, kw = wave / RW;
 
-    // This workgroup's key head of a group, row block and slice of the keys.
+    // This workgroup's key head of a group, row block and slice of the keys.  A group's workgroups go to one XCD where
+    // the groups divide among the XCDs, whose L2 then holds their keys; few groups (of an XCD) take turns, so that the
+    // row blocks with the most keys of all of them start first, many follow each other.
     int ng, tile_id;
     {
-        const int nt = a.n_tiles * a.splits, id = blockIdx.x;
-        if (((a.U * a.Hk) & 7) == 0) {  // whole groups to an XCD, whose L2 then holds their keys
-            const int i = id >> 3;
-            ng = (id & 7) + 8 * (i / nt);
-            tile_id = i % nt;
-        } else {
-            ng = id / nt;
-            tile_id = id % nt;
-        }
+        const int nt = a.n_tiles * a.splits, groups = a.U * a.Hk, id = blockIdx.x;
+        const bool by_xcd = (groups & 7) == 0;
+        const int i = by_xcd ? id >> 3 : id, n = by_xcd ? groups >> 3 : groups;
+        const bool turns = n <= 8;
+        const int g = turns ? i % n : i / nt;
+        tile_id = turns ? i / n : i % nt;
+        ng = by_xcd ? (id & 7) + 8 * g : g;
     }
     const int split = tile_id % a.splits;
     // Row blocks from the last to the first: with causal masks the later ones see more keys and start first.
@@ -411,8 +411,10 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         r_slope[qb] = a.slopes ? a.slopes[r_head[qb]] * kLog2e : 0.0f;
         r_pos[qb] = (a.slopes && a.q_start ? a.q_start[u] : 0) + r_tok[qb];  // (slopes: one sample a group)
     }
-    // Scores with a cap or a bias are formed in powers of two; plain ones are scaled on the way into exp2.
-    const float sc = a.cap != 0.0f || a.slopes ? 1.0f : a.scale;
+    // The scores' registers hold s with score = sc s + off in powers of two: plain products, capped ones as tanh or (bf16)
+    // -1 / (1 + e^2x), of which tanh x is 1 + 2 times; with a bias the scores themselves.
+    const float sc = a.slopes ? 1.0f : a.cap != 0.0f ? (BF ? 2.0f * a.cap : a.cap) : a.scale;
+    const float off = BF && a.cap != 0.0f && !a.slopes ? a.cap : 0.0f;
 
     // ---------------------------------------------------------------- tiles
     // One pass over the slice's tiles, the first one's loads under way.  Returns whether a tile of keys that some rows
@@ -488,30 +490,30 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             };
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
-                if (a.cap != 0.0f) {
+                if (a.cap != 0.0f) {  // (a.scale: the score's over the cap)
+                    const float x2 = a.scale * (2.0f * kLog2e);
 #pragma unroll
                     for (int ns = 0; ns < NS; ++ns)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float z = s[qb][ns][i] * a.scale;  // score / cap
-                            float th;
                             if constexpr (BF)
-                                th = 1.0f - 2.0f * __builtin_amdgcn_rcpf(
-                                                       __builtin_amdgcn_exp2f(z * (2.0f * kLog2e)) + 1.0f);
+                                s[qb][ns][i] =
+                                    __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s[qb][ns][i] * x2));
                             else
-                                th = tanhf(z);
-                            s[qb][ns][i] = a.cap * th;
+                                s[qb][ns][i] = tanhf(s[qb][ns][i] * a.scale);
                         }
                 }
                 if (a.slopes) {
-                    const float in = a.cap != 0.0f ? 1.0f : a.scale;
+                    const float in = a.cap == 0.0f ? a.scale : BF ? 2.0f * a.cap : a.cap;
+                    const float add = BF ? a.cap : 0.0f;
 #pragma unroll
                     for (int ns = 0; ns < NS; ++ns) {
-                        const int d0 = r_pos[qb] - (kbw + 32 * ns + 4 * hi);
+                        const float d0 = static_cast<float>(r_pos[qb] - (kbw + 32 * ns + 4 * hi));
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            s[qb][ns][i] = s[qb][ns][i] * in -
-                                           r_slope[qb] * fabsf(static_cast<float>(d0 - (8 * (i >> 2) + (i & 3))));
+                            s[qb][ns][i] = fmaf(s[qb][ns][i], in,
+                                                fmaf(-r_slope[qb], fabsf(d0 - static_cast<float>(8 * (i >> 2) + (i & 3))),
+                                                     add));
                     }
                 }
                 if (mixed) {
@@ -533,7 +535,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                 for (int ns = 0; ns < NS; ++ns)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[qb][ns][i]);
-                top = xor32_max(top) * sc;
+                top = BF ? fmaf(xor32_max(top), sc, off) : xor32_max(top) * sc;
                 // Raising the maximum of a row without sums so far (m = -inf) needs no rescaling.
                 const bool raise = top > m[qb] + kRaise;  // (false for top = -inf)
                 if (__any(raise)) {
@@ -549,7 +551,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                             for (int i = 0; i < 16; ++i) o[qb][d][i] *= f;
                     }
                 }
-                const float ref = m[qb] == -INFINITY ? 0.0f : m[qb];
+                const float ref = (m[qb] == -INFINITY ? 0.0f : m[qb]) - off;
                 float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                 constexpr int X = 4 * NS;
 #pragma unroll
