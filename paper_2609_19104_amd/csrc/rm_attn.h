@@ -118,7 +118,7 @@ __device__ __forceinline__ int divide(int n, Divisor d) {  // n < 2^30
 struct Tile {
     const char *k, *v;
     int64_t kn, vn;  // bytes from key to key
-    int kb, end, seg;
+    int kb, end, seg, before;
 };
 
 // PAD: the head is narrower than the kernel's DH columns.
@@ -271,45 +271,54 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         t.k = s.k + b * s.k_b + hk * s.k_h + t.kb * s.k_n;
         t.v = s.v + b * s.v_b + hk * s.v_h + t.kb * s.v_n;
     };
-    int64_t total = 0;
-    for (int sg = -1; sg <= s_last; sg = sg < 0 ? s_first : sg + 1) {
+    // The slices take the tiles by turns: of the shared keys' tiles followed by the samples', slice s takes those whose
+    // number is s modulo the slices, so that each has its share of both.  Every other slice walks its samples' tiles
+    // first: those come from far memory while the shared ones' are in the caches.
+    const int turns = a.splits;
+    const bool own_first = (split & 1) != 0;
+    auto tiles_of = [&](int sg) __attribute__((always_inline)) {
         int lo, end;
         seg_keys(sg, lo, end);
-        total += (end - lo + KT - 1) / KT;
-    }
-    int64_t first = 0, n_tiles = total;
-    if (a.splits > 1) {
-        first = total * split / a.splits;
-        n_tiles = total * (split + 1) / a.splits - first;
-    }
-    auto first_tile = [&](Tile &t) __attribute__((always_inline)) {
-        int64_t skip = first;
-        t.seg = -1;
-        t.kb = t.end = 0;
-        for (int sg = -1; sg <= s_last; sg = sg < 0 ? s_first : sg + 1) {
+        return (end - lo + KT - 1) / KT;
+    };
+    int64_t n_tiles = 0;
+    for (int sg = -1; sg <= s_last; sg = sg < 0 ? s_first : sg + 1) n_tiles += tiles_of(sg);
+    if (turns > 1) n_tiles = (n_tiles - split + turns - 1) / turns;
+    // Goes to the slice's first tile of t.seg or, if it has none there, of a following segment; t.before: how many tiles
+    // come before the segment, modulo the slices.
+    auto enter = [&](Tile &t) __attribute__((always_inline)) {
+        for (;;) {
             int lo, end;
-            seg_keys(sg, lo, end);
+            seg_keys(t.seg, lo, end);
             const int n = (end - lo + KT - 1) / KT;
-            t.seg = sg;
-            t.kb = lo + static_cast<int>(min(skip, static_cast<int64_t>(n))) * KT;
-            t.end = end;
-            if (skip < n) break;
-            skip -= n;
+            int skip = split - t.before;
+            if (skip < 0) skip += turns;
+            const bool final = t.seg == (own_first ? -1 : s_last);
+            if (skip < n || final) {
+                t.kb = lo + min(skip, n) * KT;
+                t.end = end;
+                break;
+            }
+            t.before = t.seg == s_last ? 0 : (turns > 1 ? (t.before + n) % turns : 0);
+            t.seg = t.seg == s_last ? -1 : (t.seg < 0 ? s_first : t.seg + 1);
         }
         seg_base(t);
     };
+    auto first_tile = [&](Tile &t) __attribute__((always_inline)) {
+        t.seg = own_first ? s_first : -1;
+        t.before = own_first ? tiles_of(-1) % turns : 0;
+        enter(t);
+    };
     auto advance = [&](Tile &t) __attribute__((always_inline)) {  // only called when another tile follows
-        t.kb += KT;
+        t.kb += turns * KT;
         if (t.kb < t.end) {
-            t.k += KT * t.kn;
-            t.v += KT * t.vn;
+            t.k += turns * KT * t.kn;
+            t.v += turns * KT * t.vn;
             return;
         }
-        do {
-            t.seg = t.seg < 0 ? s_first : t.seg + 1;
-            seg_keys(t.seg, t.kb, t.end);
-        } while (t.kb >= t.end);
-        seg_base(t);
+        t.before = t.seg == s_last ? 0 : (turns > 1 ? (t.before + tiles_of(t.seg)) % turns : 0);
+        t.seg = t.seg == s_last ? -1 : (t.seg < 0 ? s_first : t.seg + 1);
+        enter(t);
     };
 
     // ---------------------------------------------------------------- staging
@@ -417,12 +426,13 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     const float off = BF && a.cap != 0.0f && !a.slopes ? a.cap : 0.0f;
 
     // ---------------------------------------------------------------- tiles
-    // One pass over the slice's tiles, the first one's loads under way.  Returns whether a tile of keys that some rows
-    // see and others do not holds infinities or NaN among its values: 0 times those would spoil the rows that do not
-    // see them.  Such a workgroup (there is hardly ever one) makes a second pass with `clean`, which sets them to 0 in
-    // LDS, the other sums staying as they are bit for bit, and then adds them to the rows that see them.
+    // One pass over the slice's tiles, the first one's loads under way.  Returns whether the sums hold infinities or NaN
+    // and a tile had keys that some rows see and others do not: 0 times infinite values may have spoilt the rows that do
+    // not see them.  Such a workgroup (there is hardly ever one) makes a second pass with `clean`, which sets the
+    // infinities and NaN among the values to 0 in LDS, the other sums staying as they are bit for bit, and then adds
+    // them to the rows that see them.
     auto pass = [&](const bool clean) __attribute__((always_inline)) -> bool {
-        uint32_t spoilt = 0;
+        bool some = false;  // some tile had keys that not all rows see
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             m[qb] = -INFINITY;
@@ -588,22 +598,8 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                     *p = v;
                 }
                 sync(Any{});
-            } else if (mixed) {
-#pragma unroll 1
-                for (int r = 0; r < KPW; r += BF ? 8 : 1) {  // the wave's values, each lane some of them
-                    if (!BF && (r & 4)) continue;            // (float32: rows r and r + 4 in the two halves)
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        const uint8_t *vp = v_ptr[d % VP] + at + (d / VP) * 256 + r * ROWB;
-                        if constexpr (BF) {
-                            const uint2 v = *reinterpret_cast<const uint2 *>(vp);
-                            spoilt |= nonfinite_bf16x2(v.x) | nonfinite_bf16x2(v.y);
-                        } else {
-                            spoilt |= nonfinite_f32(*reinterpret_cast<const float *>(vp));
-                        }
-                    }
-                }
             }
+            some = some || mixed;
             {  // O^T += V^T P^T; with two buffers the next tile's values go out meanwhile, with one the rest of its keys
                 constexpr int X = (BF ? 2 : 16) * NS * DB, NQ = NBUF == 2 ? NP : NP - NH;
                 typedef typename std::conditional<BF, rm_bf16x8, float>::type VFrag;
@@ -653,7 +649,16 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             }
             cur = nxt;
         }
-        return spoilt != 0;
+        if (clean || !some) return false;
+        // 0 times an infinity or NaN is NaN, and a sum keeps it: o 0 summed is 0 unless o holds some (or an infinity).
+        float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i & 3] = fmaf(o[qb][d][i], 0.0f, z[i & 3]);
+        return !((z[0] + z[1]) + (z[2] + z[3]) == 0.0f);
     };
     bool clean = false;
     while (__builtin_amdgcn_readfirstlane(__syncthreads_or(pass(clean)))) {  // a pass with `clean` returns false
