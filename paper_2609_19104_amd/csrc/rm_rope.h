@@ -14,7 +14,7 @@ struct RopeArgs {
     const float *inv_freq = nullptr, *gain_q = nullptr, *gain_k = nullptr;
     int N = 0, D = 0, Hq = 0, Hk = 0, H = 0, rot = 0, rows = 0, pairs = 0;  // H: all heads of a token (v's too, if any)
     float eps = 0.0f;
-    int groups = 0, lane_bits = 0;  // head groups of a token, lanes of a group
+    int groups = 0, per = 0, lane_bits = 0;  // waves of a token, heads of a wave, logarithm of the lanes of a head
 };
 hipError_t launch_qk_norm_rope(const RopeArgs &a, bool in_bf16, bool out_bf16, hipStream_t st);
 hipError_t launch_attn_spans(int B, int T, int N, int causal, int window, const int32_t *q_start,
