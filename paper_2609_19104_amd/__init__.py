@@ -17,6 +17,8 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
+import threading
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -106,7 +108,7 @@ def load_library() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIB_PATH)
     i32, vp, sz = ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t
     sp, wp = ctypes.POINTER(FfnShape), ctypes.POINTER(LayerWeights)
-    hp, ap, f32 = ctypes.POINTER(Heads), ctypes.POINTER(AttnShape), ctypes.c_float
+    f32 = ctypes.c_float
     sigs = {
         "rm_mask_compact": [vp, i32, i32, vp, vp, vp],
         "rm_workspace_size": [sp, i32, i32, i32, ctypes.POINTER(sz)],
@@ -127,13 +129,13 @@ def load_library() -> ctypes.CDLL:
         "rm_context_ffn_packed": [sp, vp, i32, vp, vp, vp, i32, vp, vp, sz, vp],
         "rm_neuron_norms": [vp, i32, i32, i32, vp, vp],
         "rm_group_masks": [vp, i32, i32, i32, i32, vp, i32, vp, vp, vp],
-        "rm_qk_norm_rope": [i32, i32, i32, i32, i32, i32, hp, hp, hp, hp, hp, hp, i32, vp, vp, vp, i32, i32, vp, vp,
+        "rm_qk_norm_rope": [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp,
                             f32, vp],
         "rm_attn_spans": [i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp],
-        "rm_span_attention_workspace_size": [ap, i32, i32, i32, ctypes.POINTER(sz)],
-        "rm_span_attention": [ap, i32, i32, i32, hp, hp, hp, hp, vp, vp, vp, vp, sz, vp],
-        "rm_prefix_attention_workspace_size": [ap, i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
-        "rm_prefix_attention": [ap, i32, i32, i32, i32, i32, hp, hp, hp, vp, hp, hp, vp, i32, hp, vp, sz, vp],
+        "rm_span_attention_workspace_size": [vp, i32, i32, i32, ctypes.POINTER(sz)],
+        "rm_span_attention": [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+        "rm_prefix_attention_workspace_size": [vp, i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
+        "rm_prefix_attention": [vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp],
         "rm_profile_kernel_events": [i32, vp, vp],
         "rm_layer_kernels": [sp, i32, i32, i32, ctypes.POINTER(ctypes.c_uint32)],
         "rm_stream_read": [vp, sz, i32, vp, vp],
@@ -570,63 +572,79 @@ def rm_group_masks(h: torch.Tensor, norms: torch.Tensor, k: int, scores: torch.T
 _ATTN_DTYPES = {torch.float32: RM_F32, torch.bfloat16: RM_BF16}
 
 
-def _heads(name: str, t: torch.Tensor, dtype, device, ndim: int) -> Heads:
-    """Strides and pointer of a tensor of head vectors ([B][T][H][D], or [T][H][D] without a batch axis)."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == ndim and t.device == device):
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name} must be a torch.Tensor")
-        if t.device != device or not t.is_cuda:
-            raise ValueError(f"{name} must be on a HIP device, the same as the other tensors, got {t.device}")
-        if t.dtype != dtype:
-            raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+class _Marshal(threading.local):
+    """Per thread, the C structs of one call (the library reads them before it returns): up to 6 rm_heads and an
+    rm_attn_shape, filled by one pack each, and their addresses."""
+
+    def __init__(self):
+        self.heads = ctypes.create_string_buffer(6 * ctypes.sizeof(Heads))
+        self.shape = ctypes.create_string_buffer(ctypes.sizeof(AttnShape))
+        base = ctypes.addressof(self.heads)
+        self.at = [base + i * ctypes.sizeof(Heads) for i in range(6)]
+        self.shape_at = ctypes.addressof(self.shape)
+
+
+_marshal = _Marshal()
+_pack_heads = [struct.Struct("=" + "Qqqq" * n).pack_into for n in range(7)]
+_pack_shape = struct.Struct("=iiiiff").pack_into
+
+
+def _heads(name: str, t: torch.Tensor, dtype, index: int, ndim: int) -> Tuple[int, int, int, int]:
+    """The fields of an rm_heads for a tensor of head vectors ([B][T][H][D], or [T][H][D] without a batch axis) on
+    device `index`."""
+    if isinstance(t, torch.Tensor):
+        st = t.stride()
+        if t.dtype == dtype and len(st) == ndim and t.get_device() == index and (st[-1] == 1 or t.shape[-1] == 1):
+            return t.data_ptr(), st[0] if ndim == 4 else 0, st[-3], st[-2]
+    else:
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on a HIP device, the same as the other tensors, got {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.dim() != ndim:
         raise ValueError(f"{name} must have {ndim} dims, got {tuple(t.shape)}")
-    st = t.stride()
-    if st[-1] != 1 and t.shape[-1] != 1:
-        raise ValueError(f"{name}: the elements of a head must be consecutive")
-    return Heads(t.data_ptr(), st[0] if ndim == 4 else 0, st[-3], st[-2])
+    raise ValueError(f"{name}: the elements of a head must be consecutive")
 
 
-def _int32(name: str, t: Optional[torch.Tensor], device, shape) -> Optional[int]:
+def _vector(name: str, t: Optional[torch.Tensor], dtype, index: int, shape) -> Optional[int]:
+    """Pointer of an optional contiguous tensor of a dtype, device and shape."""
     if t is None:
         return None
-    _need_cuda(name, t, (torch.int32,))
-    if tuple(t.shape) != shape or t.device != device:
-        raise ValueError(f"{name} must be int32 {list(shape)} on {device}, got {list(t.shape)} on {t.device}")
-    return t.data_ptr()
+    if (isinstance(t, torch.Tensor) and t.dtype == dtype and t.get_device() == index and t.shape == shape
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _need_cuda(name, t, (dtype,))
+    raise ValueError(f"{name} must be {dtype} {list(shape)} on device {index}, got {list(t.shape)} on {t.device}")
 
 
-def _float32(name: str, t: Optional[torch.Tensor], device, n: int) -> Optional[int]:
-    if t is None:
-        return None
-    _need_cuda(name, t, (torch.float32,), 1)
-    if t.shape[0] != n or t.device != device:
-        raise ValueError(f"{name} must be float32 [{n}] on {device}, got {list(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _attn_device(t: torch.Tensor, stream):
+def _attn_device(t: torch.Tensor, stream) -> int:
     """The tensors' device; without a stream given it has to be the current one, whose stream the call runs on."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    index = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if index < 0:
         raise ValueError("tensors must be on a HIP device")
-    if stream is None and t.device.index != torch._C._cuda_getDevice():
+    if stream is None and index != torch._C._cuda_getDevice():
         raise ValueError(f"tensors are on {t.device}, which is not the current device: select it or give a stream of it")
-    return t.device
+    return index
 
 
-def _attn_shape(q: torch.Tensor, n_kv_heads: int, scale: Optional[float], softcap: float) -> AttnShape:
-    if q.dtype not in _ATTN_DTYPES:
+def _attn_shape(q: torch.Tensor, n_q_heads: int, n_kv_heads: int, D: int, scale: Optional[float], softcap: float) -> int:
+    """Address of the call's rm_attn_shape."""
+    dtype = _ATTN_DTYPES.get(q.dtype)
+    if dtype is None:
         raise ValueError(f"queries must be float32 or bfloat16, got {q.dtype}")
-    D = q.shape[-1]
-    return AttnShape(q.shape[-2], n_kv_heads, D, _ATTN_DTYPES[q.dtype],
-                     D ** -0.5 if scale is None and D > 0 else scale, softcap)
+    if scale is None:
+        scale = D ** -0.5 if D > 0 else 1.0
+    _pack_shape(_marshal.shape, 0, n_q_heads, n_kv_heads, D, dtype, scale, softcap)
+    return _marshal.shape_at
 
 
-def _attn_ws(ws: Optional[torch.Tensor], device) -> Tuple[Optional[int], int]:
+def _attn_ws(ws: Optional[torch.Tensor], index: int) -> Tuple[Optional[int], int]:
     if ws is None:
         return None, 0
-    _need_cuda("ws", ws, (torch.uint8,))
-    if ws.device != device:
-        raise ValueError(f"ws must be on {device}, got {ws.device}")
+    if ws.dtype != torch.uint8 or ws.get_device() != index or not ws.is_contiguous():
+        _need_cuda("ws", ws, (torch.uint8,))
+        raise ValueError(f"ws must be on device {index}, got {ws.device}")
     return ws.data_ptr(), ws.numel()
 
 
@@ -638,27 +656,31 @@ def rm_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor],
     """q [N][Hq][D], k and v [N][Hk][D] (views of one projection's rows will do): queries normalized and rotated into
     q_out [N][Hq][D], keys into rows slot[n] (None: n) of k_out [rows][Hk][D], values copied into those of v_out."""
     dev = _attn_device(q, stream)
-    if q.dtype not in _ATTN_DTYPES or not isinstance(q_out, torch.Tensor) or q_out.dtype not in _ATTN_DTYPES:
+    src, dst = q.dtype, q_out.dtype
+    if src not in _ATTN_DTYPES or dst not in _ATTN_DTYPES:
         raise ValueError("queries and outputs must be float32 or bfloat16")
-    hq, hk = _heads("q", q, q.dtype, dev, 3), _heads("k", k, q.dtype, dev, 3)
-    hqo, hko = _heads("q_out", q_out, q_out.dtype, dev, 3), _heads("k_out", k_out, q_out.dtype, dev, 3)
-    N, Hq, D = q.shape
-    Hk, rows = k.shape[1], k_out.shape[0]
-    if k.shape != (N, Hk, D) or q_out.shape != q.shape or k_out.shape != (rows, Hk, D):
+    fields = (_heads("q", q, src, dev, 3) + _heads("k", k, src, dev, 3) + _heads("q_out", q_out, dst, dev, 3)
+              + _heads("k_out", k_out, dst, dev, 3))
+    shape, k_shape, ko_shape = q.shape, k.shape, k_out.shape
+    N, Hq, D = shape
+    Hk, rows = k_shape[1], ko_shape[0]
+    if k_shape != (N, Hk, D) or q_out.shape != shape or ko_shape != (rows, Hk, D):
         raise ValueError("q and q_out must be [N][Hq][D], k [N][Hk][D] and k_out [rows][Hk][D]")
     if (v is None) != (v_out is None):
         raise ValueError("v and v_out go together")
-    hv, hvo = Heads(), Heads()
     if v is not None:
-        hv, hvo = _heads("v", v, q.dtype, dev, 3), _heads("v_out", v_out, q_out.dtype, dev, 3)
-        if v.shape != k.shape or v_out.shape != k_out.shape:
+        fields += _heads("v", v, src, dev, 3) + _heads("v_out", v_out, dst, dev, 3)
+        if v.shape != k_shape or v_out.shape != ko_shape:
             raise ValueError("v must have k's shape and v_out k_out's")
-    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
+    at = _marshal.at
+    _pack_heads[len(fields) // 4](_marshal.heads, 0, *fields)
     _check(load_library().rm_qk_norm_rope(
-        N, Hq, Hk, D, _ATTN_DTYPES[q.dtype], _ATTN_DTYPES[q_out.dtype], hq, hk, hv, hqo, hko, hvo, rows,
-        _int32("pos", pos, dev, (N,)), _int32("slot", slot, dev, (N,)),
-        _float32("inv_freq", inv_freq, dev, rot // 2), rot, int(pairs), _float32("gain_q", gain_q, dev, D),
-        _float32("gain_k", gain_k, dev, D), eps, _stream(stream)))
+        N, Hq, Hk, D, _ATTN_DTYPES[src], _ATTN_DTYPES[dst], at[0], at[1], None if v is None else at[4], at[2], at[3],
+        None if v is None else at[5], rows, _vector("pos", pos, torch.int32, dev, (N,)),
+        _vector("slot", slot, torch.int32, dev, (N,)), _vector("inv_freq", inv_freq, torch.float32, dev, (rot // 2,)),
+        rot, pairs, _vector("gain_q", gain_q, torch.float32, dev, (D,)),
+        _vector("gain_k", gain_k, torch.float32, dev, (D,)), eps, _stream(stream)))
 
 
 def rm_attn_spans(span: torch.Tensor, N: int, causal: bool = True, window: int = 0,
@@ -667,21 +689,20 @@ def rm_attn_spans(span: torch.Tensor, N: int, causal: bool = True, window: int =
     """span int32 [B][T][2]: the interval of the N keys that each query row sees (see the header for the rules);
     q_start, kv_len, prefix_len int32 [B], doc int32 [B][N]."""
     dev = _attn_device(span, stream)
-    _need_cuda("span", span, (torch.int32,), 3)
-    B, T, two = span.shape
-    if two != 2:
-        raise ValueError("span must be [B][T][2]")
-    _check(load_library().rm_attn_spans(B, T, int(N), int(causal), int(window), _int32("q_start", q_start, dev, (B,)),
-                                        _int32("kv_len", kv_len, dev, (B,)),
-                                        _int32("prefix_len", prefix_len, dev, (B,)), _int32("doc", doc, dev, (B, N)),
-                                        span.data_ptr(), _stream(stream)))
+    B, T = span.shape[:2]
+    i32 = torch.int32
+    at = _vector("span", span, i32, dev, (B, T, 2))
+    _check(load_library().rm_attn_spans(B, T, N, causal, window, _vector("q_start", q_start, i32, dev, (B,)),
+                                        _vector("kv_len", kv_len, i32, dev, (B,)),
+                                        _vector("prefix_len", prefix_len, i32, dev, (B,)),
+                                        _vector("doc", doc, i32, dev, (B, N)), at, _stream(stream)))
 
 
 def span_attention_workspace(q: torch.Tensor, k: torch.Tensor) -> torch.Tensor:
     """A workspace tensor (uint8) of the size rm_span_attention_workspace_size asks for (it may be 0)."""
     out = ctypes.c_size_t(0)
-    _check(load_library().rm_span_attention_workspace_size(_attn_shape(q, k.shape[2], None, 0.0), q.shape[0],
-                                                           q.shape[1], k.shape[1], ctypes.byref(out)))
+    _check(load_library().rm_span_attention_workspace_size(_attn_shape(q, q.shape[2], k.shape[2], q.shape[3], None, 0.0),
+                                                           q.shape[0], q.shape[1], k.shape[1], ctypes.byref(out)))
     return torch.empty(int(out.value), dtype=torch.uint8, device=q.device)
 
 
@@ -692,16 +713,21 @@ def rm_span_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: to
     """out = softmax(cap(scale q k^T) - slopes |q_start + i - j|) v over each row's interval of keys (span None: all);
     scale None: 1 / sqrt(D)."""
     dev = _attn_device(q, stream)
-    hq, hk = _heads("q", q, q.dtype, dev, 4), _heads("k", k, q.dtype, dev, 4)
-    hv, ho = _heads("v", v, q.dtype, dev, 4), _heads("out", out, q.dtype, dev, 4)
-    B, T, Hq, D = q.shape
-    N, Hk = k.shape[1], k.shape[2]
-    if k.shape != (B, N, Hk, D) or v.shape != k.shape or out.shape != q.shape:
+    dtype = q.dtype
+    fields = (_heads("q", q, dtype, dev, 4) + _heads("k", k, dtype, dev, 4) + _heads("v", v, dtype, dev, 4)
+              + _heads("out", out, dtype, dev, 4))
+    shape, k_shape = q.shape, k.shape
+    B, T, Hq, D = shape
+    N, Hk = k_shape[1], k_shape[2]
+    if k_shape != (B, N, Hk, D) or v.shape != k_shape or out.shape != shape:
         raise ValueError("q and out must be [B][T][Hq][D], k and v [B][N][Hk][D]")
     wp, wn = _attn_ws(ws, dev)
+    at = _marshal.at
+    _pack_heads[4](_marshal.heads, 0, *fields)
     _check(load_library().rm_span_attention(
-        _attn_shape(q, Hk, scale, softcap), B, T, N, hq, hk, hv, ho, _int32("span", span, dev, (B, T, 2)),
-        _float32("slopes", slopes, dev, Hq), _int32("q_start", q_start, dev, (B,)), wp, wn, _stream(stream)))
+        _attn_shape(q, Hq, Hk, D, scale, softcap), B, T, N, at[0], at[1], at[2], at[3],
+        _vector("span", span, torch.int32, dev, (B, T, 2)), _vector("slopes", slopes, torch.float32, dev, (Hq,)),
+        _vector("q_start", q_start, torch.int32, dev, (B,)), wp, wn, _stream(stream)))
 
 
 def prefix_attention_workspace(q: torch.Tensor, k_prefix: torch.Tensor, k_own: torch.Tensor) -> torch.Tensor:
@@ -710,8 +736,8 @@ def prefix_attention_workspace(q: torch.Tensor, k_prefix: torch.Tensor, k_own: t
     groups = k_prefix.shape[0]
     if groups <= 0 or q.shape[0] % groups != 0:
         raise ValueError("the samples must divide into the prefixes' groups")
-    _check(load_library().rm_prefix_attention_workspace_size(_attn_shape(q, k_own.shape[2], None, 0.0), groups,
-                                                             q.shape[0] // groups, q.shape[1], k_prefix.shape[1],
+    _check(load_library().rm_prefix_attention_workspace_size(_attn_shape(q, q.shape[2], k_own.shape[2], q.shape[3], None, 0.0),
+                                                             groups, q.shape[0] // groups, q.shape[1], k_prefix.shape[1],
                                                              k_own.shape[1], ctypes.byref(out)))
     return torch.empty(int(out.value), dtype=torch.uint8, device=q.device)
 
@@ -723,22 +749,26 @@ def rm_prefix_attention(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch
     """Samples q [groups * per_group][T][Hq][D] over their group's prefix keys k_prefix [groups][P][Hk][D] and their own
     k_own [groups * per_group][S][Hk][D], one softmax over both; scale None: 1 / sqrt(D)."""
     dev = _attn_device(q, stream)
-    hq, ho = _heads("q", q, q.dtype, dev, 4), _heads("out", out, q.dtype, dev, 4)
-    hkp, hvp = _heads("k_prefix", k_prefix, q.dtype, dev, 4), _heads("v_prefix", v_prefix, q.dtype, dev, 4)
-    hko, hvo = _heads("k_own", k_own, q.dtype, dev, 4), _heads("v_own", v_own, q.dtype, dev, 4)
-    B, T, Hq, D = q.shape
-    groups, P, Hk, _ = k_prefix.shape
-    S = k_own.shape[1]
+    dtype = q.dtype
+    fields = (_heads("q", q, dtype, dev, 4) + _heads("k_prefix", k_prefix, dtype, dev, 4)
+              + _heads("v_prefix", v_prefix, dtype, dev, 4) + _heads("k_own", k_own, dtype, dev, 4)
+              + _heads("v_own", v_own, dtype, dev, 4) + _heads("out", out, dtype, dev, 4))
+    shape, p_shape, o_shape = q.shape, k_prefix.shape, k_own.shape
+    B, T, Hq, D = shape
+    groups, P, Hk, _ = p_shape
+    S = o_shape[1]
     if groups <= 0 or B % groups != 0:
         raise ValueError("the samples must divide into the prefixes' groups")
-    if (k_prefix.shape != (groups, P, Hk, D) or v_prefix.shape != k_prefix.shape or k_own.shape != (B, S, Hk, D)
-            or v_own.shape != k_own.shape or out.shape != q.shape):
+    if (p_shape != (groups, P, Hk, D) or v_prefix.shape != p_shape or o_shape != (B, S, Hk, D)
+            or v_own.shape != o_shape or out.shape != shape):
         raise ValueError("q and out must be [B][T][Hq][D], the prefix [groups][P][Hk][D] and the own keys [B][S][Hk][D]")
     wp, wn = _attn_ws(ws, dev)
+    at = _marshal.at
+    _pack_heads[6](_marshal.heads, 0, *fields)
     _check(load_library().rm_prefix_attention(
-        _attn_shape(q, Hk, scale, softcap), groups, B // groups, T, P, S, hq, hkp, hvp,
-        _int32("prefix_len", prefix_len, dev, (groups,)), hko, hvo, _int32("own_len", own_len, dev, (B,)),
-        int(causal), ho, wp, wn, _stream(stream)))
+        _attn_shape(q, Hq, Hk, D, scale, softcap), groups, B // groups, T, P, S, at[0], at[1], at[2],
+        _vector("prefix_len", prefix_len, torch.int32, dev, (groups,)), at[3], at[4],
+        _vector("own_len", own_len, torch.int32, dev, (B,)), causal, at[5], wp, wn, _stream(stream)))
 
 
 def rm_profile_kernel_events(kernel: int, ev_begin: Optional[int], ev_end: Optional[int]) -> None:

@@ -15,8 +15,8 @@ __global__ __launch_bounds__(kSpanRows) void spans_kernel(int T, int N, int caus
                                                           const int32_t *__restrict__ kv_len,
                                                           const int32_t *__restrict__ prefix_len,
                                                           const int32_t *__restrict__ doc, int32_t *__restrict__ span) {
-    constexpr int kPer = 8, kStep = kSpanRows * kPer;
-    __shared__ int red[4];
+    constexpr int kPer = 8, kStep = kSpanRows * kPer, kNone = -0x7fffffff;
+    __shared__ int red[2][4];
     const int blocks = (T + kSpanRows - 1) / kSpanRows;
     const int b = blockIdx.x / blocks, i0 = (blockIdx.x - b * blocks) * kSpanRows;
     const int tid = threadIdx.x, i = i0 + tid;
@@ -37,36 +37,26 @@ __global__ __launch_bounds__(kSpanRows) void spans_kernel(int T, int N, int caus
         const int pa = static_cast<int>(min(max(start + i0, static_cast<int64_t>(0)), static_cast<int64_t>(N - 1)));
         const int pb = static_cast<int>(min(max(start + last_row, static_cast<int64_t>(0)), static_cast<int64_t>(N - 1)));
         auto begins = [&](int j) { return j == 0 || ids[j] != ids[j - 1]; };  // a run begins at j in [0, N)
-        auto block_max = [&](int v) {
-            for (int o = 32; o >= 1; o >>= 1) v = max(v, __shfl_xor(v, o));
-            __syncthreads();
-            if ((tid & 63) == 0) red[tid >> 6] = v;
-            __syncthreads();
-            return max(max(red[0], red[1]), max(red[2], red[3]));
-        };
-        int first = -1;  // the begin of pa's run; position 0 begins one, so the search ends
-        for (int base = pa; first < 0; base -= kStep) {
-            int best = -1;
+        // Both ends at a time: the greatest begin at or before pa, and minus the least one behind pb (N ends the last run,
+        // position 0 begins the first, so both searches end).
+        int first = -1, end = kNone;
+        for (int64_t step = 0; first < 0 || end == kNone; step += kStep) {
+            int best = -1, next = kNone;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
-                const int j = base - tid - k * kSpanRows;
-                if (j >= 0 && begins(j)) best = max(best, j);
+                const int64_t i = pa - step - tid - k * kSpanRows, j = pb + 1 + step + tid + k * kSpanRows;
+                if (first < 0 && i >= 0 && begins(static_cast<int>(i))) best = max(best, static_cast<int>(i));
+                if (end == kNone && (j == N || (j < N && begins(static_cast<int>(j))))) next = max(next, static_cast<int>(-j));
             }
-            first = block_max(best);
-        }
-        int end = -1;  // minus the end of pb's run, at most N
-        for (int64_t base = static_cast<int64_t>(pb) + 1;; base += kStep) {  // position N ends the last run
-            int best = -0x7fffffff;
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) {
-                const int64_t j = base + tid + k * kSpanRows;
-                if (j == N || (j < N && begins(static_cast<int>(j)))) best = max(best, static_cast<int>(-j));
+            for (int o = 32; o >= 1; o >>= 1) {
+                best = max(best, __shfl_xor(best, o));
+                next = max(next, __shfl_xor(next, o));
             }
-            best = block_max(best);
-            if (best != -0x7fffffff) {
-                end = best;
-                break;
-            }
+            __syncthreads();
+            if ((tid & 63) == 0) red[0][tid >> 6] = best, red[1][tid >> 6] = next;
+            __syncthreads();
+            if (first < 0) first = max(max(red[0][0], red[0][1]), max(red[0][2], red[0][3]));
+            if (end == kNone) end = max(max(red[1][0], red[1][1]), max(red[1][2], red[1][3]));
         }
         // This row's run: the last begin at or before p, and the first after it.
         const int p = static_cast<int>(min(max(p64, static_cast<int64_t>(0)), static_cast<int64_t>(N - 1)));

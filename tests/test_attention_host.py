@@ -18,7 +18,7 @@ def lib():
 
 
 def H(at, batch, token, head):
-    return rm.Heads(at, batch, token, head)
+    return ctypes.byref(rm.Heads(at, batch, token, head))
 
 
 def _span(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), B=2, T=4, N=100, q=None, k=None, v=None, out=None, span=None, slopes=None,
@@ -27,7 +27,7 @@ def _span(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), B=2, T=4, N=100, q=None, k=No
     k = k or H(2 * MB, N * 128, 128, 64)
     v = v or H(3 * MB, N * 128, 128, 64)
     out = out or H(4 * MB, T * 512, 512, 64)
-    return lib.rm_span_attention(rm.AttnShape(*shape), B, T, N, q, k, v, out, span, slopes, q_start, ws, ws_bytes, None)
+    return lib.rm_span_attention(ctypes.byref(rm.AttnShape(*shape)), B, T, N, q, k, v, out, span, slopes, q_start, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("kw,expected", [
@@ -80,7 +80,7 @@ def _prefix(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), G=2, per=3, T=4, P=100, S=2
     kp, vp = kp or H(2 * MB, P * 128, 128, 64), vp or H(3 * MB, P * 128, 128, 64)
     ko, vo = ko or H(5 * MB, S * 128, 128, 64), vo or H(6 * MB, S * 128, 128, 64)
     out = out or H(4 * MB, T * 512, 512, 64)
-    return lib.rm_prefix_attention(rm.AttnShape(*shape), G, per, T, P, S, q, kp, vp, plen, ko, vo, olen, 0, out, ws,
+    return lib.rm_prefix_attention(ctypes.byref(rm.AttnShape(*shape)), G, per, T, P, S, q, kp, vp, plen, ko, vo, olen, 0, out, ws,
                                    ws_bytes, None)
 
 
@@ -105,7 +105,7 @@ def test_prefix_attention_refuses(lib, kw, expected):
 
 def test_workspace_sizes(lib):
     n = ctypes.c_size_t(1)
-    s = rm.AttnShape(8, 2, 64, 1, 0.125, 0.0)
+    s = ctypes.byref(rm.AttnShape(8, 2, 64, 1, 0.125, 0.0))
     assert lib.rm_span_attention_workspace_size(s, 1, 4096, 4096, ctypes.byref(n)) == rm.RM_OK and n.value == 0
     assert lib.rm_span_attention_workspace_size(s, 1, 1, 65536, ctypes.byref(n)) == rm.RM_OK and n.value > 0
     assert n.value % 256 == 0
