@@ -99,14 +99,13 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
         return api_fail(RM_ERR_SHAPE, "too many query rows");
     const int64_t rows = static_cast<int64_t>(R), ng = static_cast<int64_t>(groups);
     q.dh = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-    q.pad = D != q.dh;
     constexpr int64_t kCUs = 256;
     const bool key_waves = ceil_div(rows, 128) * ng < 2 * kCUs || rows <= 32;
     q.kw = key_waves ? 4 : 1;
     q.rows = key_waves ? (!bf && q.dh == 256 ? 64 : 32) : 128;
     q.n_tiles = static_cast<int>(ceil_div(rows, q.rows));
     const int64_t wgs = q.n_tiles * ng;
-    if (wgs >= (static_cast<int64_t>(1) << 31)) return api_fail(RM_ERR_SHAPE, "launch grid too large");
+    if (wgs >= kMaxKeys) return api_fail(RM_ERR_SHAPE, "launch grid too large");
     // Few row blocks: several workgroups divide the keys, as many as fill the compute units once (two workgroups to one,
     // where their LDS allows it: heads up to 128 in bf16, 64 in float32), if the tiles that each of them then has less pay
     // for the second launch and the partial results.  In us: a tile of 128 keys 0.4 (64 columns), 0.8 (128), 1.6 (256);
@@ -153,8 +152,16 @@ rm_status attn_run(const rm_attn_shape *s, const rm_attn::Plan &p, rm_attn::Args
     }
     a.by_g = rm_attn::divisor(a.G);
     a.by_t = rm_attn::divisor(a.T);
+    a.by_hk = rm_attn::divisor(a.Hk);
+    a.by_splits = rm_attn::divisor(p.splits);
     a.n_tiles = p.n_tiles;
     a.splits = p.splits;
+    const int groups = a.U * a.Hk;
+    a.by_xcd = groups % 8 == 0;
+    const int of_xcd = a.by_xcd ? groups / 8 : groups;
+    a.turns = of_xcd <= 8;
+    a.order = a.turns ? of_xcd : p.n_tiles * p.splits;
+    a.by_order = rm_attn::divisor(a.order);
     if (p.total > 0) {
         a.part_o = static_cast<float *>(ws);
         a.part_ml = reinterpret_cast<float *>(static_cast<char *>(ws) + p.off_ml);

@@ -43,21 +43,19 @@ __device__ __forceinline__ const char *uniform(const char *p) {
 }
 
 // Two loads of 16 bytes per lane straight into LDS at lds + 16 lane and lds + STEP + 16 lane, each lane at its 32-bit
-// offset from a base in scalar registers; only the lanes of mask0 (mask1) take part.  M0 and EXEC are kept and put back.
+// offset from a base in scalar registers; only the lanes of mask take part.  M0 and EXEC are kept and put back.
 // No memory clobber: the buffers are read between the waits below only, which have one.
 template <int STEP>
-__device__ __forceinline__ void dma16_pair(const void *base, uint32_t off0, uint32_t off1, uint32_t lds, uint64_t mask0,
-                                           uint64_t mask1) {
+__device__ __forceinline__ void dma16_pair(const void *base, uint32_t off0, uint32_t off1, uint32_t lds, uint64_t mask) {
     uint32_t keep;
     uint64_t exec;
-    mask0 = uniform(static_cast<int64_t>(mask0));
-    mask1 = uniform(static_cast<int64_t>(mask1));
+    mask = uniform(static_cast<int64_t>(mask));
     asm volatile(
         "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_and_saveexec_b64 %1, %7\n\tglobal_load_lds_dwordx4 %2, %4\n\t"
-        "s_add_u32 m0, m0, %6\n\ts_and_b64 exec, %1, %8\n\tglobal_load_lds_dwordx4 %3, %4\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4\n\t"
         "s_mov_b64 exec, %1\n\ts_mov_b32 m0, %0"
         : "=&s"(keep), "=&s"(exec)
-        : "v"(off0), "v"(off1), "s"(uniform(static_cast<const char *>(base))), "s"(lds), "n"(STEP), "s"(mask0), "s"(mask1)
+        : "v"(off0), "v"(off1), "s"(uniform(static_cast<const char *>(base))), "s"(lds), "n"(STEP), "s"(mask)
         : "scc");
 }
 
@@ -121,21 +119,23 @@ struct Tile {
     int kb, end, seg, before;
 };
 
-// PAD: the head is narrower than the kernel's DH columns.
-template <bool BF, int DH, bool PAD, int RW, int KW, int QB, int KT, int NBUF, int WPE>
+// Rows have room for DH columns in LDS; the products take DC of them.  PAD: the head has fewer, more than LEAST.
+template <bool BF, int DH, int DC, bool PAD, int RW, int KW, int QB, int KT, int NBUF, int WPE>
 __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     constexpr int W = RW * KW, ES = BF ? 2 : 4, ROWB = DH * ES, CPR = ROWB / 16;
     constexpr int RPI = 64 / CPR;                // rows per load instruction of a wave (1 KB)
     constexpr int KPW = KT / KW, NS = KPW / 32;  // keys of a tile that a wave takes
     constexpr int NP = KPW / RPI / RW / 2;       // pairs of load instructions per wave and matrix
     constexpr int STEP = RW * RPI;               // rows from one of a wave's load instructions to the next
-    constexpr int DB = DH / 32;                  // output blocks of 32 columns
-    constexpr int QF = BF ? DH / 16 : DH / 8;    // fragments of a query row block
+    constexpr int DB = DC / 32;                  // output blocks of 32 columns
+    constexpr int QF = BF ? DC / 16 : DC / 8;    // fragments of a query row block
+    constexpr int LEAST = !PAD ? DC : DC == 256 ? 192 : DC == 192 ? 128 : DC == 128 ? 96 : DC == 96 ? 64 : 0;
+    static_assert(DC <= DH && (PAD || DC == DH), "columns");
     constexpr int AHEAD = 4;                     // LDS reads run this many matrix-core steps ahead
     static_assert(CPR >= 8 && CPR <= 64 && NP >= 1 && NP * 2 * STEP == KPW && NS * 32 == KPW, "tile shape");
     constexpr int TILEB = KPW * ROWB, KWB = 2 * NBUF * TILEB;  // one matrix's keys, and all buffers of a key wave
     // O of every wave passes through LDS when the key waves are joined.
-    constexpr int JOINB = KW > 1 ? W * QB * 32 * DH * 4 + W * QB * 32 * 8 : 0;
+    constexpr int JOINB = KW > 1 ? W * QB * 32 * DC * 4 + W * QB * 32 * 8 : 0;
     constexpr int LDSB = KW * KWB > JOINB ? KW * KWB : JOINB;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[LDSB];
 
@@ -148,18 +148,16 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     // row blocks with the most keys of all of them start first, many follow each other.
     int ng, tile_id;
     {
-        const int nt = a.n_tiles * a.splits, groups = a.U * a.Hk, id = blockIdx.x;
-        const bool by_xcd = (groups & 7) == 0;
-        const int i = by_xcd ? id >> 3 : id, n = by_xcd ? groups >> 3 : groups;
-        const bool turns = n <= 8;
-        const int g = turns ? i % n : i / nt;
-        tile_id = turns ? i / n : i % nt;
-        ng = by_xcd ? (id & 7) + 8 * g : g;
+        const int id = blockIdx.x, i = a.by_xcd ? id >> 3 : id;
+        const int x = divide(i, a.by_order), y = i - x * a.order;
+        const int g = a.turns ? y : x;
+        tile_id = a.turns ? x : y;
+        ng = a.by_xcd ? (id & 7) + 8 * g : g;
     }
-    const int split = tile_id % a.splits;
+    const int row_tile = divide(tile_id, a.by_splits), split = tile_id - row_tile * a.splits;
     // Row blocks from the last to the first: with causal masks the later ones see more keys and start first.
-    const int row0 = (a.n_tiles - 1 - tile_id / a.splits) * (32 * RW * QB);
-    const int u = ng / a.Hk, hk = ng % a.Hk;
+    const int row0 = (a.n_tiles - 1 - row_tile) * (32 * RW * QB);
+    const int u = divide(ng, a.by_hk), hk = ng - u * a.Hk;
     const int rows_end = min(row0 + 32 * RW * QB, a.R);
 
     // ---------------------------------------------------------------- queries
@@ -338,8 +336,8 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     const int lrow = rw * RPI + lane / CPR;
     const uint32_t chunk_k = (lane % CPR ^ swz_k(lrow)) * 16, chunk_v = (lane % CPR ^ swz_v(lrow)) * 16;
     // Loads of pair p of a matrix of tile t into buffer buf.  Rows past the last key are that key again (their scores are
-    // masked); columns past the head's are zeros of the keys, set once, and any of the values.  Token strides are below
-    // 2^24 bytes, so a tile's offsets fit in 32 bits.
+    // masked) and columns past the head's its last ones (set to zero where they meet queries, or not written).  Token strides are
+    // below 2^24 bytes, so a tile's offsets fit in 32 bits.
     auto stage = [&](const Tile &t, int buf, bool values, int p, uint64_t mask) __attribute__((always_inline)) {
         const uint32_t sn = static_cast<uint32_t>(values ? t.vn : t.kn);
         const int last = t.end - 1 - t.kb;
@@ -347,21 +345,17 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         uint32_t chunk = values ? chunk_v : chunk_k;
         asm volatile("" : "+v"(row), "+v"(chunk));  // (else every instruction's offset is kept in a register)
         uint32_t off[2];
-        uint64_t m[2] = {mask, mask};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int n = 2 * p + i;
             uint32_t c = chunk ^ static_cast<uint32_t>((values ? swz_v(n * STEP) : swz_k(n * STEP)) * 16);
-            if constexpr (PAD) {
-                if (values) c = min(c, static_cast<uint32_t>(a.D * ES - 16));
-                else m[i] &= __ballot(c < static_cast<uint32_t>(a.D * ES));
-            }
+            if constexpr (PAD) c = min(c, static_cast<uint32_t>(a.D * ES - 16));
             off[i] = (static_cast<uint32_t>(min(row + n * STEP, last)) & 0xffffffu) * (sn & 0xffffffu) + c;
         }
         dma16_pair<RW * 1024>(values ? t.v : t.k, off[0], off[1],
                               __builtin_amdgcn_readfirstlane(lds_at + (buf * 2 + (values ? 1 : 0)) * TILEB +
                                                              2 * p * RW * 1024),
-                              m[0], m[1]);
+                              mask);
     };
     // Waits until all but this wave's last `N` loads are there and its LDS reads are done; where several waves share
     // the buffers, until that holds for all of them.
@@ -388,12 +382,6 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             for (int p = 0; p < NP; ++p) stage(cur, 0, true, p, kAll);
         }
     };
-    if constexpr (PAD) {
-        for (int b = 0; b < NBUF; ++b)
-            for (int i = rw * 64 + lane; i < TILEB / 16; i += 64 * RW)
-                *(reinterpret_cast<rm_u32x4 *>(lds_w + 2 * b * TILEB) + i) = rm_u32x4{0, 0, 0, 0};
-        sync(None{});
-    }
     if (n_tiles > 0) start();
 
     // ---------------------------------------------------------------- fragment addresses
@@ -462,10 +450,13 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                 for (int ns = 0; ns < NS; ++ns) s[qb][ns] = rm_f32x16{};
             {  // S^T = K Q^T; with two buffers the next tile's keys go out meanwhile, with one this tile's values
                 constexpr int X = QF * NS;
-                QFrag kf[X];
+                QFrag kf[2 * AHEAD];
                 auto read_k = [&](int x) __attribute__((always_inline)) {
                     const int c = x / NS, ns = x % NS;
-                    kf[x] = *reinterpret_cast<const QFrag *>(kb_ptr[c & 7] + at + ns * 32 * ROWB + (c >> 3) * 256);
+                    QFrag f = *reinterpret_cast<const QFrag *>(kb_ptr[c & 7] + at + ns * 32 * ROWB + (c >> 3) * 256);
+                    constexpr int E = 16 / ES;  // columns past the head's, not to meet the queries' zeros there
+                    if (PAD && (2 * c + 2) * E > LEAST) f = (2 * c + hi) * E < a.D ? f : QFrag{};
+                    kf[x % (2 * AHEAD)] = f;
                 };
 #pragma unroll
                 for (int x = 0; x < AHEAD; ++x) read_k(x);
@@ -476,12 +467,12 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                     for (int qb = 0; qb < QB; ++qb) {
                         if constexpr (BF) {
                             s[qb][x % NS] =
-                                __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], qf[qb][x / NS], s[qb][x % NS], 0, 0, 0);
+                                __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x % (2 * AHEAD)], qf[qb][x / NS], s[qb][x % NS], 0, 0, 0);
                         } else {
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                s[qb][x % NS] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[x][i], qf[qb][x / NS][i],
-                                                                                    s[qb][x % NS], 0, 0, 0);
+                                s[qb][x % NS] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                                    kf[x % (2 * AHEAD)][i], qf[qb][x / NS][i], s[qb][x % NS], 0, 0, 0);
                         }
                     }
                     if (x + AHEAD < X) read_k(x + AHEAD);
@@ -540,11 +531,12 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                                     : -INFINITY;
                     }
                 }
-                float top = s[qb][0][0];
+                float part[4] = {s[qb][0][0], s[qb][0][1], s[qb][0][2], s[qb][0][3]};
 #pragma unroll
                 for (int ns = 0; ns < NS; ++ns)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[qb][ns][i]);
+                    for (int i = ns == 0 ? 4 : 0; i < 16; ++i) part[i & 3] = fmaxf(part[i & 3], s[qb][ns][i]);
+                float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
                 top = BF ? fmaf(xor32_max(top), sc, off) : xor32_max(top) * sc;
                 // Raising the maximum of a row without sums so far (m = -inf) needs no rescaling.
                 const bool raise = top > m[qb] + kRaise;  // (false for top = -inf)
@@ -704,7 +696,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) l[qb] = xor32_sum(l[qb]);
     float *join = reinterpret_cast<float *>(lds);
-    float *ml = join + W * QB * 32 * DH;  // [wave][qb][2][32]
+    float *ml = join + W * QB * 32 * DC;  // [wave][qb][2][32]
     if constexpr (KW > 1) {  // (every wave has read the last tile: the barrier after the pass)
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {

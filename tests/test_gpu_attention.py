@@ -101,6 +101,32 @@ def test_full_spans(dtype, D, T, N):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", list(range(16, 257, 24)) + [96, 192])
+@pytest.mark.parametrize("many", [False, True])
+def test_every_kernel_width(dtype, D, many):
+    """Head widths inside each of the kernels' classes, with keys whose infinite components a row sees: a score of
+    -infinity has no weight, +infinity none that is defined."""
+    g = gen(11, D, many)
+    B, T, N, Hq, Hk = (40, 130, 130, 16, 16) if many else (2, 12, 140, 4, 2)
+    q, k, v = randn(g, (B, T, Hq, D), dtype, 2.0), randn(g, (B, N, Hk, D), dtype), randn(g, (B, N, Hk, D), dtype)
+    q[..., D - 1] = q[..., D - 1].abs() + 0.5
+    out = run_span(q, k, v)
+    for b, h in ((0, 0), (B - 1, Hq - 1)):
+        kv = h // (Hq // Hk)
+        check_span(q[b:b + 1, :, h:h + 1], k[b:b + 1, :, kv:kv + 1], v[b:b + 1, :, kv:kv + 1], out=out[b:b + 1, :, h:h + 1])
+    span = torch.tensor([1, N], dtype=torch.int32, device="cuda").expand(B, T, 2).contiguous()
+    k2 = k.clone()
+    k2[:, 0, :, D - 1] = -float("inf")
+    out = run_span(q, k2, v)
+    for b, h in ((0, 0), (B - 1, Hq - 1)):  # as if the first key were not there
+        kv = h // (Hq // Hk)
+        check_span(q[b:b + 1, :, h:h + 1], k[b:b + 1, :, kv:kv + 1], v[b:b + 1, :, kv:kv + 1], span[b:b + 1],
+                   out=out[b:b + 1, :, h:h + 1])
+    k[:, 0, :, D - 1] = float("inf")
+    assert bool(run_span(q, k, v).isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("Hq,Hk", [(1, 1), (3, 3), (8, 1), (6, 2), (40, 1)])
 def test_head_layouts(dtype, Hq, Hk):
     g = gen(2, Hq, Hk)
