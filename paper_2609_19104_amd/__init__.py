@@ -589,14 +589,30 @@ _pack_heads = [struct.Struct("=" + "Qqqq" * n).pack_into for n in range(7)]
 _pack_shape = struct.Struct("=iiiiff").pack_into
 
 
+def _heads4(name: str, t: torch.Tensor, dtype, index: int) -> Tuple[int, int, int, int]:
+    """The fields of an rm_heads for a tensor of head vectors [B][T][H][D] on device `index`."""
+    try:  # the usual case first
+        b, n, h, c = t.stride()
+        if c == 1 and t.dtype is dtype and t.get_device() == index:
+            return t.data_ptr(), b, n, h
+    except (AttributeError, ValueError):
+        pass
+    return _heads(name, t, dtype, index, 4)
+
+
+def _heads3(name: str, t: torch.Tensor, dtype, index: int) -> Tuple[int, int, int, int]:
+    """The same for [T][H][D]."""
+    try:
+        n, h, c = t.stride()
+        if c == 1 and t.dtype is dtype and t.get_device() == index:
+            return t.data_ptr(), 0, n, h
+    except (AttributeError, ValueError):
+        pass
+    return _heads(name, t, dtype, index, 3)
+
+
 def _heads(name: str, t: torch.Tensor, dtype, index: int, ndim: int) -> Tuple[int, int, int, int]:
-    """The fields of an rm_heads for a tensor of head vectors ([B][T][H][D], or [T][H][D] without a batch axis) on
-    device `index`."""
-    if isinstance(t, torch.Tensor):
-        st = t.stride()
-        if t.dtype == dtype and len(st) == ndim and t.get_device() == index and (st[-1] == 1 or t.shape[-1] == 1):
-            return t.data_ptr(), st[0] if ndim == 4 else 0, st[-3], st[-2]
-    else:
+    if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.get_device() != index:
         raise ValueError(f"{name} must be on a HIP device, the same as the other tensors, got {t.device}")
@@ -604,14 +620,17 @@ def _heads(name: str, t: torch.Tensor, dtype, index: int, ndim: int) -> Tuple[in
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
     if t.dim() != ndim:
         raise ValueError(f"{name} must have {ndim} dims, got {tuple(t.shape)}")
-    raise ValueError(f"{name}: the elements of a head must be consecutive")
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] != 1:
+        raise ValueError(f"{name}: the elements of a head must be consecutive")
+    return t.data_ptr(), st[0] if ndim == 4 else 0, st[-3], st[-2]
 
 
 def _vector(name: str, t: Optional[torch.Tensor], dtype, index: int, shape) -> Optional[int]:
     """Pointer of an optional contiguous tensor of a dtype, device and shape."""
     if t is None:
         return None
-    if (isinstance(t, torch.Tensor) and t.dtype == dtype and t.get_device() == index and t.shape == shape
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape
             and t.is_contiguous()):
         return t.data_ptr()
     _need_cuda(name, t, (dtype,))
@@ -624,11 +643,12 @@ def _attn_device(t: torch.Tensor, stream) -> int:
     if index < 0:
         raise ValueError("tensors must be on a HIP device")
     if stream is None and index != torch._C._cuda_getDevice():
-        raise ValueError(f"tensors are on {t.device}, which is not the current device: select it or give a stream of it")
+        raise ValueError(f"tensors are on {t.device}, not the current device: select it or give a stream of it")
     return index
 
 
-def _attn_shape(q: torch.Tensor, n_q_heads: int, n_kv_heads: int, D: int, scale: Optional[float], softcap: float) -> int:
+def _attn_shape(q: torch.Tensor, n_q_heads: int, n_kv_heads: int, D: int, scale: Optional[float],
+                softcap: float) -> int:
     """Address of the call's rm_attn_shape."""
     dtype = _ATTN_DTYPES.get(q.dtype)
     if dtype is None:
@@ -659,8 +679,8 @@ def rm_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor],
     src, dst = q.dtype, q_out.dtype
     if src not in _ATTN_DTYPES or dst not in _ATTN_DTYPES:
         raise ValueError("queries and outputs must be float32 or bfloat16")
-    fields = (_heads("q", q, src, dev, 3) + _heads("k", k, src, dev, 3) + _heads("q_out", q_out, dst, dev, 3)
-              + _heads("k_out", k_out, dst, dev, 3))
+    fields = (_heads3("q", q, src, dev) + _heads3("k", k, src, dev) + _heads3("q_out", q_out, dst, dev)
+              + _heads3("k_out", k_out, dst, dev))
     shape, k_shape, ko_shape = q.shape, k.shape, k_out.shape
     N, Hq, D = shape
     Hk, rows = k_shape[1], ko_shape[0]
@@ -669,7 +689,7 @@ def rm_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor],
     if (v is None) != (v_out is None):
         raise ValueError("v and v_out go together")
     if v is not None:
-        fields += _heads("v", v, src, dev, 3) + _heads("v_out", v_out, dst, dev, 3)
+        fields += _heads3("v", v, src, dev) + _heads3("v_out", v_out, dst, dev)
         if v.shape != k_shape or v_out.shape != ko_shape:
             raise ValueError("v must have k's shape and v_out k_out's")
     rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
@@ -701,8 +721,9 @@ def rm_attn_spans(span: torch.Tensor, N: int, causal: bool = True, window: int =
 def span_attention_workspace(q: torch.Tensor, k: torch.Tensor) -> torch.Tensor:
     """A workspace tensor (uint8) of the size rm_span_attention_workspace_size asks for (it may be 0)."""
     out = ctypes.c_size_t(0)
-    _check(load_library().rm_span_attention_workspace_size(_attn_shape(q, q.shape[2], k.shape[2], q.shape[3], None, 0.0),
-                                                           q.shape[0], q.shape[1], k.shape[1], ctypes.byref(out)))
+    shape = _attn_shape(q, q.shape[2], k.shape[2], q.shape[3], None, 0.0)
+    _check(load_library().rm_span_attention_workspace_size(shape, q.shape[0], q.shape[1], k.shape[1],
+                                                           ctypes.byref(out)))
     return torch.empty(int(out.value), dtype=torch.uint8, device=q.device)
 
 
@@ -714,8 +735,8 @@ def rm_span_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: to
     scale None: 1 / sqrt(D)."""
     dev = _attn_device(q, stream)
     dtype = q.dtype
-    fields = (_heads("q", q, dtype, dev, 4) + _heads("k", k, dtype, dev, 4) + _heads("v", v, dtype, dev, 4)
-              + _heads("out", out, dtype, dev, 4))
+    fields = (_heads4("q", q, dtype, dev) + _heads4("k", k, dtype, dev) + _heads4("v", v, dtype, dev)
+              + _heads4("out", out, dtype, dev))
     shape, k_shape = q.shape, k.shape
     B, T, Hq, D = shape
     N, Hk = k_shape[1], k_shape[2]
@@ -736,9 +757,9 @@ def prefix_attention_workspace(q: torch.Tensor, k_prefix: torch.Tensor, k_own: t
     groups = k_prefix.shape[0]
     if groups <= 0 or q.shape[0] % groups != 0:
         raise ValueError("the samples must divide into the prefixes' groups")
-    _check(load_library().rm_prefix_attention_workspace_size(_attn_shape(q, q.shape[2], k_own.shape[2], q.shape[3], None, 0.0),
-                                                             groups, q.shape[0] // groups, q.shape[1], k_prefix.shape[1],
-                                                             k_own.shape[1], ctypes.byref(out)))
+    shape = _attn_shape(q, q.shape[2], k_own.shape[2], q.shape[3], None, 0.0)
+    _check(load_library().rm_prefix_attention_workspace_size(shape, groups, q.shape[0] // groups, q.shape[1],
+                                                             k_prefix.shape[1], k_own.shape[1], ctypes.byref(out)))
     return torch.empty(int(out.value), dtype=torch.uint8, device=q.device)
 
 
@@ -750,9 +771,9 @@ def rm_prefix_attention(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch
     k_own [groups * per_group][S][Hk][D], one softmax over both; scale None: 1 / sqrt(D)."""
     dev = _attn_device(q, stream)
     dtype = q.dtype
-    fields = (_heads("q", q, dtype, dev, 4) + _heads("k_prefix", k_prefix, dtype, dev, 4)
-              + _heads("v_prefix", v_prefix, dtype, dev, 4) + _heads("k_own", k_own, dtype, dev, 4)
-              + _heads("v_own", v_own, dtype, dev, 4) + _heads("out", out, dtype, dev, 4))
+    fields = (_heads4("q", q, dtype, dev) + _heads4("k_prefix", k_prefix, dtype, dev)
+              + _heads4("v_prefix", v_prefix, dtype, dev) + _heads4("k_own", k_own, dtype, dev)
+              + _heads4("v_own", v_own, dtype, dev) + _heads4("out", out, dtype, dev))
     shape, p_shape, o_shape = q.shape, k_prefix.shape, k_own.shape
     B, T, Hq, D = shape
     groups, P, Hk, _ = p_shape
@@ -761,7 +782,7 @@ def rm_prefix_attention(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch
         raise ValueError("the samples must divide into the prefixes' groups")
     if (p_shape != (groups, P, Hk, D) or v_prefix.shape != p_shape or o_shape != (B, S, Hk, D)
             or v_own.shape != o_shape or out.shape != shape):
-        raise ValueError("q and out must be [B][T][Hq][D], the prefix [groups][P][Hk][D] and the own keys [B][S][Hk][D]")
+        raise ValueError("q and out must be [B][T][Hq][D], the prefix [groups][P][Hk][D], the own keys [B][S][Hk][D]")
     wp, wn = _attn_ws(ws, dev)
     at = _marshal.at
     _pack_heads[6](_marshal.heads, 0, *fields)
