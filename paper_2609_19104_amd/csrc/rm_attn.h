@@ -143,6 +143,14 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rw = wave % RW, kw = wave / RW;
 
+    // Every cache line of the arguments requested at once: met one after the other, each would cost a trip to the L2.
+    {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(&a);
+        constexpr int N = sizeof(Args) / 64;
+        static_assert(N <= 8, "argument lines");
+        asm volatile("" ::"s"(w[0]), "s"(w[16]), "s"(w[32]), "s"(w[48]), "s"(w[64]), "s"(w[16 * (N < 5 ? N : 5)]),
+                     "s"(w[16 * (N < 6 ? N : 6)]), "s"(w[16 * (N < 7 ? N : 7)]));
+    }
     // This workgroup's key head of a group, row block and slice of the keys.  A group's workgroups go to one XCD where
     // the groups divide among the XCDs, whose L2 then holds their keys; few groups (of an XCD) take turns, so that the
     // row blocks with the most keys of all of them start first, many follow each other.
