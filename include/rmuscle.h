@@ -314,7 +314,8 @@ typedef struct rm_heads {
 /* n_q_heads: a multiple of n_kv_heads; query head h uses key head h / (n_q_heads / n_kv_heads).
  * head_dim: a multiple of 8, at most 256.  dtype: an rm_dtype, of queries, keys, values and output.
  * scale: finite and positive; scores are scale * <q, k>.  softcap: >= 0; not 0: scores become softcap * tanh(score / softcap).
- * Scores, maxima, sums and the output are accumulated in float32; with RM_BF16 the softmax's weights are rounded to
+ * A call takes fewer than 2^30 query rows (tokens times query heads of a key head) of one sample or group, and fewer than
+ * 2^24 blocks of 32 of them in all.  Scores, maxima, sums and the output are accumulated in float32; with RM_BF16 the softmax's weights are rounded to
  * bf16 before their product with the values (as the values are), their sum is not. */
 typedef struct rm_attn_shape {
     int32_t n_q_heads, n_kv_heads, head_dim, dtype;
@@ -334,7 +335,7 @@ typedef struct rm_attn_shape {
  *             value; NULL: row n (rows >= n_tok).  Slots are distinct: tokens that share one leave an unspecified
  *             mix of theirs in it.  Other rows keep what they hold.
  * head_dim a multiple of 8, at most 256; rot a multiple of 4 in [0, head_dim].  Angles are reduced in 64 bits,
- * everything else is float32.  n_tok >= 0.  Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN. */
+ * everything else is float32.  0 <= n_tok < 2^26, n_tok x heads < 2^30.  Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN. */
 rm_status rm_qk_norm_rope(int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t in_dtype,
                           int32_t out_dtype, const rm_heads *q, const rm_heads *k, const rm_heads *v,
                           const rm_heads *q_out, const rm_heads *k_out, const rm_heads *v_out, int32_t rows,
@@ -348,7 +349,7 @@ rm_status rm_qk_norm_rope(int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads, 
  *     with doc: both cut to the run of equal ids doc[b][.] that holds p; a row of a negative id sees nothing.
  * With causal or doc a row at a position outside [0, kv_len[b]) sees nothing.  A row that sees nothing gets (0, 0).
  *   q_start, kv_len, prefix_len: int32 [B] or NULL.  doc: int32 [B][N] or NULL.  span: int32 [B][T][2], out.
- * B, T, N >= 1, N < 2^30, window >= 0. */
+ * B, T, N >= 1, N < 2^30, B ceil(T / 256) < 2^24, window >= 0. */
 rm_status rm_attn_spans(int32_t B, int32_t T, int32_t N, int32_t causal, int32_t window, const int32_t *q_start,
                         const int32_t *kv_len, const int32_t *prefix_len, const int32_t *doc, int32_t *span,
                         void *stream);

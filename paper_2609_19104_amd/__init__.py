@@ -638,12 +638,14 @@ def _vector(name: str, t: Optional[torch.Tensor], dtype, index: int, shape) -> O
 
 
 def _attn_device(t: torch.Tensor, stream) -> int:
-    """The tensors' device; without a stream given it has to be the current one, whose stream the call runs on."""
+    """The tensors' device, which has to be the current one (the kernels are launched there), as the stream's has."""
     index = t.get_device() if isinstance(t, torch.Tensor) else -1
     if index < 0:
         raise ValueError("tensors must be on a HIP device")
-    if stream is None and index != torch._C._cuda_getDevice():
-        raise ValueError(f"tensors are on {t.device}, not the current device: select it or give a stream of it")
+    if index != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors are on {t.device}, which is not the current device")
+    if stream is not None and getattr(stream, "device_index", index) != index:
+        raise ValueError(f"the stream is of another device than the tensors, which are on {t.device}")
     return index
 
 

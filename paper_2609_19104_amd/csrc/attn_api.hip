@@ -18,6 +18,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t elem(int dtype) { return dtype == RM_BF16 ? 2 : 4; }
 
 constexpr int kMaxKeys = 1 << 30;
+constexpr int64_t kMaxGroups = 1 << 24;  // workgroups of 256 threads: a launch holds below 2^32 threads
 
 struct Extent {
     const void *p = nullptr;
@@ -105,7 +106,7 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     q.rows = key_waves ? (!bf && q.dh == 256 ? 64 : 32) : 128;
     q.n_tiles = static_cast<int>(ceil_div(rows, q.rows));
     const int64_t wgs = q.n_tiles * ng;
-    if (wgs >= kMaxKeys) return api_fail(RM_ERR_SHAPE, "launch grid too large");
+    if (wgs >= kMaxGroups) return api_fail(RM_ERR_SHAPE, "launch grid too large");
     // Few row blocks: several workgroups divide the keys, as many as fill the compute units once (two workgroups to one,
     // where their LDS allows it: heads up to 128 in bf16, 64 in float32), if the tiles that each of them then has less pay
     // for the second launch and the partial results.  In us: a tile of 128 keys 0.4 (64 columns), 0.8 (128), 1.6 (256);
@@ -198,7 +199,7 @@ RM_EXPORT rm_status rm_qk_norm_rope(int32_t n_tok, int32_t n_q_heads, int32_t n_
         return api_fail(RM_ERR_SHAPE, "rows=%d hold fewer than the n_tok=%d tokens (no slots given)", rows, n_tok);
     const bool values = v != nullptr && v->data != nullptr;
     const int64_t heads = static_cast<int64_t>(n_q_heads) + n_kv_heads * (values ? 2LL : 1LL);
-    if (heads > 65535 || n_tok * heads >= (1LL << 30))
+    if (heads > 65535 || n_tok * heads >= (1LL << 30) || n_tok >= 4 * kMaxGroups)
         return api_fail(RM_ERR_SHAPE, "n_tok x heads = %d x %lld is too large", n_tok, static_cast<long long>(heads));
     const size_t ie = elem(in_dtype), oe = elem(out_dtype);
     Extent x[6];
@@ -257,7 +258,7 @@ RM_EXPORT rm_status rm_attn_spans(int32_t B, int32_t T, int32_t N, int32_t causa
     if (!span) return api_fail(RM_ERR_INVALID_ARG, "span is NULL");
     if (!aligned(q_start, 4) || !aligned(kv_len, 4) || !aligned(prefix_len, 4) || !aligned(doc, 4) || !aligned(span, 8))
         return api_fail(RM_ERR_ALIGN, "span must be 8-byte and the other pointers 4-byte aligned");
-    if (ceil_div(T, 256) * B >= (1LL << 31)) return api_fail(RM_ERR_SHAPE, "launch grid too large");
+    if (ceil_div(T, 256) * B >= kMaxGroups) return api_fail(RM_ERR_SHAPE, "launch grid too large");
     const size_t b4 = static_cast<size_t>(B) * 4;
     const Extent out{span, static_cast<size_t>(B) * T * 8};
     const Extent in[4] = {{q_start, q_start ? b4 : 0}, {kv_len, kv_len ? b4 : 0}, {prefix_len, prefix_len ? b4 : 0},

@@ -46,6 +46,7 @@ def _span(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), B=2, T=4, N=100, q=None, k=No
     (dict(N=1 << 30), rm.RM_ERR_SHAPE),
     (dict(T=1 << 30), rm.RM_ERR_SHAPE),
     (dict(q=H(None, 2048, 512, 64)), rm.RM_ERR_INVALID_ARG),
+    (dict(B=1 << 23, T=1), rm.RM_ERR_SHAPE),                        # more workgroups than a launch takes
     (dict(q=H(MB + 8, 2048, 512, 64)), rm.RM_ERR_ALIGN),
     (dict(k=H(2 * MB, 12800, 132, 64)), rm.RM_ERR_ALIGN),
     (dict(k=H(2 * MB, 12800, -128, 64)), rm.RM_ERR_SHAPE),
@@ -139,6 +140,7 @@ def _rope(lib, *, N=5, Hq=4, Hk=2, D=64, ind=1, outd=1, q=None, k=None, v=None, 
     (dict(eps=float("nan")), rm.RM_ERR_INVALID_ARG),
     (dict(slot=None, rows=4), rm.RM_ERR_SHAPE),
     (dict(N=1 << 29), rm.RM_ERR_SHAPE),
+    (dict(N=1 << 26, rows=1 << 26), rm.RM_ERR_SHAPE),
     (dict(pos=None), rm.RM_ERR_INVALID_ARG),
     (dict(f=None), rm.RM_ERR_INVALID_ARG),
     (dict(pos=7 * MB + 2), rm.RM_ERR_ALIGN),
@@ -162,6 +164,7 @@ def test_qk_norm_rope_refuses(lib, kw, expected):
     ((1, 4, 0, 1, 0, None, None, None, None, MB), rm.RM_ERR_INVALID_ARG),
     ((1, 4, 1 << 30, 1, 0, None, None, None, None, MB), rm.RM_ERR_SHAPE),
     ((1, 4, 4, 1, -1, None, None, None, None, MB), rm.RM_ERR_INVALID_ARG),
+    ((1 << 24, 1, 4, 1, 0, None, None, None, None, MB), rm.RM_ERR_SHAPE),
     ((1, 4, 4, 0, 0, None, None, 2 * MB, None, MB), rm.RM_ERR_INVALID_ARG),  # prefix lengths without causal
     ((1, 4, 4, 1, 0, None, None, None, None, None), rm.RM_ERR_INVALID_ARG),
     ((1, 4, 4, 1, 0, None, None, None, None, MB + 4), rm.RM_ERR_ALIGN),

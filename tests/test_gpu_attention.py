@@ -282,6 +282,28 @@ def test_offsets_past_32_bits():
     assert torch.allclose(run_span(q, far, vv, span).float(), base.float(), atol=2e-2, rtol=2e-2)
 
 
+def test_widest_token_stride():
+    """Tokens just below 16 MiB apart: a tile's offsets pass 2^31 bytes."""
+    D, N, step = 64, 130, (1 << 23) - 8
+    buf = torch.zeros((N * step,), dtype=BF, device="cuda")
+    g = gen(12)
+    k, v = (torch.as_strided(buf, (1, N, 2, D), (0, step, 128, 1), at) for at in (0, 512))
+    k.copy_(randn(g, (1, N, 2, D), BF))
+    v.copy_(randn(g, (1, N, 2, D), BF))
+    q = randn(g, (1, 3, 4, D), BF)
+    out = check_span(q, k, v)
+    assert torch.equal(run_span(q, k.contiguous(), v.contiguous()), out)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Hq,Hk,T", [(35, 5, 13), (9, 3, 50), (11, 1, 3), (64, 1, 5)])
+def test_heads_that_do_not_divide_the_row_blocks(dtype, Hq, Hk, T):
+    g = gen(13, Hq, T)
+    N = 77
+    check_span(randn(g, (3, T, Hq, 64), dtype, 2.0), randn(g, (3, N, Hk, 64), dtype), randn(g, (3, N, Hk, 64), dtype),
+               random_spans(g, 3, T, N), torch.linspace(0, 0.2, Hq, device="cuda"), ints([5, 0, 70]))
+
+
 # ---------------------------------------------------------------------------------------------- shared prefix
 
 def run_prefix(q, kp, vp, ko, vo, plen=None, olen=None, causal=False, scale=None, cap=0.0):
