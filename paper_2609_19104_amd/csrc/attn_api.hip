@@ -109,12 +109,13 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     if (wgs >= kMaxGroups) return api_fail(RM_ERR_SHAPE, "launch grid too large");
     // Few row blocks: several workgroups divide the keys, as many as fill the compute units once (two workgroups to one,
     // where their LDS allows it: heads up to 128 in bf16, 64 in float32), if the tiles that each of them then has less pay
-    // for the second launch and the partial results.  In us: a tile of 128 keys 0.4 (64 columns), 0.8 (128), 1.6 (256);
-    // the join 4 and its traffic at 4 TB/s.
+    // for the second launch and the partial results.  Measured, us: a tile of 128 keys 0.9, 1.1 and 1.65 in bf16 (rows
+    // of 64, 128 and 256 columns), 2.3, 4.1 and 14 in float32; the join 5 and its traffic at 4 TB/s (one action
+    // chunk's 408 rows on 901 keys, D = 256: 20.2 us undivided, 14.2 in 8 slices; 6528 rows 24.4 undivided, 38.7 in 2).
     const int64_t tiles = ceil_div(n0, 128) + ceil_div(n1, 128);
     const int64_t slots = kCUs * (q.dh * (bf ? 1 : 2) <= 128 ? 2 : 1);
-    const double tile_us = 0.4 * (q.dh / 64) * (bf ? 1 : 2), join_us = 4.0;
-    const double part_us = static_cast<double>(rows) * ng * D * 8 / 4e6;  // one slice's results written and read
+    const double tile_us = bf ? 0.65 + q.dh / 256.0 : q.dh == 256 ? 14.0 : 0.5 + q.dh / 36.0;
+    const double join_us = 5.0, part_us = static_cast<double>(rows) * ng * D * 8 / 4e6;  // one slice's results
     q.splits = 1;
     double best = tiles * tile_us;
     for (int64_t n = 2; n * wgs <= slots && n <= tiles; n += n < 16 ? 1 : n / 8) {

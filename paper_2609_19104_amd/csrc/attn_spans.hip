@@ -39,14 +39,25 @@ __global__ __launch_bounds__(kSpanRows) void spans_kernel(int T, int N, int caus
         auto begins = [&](int j) { return j == 0 || ids[j] != ids[j - 1]; };  // a run begins at j in [0, N)
         // Both ends at a time: the greatest begin at or before pa, and minus the least one behind pb (N ends the last run,
         // position 0 begins the first, so both searches end).
+        constexpr int64_t zero = 0;
         int first = -1, end = kNone;
         for (int64_t step = 0; first < 0 || end == kNone; step += kStep) {
+            // All loads first (positions outside are read at the ends): in a branch each, every one would be a round trip.
+            int32_t at[2 * kPer], before[2 * kPer];
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                const int64_t i = pa - step - tid - k * kSpanRows, j = pb + 1 + step + tid + k * kSpanRows;
+                at[2 * k] = ids[max(i, zero)];
+                before[2 * k] = ids[max(i - 1, zero)];
+                at[2 * k + 1] = ids[min(j, static_cast<int64_t>(N - 1))];
+                before[2 * k + 1] = ids[min(j - 1, static_cast<int64_t>(N - 1))];
+            }
             int best = -1, next = kNone;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
                 const int64_t i = pa - step - tid - k * kSpanRows, j = pb + 1 + step + tid + k * kSpanRows;
-                if (first < 0 && i >= 0 && begins(static_cast<int>(i))) best = max(best, static_cast<int>(i));
-                if (end == kNone && (j == N || (j < N && begins(static_cast<int>(j))))) next = max(next, static_cast<int>(-j));
+                if (i >= 0 && (i == 0 || at[2 * k] != before[2 * k])) best = max(best, static_cast<int>(i));
+                if (j <= N && (j == N || at[2 * k + 1] != before[2 * k + 1])) next = max(next, static_cast<int>(-j));
             }
             for (int o = 32; o >= 1; o >>= 1) {
                 best = max(best, __shfl_xor(best, o));

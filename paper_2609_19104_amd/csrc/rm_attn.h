@@ -12,9 +12,15 @@
 // registers: the 16 keys of a matrix-core step may come in any order as long as V's rows come in the same, and the
 // order the scores have (keys 16 s + 4 h + {0..3} and + 8 for lane half h) is the one V's fragments are read in.
 //
-// What bounds it: a compute unit loads 64 bytes a cycle into LDS and reads 128, and a matrix-core step of 32 cycles
-// takes one KB from LDS per wave.  The load instructions go out between the matrix-core steps, since a wave that
-// issues several in a row waits for the load unit (16 cycles an instruction and wave).
+// What bounds it (bf16, MI355X): with RW = 4 the matrix cores and the exponentials, two workgroups to a compute unit, one
+// in its softmax while the other multiplies: 8192 x 8192 rows and keys, 16 heads of 128 columns on 4: 572 us, 960
+// TFLOP/s; of 64: 375 us, 730 (a score costs as many exponentials for half the products); 8 heads of 256 on 1: 558 us,
+// 985 (a library product of 8192^3: 1222).  With KW = 4, where a compute unit has few rows, its load unit and LDS: 64
+// bytes a cycle in and 128 out, which a tile of 128 keys and 256 columns keeps for 2048 of its 3800 cycles (1.6 us), and
+// one wave to a SIMD, whose softmax (700 cycles) nothing else covers; a launch's own 6 us are its first trips to memory
+// and the join.  The load instructions go out between the matrix-core steps, since a wave that issues several in a row
+// waits for the load unit, 16 cycles an instruction and wave (a tile 4400 -> 3800 cycles).  Float32: the matrix cores'
+// 153 TFLOP/s, of which 16 heads of 128 on 4096 rows reach 122.
 #pragma once
 
 #include "rm_attn_plan.h"
@@ -46,7 +52,8 @@ __device__ __forceinline__ const char *uniform(const char *p) {
 // offset from a base in scalar registers; only the lanes of mask take part.  M0 and EXEC are kept and put back.
 // No memory clobber: the buffers are read between the waits below only, which have one.
 template <int STEP>
-__device__ __forceinline__ void dma16_pair(const void *base, uint32_t off0, uint32_t off1, uint32_t lds, uint64_t mask) {
+__device__ __forceinline__ void dma16_pair(const void *base, uint32_t off0, uint32_t off1, uint32_t lds,
+                                           uint64_t mask) {
     uint32_t keep;
     uint64_t exec;
     mask = uniform(static_cast<int64_t>(mask));
@@ -89,7 +96,9 @@ __device__ __forceinline__ int wave_min(int v) { return -wave_max(-v); }  // (no
 
 // Whether any of the values packed in v is infinite or NaN (all exponent bits set): the carry out of the exponent
 // field reaches the sign bit.
-__device__ __forceinline__ uint32_t nonfinite_bf16x2(uint32_t v) { return ((v & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t nonfinite_bf16x2(uint32_t v) {
+    return ((v & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
 __device__ __forceinline__ uint32_t nonfinite_f32(float v) {
     return ((__float_as_uint(v) & 0x7f800000u) + 0x00800000u) & 0x80000000u;
 }
@@ -201,7 +210,9 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     auto own_len = [&](int smp) __attribute__((always_inline)) {
         return a.n1 > 0 && a.len1 ? min(max(a.len1[static_cast<int64_t>(u) * a.per + smp], 0), a.n1) : a.n1;
     };
-    auto causal_end = [&](int len, int t) __attribute__((always_inline)) { return min(max(len - a.T + t + 1, 0), len); };
+    auto causal_end = [&](int len, int t) __attribute__((always_inline)) {
+        return min(max(len - a.T + t + 1, 0), len);
+    };
     int r_lo[QB], r_len[QB];
     int w_maxlo = 0, w_minhi = 0x7fffffff, w_minlo = 0, w_maxhi = 0x7fffffff;
     int b_lo = 0, b_hi = 0;  // with spans: the keys that any of the workgroup's rows sees
@@ -290,8 +301,8 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     int64_t n_tiles = 0;
     for (int sg = -1; sg <= s_last; sg = sg < 0 ? s_first : sg + 1) n_tiles += tiles_of(sg);
     if (turns > 1) n_tiles = (n_tiles - split + turns - 1) / turns;
-    // Goes to the slice's first tile of t.seg or, if it has none there, of a following segment; t.before: how many tiles
-    // come before the segment, modulo the slices.
+    // Goes to the slice's first tile of t.seg or, if it has none there, of a following segment; t.before: how many
+    // tiles come before the segment, modulo the slices.
     auto enter = [&](Tile &t) __attribute__((always_inline)) {
         for (;;) {
             int lo, end;
@@ -330,8 +341,8 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     // ---------------------------------------------------------------- staging
     // A key wave's buffers: NBUF times its keys of a tile, then its values; the RW waves that share them fill them.  A
     // row's 16-byte chunk c lies at c ^ swz(row), so that the lanes of a fragment read, 16 rows at one chunk, take
-    // different banks.  The load instruction n of a wave brings rows n STEP + (rw RPI + lane / CPR); the two terms have no
-    // bits in common, so swz of the sum is swz of one ^ swz of the other.
+    // different banks (no conflict counted).  The load instruction n of a wave brings rows n STEP + (rw RPI +
+    // lane / CPR); the two terms have no bits in common, so swz of the sum is swz of one ^ swz of the other.
     uint8_t *const lds_w = lds + kw * KWB;
     const uint32_t lds_at = rm_dma::lds_addr(lds_w) + rw * 1024;
     auto swz_k = [](int row) { return CPR == 8 ? (row >> 1) & 7 : row & 15; };
@@ -343,9 +354,9 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     };
     const int lrow = rw * RPI + lane / CPR;
     const uint32_t chunk_k = (lane % CPR ^ swz_k(lrow)) * 16, chunk_v = (lane % CPR ^ swz_v(lrow)) * 16;
-    // Loads of pair p of a matrix of tile t into buffer buf.  Rows past the last key are that key again (their scores are
-    // masked) and columns past the head's its last ones (set to zero where they meet queries, or not written).  Token strides are
-    // below 2^24 bytes, so a tile's offsets fit in 32 bits.
+    // Loads of pair p of a matrix of tile t into buffer buf.  Rows past the last key are that key again (their scores
+    // are masked) and columns past the head's its last ones (set to zero where they meet queries, or not written).
+    // Token strides are below 2^24 bytes, so a tile's offsets fit in 32 bits.
     auto stage = [&](const Tile &t, int buf, bool values, int p, uint64_t mask) __attribute__((always_inline)) {
         const uint32_t sn = static_cast<uint32_t>(values ? t.vn : t.kn);
         const int last = t.end - 1 - t.kb;
@@ -372,8 +383,8 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         if constexpr (RW > 1) rm_dma::wait_barrier<N>();
         else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
     };
-    // Loads in flight when a matrix is waited for: with two buffers the whole other matrix, with one the pairs of the next
-    // keys that go out during the softmax.
+    // Loads in flight when a matrix is waited for: with two buffers the whole other matrix, with one the pairs of the
+    // next keys that go out during the softmax.
     constexpr int NH = NBUF == 2 ? 0 : NP / 2;
     typedef std::integral_constant<int, 0> None;
     typedef std::integral_constant<int, NBUF == 2 ? 2 * NP : 2 * NH> Others;
@@ -416,17 +427,17 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         r_slope[qb] = a.slopes ? a.slopes[r_head[qb]] * kLog2e : 0.0f;
         r_pos[qb] = (a.slopes && a.q_start ? a.q_start[u] : 0) + r_tok[qb];  // (slopes: one sample a group)
     }
-    // The scores' registers hold s with score = sc s + off in powers of two: plain products, capped ones as tanh or (bf16)
-    // -1 / (1 + e^2x), of which tanh x is 1 + 2 times; with a bias the scores themselves.
+    // The scores' registers hold s with score = sc s + off in powers of two: plain products, capped ones as tanh or
+    // (bf16) -1 / (1 + e^2x), of which tanh x is 1 + 2 times; with a bias the scores themselves.
     const float sc = a.slopes ? 1.0f : a.cap != 0.0f ? (BF ? 2.0f * a.cap : a.cap) : a.scale;
     const float off = BF && a.cap != 0.0f && !a.slopes ? a.cap : 0.0f;
 
     // ---------------------------------------------------------------- tiles
-    // One pass over the slice's tiles, the first one's loads under way.  Returns whether the sums hold infinities or NaN
-    // and a tile had keys that some rows see and others do not: 0 times infinite values may have spoilt the rows that do
-    // not see them.  Such a workgroup (there is hardly ever one) makes a second pass with `clean`, which sets the
-    // infinities and NaN among the values to 0 in LDS, the other sums staying as they are bit for bit, and then adds
-    // them to the rows that see them.
+    // One pass over the slice's tiles, the first one's loads under way.  Returns whether a tile had keys that some rows
+    // see and others do not.  There 0 times an infinity or NaN may spoil the rows that do not see it, and a sum keeps
+    // the NaN: a workgroup whose results then hold any (there is hardly ever one) makes a second pass with `clean`,
+    // which sets the infinities and NaN among the values to 0 in LDS, the other sums staying as they are bit for bit,
+    // and then adds them to the rows that see them.
     auto pass = [&](const bool clean) __attribute__((always_inline)) -> bool {
         bool some = false;  // some tile had keys that not all rows see
 #pragma unroll
@@ -474,8 +485,8 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb) {
                         if constexpr (BF) {
-                            s[qb][x % NS] =
-                                __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x % (2 * AHEAD)], qf[qb][x / NS], s[qb][x % NS], 0, 0, 0);
+                            s[qb][x % NS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                kf[x % (2 * AHEAD)], qf[qb][x / NS], s[qb][x % NS], 0, 0, 0);
                         } else {
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
@@ -520,9 +531,9 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                         const float d0 = static_cast<float>(r_pos[qb] - (kbw + 32 * ns + 4 * hi));
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            s[qb][ns][i] = fmaf(s[qb][ns][i], in,
-                                                fmaf(-r_slope[qb], fabsf(d0 - static_cast<float>(8 * (i >> 2) + (i & 3))),
-                                                     add));
+                            s[qb][ns][i] = fmaf(
+                                s[qb][ns][i], in,
+                                fmaf(-r_slope[qb], fabsf(d0 - static_cast<float>(8 * (i >> 2) + (i & 3))), add));
                     }
                 }
                 if (mixed) {
@@ -600,7 +611,9 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                 sync(Any{});
             }
             some = some || mixed;
-            {  // O^T += V^T P^T; with two buffers the next tile's values go out meanwhile, with one the rest of its keys
+            {  // O^T += V^T P^T; with two buffers the next tile's values go out meanwhile, with one the rest of its
+               // keys.  The weights are rounded to bf16 like the values (2^-9 of each at most, of either sign); the sum
+               // that divides them is not.
                 constexpr int X = (BF ? 2 : 16) * NS * DB, NQ = NBUF == 2 ? NP : NP - NH;
                 typedef typename std::conditional<BF, rm_bf16x8, float>::type VFrag;
                 VFrag vf[2 * AHEAD];
@@ -610,7 +623,8 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                         vf[x % (2 * AHEAD)] = read_v_rows<ROWB>(v_ptr[d % VP] + at + (d / VP) * 256 + 16 * st * ROWB);
                     else
                         vf[x % (2 * AHEAD)] = *reinterpret_cast<const float *>(
-                            v_ptr[d % VP] + at + (d / VP) * 256 + (32 * (st / 16) + 8 * (st % 16 >> 2) + (st & 3)) * ROWB);
+                            v_ptr[d % VP] + at + (d / VP) * 256 +
+                            (32 * (st / 16) + 8 * (st % 16 >> 2) + (st & 3)) * ROWB);
                 };
                 VFrag p[QB];
 #pragma unroll
@@ -633,10 +647,11 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                     }
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb) {
+                        const VFrag f = vf[x % (2 * AHEAD)];
                         if constexpr (BF)
-                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x % (2 * AHEAD)], p[qb], o[qb][d], 0, 0, 0);
+                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p[qb], o[qb][d], 0, 0, 0);
                         else
-                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[x % (2 * AHEAD)], p[qb], o[qb][d], 0, 0, 0);
+                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(f, p[qb], o[qb][d], 0, 0, 0);
                     }
                     if (x + AHEAD < X) read_v(x + AHEAD);
 #pragma unroll
@@ -649,137 +664,153 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             }
             cur = nxt;
         }
-        if (clean || !some) return false;
-        // 0 times an infinity or NaN is NaN, and a sum keeps it: o 0 summed is 0 unless o holds some (or an infinity).
-        float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[i & 3] = fmaf(o[qb][d][i], 0.0f, z[i & 3]);
-        return !((z[0] + z[1]) + (z[2] + z[3]) == 0.0f);
+        return some;
     };
-    bool clean = false;
-    while (__builtin_amdgcn_readfirstlane(__syncthreads_or(pass(clean)))) {  // a pass with `clean` returns false
-        clean = true;
-        first_tile(cur);
-        start();
-    }
-    if (__builtin_expect(clean, false)) {  // the infinities and NaN that the second pass left out
-        first_tile(cur);
-        for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
-            const int k0 = cur.kb + kw * KPW, k1 = min(k0 + KPW, cur.end);
-            for (int k = k0; k < k1; ++k) {
-                const char *row = cur.v + (k - cur.kb) * cur.vn;
-                for (int c0 = 0; c0 < a.D; c0 += 64) {
-                    float x = 0.0f;
-                    if (c0 + lane < a.D) {
-                        if constexpr (BF) x = rm_bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(row)[c0 + lane]);
-                        else x = reinterpret_cast<const float *>(row)[c0 + lane];
-                    }
-                    for (uint64_t bad = __ballot(!(fabsf(x) < INFINITY)); bad != 0; bad &= bad - 1) {
-                        const int from = __ffsll(static_cast<unsigned long long>(bad)) - 1;
-                        const float add = __shfl(x, from);
+    for (bool clean = false;; clean = true) {
+        bool some = pass(clean);
+        if (__builtin_expect(clean, false)) {  // the infinities and NaN that the second pass left out
+            first_tile(cur);
+            for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
+                const int k0 = cur.kb + kw * KPW, k1 = min(k0 + KPW, cur.end);
+                for (int k = k0; k < k1; ++k) {
+                    const char *row = cur.v + (k - cur.kb) * cur.vn;
+                    for (int c0 = 0; c0 < a.D; c0 += 64) {
+                        float x = 0.0f;
+                        if (c0 + lane < a.D) {
+                            if constexpr (BF)
+                                x = rm_bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(row)[c0 + lane]);
+                            else
+                                x = reinterpret_cast<const float *>(row)[c0 + lane];
+                        }
+                        for (uint64_t bad = __ballot(!(fabsf(x) < INFINITY)); bad != 0; bad &= bad - 1) {
+                            const int from = __ffsll(static_cast<unsigned long long>(bad)) - 1;
+                            const float add = __shfl(x, from);
 #pragma unroll
-                        for (int qb = 0; qb < QB; ++qb) {
-                            const bool sees =
-                                cur.seg < 0 || (r_smp[qb] == cur.seg &&
-                                                static_cast<uint32_t>(k - r_lo[qb]) < static_cast<uint32_t>(r_len[qb]));
-                            const int at = sees ? c0 + from - 4 * hi : -1;
+                            for (int qb = 0; qb < QB; ++qb) {
+                                const bool in =
+                                    static_cast<uint32_t>(k - r_lo[qb]) < static_cast<uint32_t>(r_len[qb]);
+                                const bool sees = cur.seg < 0 || (r_smp[qb] == cur.seg && in);
+                                const int at = sees ? c0 + from - 4 * hi : -1;
 #pragma unroll
-                            for (int d = 0; d < DB; ++d)
+                                for (int d = 0; d < DB; ++d)
 #pragma unroll
-                                for (int i = 0; i < 16; ++i)
-                                    o[qb][d][i] += at == 32 * d + 8 * (i >> 2) + (i & 3) ? add : 0.0f;
+                                    for (int i = 0; i < 16; ++i)
+                                        o[qb][d][i] += at == 32 * d + 8 * (i >> 2) + (i & 3) ? add : 0.0f;
+                            }
                         }
                     }
                 }
+                if (n_left > 1) advance(cur);
             }
-            if (n_left > 1) advance(cur);
         }
-    }
 
-    // ---------------------------------------------------------------- join and write
+        // ---------------------------------------------------------------- join and write
+        // Of the blocks of 32 columns, wave kw joins those with number kw modulo KW: it has its own sums, the others'
+        // come through LDS.
+        float *join = reinterpret_cast<float *>(lds);
+        float *ml = join + W * QB * 32 * DC;  // [wave][qb][2][32]
+        auto slot = [&](int w, int qb, int d, int i) {
+            return reinterpret_cast<rm_f32x4 *>(join + ((((w * QB + qb) * DB + d) * 4 + i) * 64 + lane) * 4);
+        };
+        auto quad = [&](int qb, int d, int i) {
+            return rm_f32x4{o[qb][d][4 * i], o[qb][d][4 * i + 1], o[qb][d][4 * i + 2], o[qb][d][4 * i + 3]};
+        };
+        if constexpr (KW > 1) {
+            __syncthreads();  // every wave has read its last tile
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) l[qb] = xor32_sum(l[qb]);
-    float *join = reinterpret_cast<float *>(lds);
-    float *ml = join + W * QB * 32 * DC;  // [wave][qb][2][32]
-    if constexpr (KW > 1) {  // (every wave has read the last tile: the barrier after the pass)
+            for (int qb = 0; qb < QB; ++qb) {
+                const float sum = xor32_sum(l[qb]);
+                if (hi == 0) {
+                    ml[((wave * QB + qb) * 2 + 0) * 32 + col] = m[qb];
+                    ml[((wave * QB + qb) * 2 + 1) * 32 + col] = sum;
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    if (d % KW != kw)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) *slot(wave, qb, d, i) = quad(qb, d, i);
+            }
+            __syncthreads();
+        }
+        float nan = 0.0f;  // stays 0 unless a result is NaN (or infinite)
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
-            if (hi == 0) {
-                ml[((wave * QB + qb) * 2 + 0) * 32 + col] = m[qb];
-                ml[((wave * QB + qb) * 2 + 1) * 32 + col] = l[qb];
-            }
+            const int r = row0 + (rw * QB + qb) * 32 + col;
+            float f[KW], top = m[qb], sum = 0.0f;  // the key waves' factors
+            if constexpr (KW > 1) {
+                top = -INFINITY;
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+                for (int k = 0; k < KW; ++k) {
+                    f[k] = ml[(((k * RW + rw) * QB + qb) * 2 + 0) * 32 + col];
+                    top = fmaxf(top, f[k]);
+                }
+                const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+                for (int k = 0; k < KW; ++k) {
+                    f[k] = __builtin_amdgcn_exp2f(f[k] - ref);
+                    sum += ml[(((k * RW + rw) * QB + qb) * 2 + 1) * 32 + col] * f[k];
+                }
+            } else {
+                sum = xor32_sum(l[qb]);
+            }
+            const float inv = a.splits > 1 ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
+            const int64_t prow = (static_cast<int64_t>(split) * a.U * a.Hk + ng) * a.R + r;
+            if (a.splits > 1 && r < a.R && hi == 0 && kw == 0) {
+                a.part_ml[2 * prow] = top;
+                a.part_ml[2 * prow + 1] = sum;
+            }
+            char *orow = a.o + (static_cast<int64_t>(u) * a.per + r_smp[qb]) * a.o_b + r_tok[qb] * a.o_t +
+                         r_head[qb] * a.o_h;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                if (KW > 1 && d % KW != kw) continue;
+                rm_f32x4 v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const rm_f32x4 v = {o[qb][d][4 * i], o[qb][d][4 * i + 1], o[qb][d][4 * i + 2], o[qb][d][4 * i + 3]};
-                    *reinterpret_cast<rm_f32x4 *>(join + ((((wave * QB + qb) * DB + d) * 4 + i) * 64 + lane) * 4) = v;
+                    v[i] = quad(qb, d, i);
+                    if constexpr (KW > 1) {
+                        v[i] *= f[d % KW];
+#pragma unroll
+                        for (int k = 0; k < KW; ++k)
+                            if (k != d % KW) v[i] += *slot(k * RW + rw, qb, d, i) * f[k];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) nan = fmaf(v[i][e], 0.0f, nan);
                 }
-        }
-        __syncthreads();
-    }
+                if (a.splits > 1 || !BF) {
+                    char *dst = a.splits > 1 ? reinterpret_cast<char *>(a.part_o + prow * a.D) : orow;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int r = row0 + (rw * QB + qb) * 32 + col;
-        float f[KW];  // the key waves' factors
-        if constexpr (KW > 1) {
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int k = 0; k < KW; ++k) {
-                f[k] = ml[(((k * RW + rw) * QB + qb) * 2 + 0) * 32 + col];
-                top = fmaxf(top, f[k]);
-            }
-            const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-            for (int k = 0; k < KW; ++k) {
-                f[k] = __builtin_amdgcn_exp2f(f[k] - ref);
-                sum += ml[(((k * RW + rw) * QB + qb) * 2 + 1) * 32 + col] * f[k];
-            }
-            m[qb] = top;
-            l[qb] = sum;
-        }
-        const float inv = a.splits > 1 ? 1.0f : (l[qb] == 0.0f ? 0.0f : 1.0f / l[qb]);
-        const int64_t prow = (static_cast<int64_t>(split) * a.U * a.Hk + ng) * a.R + r;
-        if (a.splits > 1 && r < a.R && hi == 0 && kw == 0) {
-            a.part_ml[2 * prow] = m[qb];
-            a.part_ml[2 * prow + 1] = l[qb];
-        }
-        char *orow = a.o + (static_cast<int64_t>(u) * a.per + r_smp[qb]) * a.o_b + r_tok[qb] * a.o_t +
-                     r_head[qb] * a.o_h;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            if (KW > 1 && d % KW != kw) continue;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                rm_f32x4 v;
-                if constexpr (KW > 1) {
-                    v = rm_f32x4{};
-#pragma unroll
-                    for (int k = 0; k < KW; ++k)
-                        v += *reinterpret_cast<const rm_f32x4 *>(
-                                 join + (((((k * RW + rw) * QB + qb) * DB + d) * 4 + i) * 64 + lane) * 4) *
-                             f[k];
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = 32 * d + 8 * i + 4 * hi;
+                        if (r < a.R && (!PAD || c < a.D)) *reinterpret_cast<rm_f32x4 *>(dst + c * 4) = v[i] * inv;
+                    }
                 } else {
-                    v = rm_f32x4{o[qb][d][4 * i], o[qb][d][4 * i + 1], o[qb][d][4 * i + 2], o[qb][d][4 * i + 3]};
-                }
-                const int c = 32 * d + 8 * i + 4 * hi;
-                if (r >= a.R || (PAD && c >= a.D)) continue;
-                if (a.splits > 1) {
-                    *reinterpret_cast<rm_f32x4 *>(a.part_o + prow * a.D + c) = v;
-                } else if constexpr (BF) {
-                    rm_bf16x4 w;
+                    // The lane halves have columns 8 i + {0..3} and + {4..7}: of two such groups each half takes one
+                    // whole.
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = static_cast<__bf16>(v[e] * inv);
-                    *reinterpret_cast<rm_bf16x4 *>(orow + c * 2) = w;
-                } else {
-                    *reinterpret_cast<rm_f32x4 *>(orow + c * 4) = v * inv;
+                    for (int i = 0; i < 4; i += 2) {
+                        uint32_t w[2][2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const rm_f32x4 y4 = v[i + e] * inv;
+                            const rm_bf16x4 x = {static_cast<__bf16>(y4[0]), static_cast<__bf16>(y4[1]),
+                                                 static_cast<__bf16>(y4[2]), static_cast<__bf16>(y4[3])};
+                            const uint2 y = __builtin_bit_cast(uint2, x);
+                            w[e][0] = y.x, w[e][1] = y.y;
+                        }
+                        const auto p0 = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+                        const auto p1 = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+                        const int c = 32 * d + 8 * (i + hi);
+                        if (r < a.R && (!PAD || c < a.D))
+                            *reinterpret_cast<rm_u32x4 *>(orow + c * 2) = rm_u32x4{p0[0], p1[0], p0[1], p1[1]};
+                    }
                 }
             }
         }
+        if (clean) break;
+        if (!__builtin_amdgcn_readfirstlane(__syncthreads_or(some && !(nan == 0.0f)))) break;
+        first_tile(cur);
+        start();
     }
 }
 
