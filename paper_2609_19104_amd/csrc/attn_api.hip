@@ -101,7 +101,13 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     const int64_t rows = static_cast<int64_t>(R), ng = static_cast<int64_t>(groups);
     q.dh = D <= 64 ? 64 : D <= 128 ? 128 : 256;
     constexpr int64_t kCUs = 256;
-    const bool key_waves = ceil_div(rows, 128) * ng < 2 * kCUs || rows <= 32;
+    // Waves that divide 128 rows, or the keys of 32: the former once there are enough blocks of 128 rows.  Measured on 2048
+    // (512) keys, us, the latter / the former: bf16, 128 columns, 128 blocks 31 / 48 (13 / 17), 192 48 / 49 (20 / 17), 256
+    // 60 / 50 (24 / 18), 512 110 / 77; 64 columns alike; 256 columns (one workgroup to a compute unit) 64 blocks 33 / 69
+    // (14 / 23), 128 66 / 70 (26 / 24), 256 124 / 75.  Float32, 128 columns, 256 blocks 320 / 334 (97 / 90), 384 480 / 565,
+    // 512 639 / 568; 256 columns have too few registers for it (768 blocks: 1768 / 2841) and waves that divide both.
+    const int64_t blocks = ceil_div(rows, 128) * ng;
+    const bool key_waves = rows <= 32 || (bf ? blocks < (q.dh == 256 ? 128 : 192) : q.dh == 256 || blocks < 2 * kCUs);
     q.kw = key_waves ? 4 : 1;
     q.rows = key_waves ? (!bf && q.dh == 256 ? 64 : 32) : 128;
     q.n_tiles = static_cast<int>(ceil_div(rows, q.rows));
@@ -110,11 +116,12 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     // Few row blocks: several workgroups divide the keys, as many as fill the compute units once (two workgroups to one,
     // where their LDS allows it: heads up to 128 in bf16, 64 in float32), if the tiles that each of them then has less pay
     // for the second launch and the partial results.  Measured, us: a tile of 128 keys 0.9, 1.1 and 1.65 in bf16 (rows
-    // of 64, 128 and 256 columns), 2.3, 4.1 and 14 in float32; the join 5 and its traffic at 4 TB/s (one action
+    // of 64, 128 and 256 columns), 2.3, 4.1 and 14 in float32, 2.4 times that for 128 rows; the join 5 and its traffic at 4 TB/s (one action
     // chunk's 408 rows on 901 keys, D = 256: 20.2 us undivided, 14.2 in 8 slices; 6528 rows 24.4 undivided, 38.7 in 2).
     const int64_t tiles = ceil_div(n0, 128) + ceil_div(n1, 128);
     const int64_t slots = kCUs * (q.dh * (bf ? 1 : 2) <= 128 ? 2 : 1);
-    const double tile_us = bf ? 0.65 + q.dh / 256.0 : q.dh == 256 ? 14.0 : 0.5 + q.dh / 36.0;
+    const double tile_us =
+        (bf ? 0.65 + q.dh / 256.0 : q.dh == 256 ? 14.0 : 0.5 + q.dh / 36.0) * (key_waves ? 1.0 : 2.4);
     const double join_us = 5.0, part_us = static_cast<double>(rows) * ng * D * 8 / 4e6;  // one slice's results
     q.splits = 1;
     double best = tiles * tile_us;

@@ -18,7 +18,7 @@ static hipError_t by_waves(const Plan &p, const Args &a, hipStream_t st) {
     else if constexpr (DC <= 128)
         return p.kw > 1 ? go<128, DC, PAD, 1, 4, 1, 128, 1, 1>(a, st) : go<128, DC, PAD, 4, 1, 1, 64, 1, 2>(a, st);
     else
-        return p.kw > 1 ? go<256, DC, PAD, 2, 2, 1, 64, 1, 1>(a, st) : go<256, DC, PAD, 4, 1, 1, 64, 1, 1>(a, st);
+        return go<256, DC, PAD, 2, 2, 1, 64, 1, 1>(a, st);  // (the plan has p.kw > 1 here)
 }
 
 hipError_t launch_f32(const Plan &p, const Args &a, hipStream_t st) {

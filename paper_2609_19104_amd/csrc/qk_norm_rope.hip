@@ -67,6 +67,11 @@ __device__ __forceinline__ void load_unaligned(const float *p, float (&x)[V]) {
 // token, whose sines and cosines its lanes compute once: its lane groups (a power of two lanes, as a head has chunk
 // pairs) take consecutive heads, so that the wave reads and writes consecutive memory, and then the next ones, HB at a
 // time with the following HB heads' loads in flight.
+//
+// Bound by memory: 32768 tokens of 32 + 2 x 8 heads of 128 in bf16 take 157 us, 5.1 TB/s of reads and writes (a copy: 4.7).
+// A lane group that took a token's heads one after the other, the angles anew every four, took 304 us, with them once
+// for all heads 263 (its 64 lanes then touched 8 tokens far apart).  850 tokens of 8 + 2 x 1 heads of 256 take 5.7 us
+// and 51 3.5, which are a launch and two round trips.
 template <bool IBF, bool OBF, int V, int HB>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeArgs a) {
     constexpr int IS = IBF ? 2 : 4, OS = OBF ? 2 : 4;
@@ -192,10 +197,11 @@ hipError_t go(RopeArgs a, hipStream_t st) {
     const int units = a.rot / (2 * V) + (a.D / V - a.rot / V + 1) / 2;
     a.lane_bits = 0;
     while ((1 << a.lane_bits) < units) ++a.lane_bits;
-    // All heads of a token in one wave, sharing its sines and cosines, once that gives every SIMD two waves; fewer tokens
-    // divide their heads among waves, down to as many heads as a wave has lane groups.
+    // All heads of a token in one wave, sharing its sines and cosines, once that gives every SIMD four waves; fewer tokens
+    // divide their heads among waves, down to as many heads as a wave has lane groups (bf16, us, one wave a token / as
+    // many as can be: 51 tokens of 48 heads of 128 8.3 / 3.9, 850 9.6 / 8.0, 2000 12.8 / 15.1, 4000 17.8 / 23.5).
     const int at_once = 64 >> a.lane_bits, most = (a.H + at_once - 1) / at_once;
-    const int groups = std::min(most, std::max(1, 2048 / a.N));
+    const int groups = std::min(most, std::max(1, 4096 / a.N));
     a.per = (most + groups - 1) / groups * at_once;
     a.groups = (a.H + a.per - 1) / a.per;
     const int64_t wgs = (static_cast<int64_t>(a.N) * a.groups + 3) / 4;
