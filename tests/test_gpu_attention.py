@@ -387,6 +387,34 @@ def test_prefix_many_rows(dtype, D, causal):
             check(out[b:b + 1, :, h:h + 1], ref, bound(ref, mag, big, dtype, D, P + S))
 
 
+@pytest.mark.parametrize("D,per", [(64, 24), (128, 24), (256, 16)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_row_waves_and_slices(D, per, causal):
+    """Blocks of 128 rows whose keys two workgroups divide, of a shared prefix and of spans."""
+    g = gen(25, D)
+    G, T, P, S, Hq = 2, 32, 4000, 60, 16
+    q, kp, vp, ko, vo = make_prefix(g, G, per, T, P, S, Hq, 1, D, BF)
+    assert rm.prefix_attention_workspace(q, kp, ko).numel() > 0
+    olen = torch.randint(0, S + 1, (G * per,), generator=g, dtype=torch.int32)
+    olen[0], olen[-1] = S, 0
+    plen = ints([P, 77])
+    out = run_prefix(q, kp, vp, ko, vo, plen, olen.cuda(), causal)
+    assert torch.equal(out, run_prefix(q, kp, vp, ko, vo, plen, olen.cuda(), causal))
+    for b in (0, 1, per - 1, per, G * per - 1):
+        i = b // per
+        a = [t for t in (q[b:b + 1, :, 3:5], kp[i:i + 1], vp[i:i + 1], ko[b:b + 1], vo[b:b + 1])]
+        ref, mag, big = att.prefix_attention(*(f64(t) for t in a), np.float32(D ** -0.5), 0.0, [int(plen[i])],
+                                             [int(olen[b])], causal)
+        check(out[b:b + 1, :, 3:5], ref, bound(ref, mag, big, BF, D, P + S))
+    q = randn(g, (4, 32 * per // 24 * 24, Hq * 2, D), BF, 2.0)
+    span = torch.empty((4, q.shape[1], 2), dtype=torch.int32, device="cuda")
+    k, v = randn(g, (4, P, 1, D), BF), randn(g, (4, P, 1, D), BF)
+    rm.rm_attn_spans(span, P, causal=causal, q_start=ints([0, 100, P - 500, 7]))
+    out = run_span(q, k, v, span)
+    for b, h in ((0, 0), (2, 31)):
+        check_span(q[b:b + 1, ::37, h:h + 1], k[b:b + 1], v[b:b + 1], span[b:b + 1, ::37], out=out[b:b + 1, ::37, h:h + 1])
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("T", [1, 20])
 def test_one_samples_nan_stays_its_own(dtype, T):
