@@ -3,10 +3,10 @@
 
 namespace rm_attn {
 
-template <int DH, int DC, bool PAD, int RW, int KW, int QB, int KT, int NBUF, int WPE>
+template <int DH, int DC, bool PAD, int RW, int KW, int KT, int NBUF, int WPE>
 static hipError_t go(const Args &a, hipStream_t st) {
     const dim3 grid(static_cast<unsigned>(a.n_tiles) * a.splits * a.U * a.Hk);
-    attn_kernel<true, DH, DC, PAD, RW, KW, QB, KT, NBUF, WPE><<<grid, 64 * RW * KW, 0, st>>>(a);
+    attn_kernel<true, DH, DC, PAD, RW, KW, KT, NBUF, WPE><<<grid, 64 * RW * KW, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -14,11 +14,11 @@ static hipError_t go(const Args &a, hipStream_t st) {
 template <int DC, bool PAD>
 static hipError_t by_waves(const Plan &p, const Args &a, hipStream_t st) {
     if constexpr (DC == 64)
-        return p.kw > 1 ? go<64, DC, PAD, 1, 4, 1, 128, 2, 2>(a, st) : go<64, DC, PAD, 4, 1, 1, 64, 2, 2>(a, st);
+        return p.kw > 1 ? go<64, DC, PAD, 1, 4, 128, 2, 2>(a, st) : go<64, DC, PAD, 4, 1, 64, 2, 2>(a, st);
     else if constexpr (DC <= 128)
-        return p.kw > 1 ? go<128, DC, PAD, 1, 4, 1, 128, 1, 2>(a, st) : go<128, DC, PAD, 4, 1, 1, 64, 2, 2>(a, st);
+        return p.kw > 1 ? go<128, DC, PAD, 1, 4, 128, 1, 2>(a, st) : go<128, DC, PAD, 4, 1, 64, 2, 2>(a, st);
     else
-        return p.kw > 1 ? go<256, DC, PAD, 1, 4, 1, 128, 1, 1>(a, st) : go<256, DC, PAD, 4, 1, 1, 64, 2, 1>(a, st);
+        return p.kw > 1 ? go<256, DC, PAD, 1, 4, 128, 1, 1>(a, st) : go<256, DC, PAD, 4, 1, 64, 2, 1>(a, st);
 }
 
 hipError_t launch_bf16(const Plan &p, const Args &a, hipStream_t st) {

@@ -1,7 +1,7 @@
 // The attention kernel shared by rm_span_attention and rm_prefix_attention (bf16 in attn_bf16.hip, float32 in
 // attn_f32.hip): one pass over the keys with a running maximum and sum per query row.
 //
-// A workgroup takes 32 RW QB query rows (the tokens of one group times the query heads of one key head, so that a
+// A workgroup takes 32 RW query rows (the tokens of one group times the query heads of one key head, so that a
 // key head's rows are read once for all its query heads) and walks tiles of KT keys.  RW of its waves divide the rows
 // and KW the keys of a tile; the waves that take the same keys load them straight into LDS buffers of their own, so
 // with RW = 1 no wave waits for another before the KW partial results are joined in LDS at the end.  With `splits` > 1
@@ -129,7 +129,7 @@ struct Tile {
 };
 
 // Rows have room for DH columns in LDS; the products take DC of them.  PAD: the head has fewer, more than LEAST.
-template <bool BF, int DH, int DC, bool PAD, int RW, int KW, int QB, int KT, int NBUF, int WPE>
+template <bool BF, int DH, int DC, bool PAD, int RW, int KW, int KT, int NBUF, int WPE>
 __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     constexpr int W = RW * KW, ES = BF ? 2 : 4, ROWB = DH * ES, CPR = ROWB / 16;
     constexpr int RPI = 64 / CPR;                // rows per load instruction of a wave (1 KB)
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     static_assert(CPR >= 8 && CPR <= 64 && NP >= 1 && NP * 2 * STEP == KPW && NS * 32 == KPW, "tile shape");
     constexpr int TILEB = KPW * ROWB, KWB = 2 * NBUF * TILEB;  // one matrix's keys, and all buffers of a key wave
     // O of every wave passes through LDS when the key waves are joined.
-    constexpr int JOINB = KW > 1 ? W * QB * 32 * DC * 4 + W * QB * 32 * 8 : 0;
+    constexpr int JOINB = KW > 1 ? W * 32 * DC * 4 + W * 32 * 8 : 0;
     constexpr int LDSB = KW * KWB > JOINB ? KW * KWB : JOINB;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[LDSB];
 
@@ -173,36 +173,30 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     }
     const int row_tile = divide(tile_id, a.by_splits), split = tile_id - row_tile * a.splits;
     // Row blocks from the last to the first: with causal masks the later ones see more keys and start first.
-    const int row0 = (a.n_tiles - 1 - row_tile) * (32 * RW * QB);
+    const int row0 = (a.n_tiles - 1 - row_tile) * (32 * RW);
     const int u = divide(ng, a.by_hk), hk = ng - u * a.Hk;
-    const int rows_end = min(row0 + 32 * RW * QB, a.R);
+    const int rows_end = min(row0 + 32 * RW, a.R);
 
     // ---------------------------------------------------------------- queries
     typedef typename std::conditional<BF, rm_bf16x8, rm_f32x4>::type QFrag;
-    QFrag qf[QB][QF];
-    int r_smp[QB], r_tok[QB], r_head[QB];
+    QFrag qf[QF];
+    const int row = row0 + rw * 32 + col;  // the lane's (both halves'); rows past the last are the last again
+    const int tok = divide(min(row, a.R - 1), a.by_g);
+    const int r_head = hk * a.G + min(row, a.R - 1) - tok * a.G;
+    const int r_smp = divide(tok, a.by_t), r_tok = tok - r_smp * a.T;  // sample and token
+    const char *q = a.q + (static_cast<int64_t>(u) * a.per + r_smp) * a.q_b + r_tok * a.q_t + r_head * a.q_h;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int r = min(row0 + (rw * QB + qb) * 32 + col, a.R - 1);
-        const int tok = divide(r, a.by_g);
-        r_head[qb] = hk * a.G + r - tok * a.G;
-        r_smp[qb] = divide(tok, a.by_t);
-        r_tok[qb] = tok - r_smp[qb] * a.T;
-        const char *q = a.q + (static_cast<int64_t>(u) * a.per + r_smp[qb]) * a.q_b + r_tok[qb] * a.q_t +
-                        r_head[qb] * a.q_h;
-#pragma unroll
-        for (int c = 0; c < QF; ++c) {
-            const int byte = (2 * c + hi) * 16;
-            rm_u32x4 v = {0, 0, 0, 0};
-            if (!PAD || byte < a.D * ES) v = *reinterpret_cast<const rm_u32x4 *>(q + byte);
-            qf[qb][c] = __builtin_bit_cast(QFrag, v);
-        }
+    for (int c = 0; c < QF; ++c) {
+        const int byte = (2 * c + hi) * 16;
+        rm_u32x4 v = {0, 0, 0, 0};
+        if (!PAD || byte < a.D * ES) v = *reinterpret_cast<const rm_u32x4 *>(q + byte);
+        qf[c] = __builtin_bit_cast(QFrag, v);
     }
 
     // ---------------------------------------------------------------- the keys that rows see
     // Of the wave's rows: the first and last sample, and over the own keys that rows see the least and greatest begin
     // and end (greatest begin INT_MAX or least end 0 where a row sees none: no tile is whole for it).
-    const int w_row = row0 + rw * QB * 32, w_last = min(w_row + QB * 32, a.R) - 1;
+    const int w_row = row0 + rw * 32, w_last = min(w_row + 32, a.R) - 1;
     const int w_s0 = w_row < a.R ? divide(divide(w_row, a.by_g), a.by_t) : 0x7fffffff;
     const int w_s1 = w_row < a.R ? divide(divide(w_last, a.by_g), a.by_t) : -1;
     const int s_first = divide(divide(row0, a.by_g), a.by_t), s_last = divide(divide(rows_end - 1, a.by_g), a.by_t);
@@ -213,26 +207,23 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     auto causal_end = [&](int len, int t) __attribute__((always_inline)) {
         return min(max(len - a.T + t + 1, 0), len);
     };
-    int r_lo[QB], r_len[QB];
+    int r_lo, r_len;
     int w_maxlo = 0, w_minhi = 0x7fffffff, w_minlo = 0, w_maxhi = 0x7fffffff;
     int b_lo = 0, b_hi = 0;  // with spans: the keys that any of the workgroup's rows sees
     if (a.span) {
         const int2 *span = reinterpret_cast<const int2 *>(a.span) + static_cast<int64_t>(u) * a.T;
         w_maxlo = 0, w_minhi = 0x7fffffff, w_minlo = 0x7fffffff, w_maxhi = 0;
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-            const int2 sp = span[r_tok[qb]];
-            const int lo = min(max(sp.x, 0), a.n1), end = min(max(sp.y, 0), a.n1);
-            r_lo[qb] = lo;
-            r_len[qb] = max(end - lo, 0);
-            if (lo < end) {
-                w_maxlo = max(w_maxlo, lo);
-                w_minhi = min(w_minhi, end);
-                w_minlo = min(w_minlo, lo);
-                w_maxhi = max(w_maxhi, end);
-            } else {
-                w_maxlo = 0x7fffffff;
-            }
+        const int2 sp = span[r_tok];
+        const int lo = min(max(sp.x, 0), a.n1), end = min(max(sp.y, 0), a.n1);
+        r_lo = lo;
+        r_len = max(end - lo, 0);
+        if (lo < end) {
+            w_maxlo = max(w_maxlo, lo);
+            w_minhi = min(w_minhi, end);
+            w_minlo = min(w_minlo, lo);
+            w_maxhi = max(w_maxhi, end);
+        } else {
+            w_maxlo = 0x7fffffff;
         }
         w_maxlo = wave_max(w_maxlo);
         w_minhi = wave_min(w_minhi);
@@ -256,12 +247,9 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         }
         b_lo = min(b_lo, b_hi);
     } else {
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-            const int len = own_len(r_smp[qb]);
-            r_lo[qb] = 0;
-            r_len[qb] = a.causal ? causal_end(len, r_tok[qb]) : len;
-        }
+        const int len = own_len(r_smp);
+        r_lo = 0;
+        r_len = a.causal ? causal_end(len, r_tok) : len;
         if (a.causal && w_s0 == w_s1) {  // (rows of several samples make every tile partial anyway)
             const int len = __builtin_amdgcn_readfirstlane(own_len(w_s0));
             w_minhi = causal_end(len, divide(w_row, a.by_g) - w_s0 * a.T);
@@ -419,14 +407,11 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         for (int d = 0; d < VP; ++d) v_ptr[d] = lds_w + TILEB + 4 * hi * ROWB + ((d * 128) ^ (hi * 128)) + col * 4;
     }
 
-    rm_f32x16 o[QB][DB];
-    float m[QB], l[QB], r_slope[QB];
-    int r_pos[QB];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        r_slope[qb] = a.slopes ? a.slopes[r_head[qb]] * kLog2e : 0.0f;
-        r_pos[qb] = (a.slopes && a.q_start ? a.q_start[u] : 0) + r_tok[qb];  // (slopes: one sample a group)
-    }
+    rm_f32x16 o[DB];
+    float m, l, r_slope;
+    int r_pos;
+    r_slope = a.slopes ? a.slopes[r_head] * kLog2e : 0.0f;
+    r_pos = (a.slopes && a.q_start ? a.q_start[u] : 0) + r_tok;  // (slopes: one sample a group)
     // The scores' registers hold s with score = sc s + off in powers of two: plain products, capped ones as tanh or
     // (bf16) -1 / (1 + e^2x), of which tanh x is 1 + 2 times; with a bias the scores themselves.
     const float sc = a.slopes ? 1.0f : a.cap != 0.0f ? (BF ? 2.0f * a.cap : a.cap) : a.scale;
@@ -440,20 +425,17 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     // and then adds them to the rows that see them.
     auto pass = [&](const bool clean) __attribute__((always_inline)) -> bool {
         bool some = false;  // some tile had keys that not all rows see
+        m = -INFINITY;
+        l = 0.0f;
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-            m[qb] = -INFINITY;
-            l[qb] = 0.0f;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) o[qb][d] = rm_f32x16{};
-        }
+        for (int d = 0; d < DB; ++d) o[d] = rm_f32x16{};
         int buf = 0;
         for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
             Tile nxt = cur;
             const bool more = n_left > 1;
             if (more) advance(nxt);
-            const uint64_t next = more ? kAll : 0;  // the lanes that load the next tile
-            const int at = NBUF == 2 ? buf * 2 * TILEB : 0;    // this tile's buffers
+            const uint64_t next = more ? kAll : 0;           // the lanes that load the next tile
+            const int at = NBUF == 2 ? buf * 2 * TILEB : 0;  // this tile's buffers
             if constexpr (NBUF == 2) buf ^= 1;
             sync(std::conditional_t<NBUF == 2, Others, None>{});  // the keys
 
@@ -462,11 +444,9 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             if (cur.seg >= 0)
                 mixed = mixed || cur.seg != w_s0 || cur.seg != w_s1 || kbw < w_maxlo || kbw + KPW > w_minhi;
 
-            rm_f32x16 s[QB][NS];
+            rm_f32x16 s[NS];
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-                for (int ns = 0; ns < NS; ++ns) s[qb][ns] = rm_f32x16{};
+            for (int ns = 0; ns < NS; ++ns) s[ns] = rm_f32x16{};
             {  // S^T = K Q^T; with two buffers the next tile's keys go out meanwhile, with one this tile's values
                 constexpr int X = QF * NS;
                 QFrag kf[2 * AHEAD];
@@ -482,17 +462,14 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
 #pragma unroll
                 for (int x = 0; x < X; ++x) {
                     __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (BF) {
+                        s[x % NS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            kf[x % (2 * AHEAD)], qf[x / NS], s[x % NS], 0, 0, 0);
+                    } else {
 #pragma unroll
-                    for (int qb = 0; qb < QB; ++qb) {
-                        if constexpr (BF) {
-                            s[qb][x % NS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                kf[x % (2 * AHEAD)], qf[qb][x / NS], s[qb][x % NS], 0, 0, 0);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                s[qb][x % NS] = __builtin_amdgcn_mfma_f32_32x32x2f32(
-                                    kf[x % (2 * AHEAD)][i], qf[qb][x / NS][i], s[qb][x % NS], 0, 0, 0);
-                        }
+                        for (int i = 0; i < 4; ++i)
+                            s[x % NS] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                                kf[x % (2 * AHEAD)][i], qf[x / NS][i], s[x % NS], 0, 0, 0);
                     }
                     if (x + AHEAD < X) read_k(x + AHEAD);
 #pragma unroll
@@ -504,94 +481,91 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                 __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (NBUF == 1) sync(Any{});  // every wave has read the keys: the next ones may come
-            auto interval = [&](int qb, int &lo, int &len) {  // the keys of this segment that the lane's row sees
-                lo = cur.seg < 0 ? 0 : r_lo[qb];
-                len = cur.seg < 0 ? n0 : (r_smp[qb] == cur.seg ? r_len[qb] : 0);
+            auto interval = [&](int &lo, int &len) {  // the keys of this segment that the lane's row sees
+                lo = cur.seg < 0 ? 0 : r_lo;
+                len = cur.seg < 0 ? n0 : (r_smp == cur.seg ? r_len : 0);
             };
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-                if (a.cap != 0.0f) {  // (a.scale: the score's over the cap)
-                    const float x2 = a.scale * (2.0f * kLog2e);
-#pragma unroll
-                    for (int ns = 0; ns < NS; ++ns)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            if constexpr (BF)
-                                s[qb][ns][i] =
-                                    __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s[qb][ns][i] * x2));
-                            else
-                                s[qb][ns][i] = tanhf(s[qb][ns][i] * a.scale);
-                        }
-                }
-                if (a.slopes) {
-                    const float in = a.cap == 0.0f ? a.scale : BF ? 2.0f * a.cap : a.cap;
-                    const float add = BF ? a.cap : 0.0f;
-#pragma unroll
-                    for (int ns = 0; ns < NS; ++ns) {
-                        const float d0 = static_cast<float>(r_pos[qb] - (kbw + 32 * ns + 4 * hi));
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            s[qb][ns][i] = fmaf(
-                                s[qb][ns][i], in,
-                                fmaf(-r_slope[qb], fabsf(d0 - static_cast<float>(8 * (i >> 2) + (i & 3))), add));
-                    }
-                }
-                if (mixed) {
-                    int lo, len;
-                    interval(qb, lo, len);
-#pragma unroll
-                    for (int ns = 0; ns < NS; ++ns) {
-                        const int d0 = kbw + 32 * ns + 4 * hi - lo;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            s[qb][ns][i] =
-                                static_cast<uint32_t>(d0 + 8 * (i >> 2) + (i & 3)) < static_cast<uint32_t>(len)
-                                    ? s[qb][ns][i]
-                                    : -INFINITY;
-                    }
-                }
-                float part[4] = {s[qb][0][0], s[qb][0][1], s[qb][0][2], s[qb][0][3]};
+            if (a.cap != 0.0f) {  // (a.scale: the score's over the cap)
+                const float x2 = a.scale * (2.0f * kLog2e);
 #pragma unroll
                 for (int ns = 0; ns < NS; ++ns)
 #pragma unroll
-                    for (int i = ns == 0 ? 4 : 0; i < 16; ++i) part[i & 3] = fmaxf(part[i & 3], s[qb][ns][i]);
-                float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-                top = BF ? fmaf(xor32_max(top), sc, off) : xor32_max(top) * sc;
-                // Raising the maximum of a row without sums so far (m = -inf) needs no rescaling.
-                const bool raise = top > m[qb] + kRaise;  // (false for top = -inf)
-                if (__any(raise)) {
-                    const float mn = raise ? top : m[qb];
-                    const bool any = __any(raise && m[qb] != -INFINITY);
-                    const float f = raise ? __builtin_amdgcn_exp2f(m[qb] - mn) : 1.0f;
-                    m[qb] = mn;
-                    if (any) {
-                        l[qb] *= f;
-#pragma unroll
-                        for (int d = 0; d < DB; ++d)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[qb][d][i] *= f;
+                    for (int i = 0; i < 16; ++i) {
+                        if constexpr (BF)
+                            s[ns][i] =
+                                __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s[ns][i] * x2));
+                        else
+                            s[ns][i] = tanhf(s[ns][i] * a.scale);
                     }
-                }
-                const float ref = (m[qb] == -INFINITY ? 0.0f : m[qb]) - off;
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                constexpr int X = 4 * NS;
-#pragma unroll
-                for (int x = 0; x < X; ++x) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float e = s[qb][x / 4][4 * (x % 4) + j];
-                        // (float32 rounds the score first, as the maximum was: the largest weight is 1 exactly)
-                        const float w = __builtin_amdgcn_exp2f(BF ? fmaf(e, sc, -ref) : scaled(e, sc) - ref);
-                        s[qb][x / 4][4 * (x % 4) + j] = w;
-                        sum[j] += w;
-                    }
-                    if (NBUF == 1 && qb == QB - 1) {
-#pragma unroll
-                        for (int p = x * NH / X; p < (x + 1) * NH / X; ++p) stage(nxt, 0, false, p, next);
-                    }
-                }
-                l[qb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             }
+            if (a.slopes) {
+                const float in = a.cap == 0.0f ? a.scale : BF ? 2.0f * a.cap : a.cap;
+                const float add = BF ? a.cap : 0.0f;
+#pragma unroll
+                for (int ns = 0; ns < NS; ++ns) {
+                    const float d0 = static_cast<float>(r_pos - (kbw + 32 * ns + 4 * hi));
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        s[ns][i] = fmaf(
+                            s[ns][i], in,
+                            fmaf(-r_slope, fabsf(d0 - static_cast<float>(8 * (i >> 2) + (i & 3))), add));
+                }
+            }
+            if (mixed) {
+                int lo, len;
+                interval(lo, len);
+#pragma unroll
+                for (int ns = 0; ns < NS; ++ns) {
+                    const int d0 = kbw + 32 * ns + 4 * hi - lo;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        s[ns][i] =
+                            static_cast<uint32_t>(d0 + 8 * (i >> 2) + (i & 3)) < static_cast<uint32_t>(len)
+                                ? s[ns][i]
+                                : -INFINITY;
+                }
+            }
+            float part[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
+#pragma unroll
+            for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+                for (int i = ns == 0 ? 4 : 0; i < 16; ++i) part[i & 3] = fmaxf(part[i & 3], s[ns][i]);
+            float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+            top = BF ? fmaf(xor32_max(top), sc, off) : xor32_max(top) * sc;
+            // Raising the maximum of a row without sums so far (m = -inf) needs no rescaling.
+            const bool raise = top > m + kRaise;  // (false for top = -inf)
+            if (__any(raise)) {
+                const float mn = raise ? top : m;
+                const bool any = __any(raise && m != -INFINITY);
+                const float f = raise ? __builtin_amdgcn_exp2f(m - mn) : 1.0f;
+                m = mn;
+                if (any) {
+                    l *= f;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[d][i] *= f;
+                }
+            }
+            const float ref = (m == -INFINITY ? 0.0f : m) - off;
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            constexpr int X = 4 * NS;
+#pragma unroll
+            for (int x = 0; x < X; ++x) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = s[x / 4][4 * (x % 4) + j];
+                    // (float32 rounds the score first, as the maximum was: the largest weight is 1 exactly)
+                    const float w = __builtin_amdgcn_exp2f(BF ? fmaf(e, sc, -ref) : scaled(e, sc) - ref);
+                    s[x / 4][4 * (x % 4) + j] = w;
+                    sum[j] += w;
+                }
+                if (NBUF == 1) {
+#pragma unroll
+                    for (int p = x * NH / X; p < (x + 1) * NH / X; ++p) stage(nxt, 0, false, p, next);
+                }
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             if (more) sync(Others{});  // the values
             else sync(None{});
             if (clean) {
@@ -626,7 +600,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                             v_ptr[d % VP] + at + (d / VP) * 256 +
                             (32 * (st / 16) + 8 * (st % 16 >> 2) + (st & 3)) * ROWB);
                 };
-                VFrag p[QB];
+                VFrag p;
 #pragma unroll
                 for (int x = 0; x < AHEAD; ++x) read_v(x);
 #pragma unroll
@@ -634,25 +608,19 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                     __builtin_amdgcn_sched_barrier(0);
                     const int st = x / DB, d = x % DB;
                     if (d == 0) {
+                        if constexpr (BF) {
 #pragma unroll
-                        for (int qb = 0; qb < QB; ++qb) {
-                            if constexpr (BF) {
-#pragma unroll
-                                for (int i = 0; i < 8; ++i)
-                                    p[qb][i] = static_cast<__bf16>(s[qb][st / 2][8 * (st % 2) + i]);
-                            } else {
-                                p[qb] = s[qb][st / 16][st % 16];
-                            }
+                            for (int i = 0; i < 8; ++i)
+                                p[i] = static_cast<__bf16>(s[st / 2][8 * (st % 2) + i]);
+                        } else {
+                            p = s[st / 16][st % 16];
                         }
                     }
-#pragma unroll
-                    for (int qb = 0; qb < QB; ++qb) {
-                        const VFrag f = vf[x % (2 * AHEAD)];
-                        if constexpr (BF)
-                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p[qb], o[qb][d], 0, 0, 0);
-                        else
-                            o[qb][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(f, p[qb], o[qb][d], 0, 0, 0);
-                    }
+                    const VFrag f = vf[x % (2 * AHEAD)];
+                    if constexpr (BF)
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p, o[d], 0, 0, 0);
+                    else
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(f, p, o[d], 0, 0, 0);
                     if (x + AHEAD < X) read_v(x + AHEAD);
 #pragma unroll
                     for (int q = x * NQ / X; q < (x + 1) * NQ / X; ++q) {
@@ -673,30 +641,27 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
                 const int k0 = cur.kb + kw * KPW, k1 = min(k0 + KPW, cur.end);
                 for (int k = k0; k < k1; ++k) {
-                    const char *row = cur.v + (k - cur.kb) * cur.vn;
+                    const char *values = cur.v + (k - cur.kb) * cur.vn;
                     for (int c0 = 0; c0 < a.D; c0 += 64) {
                         float x = 0.0f;
                         if (c0 + lane < a.D) {
                             if constexpr (BF)
-                                x = rm_bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(row)[c0 + lane]);
+                                x = rm_bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(values)[c0 + lane]);
                             else
-                                x = reinterpret_cast<const float *>(row)[c0 + lane];
+                                x = reinterpret_cast<const float *>(values)[c0 + lane];
                         }
                         for (uint64_t bad = __ballot(!(fabsf(x) < INFINITY)); bad != 0; bad &= bad - 1) {
                             const int from = __ffsll(static_cast<unsigned long long>(bad)) - 1;
                             const float add = __shfl(x, from);
+                            const bool in =
+                                static_cast<uint32_t>(k - r_lo) < static_cast<uint32_t>(r_len);
+                            const bool sees = cur.seg < 0 || (r_smp == cur.seg && in);
+                            const int at = sees ? c0 + from - 4 * hi : -1;
 #pragma unroll
-                            for (int qb = 0; qb < QB; ++qb) {
-                                const bool in =
-                                    static_cast<uint32_t>(k - r_lo[qb]) < static_cast<uint32_t>(r_len[qb]);
-                                const bool sees = cur.seg < 0 || (r_smp[qb] == cur.seg && in);
-                                const int at = sees ? c0 + from - 4 * hi : -1;
+                            for (int d = 0; d < DB; ++d)
 #pragma unroll
-                                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i)
-                                        o[qb][d][i] += at == 32 * d + 8 * (i >> 2) + (i & 3) ? add : 0.0f;
-                            }
+                                for (int i = 0; i < 16; ++i)
+                                    o[d][i] += at == 32 * d + 8 * (i >> 2) + (i & 3) ? add : 0.0f;
                         }
                     }
                 }
@@ -708,102 +673,95 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         // Of the blocks of 32 columns, wave kw joins those with number kw modulo KW: it has its own sums, the others'
         // come through LDS.
         float *join = reinterpret_cast<float *>(lds);
-        float *ml = join + W * QB * 32 * DC;  // [wave][qb][2][32]
-        auto slot = [&](int w, int qb, int d, int i) {
-            return reinterpret_cast<rm_f32x4 *>(join + ((((w * QB + qb) * DB + d) * 4 + i) * 64 + lane) * 4);
+        float *ml = join + W * 32 * DC;  // [wave][2][32]
+        auto slot = [&](int w, int d, int i) {
+            return reinterpret_cast<rm_f32x4 *>(join + (((w * DB + d) * 4 + i) * 64 + lane) * 4);
         };
-        auto quad = [&](int qb, int d, int i) {
-            return rm_f32x4{o[qb][d][4 * i], o[qb][d][4 * i + 1], o[qb][d][4 * i + 2], o[qb][d][4 * i + 3]};
+        auto quad = [&](int d, int i) {
+            return rm_f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
         };
         if constexpr (KW > 1) {
             __syncthreads();  // every wave has read its last tile
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-                const float sum = xor32_sum(l[qb]);
-                if (hi == 0) {
-                    ml[((wave * QB + qb) * 2 + 0) * 32 + col] = m[qb];
-                    ml[((wave * QB + qb) * 2 + 1) * 32 + col] = sum;
-                }
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    if (d % KW != kw)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) *slot(wave, qb, d, i) = quad(qb, d, i);
+            const float sum = xor32_sum(l);
+            if (hi == 0) {
+                ml[(wave * 2 + 0) * 32 + col] = m;
+                ml[(wave * 2 + 1) * 32 + col] = sum;
             }
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                if (d % KW != kw)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) *slot(wave, d, i) = quad(d, i);
             __syncthreads();
         }
         float nan = 0.0f;  // stays 0 unless a result is NaN (or infinite)
+        float f[KW], top = m, sum = 0.0f;  // the key waves' factors
+        if constexpr (KW > 1) {
+            top = -INFINITY;
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-            const int r = row0 + (rw * QB + qb) * 32 + col;
-            float f[KW], top = m[qb], sum = 0.0f;  // the key waves' factors
-            if constexpr (KW > 1) {
-                top = -INFINITY;
-#pragma unroll
-                for (int k = 0; k < KW; ++k) {
-                    f[k] = ml[(((k * RW + rw) * QB + qb) * 2 + 0) * 32 + col];
-                    top = fmaxf(top, f[k]);
-                }
-                const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-                for (int k = 0; k < KW; ++k) {
-                    f[k] = __builtin_amdgcn_exp2f(f[k] - ref);
-                    sum += ml[(((k * RW + rw) * QB + qb) * 2 + 1) * 32 + col] * f[k];
-                }
-            } else {
-                sum = xor32_sum(l[qb]);
+            for (int k = 0; k < KW; ++k) {
+                f[k] = ml[((k * RW + rw) * 2 + 0) * 32 + col];
+                top = fmaxf(top, f[k]);
             }
-            const float inv = a.splits > 1 ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
-            const int64_t prow = (static_cast<int64_t>(split) * a.U * a.Hk + ng) * a.R + r;
-            if (a.splits > 1 && r < a.R && hi == 0 && kw == 0) {
-                a.part_ml[2 * prow] = top;
-                a.part_ml[2 * prow + 1] = sum;
-            }
-            char *orow = a.o + (static_cast<int64_t>(u) * a.per + r_smp[qb]) * a.o_b + r_tok[qb] * a.o_t +
-                         r_head[qb] * a.o_h;
+            const float ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                if (KW > 1 && d % KW != kw) continue;
-                rm_f32x4 v[4];
+            for (int k = 0; k < KW; ++k) {
+                f[k] = __builtin_amdgcn_exp2f(f[k] - ref);
+                sum += ml[((k * RW + rw) * 2 + 1) * 32 + col] * f[k];
+            }
+        } else {
+            sum = xor32_sum(l);
+        }
+        const float inv = a.splits > 1 ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
+        const int64_t prow = (static_cast<int64_t>(split) * a.U * a.Hk + ng) * a.R + row;
+        if (a.splits > 1 && row < a.R && hi == 0 && kw == 0) {
+            a.part_ml[2 * prow] = top;
+            a.part_ml[2 * prow + 1] = sum;
+        }
+        char *orow = a.o + (static_cast<int64_t>(u) * a.per + r_smp) * a.o_b + r_tok * a.o_t +
+                     r_head * a.o_h;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            if (KW > 1 && d % KW != kw) continue;
+            rm_f32x4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = quad(d, i);
+                if constexpr (KW > 1) {
+                    v[i] *= f[d % KW];
+#pragma unroll
+                    for (int k = 0; k < KW; ++k)
+                        if (k != d % KW) v[i] += *slot(k * RW + rw, d, i) * f[k];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) nan = fmaf(v[i][e], 0.0f, nan);
+            }
+            if (a.splits > 1 || !BF) {
+                char *dst = a.splits > 1 ? reinterpret_cast<char *>(a.part_o + prow * a.D) : orow;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = quad(qb, d, i);
-                    if constexpr (KW > 1) {
-                        v[i] *= f[d % KW];
-#pragma unroll
-                        for (int k = 0; k < KW; ++k)
-                            if (k != d % KW) v[i] += *slot(k * RW + rw, qb, d, i) * f[k];
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) nan = fmaf(v[i][e], 0.0f, nan);
+                    const int c = 32 * d + 8 * i + 4 * hi;
+                    if (row < a.R && (!PAD || c < a.D)) *reinterpret_cast<rm_f32x4 *>(dst + c * 4) = v[i] * inv;
                 }
-                if (a.splits > 1 || !BF) {
-                    char *dst = a.splits > 1 ? reinterpret_cast<char *>(a.part_o + prow * a.D) : orow;
+            } else {
+                // The lane halves have columns 8 i + {0..3} and + {4..7}: of two such groups each half takes one
+                // whole.
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int c = 32 * d + 8 * i + 4 * hi;
-                        if (r < a.R && (!PAD || c < a.D)) *reinterpret_cast<rm_f32x4 *>(dst + c * 4) = v[i] * inv;
+                for (int i = 0; i < 4; i += 2) {
+                    uint32_t w[2][2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const rm_f32x4 y4 = v[i + e] * inv;
+                        const rm_bf16x4 x = {static_cast<__bf16>(y4[0]), static_cast<__bf16>(y4[1]),
+                                             static_cast<__bf16>(y4[2]), static_cast<__bf16>(y4[3])};
+                        const uint2 y = __builtin_bit_cast(uint2, x);
+                        w[e][0] = y.x, w[e][1] = y.y;
                     }
-                } else {
-                    // The lane halves have columns 8 i + {0..3} and + {4..7}: of two such groups each half takes one
-                    // whole.
-#pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        uint32_t w[2][2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const rm_f32x4 y4 = v[i + e] * inv;
-                            const rm_bf16x4 x = {static_cast<__bf16>(y4[0]), static_cast<__bf16>(y4[1]),
-                                                 static_cast<__bf16>(y4[2]), static_cast<__bf16>(y4[3])};
-                            const uint2 y = __builtin_bit_cast(uint2, x);
-                            w[e][0] = y.x, w[e][1] = y.y;
-                        }
-                        const auto p0 = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
-                        const auto p1 = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
-                        const int c = 32 * d + 8 * (i + hi);
-                        if (r < a.R && (!PAD || c < a.D))
-                            *reinterpret_cast<rm_u32x4 *>(orow + c * 2) = rm_u32x4{p0[0], p1[0], p0[1], p1[1]};
-                    }
+                    const auto p0 = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+                    const auto p1 = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+                    const int c = 32 * d + 8 * (i + hi);
+                    if (row < a.R && (!PAD || c < a.D))
+                        *reinterpret_cast<rm_u32x4 *>(orow + c * 2) = rm_u32x4{p0[0], p1[0], p0[1], p1[1]};
                 }
             }
         }
