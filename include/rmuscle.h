@@ -313,10 +313,12 @@ typedef struct rm_heads {
 
 /* n_q_heads: a multiple of n_kv_heads; query head h uses key head h / (n_q_heads / n_kv_heads).
  * head_dim: a multiple of 8, at most 256.  dtype: an rm_dtype, of queries, keys, values and output.
- * scale: finite and positive; scores are scale * <q, k>.  softcap: >= 0; not 0: scores become softcap * tanh(score / softcap).
- * A call takes fewer than 2^30 query rows (tokens times query heads of a key head) of one sample or group, and fewer than
- * 2^24 blocks of 32 of them in all.  Scores, maxima, sums and the output are accumulated in float32; with RM_BF16 the softmax's weights are rounded to
- * bf16 before their product with the values (as the values are), their sum is not. */
+ * scale: finite and positive; scores are scale * <q, k>.  softcap: >= 0; not 0: scores become
+ * softcap * tanh(score / softcap).
+ * A call takes fewer than 2^30 query rows (tokens times query heads of a key head) of one sample or group, and fewer
+ * than 2^24 blocks of 32 of them in all.  Scores, maxima, sums and the output are accumulated in float32; with RM_BF16
+ * the softmax's weights are rounded to bf16 before their product with the values (as the values are), their sum is
+ * not. */
 typedef struct rm_attn_shape {
     int32_t n_q_heads, n_kv_heads, head_dim, dtype;
     float scale, softcap;
@@ -335,7 +337,8 @@ typedef struct rm_attn_shape {
  *             value; NULL: row n (rows >= n_tok).  Slots are distinct: tokens that share one leave an unspecified
  *             mix of theirs in it.  Other rows keep what they hold.
  * head_dim a multiple of 8, at most 256; rot a multiple of 4 in [0, head_dim].  Angles are reduced in 64 bits,
- * everything else is float32.  0 <= n_tok < 2^26, n_tok x heads < 2^30.  Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN. */
+ * everything else is float32.  0 <= n_tok < 2^26, n_tok x heads < 2^30.
+ * Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN. */
 rm_status rm_qk_norm_rope(int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t in_dtype,
                           int32_t out_dtype, const rm_heads *q, const rm_heads *k, const rm_heads *v,
                           const rm_heads *q_out, const rm_heads *k_out, const rm_heads *v_out, int32_t rows,

@@ -101,11 +101,12 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     const int64_t rows = static_cast<int64_t>(R), ng = static_cast<int64_t>(groups);
     q.dh = D <= 64 ? 64 : D <= 128 ? 128 : 256;
     constexpr int64_t kCUs = 256;
-    // Waves that divide 128 rows, or the keys of 32: the former once there are enough blocks of 128 rows.  Measured on 2048
-    // (512) keys, us, the latter / the former: bf16, 128 columns, 128 blocks 31 / 48 (13 / 17), 192 48 / 49 (20 / 17), 256
-    // 60 / 50 (24 / 18), 512 110 / 77; 64 columns alike; 256 columns (one workgroup to a compute unit) 64 blocks 33 / 69
-    // (14 / 23), 128 66 / 70 (26 / 24), 256 124 / 75.  Float32, 128 columns, 256 blocks 320 / 334 (97 / 90), 384 480 / 565,
-    // 512 639 / 568; 256 columns have too few registers for it (768 blocks: 1768 / 2841) and waves that divide both.
+    // Waves that divide 128 rows, or the keys of 32: the former once there are enough blocks of 128 rows.  Measured on
+    // 2048 (512) keys, us, the latter / the former: bf16, 128 columns, 128 blocks 31 / 48 (13 / 17), 192 48 / 49
+    // (20 / 17), 256 60 / 50 (24 / 18), 512 110 / 77; 64 columns alike; 256 columns (one workgroup to a compute unit)
+    // 64 blocks 33 / 69 (14 / 23), 128 66 / 70 (26 / 24), 256 124 / 75.  Float32, 128 columns, 256 blocks 320 / 334
+    // (97 / 90), 384 480 / 565, 512 639 / 568; 256 columns have too few registers for it (768 blocks: 1768 / 2841) and
+    // waves that divide both.
     const int64_t blocks = ceil_div(rows, 128) * ng;
     const bool key_waves = rows <= 32 || (bf ? blocks < (q.dh == 256 ? 128 : 192) : q.dh == 256 || blocks < 2 * kCUs);
     q.kw = key_waves ? 4 : 1;

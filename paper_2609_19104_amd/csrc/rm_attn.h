@@ -4,18 +4,18 @@
 // A workgroup takes 32 RW query rows (the tokens of one group times the query heads of one key head, so that a
 // key head's rows are read once for all its query heads) and walks tiles of KT keys.  RW of its waves divide the rows
 // and KW the keys of a tile; the waves that take the same keys load them straight into LDS buffers of their own, so
-// with RW = 1 no wave waits for another before the KW partial results are joined in LDS at the end.  With `splits` > 1
-// several workgroups divide a row block's tiles and leave partial results in the workspace for the combine kernel.
+// with RW = 1 no wave waits for another before the KW partial results are joined in LDS at the end.  With
+// `splits` > 1 several workgroups divide a row block's tiles and leave partial results for the combine kernel.
 //
 // Matrix-core layout (32x32 tiles): S^T = K Q^T, so a lane holds scores of one query row (column lane % 32) and
 // row statistics, spans and slopes are one register per lane; O^T = V^T P^T takes P straight from the score
 // registers: the 16 keys of a matrix-core step may come in any order as long as V's rows come in the same, and the
 // order the scores have (keys 16 s + 4 h + {0..3} and + 8 for lane half h) is the one V's fragments are read in.
 //
-// What bounds it (bf16, MI355X): with RW = 4 the matrix cores and the exponentials, two workgroups to a compute unit, one
-// in its softmax while the other multiplies: 8192 x 8192 rows and keys, 16 heads of 128 columns on 4: 572 us, 960
-// TFLOP/s; of 64: 375 us, 730 (a score costs as many exponentials for half the products); 8 heads of 256 on 1: 558 us,
-// 985 (a library product of 8192^3: 1222).  With KW = 4, where a compute unit has few rows, its load unit and LDS: 64
+// What bounds it (bf16, MI355X): with RW = 4 the matrix cores and the exponentials, two workgroups to a compute unit,
+// one in its softmax while the other multiplies: 8192 x 8192 rows and keys, 16 heads of 128 columns on 4: 572 us, 960
+// TFLOP/s; of 64: 375 us, 730 (a score costs as many exponentials for half the products); 8 heads of 256 on 1:
+// 558 us, 985 (a library product of 8192^3: 1222).  With KW = 4, where a compute unit has few rows, its load unit and LDS: 64
 // bytes a cycle in and 128 out, which a tile of 128 keys and 256 columns keeps for 2048 of its 3800 cycles (1.6 us), and
 // one wave to a SIMD, whose softmax (700 cycles) nothing else covers; a launch's own 6 us are its first trips to memory
 // and the join.  The load instructions go out between the matrix-core steps, since a wave that issues several in a row

@@ -43,13 +43,14 @@ struct Args {
     const int32_t *q_start = nullptr;
     int D = 0, Hk = 0, G = 0, T = 0, per = 0, U = 0, causal = 0;
     Divisor by_g, by_t, by_hk, by_splits;  // G, T, Hk and splits
-    // The workgroups' order over the groups and key heads (of an XCD, by_xcd): by turns, or one after the other; order: how
-    // many of them there are, or how many workgroups each has.
+    // The workgroups' order over the groups and key heads (of an XCD, by_xcd): by turns, or one after the other;
+    // order: how many of them there are, or how many workgroups each has.
     int by_xcd = 0, turns = 0, order = 1;
     Divisor by_order;
     int R = 0;                      // rows of a group and key head: per T G
     int n_tiles = 0, splits = 1;    // row blocks, and workgroups that divide one's keys
-    float scale = 0.0f, cap = 0.0f; // scores times scale in powers of two; with a cap: scale = score scale / cap, cap in powers of two
+    // Scores times scale in powers of two; with a cap: scale = score scale / cap, cap in powers of two.
+    float scale = 0.0f, cap = 0.0f;
     float *part_o = nullptr, *part_ml = nullptr;  // [splits][U Hk][R][D] and [..][2], with splits > 1
 };
 
