@@ -108,17 +108,32 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     // (97 / 90), 384 480 / 565, 512 639 / 568; 256 columns have too few registers for it (768 blocks: 1768 / 2841) and
     // waves that divide both.
     const int64_t blocks = ceil_div(rows, 128) * ng;
-    const bool key_waves = rows <= 32 || (bf ? blocks < (q.dh == 256 ? 128 : 192) : q.dh == 256 || blocks < 2 * kCUs);
+    bool key_waves = rows <= 32 || (bf ? blocks < (q.dh == 256 ? 128 : 192) : q.dh == 256 || blocks < 2 * kCUs);
+    // Few blocks on many keys, where slices of the keys fill the compute units either way: bf16, 128 columns, 32 blocks
+    // on 8192 keys 39 / 38, on 32768 111 / 89, 64 blocks on 32768 210 / 161; 64 columns, 32 on 8192 28 / 32, on 32768
+    // 76 / 66; 256 columns, 8 on 8192 28 / 31, 32 on 8192 66 / 56, on 32768 221 / 156.  (A window that hides most of
+    // the keys turns the second, 111 / 89, into 18 / 23: the plan does not know the spans.)
+    auto keys = [&](int64_t r) {  // read by a block of r rows, which may hold rows of several samples
+        return n0 + std::min<int64_t>(per, ceil_div(r, static_cast<int64_t>(T) * G)) * n1;
+    };
+    const int64_t many = q.dh == 256 ? int64_t{1} << 18 : int64_t{1} << 20;
+    if (bf && rows > 32 && keys(128) >= ceil_div(many, blocks)) key_waves = false;
+    // Own keys that few of a block's rows see pass through all its waves: 1024 (256) single tokens of 8 (4) query heads
+    // to a key head on 1024 shared and 64 (256) own keys, bf16, 128 columns 53 / 58 (57 / 90), 64 columns 38 / 48
+    // (33 / 73), 256 columns 123 / 88 (116 / 186); float32, 2048 of 8 (4) on 1024 and 64 (256 and 128), 128 columns
+    // 511 / 577 (505 / 1225), 64 columns 250 / 286 (247 / 590).
+    if (2 * keys(128) > (q.dh == 256 ? 4 : 3) * keys(32)) key_waves = true;
     q.kw = key_waves ? 4 : 1;
     q.rows = key_waves ? (!bf && q.dh == 256 ? 64 : 32) : 128;
     q.n_tiles = static_cast<int>(ceil_div(rows, q.rows));
     const int64_t wgs = q.n_tiles * ng;
     if (wgs >= kMaxGroups) return api_fail(RM_ERR_SHAPE, "launch grid too large");
-    // Few row blocks: several workgroups divide the keys, as many as fill the compute units once (two workgroups to one,
-    // where their LDS allows it: heads up to 128 in bf16, 64 in float32), if the tiles that each of them then has less pay
-    // for the second launch and the partial results.  Measured, us: a tile of 128 keys 0.9, 1.1 and 1.65 in bf16 (rows
-    // of 64, 128 and 256 columns), 2.3, 4.1 and 14 in float32, 2.4 times that for 128 rows; the join 5 and its traffic at 4 TB/s (one action
-    // chunk's 408 rows on 901 keys, D = 256: 20.2 us undivided, 14.2 in 8 slices; 6528 rows 24.4 undivided, 38.7 in 2).
+    // Few row blocks: several workgroups divide the keys, as many as fill the compute units once (two workgroups to
+    // one, where their LDS allows it: heads up to 128 in bf16, 64 in float32), if the tiles that each of them then has
+    // less pay for the second launch and the partial results.  Measured, us: a tile of 128 keys 0.9, 1.1 and 1.65 in
+    // bf16 (rows of 64, 128 and 256 columns), 2.3, 4.1 and 14 in float32, 2.4 times that for 128 rows; the join 5 and
+    // its traffic at 4 TB/s (one action chunk's 408 rows on 901 keys, D = 256: 20.2 us undivided, 14.2 in 8 slices;
+    // 6528 rows 24.4 undivided, 38.7 in 2).
     const int64_t tiles = ceil_div(n0, 128) + ceil_div(n1, 128);
     const int64_t slots = kCUs * (q.dh * (bf ? 1 : 2) <= 128 ? 2 : 1);
     const double tile_us =

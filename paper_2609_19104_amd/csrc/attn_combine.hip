@@ -6,7 +6,8 @@ namespace rm_attn {
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 // LPR lanes per row, 4 columns a lane (D <= 4 LPR).  Slices are added in order, so the sums are the same on every
-// call.  One launch of latency: 4 us for 408 rows of 256 columns in 8 slices, 7 for 128 rows of 128 in 32.  A slice without keys for the row has m = -inf and sums of 0.
+// call.  One launch of latency: 4 us for 408 rows of 256 columns in 8 slices, 7 for 128 rows of 128 in 32.  A slice
+// without keys for the row has m = -inf and l = 0; its other sums are 0 or were not written, and are not used.
 template <bool BF, int LPR>
 __global__ __launch_bounds__(256) void combine_kernel(Args a) {
     const int64_t rows = static_cast<int64_t>(a.U) * a.Hk * a.R;
@@ -36,7 +37,7 @@ __global__ __launch_bounds__(256) void combine_kernel(Args a) {
             for (int i = 0; i < 8; ++i) {
                 const int from = (i0 + i) % LPR;
                 const float fi = __shfl(f, from, LPR), li = __shfl(mine.y, from, LPR);
-                if (i0 + i < n) {
+                if (i0 + i < n && li != 0.0f) {
                     l += li * fi;
                     o += v[i] * fi;
                 }

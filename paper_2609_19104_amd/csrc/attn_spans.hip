@@ -7,9 +7,9 @@ namespace {
 
 constexpr int kSpanRows = 256;  // rows per workgroup
 
-// A document is a run of equal ids.  A workgroup's first row may lie inside a run that begins before its rows, and
-// its last in one that ends after them: those two ends are searched for outwards, 8 ids a thread and step, and the
-// runs in between come from a running maximum (minimum) of the positions where the id changes.  Bound by round trips (lengths,
+// A document is a run of equal ids.  A workgroup's first row may lie inside a run that begins before its rows, and its
+// last in one that ends after them: those two ends are searched for outwards, 8 ids a thread and step, and the runs in
+// between come from a running maximum (minimum) of the positions where the id changes.  Bound by round trips (lengths,
 // the search's loads, two joins of the workgroup): 8 x 16384 rows of 24 documents each take 7.3 us, 2.1 MB of ids and
 // intervals; without documents 850 rows take 2.2.
 __global__ __launch_bounds__(kSpanRows) void spans_kernel(int T, int N, int causal, int window,
@@ -39,12 +39,13 @@ __global__ __launch_bounds__(kSpanRows) void spans_kernel(int T, int N, int caus
         const int pa = static_cast<int>(min(max(start + i0, static_cast<int64_t>(0)), static_cast<int64_t>(N - 1)));
         const int pb = static_cast<int>(min(max(start + last_row, static_cast<int64_t>(0)), static_cast<int64_t>(N - 1)));
         auto begins = [&](int j) { return j == 0 || ids[j] != ids[j - 1]; };  // a run begins at j in [0, N)
-        // Both ends at a time: the greatest begin at or before pa, and minus the least one behind pb (N ends the last run,
-        // position 0 begins the first, so both searches end).
+        // Both ends at a time: the greatest begin at or before pa, and minus the least one behind pb (N ends the last
+        // run, position 0 begins the first, so both searches end).
         constexpr int64_t zero = 0;
         int first = -1, end = kNone;
         for (int64_t step = 0; first < 0 || end == kNone; step += kStep) {
-            // All loads first (positions outside are read at the ends): in a branch each, every one would be a round trip.
+            // All loads first (positions outside are read at the ends): in a branch each, every one would be a round
+            // trip.
             int32_t at[2 * kPer], before[2 * kPer];
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {

@@ -14,13 +14,13 @@
 //
 // What bounds it (bf16, MI355X): with RW = 4 the matrix cores and the exponentials, two workgroups to a compute unit,
 // one in its softmax while the other multiplies: 8192 x 8192 rows and keys, 16 heads of 128 columns on 4: 572 us, 960
-// TFLOP/s; of 64: 375 us, 730 (a score costs as many exponentials for half the products); 8 heads of 256 on 1:
-// 558 us, 985 (a library product of 8192^3: 1222).  With KW = 4, where a compute unit has few rows, its load unit and LDS: 64
-// bytes a cycle in and 128 out, which a tile of 128 keys and 256 columns keeps for 2048 of its 3800 cycles (1.6 us), and
-// one wave to a SIMD, whose softmax (700 cycles) nothing else covers; a launch's own 6 us are its first trips to memory
-// and the join.  The load instructions go out between the matrix-core steps, since a wave that issues several in a row
-// waits for the load unit, 16 cycles an instruction and wave (a tile 4400 -> 3800 cycles).  Float32: the matrix cores'
-// 153 TFLOP/s, of which 16 heads of 128 on 4096 rows reach 122.
+// TFLOP/s; of 64: 375 us, 730 (a score costs as many exponentials for half the products); 8 heads of 256 on 1: 558 us,
+// 985 (a library product of 8192^3: 1222).  With KW = 4, where a compute unit has few rows, its load unit and LDS: 64
+// bytes a cycle in and 128 out, which a tile of 128 keys and 256 columns keeps for 2048 of its 3800 cycles (1.6 us),
+// and one wave to a SIMD, whose softmax (700 cycles) nothing else covers; a launch's own 6 us are its first trips to
+// memory and the join.  The load instructions go out between the matrix-core steps, since a wave that issues several in
+// a row waits for the load unit, 16 cycles an instruction and wave (a tile 4400 -> 3800 cycles).  Float32: the matrix
+// cores' 153 TFLOP/s, of which 16 heads of 128 on 4096 rows reach 122.
 #pragma once
 
 #include "rm_attn_plan.h"
@@ -378,6 +378,16 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     typedef std::integral_constant<int, NBUF == 2 ? 2 * NP : 2 * NH> Others;
     typedef std::integral_constant<int, 63> Any;  // reads only
     constexpr uint64_t kAll = ~0ull;
+
+    // A slice without tiles (its row block sees few keys) leaves only its rows' empty maximum and sum.
+    if (a.splits > 1 && n_tiles <= 0) {
+        if (row < a.R && hi == 0 && kw == 0) {
+            const int64_t prow = (static_cast<int64_t>(split) * a.U * a.Hk + ng) * a.R + row;
+            a.part_ml[2 * prow] = -INFINITY;
+            a.part_ml[2 * prow + 1] = 0.0f;
+        }
+        return;
+    }
 
     Tile cur;
     first_tile(cur);

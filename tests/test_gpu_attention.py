@@ -368,10 +368,12 @@ def test_prefix_long_and_few_rows(dtype, D):
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("causal", [False, True])
-def test_prefix_many_rows(dtype, D, causal):
-    """Enough rows for the kernel whose waves divide them, each wave with samples of its own; two samples hold NaN."""
+@pytest.mark.parametrize("P", [70, 400])
+def test_prefix_many_rows(dtype, D, causal, P):
+    """Many rows, each wave with samples of its own, on many own keys (waves that divide the keys) and on a longer
+    prefix (waves that divide the rows); two samples hold NaN."""
     g = gen(24, D)
-    G, per, T, P, S, H = 2, 75, 33, 70, 40, 16
+    G, per, T, S, H = 2, 75, 33, 40, 16
     q, kp, vp, ko, vo = make_prefix(g, G, per, T, P, S, H, H, D, dtype)
     olen = torch.randint(0, S + 1, (G * per,), generator=g, dtype=torch.int32)
     olen[0], olen[1], olen[-1] = S, 0, 1
@@ -413,6 +415,25 @@ def test_row_waves_and_slices(D, per, causal):
     out = run_span(q, k, v, span)
     for b, h in ((0, 0), (2, 31)):
         check_span(q[b:b + 1, ::37, h:h + 1], k[b:b + 1], v[b:b + 1], span[b:b + 1, ::37], out=out[b:b + 1, ::37, h:h + 1])
+
+
+@pytest.mark.parametrize("dtype,D,T,N", [(BF, 64, 512, 20000), (BF, 128, 512, 20000), (BF, 256, 128, 20000),
+                                         (BF, 128, 512, 33000), (BF, 256, 128, 33000), (F32, 128, 40, 9000),
+                                         (BF, 128, 3, 9000)])
+def test_slices_that_see_no_keys(dtype, D, T, N):
+    """Few rows on many keys, of which each sees few or none: most workgroups of a row block have nothing to do."""
+    g = gen(26, D, T, N)
+    q = randn(g, (2, T, 8, D), dtype, 2.0)
+    k, v = randn(g, (2, N, 1, D), dtype), randn(g, (2, N, 1, D), dtype)
+    assert rm.span_attention_workspace(q, k).numel() > 0
+    lo = torch.randint(0, N, (2, 1, 1), generator=g) + torch.randint(0, 200, (2, T, 1), generator=g)
+    span = torch.cat([lo, lo + torch.randint(0, 300, (2, T, 1), generator=g)], -1).clamp(max=N).to(torch.int32)
+    span[1, T // 2:] = 0
+    span = span.cuda()
+    out = run_span(q, k, v, span)
+    step = max(1, T // 9)
+    for h in (0, 7):
+        check_span(q[:, ::step, h:h + 1], k, v, span[:, ::step], out=out[:, ::step, h:h + 1])
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
