@@ -109,15 +109,20 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     // waves that divide both.
     const int64_t blocks = ceil_div(rows, 128) * ng;
     bool key_waves = rows <= 32 || (bf ? blocks < (q.dh == 256 ? 128 : 192) : q.dh == 256 || blocks < 2 * kCUs);
+    // Blocks that are at most half full: 256 of them (64 rows) on 2048 keys, bf16, 64 columns 26 / 39, 128 51 / 56, 256
+    // 124 / 106.
+    if (rows <= 64 && q.dh <= 128) key_waves = true;
     // Few blocks on many keys, where slices of the keys fill the compute units either way: bf16, 128 columns, 32 blocks
     // on 8192 keys 39 / 38, on 32768 111 / 89, 64 blocks on 32768 210 / 161; 64 columns, 32 on 8192 28 / 32, on 32768
     // 76 / 66; 256 columns, 8 on 8192 28 / 31, 32 on 8192 66 / 56, on 32768 221 / 156.  (A window that hides most of
     // the keys turns the second, 111 / 89, into 18 / 23: the plan does not know the spans.)
+    // 4 (16) blocks of 96 rows on 131072: 64 columns 56 / 54 (166 / 143), 128 97 / 69 (300 / 208), 256 160 / 110
+    // (545 / 383); of 64 rows: 64 columns 41 / 55 (130 / 141), 128 60 / 67 (240 / 209), 256 119 / 106 (414 / 381).
     auto keys = [&](int64_t r) {  // read by a block of r rows, which may hold rows of several samples
         return n0 + std::min<int64_t>(per, ceil_div(r, static_cast<int64_t>(T) * G)) * n1;
     };
-    const int64_t many = q.dh == 256 ? int64_t{1} << 18 : int64_t{1} << 20;
-    if (bf && rows > 32 && keys(128) >= ceil_div(many, blocks)) key_waves = false;
+    const int64_t many = int64_t{1} << (q.dh == 256 ? 18 : q.dh == 128 && rows > 64 ? 19 : 20);
+    if (bf && rows > (q.dh == 64 ? 64 : 32) && keys(128) >= ceil_div(many, blocks)) key_waves = false;
     // Own keys that few of a block's rows see pass through all its waves: 1024 (256) single tokens of 8 (4) query heads
     // to a key head on 1024 shared and 64 (256) own keys, bf16, 128 columns 53 / 58 (57 / 90), 64 columns 38 / 48
     // (33 / 73), 256 columns 123 / 88 (116 / 186); float32, 2048 of 8 (4) on 1024 and 64 (256 and 128), 128 columns

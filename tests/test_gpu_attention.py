@@ -417,6 +417,20 @@ def test_row_waves_and_slices(D, per, causal):
         check_span(q[b:b + 1, ::37, h:h + 1], k[b:b + 1], v[b:b + 1], span[b:b + 1, ::37], out=out[b:b + 1, ::37, h:h + 1])
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("T,B,N", [(5, 2, 70000), (12, 2, 70000), (5, 200, 130)])
+def test_blocks_that_are_not_full(D, T, B, N):
+    """40 and 96 rows to a key head: few blocks on many keys, many on few."""
+    g = gen(27, D, T, B)
+    q, k, v = randn(g, (B, T, 32, D), BF, 2.0), randn(g, (B, N, 4, D), BF), randn(g, (B, N, 4, D), BF)
+    hi = torch.randint(0, N + 1, (B, T, 1), generator=g)
+    span = torch.cat([torch.zeros_like(hi), hi], -1).to(torch.int32).cuda()
+    out = run_span(q, k, v, span)
+    for b, h in ((0, 0), (B // 2, 17), (B - 1, 31)):
+        check_span(q[b:b + 1, :, h:h + 1], k[b:b + 1, :, h // 8:h // 8 + 1], v[b:b + 1, :, h // 8:h // 8 + 1],
+                   span[b:b + 1], out=out[b:b + 1, :, h:h + 1])
+
+
 @pytest.mark.parametrize("dtype,D,T,N", [(BF, 64, 512, 20000), (BF, 128, 512, 20000), (BF, 256, 128, 20000),
                                          (BF, 128, 512, 33000), (BF, 256, 128, 33000), (F32, 128, 40, 9000),
                                          (BF, 128, 3, 9000)])
