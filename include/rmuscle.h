@@ -314,7 +314,7 @@ typedef struct rm_heads {
 /* n_q_heads: a multiple of n_kv_heads; query head h uses key head h / (n_q_heads / n_kv_heads).
  * head_dim: a multiple of 8, at most 256.  dtype: an rm_dtype, of queries, keys, values and output.
  * scale: finite and positive; scores are scale * <q, k>.  softcap: >= 0; not 0: scores become
- * softcap * tanh(score / softcap).
+ * softcap * tanh(score / softcap), with scale / softcap in [2^-126, 2^126) and softcap < 2^127.
  * A call takes fewer than 2^30 query rows (tokens times query heads of a key head) of one sample or group, and fewer
  * than 2^24 blocks of 32 of them in all.  Scores, maxima, sums and the output are accumulated in float32; with RM_BF16
  * the softmax's weights are rounded to bf16 before their product with the values (as the values are), their sum is

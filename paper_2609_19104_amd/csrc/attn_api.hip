@@ -1,5 +1,6 @@
 // C ABI entry points of the attention side: argument checks, launch plans and launches.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "rm_attn_plan.h"
@@ -80,6 +81,12 @@ rm_status check_attn_shape(const rm_attn_shape *s) {
         return api_fail(RM_ERR_INVALID_ARG, "scale must be finite and positive");
     if (!(s->softcap >= 0.0f) || !std::isfinite(s->softcap))
         return api_fail(RM_ERR_INVALID_ARG, "softcap must be finite and not negative");
+    if (s->softcap > 0.0f) {  // both factors of the capped score, scale / softcap and softcap log2 e, in float32
+        const float x = s->scale / s->softcap;
+        if (!(x >= FLT_MIN && x <= FLT_MAX / 4) || s->softcap > FLT_MAX / 2)
+            return api_fail(RM_ERR_INVALID_ARG, "softcap=%g is out of float32's range at scale=%g",
+                            static_cast<double>(s->softcap), static_cast<double>(s->scale));
+    }
     return RM_OK;
 }
 
@@ -198,7 +205,9 @@ rm_status attn_run(const rm_attn_shape *s, const rm_attn::Plan &p, rm_attn::Args
     }
     const auto hs = static_cast<hipStream_t>(stream);
     const bool bf = s->dtype == RM_BF16;
-    hipError_t e = bf ? rm_attn::launch_bf16(p, a, hs) : rm_attn::launch_f32(p, a, hs);
+    hipError_t e = !bf                              ? rm_attn::launch_f32(p, a, hs)
+                   : s->softcap <= rm_attn::kLowCap ? rm_attn::launch_bf16(p, a, hs)
+                                                    : rm_attn::launch_bf16_high_cap(p, a, hs);
     if (e != hipSuccess) return api_fail(RM_ERR_HIP, "attention launch: %s", hipGetErrorString(e));
     if (p.splits > 1) e = rm_attn::launch_combine(bf, a, hs);
     if (e != hipSuccess) return api_fail(RM_ERR_HIP, "attention join launch: %s", hipGetErrorString(e));

@@ -6,7 +6,7 @@ namespace rm_attn {
 template <int DH, int DC, bool PAD, int RW, int KW, int KT, int NBUF, int WPE>
 static hipError_t go(const Args &a, hipStream_t st) {
     const dim3 grid(static_cast<unsigned>(a.n_tiles) * a.splits * a.U * a.Hk);
-    attn_kernel<false, DH, DC, PAD, RW, KW, KT, NBUF, WPE><<<grid, 64 * RW * KW, 0, st>>>(a);
+    attn_kernel<false, false, DH, DC, PAD, RW, KW, KT, NBUF, WPE><<<grid, 64 * RW * KW, 0, st>>>(a);
     return hipGetLastError();
 }
 

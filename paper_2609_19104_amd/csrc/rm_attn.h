@@ -1,5 +1,5 @@
-// The attention kernel shared by rm_span_attention and rm_prefix_attention (bf16 in attn_bf16.hip, float32 in
-// attn_f32.hip): one pass over the keys with a running maximum and sum per query row.
+// The attention kernel shared by rm_span_attention and rm_prefix_attention (bf16 in attn_bf16.hip and
+// attn_bf16_cap.hip, float32 in attn_f32.hip): one pass over the keys with a running maximum and sum per query row.
 //
 // A workgroup takes 32 RW query rows (the tokens of one group times the query heads of one key head, so that a
 // key head's rows are read once for all its query heads) and walks tiles of KT keys.  RW of its waves divide the rows
@@ -76,6 +76,17 @@ __device__ __forceinline__ float xor32_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// tanh x to 16 roundings of its value, for every x: -1 / (1 + e^2x) is off by a last place of 1, which 1 + 2 times it
+// keeps where tanh x is small, so there x (1 - x^2 / 3 + 2 x^4 / 15 - 17 x^6 / 315 + 62 x^8 / 2835) takes its place (the
+// next term is 4 roundings at 0.35; with a correctly rounded power and reciprocal all of it is at most 7 for x from 1e-30
+// to 12).
+__device__ __forceinline__ float tanh_relative(float x) {
+    const float e = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)));
+    const float z = x * x;
+    const float p = fmaf(fmaf(fmaf(62.0f / 2835.0f, z, -17.0f / 315.0f), z, 2.0f / 15.0f), z, -1.0f / 3.0f);
+    return fabsf(x) < 0.35f ? fmaf(x * z, p, x) : fmaf(2.0f, e, 1.0f);
+}
+
 // a * b rounded, not part of a fused multiply-add.
 __device__ __forceinline__ float scaled(float a, float b) {
 #pragma clang fp contract(off)
@@ -128,8 +139,9 @@ struct Tile {
     int kb, end, seg, before;
 };
 
-// Rows have room for DH columns in LDS; the products take DC of them.  PAD: the head has fewer, more than LEAST.
-template <bool BF, int DH, int DC, bool PAD, int RW, int KW, int KT, int NBUF, int WPE>
+// Rows have room for DH columns in LDS; the products take DC of them.  PAD: the head has at most DC, more than LEAST.
+// LOW: caps up to kLowCap (bf16).
+template <bool BF, bool LOW, int DH, int DC, bool PAD, int RW, int KW, int KT, int NBUF, int WPE>
 __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     constexpr int W = RW * KW, ES = BF ? 2 : 4, ROWB = DH * ES, CPR = ROWB / 16;
     constexpr int RPI = 64 / CPR;                // rows per load instruction of a wave (1 KB)
@@ -423,9 +435,9 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     r_slope = a.slopes ? a.slopes[r_head] * kLog2e : 0.0f;
     r_pos = (a.slopes && a.q_start ? a.q_start[u] : 0) + r_tok;  // (slopes: one sample a group)
     // The scores' registers hold s with score = sc s + off in powers of two: plain products, capped ones as tanh or
-    // (bf16) -1 / (1 + e^2x), of which tanh x is 1 + 2 times; with a bias the scores themselves.
-    const float sc = a.slopes ? 1.0f : a.cap != 0.0f ? (BF ? 2.0f * a.cap : a.cap) : a.scale;
-    const float off = BF && a.cap != 0.0f && !a.slopes ? a.cap : 0.0f;
+    // (LOW) -1 / (1 + e^2x), of which tanh x is 1 + 2 times; with a bias the scores themselves.
+    const float sc = a.slopes ? 1.0f : a.cap != 0.0f ? (LOW ? 2.0f * a.cap : a.cap) : a.scale;
+    const float off = LOW && a.cap != 0.0f && !a.slopes ? a.cap : 0.0f;
 
     // ---------------------------------------------------------------- tiles
     // One pass over the slice's tiles, the first one's loads under way.  Returns whether a tile had keys that some rows
@@ -501,16 +513,16 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                 for (int ns = 0; ns < NS; ++ns)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        if constexpr (BF)
+                        if constexpr (LOW)
                             s[ns][i] =
                                 __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s[ns][i] * x2));
                         else
-                            s[ns][i] = tanhf(s[ns][i] * a.scale);
+                            s[ns][i] = BF ? tanh_relative(s[ns][i] * a.scale) : tanhf(s[ns][i] * a.scale);
                     }
             }
             if (a.slopes) {
-                const float in = a.cap == 0.0f ? a.scale : BF ? 2.0f * a.cap : a.cap;
-                const float add = BF ? a.cap : 0.0f;
+                const float in = a.cap == 0.0f ? a.scale : LOW ? 2.0f * a.cap : a.cap;
+                const float add = LOW ? a.cap : 0.0f;
 #pragma unroll
                 for (int ns = 0; ns < NS; ++ns) {
                     const float d0 = static_cast<float>(r_pos - (kbw + 32 * ns + 4 * hi));

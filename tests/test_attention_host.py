@@ -186,3 +186,20 @@ def test_binding_refuses_cpu_tensors():
         rm.rm_qk_norm_rope(x[0], x[0], None, x[0], x[0], None, torch.zeros(4, dtype=torch.int32), None)
     with pytest.raises(ValueError):
         rm.rm_attn_spans(torch.zeros((1, 4, 2), dtype=torch.int32), 4)
+
+
+@pytest.mark.parametrize("scale,cap,ok", [
+    (0.125, 0.0, True), (0.125, 30.0, True), (0.125, 1e8, True), (0.125, 1e-30, True), (1.0, 1e37, True),
+    (0.125, 3e38, False),   # the cap in powers of two is infinite
+    (1e-10, 1e30, False),   # scale / softcap is denormal
+    (1.0, 1e-39, False),    # or infinite
+])
+def test_softcaps_that_float32_does_not_hold(lib, scale, cap, ok):
+    n = ctypes.c_size_t(1)
+    for dtype in (rm.RM_BF16, rm.RM_F32):
+        s = ctypes.byref(rm.AttnShape(8, 2, 64, dtype, scale, cap))
+        want = rm.RM_OK if ok else rm.RM_ERR_INVALID_ARG
+        assert lib.rm_span_attention_workspace_size(s, 1, 4, 64, ctypes.byref(n)) == want
+        assert lib.rm_prefix_attention_workspace_size(s, 1, 1, 4, 64, 4, ctypes.byref(n)) == want
+        if not ok:
+            assert _span(lib, shape=(8, 2, 64, dtype, scale, cap), out=H(4 * MB, 4096, 1024, 128)) == want

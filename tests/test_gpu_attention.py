@@ -264,6 +264,30 @@ def test_large_scores():
         check_span(q, k, v, scale=1.0)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D,many", [(8, False), (64, False), (72, False), (128, False), (200, False),
+                                    (256, False), (64, True), (128, True), (256, True)])
+@pytest.mark.parametrize("cap", [256.0, 257.0, 1e4, 1e6, 1e8, 1e30])
+@pytest.mark.parametrize("bias", [False, True])
+def test_high_caps(dtype, D, many, cap, bias):
+    """Caps far above the scores leave these as they are: from 256 on the tanh is off by 16 roundings of its value (the
+    polynomial 7, the product with the cap and the score over the cap one each; float32's tanhf 5), so the bound's e has
+    16 u32 of the score and no term of the cap's size.  At 256 itself such a term is 16 u32 256 = 0.00024."""
+    g = gen(14, D, many, bias)
+    B, T, N, Hq, Hk = (40, 130, 130, 16, 16) if many else (2, 12, 300, 4, 2)
+    q, k, v = randn(g, (B, T, Hq, D), dtype, 2.0), randn(g, (B, N, Hk, D), dtype), randn(g, (B, N, Hk, D), dtype)
+    slopes = torch.linspace(0.01, 0.1, Hq, device="cuda") if bias else None
+    out = run_span(q, k, v, slopes=slopes, cap=cap)
+    for b, h in ((0, 0), (B - 1, Hq - 1)):
+        kv = h // (Hq // Hk)
+        one = None if slopes is None else f64(slopes)[h:h + 1]
+        cut = [f64(t) for t in (q[b:b + 1, :, h:h + 1], k[b:b + 1, :, kv:kv + 1], v[b:b + 1, :, kv:kv + 1])]
+        span = np.broadcast_to(np.array([0, N]), (1, T, 2))
+        ref, mag, big = att.span_attention(*cut, span, np.float32(D ** -0.5), cap, one)
+        tol = bound(ref, mag, big, dtype, D + 16, N, cap if cap == 256.0 else 0.0, 0.0 if one is None else float(one[0]) * N)
+        check(out[b:b + 1, :, h:h + 1], ref, tol)
+
+
 def test_offsets_past_32_bits():
     D, Hk, N = 128, 8, 4096
     big = torch.zeros((300, N, Hk, D), dtype=BF, device="cuda")  # 2.5 GB a tensor, in elements past 2^31
