@@ -363,7 +363,8 @@ rm_status rm_attn_spans(int32_t B, int32_t T, int32_t N, int32_t causal, int32_t
  * Keys outside a row's interval do not affect it, whatever they hold (NaN and infinities too).
  *   q, out: [B][T][n_q_heads][head_dim]; k, v: [B][N][n_kv_heads][head_dim]; T >= 1, 0 <= N < 2^30.
  *   span:    int32 [B][T][2], 8-byte aligned, clamped to [0, N] (rm_attn_spans makes it), or NULL: every row sees all.
- *   slopes:  float32 [n_q_heads] or NULL: no bias.  q_start: int32 [B] or NULL (0); read with slopes only.
+ *   slopes:  float32 [n_q_heads] or NULL: no bias.  q_start: int32 [B] or NULL (0), any value; read with slopes
+ *            only.
  *   ws, ws_bytes: at least rm_span_attention_workspace_size bytes (which may be 0: ws may then be NULL), 256-byte
  *            aligned; scratch as for rm_workspace_size.
  * A single token's step is the same call with T = 1. */

@@ -288,6 +288,24 @@ def test_high_caps(dtype, D, many, cap, bias):
         check(out[b:b + 1, :, h:h + 1], ref, tol)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D,T,N", [(64, 5, 300), (128, 40, 150), (256, 3, 4000)])
+@pytest.mark.parametrize("start", [-(1 << 31), -(1 << 30) - 3, -100000001, 100000001, (1 << 30) + 7, (1 << 31) - 2])
+def test_positions_far_from_the_keys(dtype, D, T, N, start):
+    """Every key is on one side of such a row, so its distances are those from that end but for a constant that the
+    softmax does not see: their error is that of distances up to N."""
+    g = gen(15, D, T, start & 0xffffffff)
+    Hq, Hk = 4, 2
+    q, k, v = randn(g, (2, T, Hq, D), dtype, 2.0), randn(g, (2, N, Hk, D), dtype), randn(g, (2, N, Hk, D), dtype)
+    slopes = torch.tensor([0.25, 0.1, 0.0, 0.03], device="cuda")
+    starts = ints([start, N - T])
+    out = run_span(q, k, v, None, slopes, starts)
+    span = np.broadcast_to(np.array([0, N]), (2, T, 2))
+    ref, mag, big = att.span_attention(f64(q), f64(k), f64(v), span, np.float32(D ** -0.5), 0.0, f64(slopes),
+                                       starts.cpu().numpy().astype(np.int64))
+    check(out, ref, bound(ref, mag, big, dtype, D, N, 0.0, 0.25 * (N + T)))
+
+
 def test_offsets_past_32_bits():
     D, Hk, N = 128, 8, 4096
     big = torch.zeros((300, N, Hk, D), dtype=BF, device="cuda")  # 2.5 GB a tensor, in elements past 2^31
