@@ -332,6 +332,9 @@ typedef struct rm_attn_shape {
  *     q_out[n] = u of q[n];  k_out[slot[n]] = u of k[n];  v_out[slot[n]] = v[n]
  *   in_dtype, out_dtype: of q, k, v and of the outputs.  q, k, v, q_out, k_out, v_out: their batch stride is not used;
  *             q and q_out hold n_tok tokens, k and v too, k_out and v_out `rows` rows.  v.data NULL: no values.
+ *             The outputs may lie in one buffer if no element belongs to two of them, as keys beside values in a cache
+ *             [rows][2][n_kv_heads][head_dim] or all three in rows [n_tok][n_q_heads + 2 n_kv_heads][head_dim]; this is
+ *             told from their strides, and where those have no common step an overlap of the extents is refused.
  *   pos:      int32 [n_tok], any value.  inv_freq: float32 [rot / 2] (may be NULL with rot = 0).
  *   slot:     int32 [n_tok] row of each token in k_out and v_out; a slot outside [0, rows) drops the token's key and
  *             value; NULL: row n (rows >= n_tok).  Slots are distinct: tokens that share one leave an unspecified

@@ -30,6 +30,34 @@ bool overlap(const Extent &a, const Extent &b) {
     return a.n != 0 && b.n != 0 && pa < pb + b.n && pb < pa + a.n;
 }
 
+// The head vectors of a tensor of T x H, by byte offsets: `width` bytes at at + i step[0] + j step[1], the steps falling
+// (0: no such axis); reach[n]: how far axis n and the later ones go.
+struct Vectors {
+    int64_t step[3] = {0, 0, 0}, reach[3] = {0, 0, 0};
+};
+Vectors vectors(const int64_t st[3], int64_t T, int64_t H, int64_t width) {
+    Vectors v;
+    const bool token_first = st[1] >= st[2];
+    v.step[0] = st[token_first ? 1 : 2], v.step[1] = st[token_first ? 2 : 1];
+    v.reach[2] = width;
+    v.reach[1] = width + ((token_first ? H : T) - 1) * v.step[1];
+    v.reach[0] = v.reach[1] + ((token_first ? T : H) - 1) * v.step[0];
+    return v;
+}
+
+// Whether a's vectors, from axis i on, and b's, from axis j on and `at` bytes further, share no byte.  Of the larger step
+// both are taken to repeat endlessly (or stand once); what they repeat fits into a step, so that only two of b's
+// places can meet one of a's.  False where that does not decide it.
+bool apart(const Vectors &a, int i, const Vectors &b, int j, int64_t at) {
+    if (at >= a.reach[i] || at + b.reach[j] <= 0) return true;
+    const int64_t step = std::max(a.step[i], b.step[j]);
+    if (step == 0) return false;
+    i += a.step[i] == step, j += b.step[j] == step;
+    if (a.reach[i] > step || b.reach[j] > step) return false;
+    const int64_t d = (at % step + step) % step;
+    return apart(a, i, b, j, d) && apart(a, i, b, j, d - step);
+}
+
 // Checks one tensor of B x T x H head vectors of D elements of `es` bytes; gives its extent and its strides in bytes
 // (0 for axes of size 1).  out: its elements must be distinct.  max_token: bound of the token stride in bytes.
 rm_status check_heads(const char *name, const rm_heads *t, int64_t B, int64_t T, int64_t H, int D, size_t es, bool out,
@@ -258,12 +286,18 @@ RM_EXPORT rm_status rm_qk_norm_rope(int32_t n_tok, int32_t n_q_heads, int32_t n_
     const size_t n4 = static_cast<size_t>(n_tok) * 4, g4 = static_cast<size_t>(head_dim) * 4;
     const Extent in[8] = {x[0], x[1], x[2], {pos, n4}, {slot, slot ? n4 : 0},
                           {inv_freq, static_cast<size_t>(rot) * 2}, {gain_q, gain_q ? g4 : 0}, {gain_k, gain_k ? g4 : 0}};
-    for (int o = 3; o < 6; ++o) {
+    const int64_t width = static_cast<int64_t>(head_dim) * static_cast<int64_t>(oe);
+    const Vectors out[3] = {vectors(st[3], n_tok, n_q_heads, width), vectors(st[4], rows, n_kv_heads, width),
+                            vectors(st[5], rows, n_kv_heads, width)};
+    for (int o = 3; o < 6; ++o)
+        for (int p = o + 1; p < 6; ++p)
+            if (overlap(x[o], x[p]) && !apart(out[o - 3], 0, out[p - 3], 0,
+                                              static_cast<int64_t>(reinterpret_cast<uintptr_t>(x[p].p) -
+                                                                   reinterpret_cast<uintptr_t>(x[o].p))))
+                return api_fail(RM_ERR_INVALID_ARG, "the outputs overlap each other");
+    for (int o = 3; o < 6; ++o)
         for (const Extent &i : in)
             if (overlap(i, x[o])) return api_fail(RM_ERR_INVALID_ARG, "an output overlaps an input");
-        for (int p = o + 1; p < 6; ++p)
-            if (overlap(x[o], x[p])) return api_fail(RM_ERR_INVALID_ARG, "the outputs overlap each other");
-    }
     rm::RopeArgs a;
     a.q = static_cast<const char *>(q->data);
     a.k = static_cast<const char *>(k->data);

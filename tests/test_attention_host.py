@@ -203,3 +203,64 @@ def test_softcaps_that_float32_does_not_hold(lib, scale, cap, ok):
         assert lib.rm_prefix_attention_workspace_size(s, 1, 1, 4, 64, 4, ctypes.byref(n)) == want
         if not ok:
             assert _span(lib, shape=(8, 2, 64, dtype, scale, cap), out=H(4 * MB, 4096, 1024, 128)) == want
+
+
+@pytest.mark.parametrize("N,qo,ko,vo,ok", [
+    # rows of one buffer, 4 + 2 + 2 heads of 128 bytes: q_out, k_out, v_out side by side
+    (9, (0, 512, 64), (512, 512, 64), (768, 512, 64), True),
+    (9, (0, 512, 64), (384, 512, 64), (768, 512, 64), False),          # the keys begin in the queries' last head
+    (9, (0, 512, 64), (512, 512, 64), (640, 512, 64), False),          # the values in the keys' second head
+    (9, (0, 512, 64), (512, 512, 64), (896, 512, 64), False),          # the values' second head in the next row's queries
+    (9, (0, 512, 64), (512 + 1024, 512, 64), (768 + 2048, 512, 64), True),  # keys a row further, values two
+    (9, (0, 512, 64), (512, 448, 64), (768, 512, 64), False),          # another step
+    (1, (0, 512, 64), (512, 512, 64), (768, 512, 64), True),           # one token
+    # caches beside the queries' own buffer: keys beside values in a row, in a head, and by heads
+    (9, (8 * MB, 256, 64), (0, 256, 64), (256, 256, 64), True),
+    (9, (8 * MB, 256, 64), (0, 256, 128), (128, 256, 128), True),
+    (9, (8 * MB, 256, 64), (0, 64, 2 * 9 * 64), (9 * 128, 64, 2 * 9 * 64), True),
+    (9, (8 * MB, 256, 64), (0, 64, 2 * 9 * 64), (8 * 128, 64, 2 * 9 * 64), False),
+    (9, (8 * MB, 256, 64), (0, 256, 128), (0, 256, 128), False),       # the same
+    (9, (8 * MB, 256, 64), (0, 256, 128), (64, 256, 128), False),      # half a vector into each other
+    (9, (8 * MB, 256, 64), (256, 256, 128), (0, 256, 128), False),     # the same, a row apart
+])
+def test_outputs_in_one_buffer(lib, N, qo, ko, vo, ok):
+    """Distinct elements are told from shared ones before the pointers meet the inputs: pos lies in q_out, so that no
+    call reaches the GPU."""
+    at = 64 * MB
+    heads = [H(at + o, 0, t, h) for o, t, h in (qo, ko, vo)]
+    status = _rope(lib, N=N, rows=9, qo=heads[0], ko=heads[1], vo=heads[2], slot=None, pos=at + qo[0])
+    assert status == rm.RM_ERR_INVALID_ARG
+    assert rm.last_error() == ("an output overlaps an input" if ok else "the outputs overlap each other")
+
+
+def test_outputs_in_one_buffer_against_their_bytes(lib):
+    """Random layouts: every one that is taken has no byte in two outputs."""
+    import random
+
+    r = random.Random(5)
+    taken = 0
+    for _ in range(3000):
+        N, Hq, Hk, D = r.randint(1, 4), r.choice((2, 4)), r.choice((1, 2)), 8
+        rows = N + r.randint(0, 2)
+        def axes(n, h):  # noqa: E306
+            t, s = r.choice([(8 * h * r.randint(1, 3), 8), (8, 8 * n * r.randint(1, 3)), (16 * h, 16), (64, 8), (64, 16)])
+            return t, s
+        steps = [axes(N, Hq), axes(rows, Hk)]
+        steps.append(steps[1] if r.random() < 0.7 else axes(rows, Hk))
+        if r.random() < 0.3:
+            steps = [(64, 8)] * 3
+        at = [16 * r.randint(0, 20) for _ in range(3)]
+        def covered(at, t, s, n, h):  # noqa: E306
+            return [at + (i * t + j * s) * 2 + c for i in range(n) for j in range(h) for c in range(2 * D)]
+        cells = [covered(at[i], *steps[i], (N, rows, rows)[i], (Hq, Hk, Hk)[i]) for i in range(3)]
+        if any(len(set(c)) != len(c) for c in cells):
+            continue
+        shared = len(set().union(*cells)) != sum(len(c) for c in cells)
+        heads = [H(64 * MB + at[i], 0, *steps[i]) for i in range(3)]
+        assert _rope(lib, N=N, Hq=Hq, Hk=Hk, D=D, rot=8, rows=rows, q=H(MB, 0, 64, 8), k=H(2 * MB, 0, 64, 8),
+                     v=H(3 * MB, 0, 64, 8), qo=heads[0], ko=heads[1], vo=heads[2], slot=None,
+                     pos=64 * MB + at[0]) != rm.RM_OK
+        if rm.last_error() == "an output overlaps an input":
+            assert not shared
+            taken += 1
+    assert taken > 300

@@ -607,6 +607,42 @@ def test_rope_without_values_slots_and_norm_of_zeros(dst):
     assert bool((ko[33:] == 9.0).all())
 
 
+@pytest.mark.parametrize("dst", [BF, F32])
+@pytest.mark.parametrize("N", [1, 5, 700])
+@pytest.mark.parametrize("D", [64, 72])
+def test_rope_into_one_buffer(dst, N, D):
+    """Keys beside values in a cache's rows, heads and head-major planes, and all three in packed rows: the same bits as
+    in tensors of their own, and nothing else written."""
+    g = gen(42, N, D)
+    Hq, Hk, rows = 6, 2, N + 3
+    qkv = randn(g, (N, Hq + 2 * Hk, D), BF)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:]
+    pos = torch.randint(0, 5000, (N,), generator=g, dtype=torch.int32).cuda()
+    slot = torch.randperm(rows, generator=g)[:N].to(torch.int32).cuda()
+    freq, gain = torch.linspace(1, 0.001, D // 2, device="cuda"), randn(g, (D,), F32)
+
+    def run(qo, ko, vo, at):
+        for t in (qo, ko, vo):
+            t.fill_(3.0)
+        rm.rm_qk_norm_rope(q, k, v, qo, ko, vo, pos, freq, gain, gain, at)
+
+    def new(*shape):
+        return torch.full(shape, 7.0, dtype=dst, device="cuda")
+
+    want = [new(N, Hq, D), new(rows, Hk, D), new(rows, Hk, D)]
+    run(*want, slot)
+    by_row, by_head, planes = new(rows, 2, Hk, D), new(rows, Hk, 2, D), new(Hk, 2, rows, D)
+    for got in ([new(N, Hq, D), by_row[:, 0], by_row[:, 1]], [new(N, Hq, D), by_head[:, :, 0], by_head[:, :, 1]],
+                [new(N, Hq, D), planes[:, 0].transpose(0, 1), planes[:, 1].transpose(0, 1)]):
+        run(*got, slot)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    own = [new(N, Hq, D), new(N, Hk, D), new(N, Hk, D)]
+    run(*own, None)
+    packed = new(N, Hq + 2 * Hk + 1, D)
+    run(packed[:, :Hq], packed[:, Hq:Hq + Hk], packed[:, Hq + Hk:-1], None)
+    assert torch.equal(packed[:, :-1], torch.cat(own, 1)) and bool((packed[:, -1] == 7.0).all())
+
+
 # ---------------------------------------------------------------------------------------------- together
 
 def test_layer_of_an_observation_and_its_samples_in_a_graph():
