@@ -340,7 +340,7 @@ typedef struct rm_attn_shape {
  *             value; NULL: row n (rows >= n_tok).  Slots are distinct: tokens that share one leave an unspecified
  *             mix of theirs in it.  Other rows keep what they hold.
  * head_dim a multiple of 8, at most 256; rot a multiple of 4 in [0, head_dim].  Angles are reduced in 64 bits,
- * everything else is float32.  0 <= n_tok < 2^26, n_tok x heads < 2^30.
+ * everything else is float32.  0 <= n_tok <= 2^26 - 4, n_tok x heads < 2^30.
  * Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN. */
 rm_status rm_qk_norm_rope(int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t in_dtype,
                           int32_t out_dtype, const rm_heads *q, const rm_heads *k, const rm_heads *v,

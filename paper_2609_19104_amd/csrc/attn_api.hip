@@ -265,7 +265,7 @@ RM_EXPORT rm_status rm_qk_norm_rope(int32_t n_tok, int32_t n_q_heads, int32_t n_
         return api_fail(RM_ERR_SHAPE, "rows=%d hold fewer than the n_tok=%d tokens (no slots given)", rows, n_tok);
     const bool values = v != nullptr && v->data != nullptr;
     const int64_t heads = static_cast<int64_t>(n_q_heads) + n_kv_heads * (values ? 2LL : 1LL);
-    if (heads > 65535 || n_tok * heads >= (1LL << 30) || n_tok >= 4 * kMaxGroups)
+    if (heads > 65535 || n_tok * heads >= (1LL << 30) || ceil_div(n_tok, 4) >= kMaxGroups)
         return api_fail(RM_ERR_SHAPE, "n_tok x heads = %d x %lld is too large", n_tok, static_cast<long long>(heads));
     const size_t ie = elem(in_dtype), oe = elem(out_dtype);
     Extent x[6];

@@ -264,3 +264,12 @@ def test_outputs_in_one_buffer_against_their_bytes(lib):
             assert not shared
             taken += 1
     assert taken > 300
+
+
+def test_most_tokens(lib):
+    """A wave a token and four waves a workgroup: below 2^24 workgroups, 2^32 threads.  The tokens that are taken get as
+    far as the overlap of q_out with q, 1 MB behind it."""
+    most = (1 << 26) - 4
+    for n in (most, most + 1, most + 2, most + 3):
+        want = rm.RM_ERR_INVALID_ARG if n <= most else rm.RM_ERR_SHAPE
+        assert _rope(lib, N=n, rows=n, Hq=2, Hk=1, slot=None, qo=H(2 * MB, 0, 256, 64)) == want, n
