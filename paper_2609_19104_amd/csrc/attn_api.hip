@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <numeric>
 
 #include "rm_attn_plan.h"
 #include "rm_rope.h"
@@ -174,7 +175,12 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     // bf16 (rows of 64, 128 and 256 columns), 2.3, 4.1 and 14 in float32, 2.4 times that for 128 rows; the join 5 and
     // its traffic at 4 TB/s (one action chunk's 408 rows on 901 keys, D = 256: 20.2 us undivided, 14.2 in 8 slices;
     // 6528 rows 24.4 undivided, 38.7 in 2).
-    const int64_t tiles = ceil_div(n0, 128) + ceil_div(n1, 128);
+    // A row block walks the own keys of every sample it has rows of, (t + r - gcd(t, r)) / t of them on average for r
+    // rows and t to a sample (32 single tokens of 8 heads on 8, 128 shared and 256 own keys: 65 tiles; one sample's
+    // counted for all of them, 3, the call took 91 us undivided, 23 in slices).
+    const int64_t t = static_cast<int64_t>(T) * G, own_tiles = ceil_div(n1, 128);
+    const int64_t tiles =
+        ceil_div(n0, 128) + std::min(per * own_tiles, own_tiles * (t + q.rows - std::gcd(t, int64_t{q.rows})) / t);
     const int64_t slots = kCUs * (q.dh * (bf ? 1 : 2) <= 128 ? 2 : 1);
     const double tile_us =
         (bf ? 0.65 + q.dh / 256.0 : q.dh == 256 ? 14.0 : 0.5 + q.dh / 36.0) * (key_waves ? 1.0 : 2.4);

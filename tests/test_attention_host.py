@@ -273,3 +273,19 @@ def test_most_tokens(lib):
     for n in (most, most + 1, most + 2, most + 3):
         want = rm.RM_ERR_INVALID_ARG if n <= most else rm.RM_ERR_SHAPE
         assert _rope(lib, N=n, rows=n, Hq=2, Hk=1, slot=None, qo=H(2 * MB, 0, 256, 64)) == want, n
+
+
+@pytest.mark.parametrize("Hq,Hk,D,per,T,P,S,slices", [
+    (8, 8, 128, 32, 1, 128, 256, 2),    # 8 workgroups with 32 samples' keys each
+    (4, 1, 128, 16, 1, 256, 512, 2),    # 4 rows a sample, 8 samples a block
+    (8, 8, 64, 32, 1, 0, 512, 2),       # own keys alone
+    (8, 1, 256, 3, 51, 0, 8192, 2),     # blocks that hold the end of one sample and the begin of the next
+    (8, 8, 128, 32, 1, 128, 0, 1),      # one tile
+    (8, 8, 128, 1, 1, 128, 128, 1),
+])
+def test_slices_count_the_own_keys_of_every_sample_of_a_block(lib, Hq, Hk, D, per, T, P, S, slices):
+    n = ctypes.c_size_t(0)
+    s = ctypes.byref(rm.AttnShape(Hq, Hk, D, 1, 0.1, 0.0))
+    assert lib.rm_prefix_attention_workspace_size(s, 1, per, T, P, S, ctypes.byref(n)) == rm.RM_OK
+    one = per * T * Hq * (D * 4 + 8)
+    assert n.value >= slices * one if slices > 1 else n.value == 0

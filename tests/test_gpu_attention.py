@@ -459,6 +459,22 @@ def test_row_waves_and_slices(D, per, causal):
         check_span(q[b:b + 1, ::37, h:h + 1], k[b:b + 1], v[b:b + 1], span[b:b + 1, ::37], out=out[b:b + 1, ::37, h:h + 1])
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("G,per,T,P,S,Hq,Hk,D", [
+    (1, 32, 1, 128, 256, 8, 8, 128), (1, 32, 1, 0, 300, 8, 8, 64), (2, 16, 1, 200, 512, 4, 1, 128), (1, 40, 2, 33, 400, 6, 2, 72),
+    (1, 3, 51, 100, 1500, 8, 1, 256),
+])
+def test_slices_of_many_samples(dtype, G, per, T, P, S, Hq, Hk, D):
+    """Workgroups that divide the own keys of a row block's many samples; every other sample has few, some none."""
+    g = gen(28, per, T, P, S, D)
+    args = make_prefix(g, G, per, T, P, S, Hq, Hk, D, dtype)
+    assert rm.prefix_attention_workspace(args[0], args[1], args[3]).numel() > 0
+    olen = torch.randint(0, S + 1, (G * per,), generator=g, dtype=torch.int32)
+    olen[1::2] = torch.randint(0, 9, olen[1::2].shape, generator=g, dtype=torch.int32)
+    check_prefix(args, None, olen.cuda(), True)
+    check_prefix(args, ints([P // 2] * G), olen.cuda())
+
+
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("T,B,N", [(5, 2, 70000), (12, 2, 70000), (5, 200, 130)])
 def test_blocks_that_are_not_full(D, T, B, N):
