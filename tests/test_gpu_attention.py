@@ -526,6 +526,117 @@ def test_one_samples_nan_stays_its_own(dtype, T):
     assert bool(got[2].isnan().all()) and bool((got[7] == float("inf")).all())
 
 
+def poisoned(v, keys):
+    """v with NaN, infinities or both signs of them in five columns of the listed keys ([(sample, key)]), and per column
+    what a row that sees the key gets."""
+    D = v.shape[-1]
+    out = v.clone()
+    marks = {c: torch.zeros(v.shape[:2] + (3,), dtype=torch.bool) for c in (0, 1, 2, 3, D - 1)}  # NaN, +, - of each key
+    for n, (b, j) in enumerate(keys):
+        for c, kind in ((0, 0), (1, 1), (2, 2), (3, 1 + n % 2), (D - 1, n % 3)):
+            out[b, j, :, c] = (float("nan"), float("inf"), -float("inf"))[kind]
+            marks[c][b, j, kind] = True
+    return out, marks
+
+
+def check_poisoned(got, want, seen, marks):
+    """got, want [B][T][H][D], seen [B][T][N] on the host: columns of rows that see marked keys get their infinity or
+    NaN, everything else its bits."""
+    got, want = got.cpu(), want.cpu()
+    for c in range(got.shape[-1]):
+        if c not in marks:
+            assert torch.equal(got[..., c], want[..., c]), c
+            continue
+        hit = torch.einsum("btn,bnk->btk", seen.float(), marks[c].float()) > 0
+        nan = hit[..., 0] | (hit[..., 1] & hit[..., 2])
+        kinds = ((nan, "nan"), (hit[..., 1] & ~nan, "inf"), (hit[..., 2] & ~nan, "-inf"), (~hit.any(-1), None))
+        for rows, value in kinds:
+            x = got[..., c][rows]
+            if value is None:
+                assert torch.equal(x, want[..., c][rows]), c
+            else:
+                assert bool(x.isnan().all() if value == "nan" else (x == float(value)).all()), (c, value)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [8, 64, 72, 128, 136, 200, 256])
+@pytest.mark.parametrize("T,N", [(20, 5000), (3, 3001), (20, 150)])
+def test_unseen_values_in_slices(dtype, D, T, N):
+    """Infinities and NaN among the values of a few keys of many tiles, which some rows of a block see and others not:
+    in whole calls (N = 150 up to 128 columns) and in those whose keys many workgroups divide."""
+    g = gen(16, D, T, N)
+    B, Hq, Hk = 2, 4, 2
+    q, k, v = randn(g, (B, T, Hq, D), dtype), randn(g, (B, N, Hk, D), dtype), randn(g, (B, N, Hk, D), dtype)
+    lo = torch.randint(0, N, (B, T), generator=g)
+    hi = lo + torch.where(torch.rand((B, T), generator=g) < 0.5, torch.randint(0, 60, (B, T), generator=g),
+                          torch.randint(0, N, (B, T), generator=g))
+    span = torch.stack([lo, hi.clamp(max=N)], -1).to(torch.int32)
+    span[0, 1] = 0
+    assert N < 1000 or rm.span_attention_workspace(q, k).numel() > 0
+    j = torch.arange(N)
+    seen = (j >= span[..., :1]) & (j < span[..., 1:])
+    want = run_span(q, k, v, span.cuda())
+    step = 131 if N > 1000 else 40
+    v2, marks = poisoned(v, [(b, i) for b in range(B) for i in range(5 + 7 * b, N, step)])
+    got = run_span(q, k, v2, span.cuda())
+    check_poisoned(got, want, seen, marks)
+    graph = torch.cuda.CUDAGraph()
+    out, ws, sp = torch.empty_like(q), rm.span_attention_workspace(q, k), span.cuda()
+    rm.rm_span_attention(q, k, v2, out, ws, span=sp)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        rm.rm_span_attention(q, k, v2, out, ws, span=sp)
+    for _ in range(3):
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16 if dtype == BF else torch.int32),
+                           got.view(torch.int16 if dtype == BF else torch.int32))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 72, 128, 256])
+@pytest.mark.parametrize("G,per,T,P,S,Hq,Hk", [(1, 6, 2, 3000, 400, 4, 1), (2, 5, 3, 40, 700, 8, 2), (1, 40, 1, 0, 300, 2, 1)])
+def test_own_keys_infinite_values_in_slices(dtype, D, G, per, T, P, S, Hq, Hk):
+    """The same among the samples' own keys and in the shared ones, with lengths that hide some of them."""
+    g = gen(17, D, per, P, S)
+    q, kp, vp, ko, vo = make_prefix(g, G, per, T, P, S, Hq, Hk, D, dtype)
+    q = q * 0.5
+    assert rm.prefix_attention_workspace(q, kp, ko).numel() > 0
+    olen = torch.randint(0, S + 1, (G * per,), generator=g, dtype=torch.int32)
+    olen[0], olen[1] = S, 0
+    plen = torch.tensor([P - P // 3, P // 2][:G], dtype=torch.int32)
+    want = run_prefix(q, kp, vp, ko, vo, plen.cuda(), olen.cuda(), True)
+    own_bad = [(b, i) for b in range(0, G * per, 2) for i in range(3 + b % 5, S, 77)]
+    vo2, marks = poisoned(vo, own_bad)
+    j = torch.arange(S)
+    seen = (j < olen[:, None, None]) & (j <= (olen[:, None, None] - T + torch.arange(T)[:, None]))
+    check_poisoned(run_prefix(q, kp, vp, ko, vo2, plen.cuda(), olen.cuda(), True), want, seen, marks)
+    if P > 0:
+        vp2, marks = poisoned(vp, [(u, i) for u in range(G) for i in range(int(plen[u]) - 200 * (u + G - 2), P, 150)
+                                   if i >= 0])
+        sees = (torch.arange(P) < plen[:, None]).repeat_interleave(per, 0)[:, None].expand(G * per, T, P)
+        marks = {c: m.repeat_interleave(per, 0) for c, m in marks.items()}
+        check_poisoned(run_prefix(q, kp, vp2, ko, vo, plen.cuda(), olen.cuda(), True), want, sees, marks)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128, 200, 256])
+def test_row_waves_infinite_values_in_slices(D):
+    """And where four waves divide 128 rows and two workgroups or more a block's keys."""
+    g = gen(18, D)
+    B, T, N, Hq, Hk = 2, 512, 20000, 8, 1
+    q, k, v = randn(g, (B, T, Hq, D), BF), randn(g, (B, N, Hk, D), BF), randn(g, (B, N, Hk, D), BF)
+    assert rm.span_attention_workspace(q, k).numel() > 0
+    span = torch.zeros((B, T, 2), dtype=torch.int32)
+    span[..., 1] = torch.randint(0, N + 1, (B, T), generator=g, dtype=torch.int32)
+    span[0, :, 0] = torch.randint(0, N, (T,), generator=g, dtype=torch.int32)
+    j = torch.arange(N)
+    seen = (j >= span[..., :1]) & (j < span[..., 1:])
+    want = run_span(q, k, v, span.cuda())
+    v2, marks = poisoned(v, [(0, i) for i in range(7, N, 4099)] + [(1, 9000), (1, 17777)])
+    check_poisoned(run_span(q, k, v2, span.cuda()), want, seen, marks)
+
+
 # ---------------------------------------------------------------------------------------------- spans
 
 @pytest.mark.parametrize("B,T,N", [(1, 1, 1), (2, 7, 7), (3, 300, 300), (2, 5, 260), (2, 600, 5000)])
