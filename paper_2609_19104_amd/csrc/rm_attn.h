@@ -105,13 +105,16 @@ __device__ __forceinline__ int wave_max(int v) {
 }
 __device__ __forceinline__ int wave_min(int v) { return -wave_max(-v); }  // (no value here is INT_MIN)
 
-// Whether any of the values packed in v is infinite or NaN (all exponent bits set): the carry out of the exponent
-// field reaches the sign bit.
-__device__ __forceinline__ uint32_t nonfinite_bf16x2(uint32_t v) {
-    return ((v & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-}
-__device__ __forceinline__ uint32_t nonfinite_f32(float v) {
-    return ((__float_as_uint(v) & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+// A value's bits in the passes over a block whose results are not finite: in kClean infinities and NaN are 0, in kPlus
+// (kMinus) those that add +infinity (-infinity), an infinity of that sign or NaN, are 1 and all others 0.
+enum : int { kFirst = 0, kClean = 1, kPlus = 2, kMinus = 3 };
+template <bool BF>
+__device__ __forceinline__ uint32_t marked(uint32_t v, int mode) {
+    constexpr uint32_t EXP = BF ? 0x7f80u : 0x7f800000u, ONE = BF ? 0x3f80u : 0x3f800000u;
+    constexpr uint32_t SIGN = BF ? 0x8000u : 0x80000000u;
+    const bool bad = (v & EXP) == EXP, nan = (v & ~SIGN) > EXP;
+    if (mode == kClean) return bad ? 0u : v;
+    return bad && (nan || ((v & SIGN) != 0) == (mode == kMinus)) ? ONE : 0u;
 }
 
 // A fragment of V^T (32 columns x 16 keys) from rows of V in LDS: two transposing reads of 4 keys x 16 columns per 16
@@ -445,16 +448,22 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     // ---------------------------------------------------------------- tiles
     // One pass over the slice's tiles, the first one's loads under way.  Returns whether a tile had keys that some rows
     // see and others do not.  There 0 times an infinity or NaN may spoil the rows that do not see it, and a sum keeps
-    // the NaN: a workgroup whose results then hold any (there is hardly ever one) makes a second pass with `clean`,
-    // which sets the infinities and NaN among the values to 0 in LDS, the other sums staying as they are bit for bit,
-    // and then adds them to the rows that see them.
-    auto pass = [&](const bool clean) __attribute__((always_inline)) -> bool {
+    // the NaN: a workgroup whose results then hold any (there is hardly ever one) makes three more passes.  kClean sets
+    // the infinities and NaN among the values to 0 in LDS, the other sums staying as they are bit for bit; kPlus and
+    // kMinus count, with weights of 1, the ones of either sign that a row sees, which are then added to its results.
+    // So the values' contents bound the time: a call whose values are NaN throughout takes 5 to 12 times the usual (4096
+    // causal rows of 16 heads of 128 109 -> 811 us, 850 rows of 256 columns 20 -> 237).
+    auto pass = [&](const auto mode) __attribute__((always_inline)) -> bool {
         bool some = false;  // some tile had keys that not all rows see
         m = -INFINITY;
         l = 0.0f;
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] = rm_f32x16{};
         int buf = 0;
+        // Queries and scalars are waited for here: the compiler would do so in front of their first use, in the loop, and
+        // there on every tile for the tile's loads and LDS reads as well (256 single tokens on 1024 shared and 256 own
+        // keys 56 -> 67 us, 850 rows on 850 keys 20.4 -> 20.9).
+        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
         for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
             Tile nxt = cur;
             const bool more = n_left > 1;
@@ -465,7 +474,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             sync(std::conditional_t<NBUF == 2, Others, None>{});  // the keys
 
             const int kbw = cur.kb + kw * KPW;
-            bool mixed = kbw + KPW > cur.end;  // keys that not all rows see
+            bool mixed = kbw + KPW > cur.end || mode >= kPlus;  // keys that not all rows see
             if (cur.seg >= 0)
                 mixed = mixed || cur.seg != w_s0 || cur.seg != w_s1 || kbw < w_maxlo || kbw + KPW > w_minhi;
 
@@ -549,6 +558,12 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                                 ? s[ns][i]
                                 : -INFINITY;
                 }
+                if (__builtin_expect(mode >= kPlus, false)) {  // (sc 0 + off: a weight of 1)
+#pragma unroll
+                    for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[ns][i] = s[ns][i] == -INFINITY ? -INFINITY : 0.0f;
+                }
             }
             float part[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
 #pragma unroll
@@ -593,18 +608,13 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             if (more) sync(Others{});  // the values
             else sync(None{});
-            if (clean) {
+            if (__builtin_expect(mode != kFirst, false)) {
                 for (int i = rw * 64 + lane; i < TILEB / 16; i += 64 * RW) {
                     rm_u32x4 *p = reinterpret_cast<rm_u32x4 *>(lds_w + TILEB + at) + i;
                     rm_u32x4 v = *p;
-                    for (int e = 0; e < 4; ++e) {
-                        if constexpr (BF) {
-                            const uint32_t bad = nonfinite_bf16x2(v[e]);
-                            v[e] &= (bad & 0x8000u ? 0u : 0xffffu) | (bad >> 31 ? 0u : 0xffff0000u);
-                        } else {
-                            v[e] = nonfinite_f32(__uint_as_float(v[e])) ? 0u : v[e];
-                        }
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        v[e] = BF ? marked<BF>(v[e] & 0xffffu, mode) | marked<BF>(v[e] >> 16, mode) << 16
+                                  : marked<BF>(v[e], mode);
                     *p = v;
                 }
                 sync(Any{});
@@ -659,45 +669,10 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         }
         return some;
     };
-    // The queries are waited for here: the compiler would do so in front of their first use, in the loop, and there on
-    // every tile for the tile's loads as well (256 single tokens on 1024 shared and 256 own keys 56 -> 67 us).
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-    for (bool clean = false;; clean = true) {
-        bool some = pass(clean);
-        if (__builtin_expect(clean, false)) {  // the infinities and NaN that the second pass left out
-            first_tile(cur);
-            for (int64_t n_left = n_tiles; n_left > 0; --n_left) {
-                const int k0 = cur.kb + kw * KPW, k1 = min(k0 + KPW, cur.end);
-                for (int k = k0; k < k1; ++k) {
-                    const char *values = cur.v + (k - cur.kb) * cur.vn;
-                    for (int c0 = 0; c0 < a.D; c0 += 64) {
-                        float x = 0.0f;
-                        if (c0 + lane < a.D) {
-                            if constexpr (BF)
-                                x = rm_bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(values)[c0 + lane]);
-                            else
-                                x = reinterpret_cast<const float *>(values)[c0 + lane];
-                        }
-                        for (uint64_t bad = __ballot(!(fabsf(x) < INFINITY)); bad != 0; bad &= bad - 1) {
-                            const int from = __ffsll(static_cast<unsigned long long>(bad)) - 1;
-                            const float add = __shfl(x, from);
-                            const bool in =
-                                static_cast<uint32_t>(k - r_lo) < static_cast<uint32_t>(r_len);
-                            const bool sees = cur.seg < 0 || (r_smp == cur.seg && in);
-                            const int at = sees ? c0 + from - 4 * hi : -1;
-#pragma unroll
-                            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i)
-                                    o[d][i] += at == 32 * d + 8 * (i >> 2) + (i & 3) ? add : 0.0f;
-                        }
-                    }
-                }
-                if (n_left > 1) advance(cur);
-            }
-        }
 
-        // ---------------------------------------------------------------- join and write
+    // ---------------------------------------------------------------- join and write
+    // Returns whether another pass is needed.
+    auto write = [&](const auto mode, const bool some) __attribute__((always_inline)) -> bool {
         // Of the blocks of 32 columns, wave kw joins those with number kw modulo KW: it has its own sums, the others'
         // come through LDS.
         float *join = reinterpret_cast<float *>(lds);
@@ -708,6 +683,43 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         auto quad = [&](int d, int i) {
             return rm_f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
         };
+        auto partial_row = [&](int r) { return (static_cast<int64_t>(split) * a.U * a.Hk + ng) * a.R + r; };
+        auto out_row = [&](int t) {
+            return a.o + (static_cast<int64_t>(u) * a.per + r_smp) * a.o_b + t * a.o_t + r_head * a.o_h;
+        };
+        if (__builtin_expect(mode >= kPlus, false)) {
+            // The counts of all key waves, by way of LDS, to the results of the passes before, which this workgroup wrote
+            // before the barrier between them.
+            static_assert(LDSB >= W * 32 * DC * 4, "room for the counts");
+            __syncthreads();  // every wave has read its last tile
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *slot(wave, d, i) = quad(d, i);
+            __syncthreads();
+            const int64_t prow = partial_row(row);
+            char *orow = out_row(r_tok);
+            const float add = mode == kPlus ? INFINITY : -INFINITY;
+#pragma unroll 1
+            for (int d = kw; d < DB; d += KW)
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    const int c = 32 * d + 8 * i + 4 * hi;
+                    if (row >= a.R || c >= a.D) continue;
+                    rm_f32x4 n = {0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int k = 0; k < KW; ++k) n += *slot(k * RW + rw, d, i);
+                    auto added = [&](auto *p) {
+                        auto x = *p;
+                        for (int e = 0; e < 4; ++e) x[e] = n[e] == 0.0f ? x[e] : x[e] + add;
+                        *p = x;
+                    };
+                    if (a.splits > 1) added(reinterpret_cast<rm_f32x4 *>(a.part_o + prow * a.D + c));
+                    else if constexpr (BF) added(reinterpret_cast<rm_bf16x4 *>(orow + c * 2));
+                    else added(reinterpret_cast<rm_f32x4 *>(orow + c * 4));
+                }
+            __syncthreads();
+            return mode == kPlus;
+        }
         if constexpr (KW > 1) {
             __syncthreads();  // every wave has read its last tile
             const float sum = xor32_sum(l);
@@ -740,14 +752,13 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         } else {
             sum = xor32_sum(l);
         }
+        const int64_t prow = partial_row(row);
+        char *orow = out_row(r_tok);
         const float inv = a.splits > 1 ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
-        const int64_t prow = (static_cast<int64_t>(split) * a.U * a.Hk + ng) * a.R + row;
         if (a.splits > 1 && row < a.R && hi == 0 && kw == 0) {
             a.part_ml[2 * prow] = top;
             a.part_ml[2 * prow + 1] = sum;
         }
-        char *orow = a.o + (static_cast<int64_t>(u) * a.per + r_smp) * a.o_b + r_tok * a.o_t +
-                     r_head * a.o_h;
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
             if (KW > 1 && d % KW != kw) continue;
@@ -793,10 +804,18 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                 }
             }
         }
-        if (clean) break;
-        if (!__builtin_amdgcn_readfirstlane(__syncthreads_or(some && !(nan == 0.0f)))) break;
+        return __builtin_amdgcn_readfirstlane(__syncthreads_or(mode == kClean || (some && !(nan == 0.0f)))) != 0;
+    };
+    const std::integral_constant<int, kFirst> first;
+    if (__builtin_expect(!write(first, pass(first)), true)) return;
+    // A second copy of the code above: one copy for all passes costs the usual one up to 4 % (517 rows in float32 15.1 ->
+    // 15.7 us, two copies 14.6).
+#pragma unroll 1
+    for (int mode = kClean;; ++mode) {
         first_tile(cur);
         start();
+        pass(mode);
+        if (!write(mode, false)) break;
     }
 }
 

@@ -637,6 +637,32 @@ def test_row_waves_infinite_values_in_slices(D):
     check_poisoned(run_span(q, k, v2, span.cuda()), want, seen, marks)
 
 
+@pytest.mark.parametrize("dtype,T,D", [(BF, 2048, 128), (BF, 850, 256), (F32, 1024, 64)])
+def test_time_with_nan_values(dtype, T, D):
+    """Values that are NaN throughout take a bounded number of passes: 5 to 12 times the usual time measured, a key at a
+    time it was thousands."""
+    g = gen(19, T, D)
+    q, k, v = randn(g, (1, T, 8, D), dtype), randn(g, (1, T, 2, D), dtype), randn(g, (1, T, 2, D), dtype)
+    span = torch.empty((1, T, 2), dtype=torch.int32, device="cuda")
+    rm.rm_attn_spans(span, T)
+    out, ws = torch.empty_like(q), rm.span_attention_workspace(q, k)
+
+    def ms(values):
+        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        for i in range(6):
+            if i == 1:
+                begin.record()
+            rm.rm_span_attention(q, k, values, out, ws, span=span)
+        end.record()
+        torch.cuda.synchronize()
+        return begin.elapsed_time(end)
+
+    usual = ms(v)
+    slow = ms(torch.full_like(v, float("nan")))
+    assert bool(out.isnan().all())
+    assert slow < 100 * usual
+
+
 # ---------------------------------------------------------------------------------------------- spans
 
 @pytest.mark.parametrize("B,T,N", [(1, 1, 1), (2, 7, 7), (3, 300, 300), (2, 5, 260), (2, 600, 5000)])
