@@ -47,3 +47,25 @@ def test_action_layer_bytes():
     assert bench.active_weight_bytes(1229, 1024, 2) == 3 * 1229 * 1024 * 2 == 7_550_976
     assert bench.gateup_bytes(1229, 1024, 2) == 2 * bench.down_bytes(1229, 1024, 2)
     assert bench.active_weight_bytes(4096, 1024, 2) == 3 * bench.matrix_bytes(1024, 4096, 2)
+
+
+def test_digest_follows_the_counted_kernels_sources_only(tmp_path, monkeypatch):
+    """An edit of the attention side's files, or of comments, leaves the counted traffic valid; one of any other file of
+    code does not.  No other file includes the attention side's headers."""
+    import re
+    import shutil
+
+    csrc = tmp_path / "csrc"
+    shutil.copytree(bench.CSRC, csrc)
+    monkeypatch.setattr(bench, "CSRC", str(csrc))
+    digest = bench.kernel_source_digest()
+    for f in sorted(csrc.iterdir()):
+        text = f.read_text()
+        f.write_text(text + "\n// a comment\n")
+        assert bench.kernel_source_digest() == digest, f.name
+        f.write_text(text + "\nstatic int another;\n")
+        attention = f.name.startswith(bench.ATTENTION_SOURCES)
+        assert (bench.kernel_source_digest() == digest) == attention, f.name
+        f.write_text(text)
+        included = re.findall(r'#include "([^"]+)"', text)
+        assert attention or not any(i.startswith(bench.ATTENTION_SOURCES) for i in included), f.name
