@@ -671,8 +671,8 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
     };
 
     // ---------------------------------------------------------------- join and write
-    // Returns whether another pass is needed.
-    auto write = [&](const auto mode, const bool some) __attribute__((always_inline)) -> bool {
+    // Returns whether a result is not finite, or after kClean and kPlus that a pass follows: the same in every wave.
+    auto write = [&](const auto mode) __attribute__((always_inline)) -> bool {
         // Of the blocks of 32 columns, wave kw joins those with number kw modulo KW: it has its own sums, the others'
         // come through LDS.
         float *join = reinterpret_cast<float *>(lds);
@@ -804,10 +804,13 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
                 }
             }
         }
-        return __builtin_amdgcn_readfirstlane(__syncthreads_or(mode == kClean || (some && !(nan == 0.0f)))) != 0;
+        return __builtin_amdgcn_readfirstlane(__syncthreads_or(!(nan == 0.0f))) != 0 || mode == kClean;
     };
     const std::integral_constant<int, kFirst> first;
-    if (__builtin_expect(!write(first, pass(first)), true)) return;
+    const bool some = pass(first);
+    if (__builtin_expect(!write(first), true)) return;
+    // Of any wave: the one that joins a column need not be the one whose keys spoiled it.
+    if (!__builtin_amdgcn_readfirstlane(__syncthreads_or(some))) return;
     // A second copy of the code above: one copy for all passes costs the usual one up to 4 % (517 rows in float32 15.1 ->
     // 15.7 us, two copies 14.6).
 #pragma unroll 1
@@ -815,7 +818,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
         first_tile(cur);
         start();
         pass(mode);
-        if (!write(mode, false)) break;
+        if (!write(mode)) break;
     }
 }
 

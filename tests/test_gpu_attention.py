@@ -637,6 +637,45 @@ def test_row_waves_infinite_values_in_slices(D):
     check_poisoned(run_span(q, k, v2, span.cuda()), want, seen, marks)
 
 
+def check_one_column_each(run, v, key, sees):
+    """v [B][N][Hk][D] with an infinity in one column of `key`, another one in every sample (8 b): rows that see the key
+    (sees [T]) get it there, and nothing else changes."""
+    B, D = v.shape[0], v.shape[-1]
+    want = run(v)
+    v2, at = v.clone(), torch.arange(B)
+    v2[at, key, :, 8 * at % D] = float("inf")
+    got = run(v2)
+    expected = want.clone()
+    for b in range(B):
+        expected[b, sees, :, 8 * b % D] = float("inf")
+    assert torch.equal(got, expected)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 72, 128, 200, 256])
+@pytest.mark.parametrize("start,N", [(0, 128), (30, 128), (40, 300), (66, 128), (100, 128), (225, 300), (100, 9000)])
+def test_one_wave_has_the_unseen_key(dtype, D, start, N):
+    """Rows whose keys end inside the 32 of one wave, the other waves' being all seen or all unseen: an infinity there, in
+    each column, which another wave may join."""
+    g = gen(29, D, start, N)
+    B, T, H = D // 8, 20, 2
+    q, k, v = randn(g, (B, T, H, D), dtype), randn(g, (B, N, H, D), dtype), randn(g, (B, N, H, D), dtype)
+    span = torch.empty((B, T, 2), dtype=torch.int32, device="cuda")
+    rm.rm_attn_spans(span, N, q_start=torch.full((B,), start, dtype=torch.int32, device="cuda"))
+    check_one_column_each(lambda x: run_span(q, k, x, span), v, start + T // 2, torch.arange(T) >= T // 2)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 72, 128, 200, 256])
+@pytest.mark.parametrize("P,S", [(128, 128), (0, 100), (300, 65), (4000, 128)])
+def test_one_wave_has_the_unseen_own_key(dtype, D, P, S):
+    g = gen(33, D, P, S)
+    B, T, H = D // 8, 32, 1
+    q, kp, vp, ko, vo = make_prefix(g, 1, B, T, P, S, H, H, D, dtype)
+    q = q * 0.5
+    check_one_column_each(lambda x: run_prefix(q, kp, vp, ko, x, None, None, True), vo, S - 10, torch.arange(T) >= T - 10)
+
+
 @pytest.mark.parametrize("dtype,T,D", [(BF, 2048, 128), (BF, 850, 256), (F32, 1024, 64)])
 def test_time_with_nan_values(dtype, T, D):
     """Values that are NaN throughout take a bounded number of passes: 5 to 12 times the usual time measured, a key at a
