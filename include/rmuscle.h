@@ -362,10 +362,10 @@ rm_status rm_attn_spans(int32_t B, int32_t T, int32_t N, int32_t causal, int32_t
 
 /* Attention of query rows over one interval of their sample's keys each:
  *     s_j = cap(scale * <q[b,i,h], k[b,j,h']>) - slopes[h] * |q_start[b] + i - j|,   lo[b,i] <= j < hi[b,i]
- *     out[b,i,h] = sum_j softmax(s)_j v[b,j,h']            (no key, or no score above -infinity: 0)
- * Keys outside a row's interval do not affect it, whatever they hold (NaN and infinities too).  Rows whose interval
- * ends among infinite or NaN values that others of their block see are computed again, in 5 to 12 times the usual time.
- *   q, out: [B][T][n_q_heads][head_dim]; k, v: [B][N][n_kv_heads][head_dim]; T >= 1, 0 <= N < 2^30.
+ *     out[b,i,h] = sum_j softmax(s)_j v[b,j,h']       (no key, or finite values and no score above -infinity: 0)
+ * Keys outside a row's interval do not affect it, whatever they hold (NaN and infinities too).  Blocks of rows whose
+ * intervals end among infinite or NaN values that some of them see take 5 to 12 times the usual time.
+ *   q, out: [B][T][n_q_heads][head_dim]; k, v: [B][N][n_kv_heads][head_dim]; B, T >= 1, 0 <= N < 2^30.
  *   span:    int32 [B][T][2], 8-byte aligned, clamped to [0, N] (rm_attn_spans makes it), or NULL: every row sees all.
  *   slopes:  float32 [n_q_heads] or NULL: no bias.  q_start: int32 [B] or NULL (0), any value; read with slopes
  *            only.

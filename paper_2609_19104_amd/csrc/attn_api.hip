@@ -152,7 +152,7 @@ rm_status attn_plan(const rm_attn_shape *s, int U, int per, int T, int n0, int n
     // on 8192 keys 39 / 38, on 32768 111 / 89, 64 blocks on 32768 210 / 161; 64 columns, 32 on 8192 28 / 32, on 32768
     // 76 / 66; 256 columns, 8 on 8192 28 / 31, 32 on 8192 66 / 56, on 32768 221 / 156.  (A window that hides most of
     // the keys turns the second, 111 / 89, into 18 / 23: the plan does not know the spans.)
-    // 4 (16) blocks of 96 rows on 131072: 64 columns 56 / 54 (166 / 143), 128 97 / 69 (300 / 208), 256 160 / 110
+    // 4 (16) blocks of 96 rows on 131072: 64 columns 56 / 54 (166 / 143), 128 97 / 76 (300 / 216), 256 160 / 110
     // (545 / 383); of 64 rows: 64 columns 41 / 55 (130 / 141), 128 60 / 67 (240 / 209), 256 119 / 106 (414 / 381).
     auto keys = [&](int64_t r) {  // read by a block of r rows, which may hold rows of several samples
         return n0 + std::min<int64_t>(per, ceil_div(r, static_cast<int64_t>(T) * G)) * n1;
