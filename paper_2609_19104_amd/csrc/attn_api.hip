@@ -275,7 +275,7 @@ RM_EXPORT rm_status rm_qk_norm_rope(int32_t n_tok, int32_t n_q_heads, int32_t n_
         return api_fail(RM_ERR_SHAPE, "n_tok x heads = %d x %lld is too large", n_tok, static_cast<long long>(heads));
     const size_t ie = elem(in_dtype), oe = elem(out_dtype);
     Extent x[6];
-    int64_t st[6][3];
+    int64_t st[6][3] = {};
     rm_status r = check_heads("q", q, 1, n_tok, n_q_heads, head_dim, ie, false, INT64_MAX, &x[0], st[0]);
     if (r == RM_OK) r = check_heads("k", k, 1, n_tok, n_kv_heads, head_dim, ie, false, INT64_MAX, &x[1], st[1]);
     if (r == RM_OK) r = check_heads("q_out", q_out, 1, n_tok, n_q_heads, head_dim, oe, true, INT64_MAX, &x[3], st[3]);
@@ -369,7 +369,7 @@ RM_EXPORT rm_status rm_span_attention(const rm_attn_shape *s, int32_t B, int32_t
     const int D = s->head_dim;
     const size_t es = elem(s->dtype);
     Extent x[4];
-    int64_t st[4][3];
+    int64_t st[4][3] = {};
     r = check_heads("q", q, B, T, s->n_q_heads, D, es, false, INT64_MAX, &x[0], st[0]);
     if (r == RM_OK) r = check_heads("k", k, B, N, s->n_kv_heads, D, es, false, kMaxTokenBytes, &x[1], st[1]);
     if (r == RM_OK) r = check_heads("v", v, B, N, s->n_kv_heads, D, es, false, kMaxTokenBytes, &x[2], st[2]);
@@ -417,7 +417,7 @@ RM_EXPORT rm_status rm_prefix_attention(const rm_attn_shape *s, int32_t n_groups
     const int64_t B = static_cast<int64_t>(n_groups) * per_group;
     const size_t es = elem(s->dtype);
     Extent x[6];
-    int64_t st[6][3];
+    int64_t st[6][3] = {};
     r = check_heads("q", q, B, T, s->n_q_heads, D, es, false, INT64_MAX, &x[0], st[0]);
     if (r == RM_OK) r = check_heads("k_prefix", k_prefix, n_groups, P, hk, D, es, false, kMaxTokenBytes, &x[1], st[1]);
     if (r == RM_OK) r = check_heads("v_prefix", v_prefix, n_groups, P, hk, D, es, false, kMaxTokenBytes, &x[2], st[2]);
