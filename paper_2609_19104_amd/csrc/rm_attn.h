@@ -621,7 +621,7 @@ __global__ __launch_bounds__(64 * RW * KW, WPE) void attn_kernel(Args a) {
             }
             some = some || mixed;
             {  // O^T += V^T P^T; with two buffers the next tile's values go out meanwhile, with one the rest of its
-               // keys.  The weights are rounded to bf16 like the values (2^-9 of each at most, of either sign); the sum
+               // keys.  The weights are rounded to bf16 like the values (2^-8 of each at most, of either sign); the sum
                // that divides them is not.
                 constexpr int X = (BF ? 2 : 16) * NS * DB, NQ = NBUF == 2 ? NP : NP - NH;
                 typedef typename std::conditional<BF, rm_bf16x8, float>::type VFrag;
