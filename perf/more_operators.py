@@ -1,0 +1,446 @@
+"""The serving-step operators' measured calls: their inputs, plain forms, work and 64-bit results.
+
+Three operators, which with the norm and rotation of heads and the FFN calls make a layer of a serving step:
+
+  page_slots       a paged cache's tables, and the cache row of every new token, from the requests' lengths
+  paged_attention  one new token per row over its sequence's pages
+  block_norm       norm of a block's output, gate, residual, and the next block's norm and modulation
+
+run() computes the plain form in elementary torch operations in 32 bits, or with own = True makes the library's calls.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+BYTES = {"bf16": 2, "f32": 4}
+EPS = 1e-6
+
+
+# ----------------------------------------------------------------------------------------------------------
+# Cases
+# ----------------------------------------------------------------------------------------------------------
+
+def listed():
+    return [
+        # One decode step of 64 requests, a token each: the smallest call, before every step's first layer.
+        dict(name="slots-decode-64", op="slots", B=64, page=16, cap=4096, new="one", chunk=1, scarce=False),
+        # A step that mixes ended requests, prompts that come in chunks of up to 512 tokens, and single tokens.
+        dict(name="slots-mixed-256", op="slots", B=256, page=16, cap=8192, new="mixed", chunk=512, scarce=False),
+        # Prompts of a thousand requests at once, ragged, with fewer free pages than they ask for.
+        dict(name="slots-prefill-1024", op="slots", B=1024, page=32, cap=4096, new="ragged", chunk=128, scarce=True),
+        # One sequence behind a VLM prefix of 850 rows, 8 query heads on 1 of 256: the smallest attention call.
+        dict(name="paged-decode-1", op="paged", N=1, page=16, cap=1024, lens="near", at=850, Hq=8, Hk=1, D=256, dtype="bf16",
+             cap_score=0.0, window=0, bias=False, seq=False),
+        # A serving batch of ragged lengths, grouped heads.
+        dict(name="paged-decode-64", op="paged", N=64, page=16, cap=8192, lens="ragged", at=8192, Hq=32, Hk=8, D=128,
+             dtype="bf16", cap_score=0.0, window=0, bias=False, seq=True),
+        # Many short sequences, capped scores.
+        dict(name="paged-decode-512", op="paged", N=512, page=32, cap=1024, lens="ragged", at=1000, Hq=16, Hk=4, D=128,
+             dtype="bf16", cap_score=50.0, window=0, bias=False, seq=True),
+        # Four long caches, distance bias.
+        dict(name="paged-decode-128k", op="paged", N=4, page=64, cap=131072, lens="near", at=131072, Hq=32, Hk=4, D=128,
+             dtype="bf16", cap_score=0.0, window=0, bias=True, seq=False),
+        # float32, odd sizes: a head width of no power of two, pages of 24 rows, a window.
+        dict(name="paged-f32-37", op="paged", N=37, page=24, cap=3000, lens="ragged", at=2777, Hq=6, Hk=3, D=72, dtype="f32",
+             cap_score=0.0, window=1111, bias=False, seq=True),
+        # The boundary between two blocks of the action expert: 51 tokens, adaptive gate, scale and shift.
+        dict(name="norm-action-51", op="norm", B=1, T=51, d=1024, x="f32", f="f32", out="f32", post=False, gains=False,
+             gate=True, mod=True, x_scale=1.0, f_scale=1.0),
+        # Between two blocks of a VLM prefill of 850 rows, with a norm behind each block too.
+        dict(name="norm-prefill-850", op="norm", B=1, T=850, d=2048, x="f32", f="bf16", out="bf16", post=True, gains=True,
+             gate=False, mod=False, x_scale=1.0, f_scale=1.0),
+        # Ragged: three samples of 257 tokens of 1152 columns, everything on, residual and block scaled.
+        dict(name="norm-odd-771", op="norm", B=3, T=257, d=1152, x="bf16", f="bf16", out="bf16", post=True, gains=True,
+             gate=True, mod=True, x_scale=0.75, f_scale=1.5),
+        # A long packed batch.
+        dict(name="norm-packed-16k", op="norm", B=8, T=2048, d=2048, x="f32", f="bf16", out="bf16", post=True, gains=True,
+             gate=True, mod=True, x_scale=1.0, f_scale=1.0),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+HEADS = ((8, 1), (16, 4), (32, 8), (6, 3), (4, 4), (12, 2), (20, 1))
+
+
+def draw(rng):
+    op = rng.choice(("slots", "paged", "paged", "paged", "norm", "norm"))
+    if op == "slots":
+        new = rng.choice(("one", "mixed", "ragged"))
+        B = _log(rng, 1, 1024)
+        return dict(op=op, B=B, page=rng.choice((8, 16, 24, 64)), cap=_log(rng, 256, 8192), new=new,
+                    chunk=1 if new == "one" else _log(rng, 2, min(2048, 131072 // B)), scarce=rng.random() < 0.4)
+    if op == "norm":
+        d = 8 * _log(rng, 8, 1024)
+        return dict(op=op, B=rng.randint(1, 8), T=_log(rng, 1, min(16384, 33554432 // d) // 8), d=d,
+                    x=rng.choice(("f32", "bf16")), f=rng.choice(("f32", "bf16")), out=rng.choice(("f32", "bf16")),
+                    post=rng.random() < 0.5,
+                    gains=rng.random() < 0.5, gate=rng.random() < 0.5, mod=rng.random() < 0.5,
+                    x_scale=rng.choice((1.0, 0.75)), f_scale=rng.choice((1.0, 1.5)))
+    Hq, Hk = rng.choice(HEADS)
+    D = rng.choice((64, 72, 80, 128, 128, 256))
+    dtype = rng.choice(("bf16", "bf16", "f32"))
+    N = _log(rng, 1, 512)
+    room = 67108864 * 2 // (N * Hk * D * BYTES[dtype])
+    cap = _log(rng, 16, max(17, min(131072, room)))
+    return dict(op=op, N=N, page=rng.choice((8, 16, 16, 24, 32, 64)), cap=cap, lens=rng.choice(("ragged", "near")),
+                at=rng.randint(max(1, cap // 2), cap), Hq=Hq, Hk=Hk, D=D, dtype=dtype, cap_score=rng.choice((0.0, 0.0, 30.0)),
+                window=rng.choice((0, 0, 0, _log(rng, 1, cap))), bias=rng.random() < 0.3, seq=rng.random() < 0.5)
+
+
+# ----------------------------------------------------------------------------------------------------------
+# Inputs
+# ----------------------------------------------------------------------------------------------------------
+
+def _generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed))
+    return g
+
+
+def _randn(g, shape, dtype, scale=1.0):
+    return (torch.randn(shape, generator=g, device="cuda", dtype=torch.float32) * scale).to(DTYPES[dtype])
+
+
+def _randint(g, lo, hi, shape):
+    """Whole numbers in [lo, hi]."""
+    return torch.randint(lo, hi + 1, shape, generator=g, device="cuda", dtype=torch.int32)
+
+
+def _max_pages(c):
+    return -(-c["cap"] // c["page"])
+
+
+def _max_tok(c):
+    """Room for the tokens of a step."""
+    if c["new"] == "one":
+        return c["B"]
+    if c["new"] == "mixed":
+        return c["B"] + (c["B"] // 8 + 1) * c["chunk"]
+    return c["B"] * c["chunk"]
+
+
+def _prepare_slots(c, g):
+    B, page, per = c["B"], c["page"], _max_pages(c)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    longest = max(0, per * page - c["chunk"])
+    length = _randint(g, 0, longest, (B,))
+    if c["new"] == "one":
+        n_new = torch.ones((B,), **i32)
+    elif c["new"] == "ragged":
+        n_new = _randint(g, 1, c["chunk"], (B,))
+    else:
+        kind = torch.arange(B, device="cuda") % 16  # one of 16 has ended, two bring a chunk of their prompt
+        kind = kind[torch.randperm(B, generator=g, device="cuda")]
+        n_new = torch.where(kind == 0, -torch.ones((B,), **i32),
+                            torch.where(kind <= 2, _randint(g, 1, c["chunk"], (B,)), torch.ones((B,), **i32)))
+    n_pages = B * per + 5
+    page_of = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32)
+    table = page_of[:B * per].view(B, per).clone()
+    # The pages that no request holds are free: the table's entries past a request's length, and five more.
+    have = (length + page - 1) // page
+    held = torch.arange(per, device="cuda") < have[:, None]
+    is_free = torch.cat((~held.flatten(), torch.ones((5,), dtype=torch.bool, device="cuda")))
+    order = torch.argsort((~is_free).to(torch.int32), stable=True)
+    free_pages = page_of[order].contiguous()
+    n_free = is_free.sum().to(torch.int32).view(1)
+    if c["scarce"]:  # about half of what the step would take if every request's tokens began a page
+        n_free = torch.minimum(n_free, torch.full((1,), max(1, B * c["chunk"] // (4 * page)), **i32))
+    table = torch.where(held, table, torch.full_like(table, -1))
+    n = _max_tok(c)
+    return dict(n_new=n_new, length=length, table=table, free_pages=free_pages, n_free=n_free, page=page,
+                length_out=torch.zeros((B,), **i32), n_free_out=torch.zeros((1,), **i32), refused=torch.zeros((1,), **i32),
+                first=torch.zeros((B + 1,), **i32), seq=torch.zeros((n,), **i32), pos=torch.zeros((n,), **i32),
+                slot=torch.zeros((n,), **i32))
+
+
+def _prepare_paged(c, g):
+    N, page, Hq, Hk, D, dt = (c[k] for k in ("N", "page", "Hq", "Hk", "D", "dtype"))
+    per = _max_pages(c)
+    n_pages = N * per + 3
+    lo = c["at"] // 8 if c["lens"] == "ragged" else c["at"] - c["at"] // 64
+    s = dict(q=_randn(g, (N, Hq, D), dt, 2.0), k=_randn(g, (n_pages, page, Hk, D), dt), v=_randn(g, (n_pages, page, Hk, D), dt),
+             table=torch.randperm(n_pages, generator=g, device="cuda")[:N * per].to(torch.int32).view(N, per),
+             pos=_randint(g, max(lo, 1), c["at"], (N,)) - 1, seq=None, slopes=None, scale=D ** -0.5,
+             out=torch.empty((N, Hq, D), dtype=DTYPES[dt], device="cuda"))
+    if c["seq"]:  # the batch's rows are not in the table's order
+        s["seq"] = torch.randperm(N, generator=g, device="cuda").to(torch.int32)
+    if c["bias"]:  # a geometric row of slopes, one a head
+        s["slopes"] = 2.0 ** (-8.0 * torch.arange(1, Hq + 1, device="cuda", dtype=torch.float32) / Hq)
+    return s
+
+
+def _prepare_norm(c, g):
+    B, T, d = c["B"], c["T"], c["d"]
+    s = dict(x=_randn(g, (B, T, d), c["x"], 2.0), f=_randn(g, (B, T, d), c["f"]), gain_post=None, gain_pre=None, gate=None,
+             scale=None, shift=None, y=torch.empty((B, T, d), dtype=DTYPES[c["x"]], device="cuda"),
+             out=torch.empty((B, T, d), dtype=DTYPES[c["out"]], device="cuda"))
+    if c["gains"]:
+        s["gain_pre"] = 1.0 + 0.1 * _randn(g, (d,), "f32")
+        if c["post"]:
+            s["gain_post"] = 1.0 + 0.1 * _randn(g, (d,), "f32")
+    # Scale, shift and gate lie side by side in one projection's output, as an adaptive norm makes them.
+    mod = 0.3 * _randn(g, (B, 3 * d), "f32")
+    if c["mod"]:
+        s["scale"], s["shift"] = mod[:, :d], mod[:, d:2 * d]
+    if c["gate"]:
+        s["gate"] = mod[:, 2 * d:]
+    return s
+
+
+def prepare(case, seed):
+    g = _generator(seed)
+    s = {"slots": _prepare_slots, "paged": _prepare_paged, "norm": _prepare_norm}[case["op"]](case, g)
+    s["case"] = case
+    return s
+
+
+# ----------------------------------------------------------------------------------------------------------
+# Plain forms
+# ----------------------------------------------------------------------------------------------------------
+
+def _plain_slots(s):
+    page, table, free = s["page"], s["table"], s["free_pages"]
+    B, per = table.shape
+    n_pages, n_tok = free.shape[0], s["seq"].shape[0]
+    new, old = s["n_new"].long(), s["length"].long().clamp(0, per * page)
+    at = torch.arange(per, device="cuda")
+    have = (old + page - 1) // page
+    # Ended requests give their pages back, in order, on top of the free list.
+    back = torch.where(new < 0, have, torch.zeros_like(have))
+    begin = back.cumsum(0) - back + s["n_free"].long().clamp(0, n_pages)
+    dest = begin[:, None] + at
+    dest = torch.where((at < back[:, None]) & (dest < n_pages), dest, torch.full_like(dest, n_pages))
+    wide = torch.cat((free, free.new_zeros((1,))))
+    wide[dest.flatten()] = table.flatten()
+    free.copy_(wide[:n_pages])
+    avail = (s["n_free"].long().clamp(0, n_pages) + back.sum()).clamp(max=n_pages)
+    # Pages for the others, while there are any.
+    add = new.clamp(min=0)
+    ends = add.cumsum(0)
+    s["first"][1:] = ends.to(torch.int32)
+    fits = (new >= 0) & (old + add <= per * page) & (ends <= n_tok)
+    want = torch.where(fits, (old + add + page - 1) // page - have, torch.zeros_like(have))
+    upto = want.cumsum(0)
+    served = fits & ((want == 0) | (upto <= avail))
+    k = (upto - want)[:, None] + at - have[:, None]
+    fresh = served[:, None] & (at >= have[:, None]) & (at < (have + want)[:, None])
+    table.copy_(torch.where(fresh, free[(avail - 1 - k).clamp(0, n_pages - 1)], table))
+    s["length_out"].copy_(torch.where(new < 0, torch.zeros_like(old), torch.where(served, old + add, old)))
+    s["n_free_out"].copy_(avail - torch.where(served, want, torch.zeros_like(want)).sum())
+    s["refused"].copy_(((new >= 0) & ~served).sum())
+    # Every token's request, position and row.
+    t = torch.arange(n_tok, device="cuda")
+    b = torch.searchsorted(ends, t, right=True)
+    real = b < B
+    b = b.clamp(max=B - 1)
+    ok = real & served[b]
+    pos = torch.where(ok, old[b] + t - (ends - add)[b], torch.full_like(t, -1))
+    p = pos.clamp(min=0)
+    in_page = table[b, (p // page).clamp(max=per - 1)].long()
+    ok = ok & (in_page >= 0) & (in_page < n_pages)
+    s["seq"].copy_(torch.where(real, b, torch.full_like(b, -1)))
+    s["pos"].copy_(pos)
+    s["slot"].copy_(torch.where(ok, in_page * page + p % page, torch.full_like(p, -1)))
+    return _slots_out(s)
+
+
+def _slots_out(s):
+    return tuple(s[k] for k in ("seq", "pos", "slot", "first", "length_out", "n_free_out", "refused", "table", "free_pages"))
+
+
+def _plain_paged(s):
+    c = s["case"]
+    N, page, Hq, Hk, D = (c[k] for k in ("N", "page", "Hq", "Hk", "D"))
+    rows = s["table"].long()
+    if s["seq"] is not None:
+        rows = rows[s["seq"].long()]
+    L = rows.shape[1] * page
+    k = s["k"][rows].view(N, L, Hk, D).float().permute(0, 2, 3, 1)
+    q = s["q"].float().view(N, Hk, Hq // Hk, D)
+    scores = torch.matmul(q, k.contiguous()) * s["scale"]
+    del k
+    if c["cap_score"]:
+        scores = c["cap_score"] * torch.tanh(scores / c["cap_score"])
+    j = torch.arange(L, device="cuda")
+    dist = s["pos"].long()[:, None] - j
+    if s["slopes"] is not None:
+        scores = scores - s["slopes"].view(1, Hk, Hq // Hk, 1) * dist[:, None, None].float()
+    seen = dist >= 0
+    if c["window"]:
+        seen = seen & (dist < c["window"])
+    scores = scores.masked_fill(~seen[:, None, None], float("-inf"))
+    top = scores.amax(-1, keepdim=True)
+    p = torch.exp(scores - torch.where(torch.isinf(top), torch.zeros_like(top), top))
+    total = p.sum(-1, keepdim=True)
+    v = s["v"][rows].view(N, L, Hk, D).float().permute(0, 2, 1, 3)
+    o = torch.matmul(p / torch.where(total == 0, torch.ones_like(total), total), v.contiguous())
+    s["out"].copy_(o.reshape(N, Hq, D))
+    return s["out"]
+
+
+def _rms(x):
+    return x / torch.sqrt((x * x).mean(-1, keepdim=True) + EPS)
+
+
+def _plain_norm(s):
+    c = s["case"]
+    f = s["f"].float()
+    if c["post"]:
+        f = _rms(f)
+        if s["gain_post"] is not None:
+            f = f * s["gain_post"]
+    if s["gate"] is not None:
+        f = f * s["gate"][:, None]
+    u = c["x_scale"] * s["x"].float() + c["f_scale"] * f
+    o = _rms(u)
+    if s["gain_pre"] is not None:
+        o = o * s["gain_pre"]
+    if s["scale"] is not None:
+        o = o * (1.0 + s["scale"][:, None]) + s["shift"][:, None]
+    s["y"].copy_(u)
+    s["out"].copy_(o)
+    return s["y"], s["out"]
+
+
+# ----------------------------------------------------------------------------------------------------------
+# The library's calls
+# ----------------------------------------------------------------------------------------------------------
+
+def _own_run(s):
+    import paper_2609_19104_amd as rm
+
+    c = s["case"]
+    op = c["op"]
+    if op == "slots":
+        rm.rm_page_slots(s["n_new"], s["length"], s["table"], s["free_pages"], s["n_free"], s["first"], s["seq"], s["pos"],
+                         s["slot"], s["page"], length_out=s["length_out"], n_free_out=s["n_free_out"], refused=s["refused"])
+        return _slots_out(s)
+    if op == "paged":
+        if "ws" not in s:
+            s["ws"] = rm.paged_attention_workspace(s["q"], s["k"], s["table"])
+        rm.rm_paged_attention(s["q"], s["k"], s["v"], s["table"], s["pos"], s["out"], s["ws"], seq=s["seq"],
+                              window=c["window"], slopes=s["slopes"], scale=s["scale"], softcap=c["cap_score"])
+        return s["out"]
+    rm.rm_block_norm(s["x"], s["f"], s["y"], s["out"], norm_post=c["post"], gain_post=s["gain_post"], gate=s["gate"],
+                     gain_pre=s["gain_pre"], scale=s["scale"], shift=s["shift"], x_scale=c["x_scale"], f_scale=c["f_scale"],
+                     eps=EPS)
+    return s["y"], s["out"]
+
+
+def run(state):
+    if own:
+        return _own_run(state)
+    return {"slots": _plain_slots, "paged": _plain_paged, "norm": _plain_norm}[state["case"]["op"]](state)
+
+
+# ----------------------------------------------------------------------------------------------------------
+# Work
+# ----------------------------------------------------------------------------------------------------------
+
+def work(case):
+    op = case["op"]
+    if op == "slots":
+        n = _max_tok(case)
+        moved = n / 2 / case["page"] + case["B"] / case["page"]  # pages taken and given back, about
+        return {"bytes": 12 * n + 16 * case["B"] + 12 * moved, "flops": 0}
+    if op == "norm":
+        n = case["B"] * case["T"] * case["d"]
+        return {"bytes": n * (2 * BYTES[case["x"]] + BYTES[case["f"]] + BYTES[case["out"]]), "flops": 12 * n}
+    at = case["at"]
+    keys = at * 9 / 16 if case["lens"] == "ragged" else at - at / 128
+    if case["window"]:
+        keys = min(keys, case["window"])
+    N, Hq, Hk, D = (case[k] for k in ("N", "Hq", "Hk", "D"))
+    return {"bytes": N * (2 * keys * Hk + 2 * Hq) * D * BYTES[case["dtype"]] + 4 * N * keys / case["page"],
+            "flops": 4 * N * keys * Hq * D}
+
+
+# ----------------------------------------------------------------------------------------------------------
+# 64-bit results, from the definitions: one request, one row or one sample at a time
+# ----------------------------------------------------------------------------------------------------------
+
+def _exact_slots(c, s):
+    page, per, n_tok = c["page"], _max_pages(c), _max_tok(c)
+    new, old, table = s["n_new"].tolist(), s["length"].tolist(), s["table"].tolist()
+    free = s["free_pages"].tolist()
+    stack = free[:int(s["n_free"])]
+    for b, n in enumerate(new):
+        if n < 0:
+            stack += table[b][:-(-old[b] // page)]
+    free[:len(stack)] = stack
+    seq, pos, slot, first, length = [-1] * n_tok, [-1] * n_tok, [-1] * n_tok, [0], []
+    refused, room = 0, True
+    for b, n in enumerate(new):
+        begin, end = first[-1], first[-1] + max(n, 0)
+        first.append(end)
+        if n < 0:
+            length.append(0)
+            continue
+        held, needed = -(-old[b] // page), -(-(old[b] + n) // page)
+        ok = old[b] + n <= per * page and end <= n_tok
+        if ok and needed > held:
+            room = room and needed - held <= len(stack)
+            ok = room
+        refused += not ok
+        length.append(old[b] + n if ok else old[b])
+        if ok:
+            for i in range(held, needed):
+                table[b][i] = stack.pop()
+        for t in range(begin, min(end, n_tok)):
+            seq[t] = b
+            if ok:
+                pos[t] = old[b] + t - begin
+                slot[t] = table[b][pos[t] // page] * page + pos[t] % page
+    return tuple(torch.tensor(x, dtype=torch.int32, device="cuda")
+                 for x in (seq, pos, slot, first, length, [len(stack)], [refused], table, free))
+
+
+def _exact_paged(c, s):
+    N, page, Hq, Hk, D = (c[k] for k in ("N", "page", "Hq", "Hk", "D"))
+    out = torch.zeros((N, Hq, D), dtype=torch.float64, device="cuda")
+    pos = s["pos"].tolist()
+    seq = s["seq"].tolist() if s["seq"] is not None else list(range(N))
+    group = Hq // Hk
+    for n in range(N):
+        end = pos[n] + 1
+        j = torch.arange(max(0, end - c["window"]) if c["window"] else 0, end, device="cuda")
+        row, col = s["table"][seq[n]].long()[j // page], j % page
+        k, v = s["k"][row, col].double().transpose(0, 1), s["v"][row, col].double().transpose(0, 1)
+        x = torch.bmm(s["q"][n].double().view(Hk, group, D), k.transpose(1, 2).contiguous()) * s["scale"]
+        if c["cap_score"]:
+            x = torch.tanh(x / c["cap_score"]) * c["cap_score"]
+        if s["slopes"] is not None:
+            x = x + s["slopes"].double().view(Hk, group, 1) * (j - pos[n]).double()
+        out[n] = torch.bmm(torch.softmax(x, -1), v.contiguous()).view(Hq, D)
+    return out
+
+
+def _exact_norm(c, s):
+    y = torch.empty(s["x"].shape, dtype=torch.float64, device="cuda")
+    out = torch.empty_like(y)
+    for b in range(c["B"]):
+        f = s["f"][b].double()
+        if c["post"]:
+            f = f * (f.square().mean(-1, keepdim=True) + EPS).rsqrt()
+        if s["gain_post"] is not None:
+            f = f * s["gain_post"].double()
+        factor = c["f_scale"] if s["gate"] is None else c["f_scale"] * s["gate"][b].double()
+        y[b] = s["x"][b].double() * c["x_scale"] + f * factor
+        o = y[b] * (y[b].square().mean(-1, keepdim=True) + EPS).rsqrt()
+        if s["gain_pre"] is not None:
+            o = o * s["gain_pre"].double()
+        out[b] = o if s["scale"] is None else o + o * s["scale"][b].double() + s["shift"][b].double()
+    return y, out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"slots": _exact_slots, "paged": _exact_paged, "norm": _exact_norm}[case["op"]](case, s)
