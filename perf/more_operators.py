@@ -157,7 +157,7 @@ def _prepare_slots(c, g):
     n = _max_tok(c)
     return dict(n_new=n_new, length=length, table=table, free_pages=free_pages, n_free=n_free, page=page,
                 length_out=torch.zeros((B,), **i32), n_free_out=torch.zeros((1,), **i32), refused=torch.zeros((1,), **i32),
-                first=torch.zeros((B + 1,), **i32), seq=torch.zeros((n,), **i32), pos=torch.zeros((n,), **i32),
+                first=torch.zeros((B + 1,), **i32), start=torch.zeros((B,), **i32), seq=torch.zeros((n,), **i32), pos=torch.zeros((n,), **i32),
                 slot=torch.zeros((n,), **i32))
 
 
@@ -226,7 +226,7 @@ def _plain_slots(s):
     add = new.clamp(min=0)
     ends = add.cumsum(0)
     s["first"][1:] = ends.to(torch.int32)
-    fits = (new >= 0) & (old + add <= per * page) & (ends <= n_tok)
+    fits = (new >= 0) & (old + add <= per * page) & ((add == 0) | (ends <= n_tok))
     want = torch.where(fits, (old + add + page - 1) // page - have, torch.zeros_like(have))
     upto = want.cumsum(0)
     served = fits & ((want == 0) | (upto <= avail))
@@ -236,6 +236,7 @@ def _plain_slots(s):
     s["length_out"].copy_(torch.where(new < 0, torch.zeros_like(old), torch.where(served, old + add, old)))
     s["n_free_out"].copy_(avail - torch.where(served, want, torch.zeros_like(want)).sum())
     s["refused"].copy_(((new >= 0) & ~served).sum())
+    s["start"].copy_(torch.where(served, old, torch.full_like(old, -1)))
     # Every token's request, position and row.
     t = torch.arange(n_tok, device="cuda")
     b = torch.searchsorted(ends, t, right=True)
@@ -253,7 +254,7 @@ def _plain_slots(s):
 
 
 def _slots_out(s):
-    return tuple(s[k] for k in ("seq", "pos", "slot", "first", "length_out", "n_free_out", "refused", "table", "free_pages"))
+    return tuple(s[k] for k in ("seq", "pos", "slot", "first", "start", "length_out", "n_free_out", "refused", "table", "free_pages"))
 
 
 def _plain_paged(s):
@@ -320,8 +321,8 @@ def _own_run(s):
     c = s["case"]
     op = c["op"]
     if op == "slots":
-        rm.rm_page_slots(s["n_new"], s["length"], s["table"], s["free_pages"], s["n_free"], s["first"], s["seq"], s["pos"],
-                         s["slot"], s["page"], length_out=s["length_out"], n_free_out=s["n_free_out"], refused=s["refused"])
+        rm.rm_page_slots(s["n_new"], s["length"], s["table"], s["free_pages"], s["n_free"], s["first"], s["start"],
+                         s["seq"], s["pos"], s["slot"], s["page"], length_out=s["length_out"], n_free_out=s["n_free_out"], refused=s["refused"])
         return _slots_out(s)
     if op == "paged":
         if "ws" not in s:
@@ -350,7 +351,7 @@ def work(case):
     if op == "slots":
         n = _max_tok(case)
         moved = n / 2 / case["page"] + case["B"] / case["page"]  # pages taken and given back, about
-        return {"bytes": 12 * n + 16 * case["B"] + 12 * moved, "flops": 0}
+        return {"bytes": 12 * n + 20 * case["B"] + 12 * moved, "flops": 0}
     if op == "norm":
         n = case["B"] * case["T"] * case["d"]
         return {"bytes": n * (2 * BYTES[case["x"]] + BYTES[case["f"]] + BYTES[case["out"]]), "flops": 12 * n}
@@ -376,21 +377,23 @@ def _exact_slots(c, s):
         if n < 0:
             stack += table[b][:-(-old[b] // page)]
     free[:len(stack)] = stack
-    seq, pos, slot, first, length = [-1] * n_tok, [-1] * n_tok, [-1] * n_tok, [0], []
+    seq, pos, slot, first, start, length = [-1] * n_tok, [-1] * n_tok, [-1] * n_tok, [0], [], []
     refused, room = 0, True
     for b, n in enumerate(new):
         begin, end = first[-1], first[-1] + max(n, 0)
         first.append(end)
         if n < 0:
             length.append(0)
+            start.append(-1)
             continue
         held, needed = -(-old[b] // page), -(-(old[b] + n) // page)
-        ok = old[b] + n <= per * page and end <= n_tok
+        ok = old[b] + n <= per * page and (n == 0 or end <= n_tok)
         if ok and needed > held:
             room = room and needed - held <= len(stack)
             ok = room
         refused += not ok
         length.append(old[b] + n if ok else old[b])
+        start.append(old[b] if ok else -1)
         if ok:
             for i in range(held, needed):
                 table[b][i] = stack.pop()
@@ -400,7 +403,7 @@ def _exact_slots(c, s):
                 pos[t] = old[b] + t - begin
                 slot[t] = table[b][pos[t] // page] * page + pos[t] % page
     return tuple(torch.tensor(x, dtype=torch.int32, device="cuda")
-                 for x in (seq, pos, slot, first, length, [len(stack)], [refused], table, free))
+                 for x in (seq, pos, slot, first, start, length, [len(stack)], [refused], table, free))
 
 
 def _exact_paged(c, s):
