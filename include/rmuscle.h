@@ -397,6 +397,84 @@ rm_status rm_prefix_attention(const rm_attn_shape *s, int32_t n_groups, int32_t 
                               const int32_t *own_len, int32_t causal, const rm_heads *out, void *ws, size_t ws_bytes,
                               void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * A serving step around the layers: which cache rows the new tokens of a batch of requests take, the attention of those
+ * tokens over their requests' pages, and the passage from one block to the next.  Forward only.
+ * ---------------------------------------------------------------------------------------------------------- */
+
+/* A cache in pages.  The cache is n_pages pages of `page` rows each; token j of request b lies in row
+ * table[b][j / page] * page + j % page.  A call appends n_new[b] tokens to every request, whose tokens are packed one
+ * request after the other, and gives back the pages of ended ones:
+ *   1. ended requests (n_new[b] < 0), in order: their pages table[b][0 .. ceil(len[b] / page) - 1] go on top of the free
+ *      list free_pages[0 .. n_free - 1], one after the other; their length becomes 0.
+ *   2. first[b] = the sum of max(n_new, 0) of the requests before b; its tokens are first[b] .. first[b + 1] - 1.  A
+ *      request fits if its tokens fit into its table, len[b] + n_new[b] <= max_pages * page, and into the batch,
+ *      first[b + 1] <= max_tok (no tokens always do), and then wants ceil((len[b] + n_new[b]) / page) - ceil(len[b] / page)
+ *      pages.
+ *   3. A request that fits is served if it wants no page, or if the pages wanted up to and with it are no more than are
+ *      free.  Pages are taken from the top of the free list: the k-th (from 0) is free_pages[n_free - 1 - k], n_free
+ *      counting those of step 1; they follow the request's others in its table.
+ *   n_new:    int32 [n_seqs].  len: int32 [n_seqs], tokens that a request has (taken in [0, max_pages * page]).
+ *   n_free:   int32 [1], taken in [0, n_pages].
+ *   table:    int32 [n_seqs][max_pages], in/out; entries of other pages keep what they hold.
+ *   free_pages: int32 [n_pages], in/out; only entries that step 1 puts there are written.
+ *   len_out:  int32 [n_seqs] out, the new lengths (may be len).  n_free_out: int32 [1] out (may be n_free).
+ *   refused:  int32 [1] out or NULL: how many requests were not served; their lengths and tables stay as they were.
+ *   first:    int32 [n_seqs + 1] out (at most 2^30).
+ *   start:    int32 [n_seqs] out: the position of the request's first new token, -1 for refused and ended ones.
+ *   seq, pos, slot: int32 [max_tok] out: each token's request, its position in it and its cache row.  pos and slot are -1
+ *             for the tokens of a refused request, and all three behind the last token; slot is -1 too where the table
+ *             names a page outside [0, n_pages).  rm_qk_norm_rope drops the key and value of such a slot, and
+ *             rm_paged_attention gives 0 for such a position.
+ * 1 <= n_seqs <= 2^20, 1 <= max_tok < 2^30, n_pages < 2^30, n_pages * page < 2^31, max_pages * page < 2^30.  The outputs
+ * must not overlap each other or the inputs.  Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_ALIGN (4 bytes). */
+rm_status rm_page_slots(int32_t n_seqs, int32_t max_tok, int32_t page, int32_t n_pages, int32_t max_pages,
+                        const int32_t *n_new, const int32_t *len, const int32_t *n_free, int32_t *table,
+                        int32_t *free_pages, int32_t *len_out, int32_t *n_free_out, int32_t *refused, int32_t *first,
+                        int32_t *start, int32_t *seq, int32_t *pos, int32_t *slot, void *stream);
+
+/* Attention of new tokens over a paged cache, a token at position pos[n] of request seq[n] over keys of that request:
+ *     s_j = cap(scale * <q[n,h], k_j>) - slopes[h] * (pos[n] - j),   max(0, pos[n] - window + 1) <= j <= pos[n]
+ *     out[n,h] = sum_j softmax(s)_j v_j               (no key, or finite values and no score above -infinity: 0)
+ * with k_j, v_j the head h' of the row that the request's table names for j.  The new token's own key and value are in the
+ * cache already.  Keys that a token does not see do not affect it, whatever they hold.
+ *   q, out:   [n_tok][n_q_heads][head_dim] (their batch stride is not used).
+ *   k, v:     [n_pages][page][n_kv_heads][head_dim]: batch is the stride from page to page, so that the cache rows of
+ *             rm_qk_norm_rope (batch = page * token) serve, and pages that hold their heads one after the other too.
+ *   table:    int32 [n_seqs][max_pages]; keys on a page outside [0, n_pages) are not seen.
+ *   seq:      int32 [n_tok] or NULL (token n is of request n, n_seqs >= n_tok); outside [0, n_seqs): sees nothing.
+ *   pos:      int32 [n_tok]; negative: sees nothing; positions from max_pages * page on see the table's last key too.
+ *   window:   0: no window.  slopes: float32 [n_q_heads] or NULL: no bias.
+ *   ws, ws_bytes: at least rm_paged_attention_workspace_size bytes (which may be 0: ws may then be NULL), 256-byte
+ *             aligned; scratch as for rm_workspace_size.
+ * Several new tokens of one request are several n with its seq and rising pos; its keys are read for each of them, so a
+ * long chunk of a prompt is better served by rm_span_attention on keys in a row.  n_tok * n_q_heads < 2^24.
+ * Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN, RM_ERR_WORKSPACE, RM_ERR_HIP. */
+rm_status rm_paged_attention_workspace_size(const rm_attn_shape *s, int32_t n_tok, int32_t page, int32_t max_pages,
+                                            size_t *bytes);
+rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, int32_t n_seqs, int32_t page, int32_t n_pages,
+                             int32_t max_pages, const rm_heads *q, const rm_heads *k, const rm_heads *v,
+                             const rm_heads *out, const int32_t *table, const int32_t *seq, const int32_t *pos,
+                             int32_t window, const float *slopes, void *ws, size_t ws_bytes, void *stream);
+
+/* From one block to the next: norm of the block's output, adaptive gate (section 4.1), residual, and the next block's
+ * norm with its adaptive scale and shift, in one pass.  For every row of d columns of sample b:
+ *     u   = x_scale * x + f_scale * gate[b] * (norm_post ? f / sqrt(mean(f^2) + eps) * gain_post : f)
+ *     y   = u
+ *     out = u / sqrt(mean(u^2) + eps) * gain_pre * (1 + scale[b]) + shift[b]
+ *   x, y:     [B][T][d] in x_dtype: the residual stream.  f: [B][T][d] in f_dtype, the block's output; NULL: u = x_scale x.
+ *   out:      [B][T][d] in out_dtype, made of u before it is rounded to x_dtype.  y or out may be NULL.
+ *   gains:    float32 [d] or NULL (1).  gate, scale, shift: float32 [B][d] or NULL (1, 0, 0), rows gate_stride,
+ *             scale_stride and shift_stride elements apart (parts of one projection's rows will do).
+ * d a multiple of 8 of at most 32768, B * T < 2^24; all pointers and strides multiples of 16 bytes.  y may be x, and out may
+ * be f of the same type; any other overlap of an output is refused.  Sums and norms are float32.
+ * Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN. */
+rm_status rm_block_norm(int32_t B, int32_t T, int32_t d, int32_t x_dtype, int32_t f_dtype, int32_t out_dtype,
+                        const void *x, const void *f, int32_t norm_post, const float *gain_post, const float *gate,
+                        int64_t gate_stride, float x_scale, float f_scale, void *y, const float *gain_pre,
+                        const float *scale, int64_t scale_stride, const float *shift, int64_t shift_stride, float eps,
+                        void *out, void *stream);
+
 /* Down-projection row norms ||W_down[n]||_2 of one layer (the weight factor of Eq. 1, section 3.4), float32.
  *   w_down: [d_ff][d] in wdtype (the layout of rm_ffn_layer_weights.w_down), 16-byte aligned; d a multiple of 32.
  *   norms:  float32 [d_ff] out.

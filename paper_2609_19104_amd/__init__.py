@@ -12,6 +12,8 @@ Layouts (see include/rmuscle.h for the full contract):
   Eq. 4 anchor state: y_anchor float32 [L][B][T][d], h_anchor float32 [L][B][max_count][T]
   attention: q, out [B][T][n_q_heads][D], k, v [B][N][n_kv_heads][D], float32 or bfloat16, any strides whose last
   is 1; span int32 [B][T][2]
+  paged caches: [n_pages][page][n_kv_heads][D], float32 or bfloat16, any strides whose last is 1; table int32
+  [n_seqs][max_pages]
 """
 from __future__ import annotations
 
@@ -56,6 +58,7 @@ EXPORTED = ("rm_mask_compact", "rm_workspace_size", "rm_sparse_ffn_layer", "rm_s
             "rm_group_masks",
             "rm_qk_norm_rope", "rm_attn_spans", "rm_span_attention_workspace_size", "rm_span_attention",
             "rm_prefix_attention_workspace_size", "rm_prefix_attention",
+            "rm_page_slots", "rm_paged_attention_workspace_size", "rm_paged_attention", "rm_block_norm",
             "rm_profile_kernel_events", "rm_layer_kernels", "rm_stream_read",
             "rm_status_string", "rm_last_error")
 
@@ -106,7 +109,7 @@ def load_library() -> ctypes.CDLL:
         raise RuntimeError(f"{LIB_PATH} is not built: run `python -m paper_2609_19104_amd.build` "
                            "(or __graft_entry__.build()) first")
     lib = ctypes.CDLL(LIB_PATH)
-    i32, vp, sz = ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t
+    i32, i64, vp, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
     sp, wp = ctypes.POINTER(FfnShape), ctypes.POINTER(LayerWeights)
     f32 = ctypes.c_float
     sigs = {
@@ -136,6 +139,11 @@ def load_library() -> ctypes.CDLL:
         "rm_span_attention": [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
         "rm_prefix_attention_workspace_size": [vp, i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
         "rm_prefix_attention": [vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp],
+        "rm_page_slots": [i32] * 5 + [vp] * 14,
+        "rm_paged_attention_workspace_size": [vp, i32, i32, i32, ctypes.POINTER(sz)],
+        "rm_paged_attention": [vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp],
+        "rm_block_norm": [i32, i32, i32, i32, i32, i32, vp, vp, i32, vp, vp, i64, f32, f32, vp, vp, vp, i64, vp, i64, f32,
+                          vp, vp],
         "rm_profile_kernel_events": [i32, vp, vp],
         "rm_layer_kernels": [sp, i32, i32, i32, ctypes.POINTER(ctypes.c_uint32)],
         "rm_stream_read": [vp, sz, i32, vp, vp],
@@ -792,6 +800,116 @@ def rm_prefix_attention(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch
         _attn_shape(q, Hq, Hk, D, scale, softcap), groups, B // groups, T, P, S, at[0], at[1], at[2],
         _vector("prefix_len", prefix_len, torch.int32, dev, (groups,)), at[3], at[4],
         _vector("own_len", own_len, torch.int32, dev, (B,)), causal, at[5], wp, wn, _stream(stream)))
+
+
+def rm_page_slots(n_new: torch.Tensor, length: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
+                  n_free: torch.Tensor, first: torch.Tensor, start: torch.Tensor, seq: torch.Tensor, pos: torch.Tensor,
+                  slot: torch.Tensor, page: int, length_out: Optional[torch.Tensor] = None,
+                  n_free_out: Optional[torch.Tensor] = None, refused: Optional[torch.Tensor] = None,
+                  stream=None) -> None:
+    """Appends n_new [B] tokens (negative: the request has ended) to requests of length [B] on pages of table
+    [B][max_pages], pages taken from and given back to free_pages [n_pages], of which the first n_free [1] are free; the
+    packed tokens' seq, pos and slot [max_tok], their requests' first [B + 1] and start [B].  length and n_free are updated
+    in place unless length_out and n_free_out are given; all int32."""
+    dev = _attn_device(table, stream)
+    B, per = table.shape
+    i32 = torch.int32
+    n_tok, one = (seq.shape[0],), (1,)
+    n_pages = free_pages.shape[0]
+    at_len, at_free = _vector("length", length, i32, dev, (B,)), _vector("n_free", n_free, i32, dev, one)
+    _check(load_library().rm_page_slots(
+        B, seq.shape[0], page, n_pages, per, _vector("n_new", n_new, i32, dev, (B,)), at_len, at_free,
+        _vector("table", table, i32, dev, (B, per)), _vector("free_pages", free_pages, i32, dev, (n_pages,)),
+        at_len if length_out is None else _vector("length_out", length_out, i32, dev, (B,)),
+        at_free if n_free_out is None else _vector("n_free_out", n_free_out, i32, dev, one),
+        _vector("refused", refused, i32, dev, one), _vector("first", first, i32, dev, (B + 1,)),
+        _vector("start", start, i32, dev, (B,)), _vector("seq", seq, i32, dev, n_tok),
+        _vector("pos", pos, i32, dev, n_tok), _vector("slot", slot, i32, dev, n_tok), _stream(stream)))
+
+
+def paged_attention_workspace(q: torch.Tensor, k_cache: torch.Tensor, table: torch.Tensor) -> torch.Tensor:
+    """A workspace tensor (uint8) of the size rm_paged_attention_workspace_size asks for (it may be 0)."""
+    out = ctypes.c_size_t(0)
+    shape = _attn_shape(q, q.shape[1], k_cache.shape[2], q.shape[2], None, 0.0)
+    _check(load_library().rm_paged_attention_workspace_size(shape, q.shape[0], k_cache.shape[1], table.shape[1],
+                                                            ctypes.byref(out)))
+    return torch.empty(int(out.value), dtype=torch.uint8, device=q.device)
+
+
+def rm_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
+                       pos: torch.Tensor, out: torch.Tensor, ws: Optional[torch.Tensor],
+                       seq: Optional[torch.Tensor] = None, window: int = 0, slopes: Optional[torch.Tensor] = None,
+                       scale: Optional[float] = None, softcap: float = 0.0, stream=None) -> None:
+    """Tokens q [N][Hq][D] at positions pos [N] of requests seq [N] (None: n) over their requests' keys up to pos in
+    k_cache [n_pages][page][Hk][D] by table [n_seqs][max_pages]; scale None: 1 / sqrt(D)."""
+    dev = _attn_device(q, stream)
+    dtype = q.dtype
+    fields = (_heads3("q", q, dtype, dev) + _heads4("k_cache", k_cache, dtype, dev)
+              + _heads4("v_cache", v_cache, dtype, dev) + _heads3("out", out, dtype, dev))
+    shape, k_shape = q.shape, k_cache.shape
+    N, Hq, D = shape
+    n_pages, page, Hk, _ = k_shape
+    if k_shape[3] != D or v_cache.shape != k_shape or out.shape != shape:
+        raise ValueError("q and out must be [N][Hq][D], k_cache and v_cache [n_pages][page][Hk][D]")
+    n_seqs, per = table.shape
+    wp, wn = _attn_ws(ws, dev)
+    at = _marshal.at
+    _pack_heads[4](_marshal.heads, 0, *fields)
+    i32 = torch.int32
+    _check(load_library().rm_paged_attention(
+        _attn_shape(q, Hq, Hk, D, scale, softcap), N, n_seqs, page, n_pages, per, at[0], at[1], at[2], at[3],
+        _vector("table", table, i32, dev, (n_seqs, per)), _vector("seq", seq, i32, dev, (N,)),
+        _vector("pos", pos, i32, dev, (N,)), window, _vector("slopes", slopes, torch.float32, dev, (Hq,)), wp, wn,
+        _stream(stream)))
+
+
+def _rows(name: str, t: torch.Tensor, dtype, index: int, shape) -> int:
+    """Pointer of a contiguous activation tensor."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == index and t.is_contiguous():
+        return t.data_ptr()
+    _need_cuda(name, t, (dtype,), len(shape))
+    raise ValueError(f"{name} must be {list(shape)} on device {index}, got {list(t.shape)} on {t.device}")
+
+
+def _modulation(name: str, t: Optional[torch.Tensor], index: int, shape) -> Tuple[Optional[int], int]:
+    """Pointer and row stride of a float32 [B][d] tensor whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.shape != shape or t.dtype is not torch.float32 or t.get_device() != index or t.stride(1) != 1:
+        raise ValueError(f"{name} must be float32 {list(shape)} on device {index} with contiguous rows, got {t.dtype} "
+                         f"{list(t.shape)} on {t.device}")
+    return t.data_ptr(), t.stride(0)
+
+
+def rm_block_norm(x: torch.Tensor, f: Optional[torch.Tensor], y: Optional[torch.Tensor], out: Optional[torch.Tensor],
+                  norm_post: bool = False, gain_post: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, gain_pre: Optional[torch.Tensor] = None,
+                  scale: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None, x_scale: float = 1.0,
+                  f_scale: float = 1.0, eps: float = 1e-6, stream=None) -> None:
+    """y = x_scale x + f_scale gate norm_post(f), out = norm(y) gain_pre (1 + scale) + shift, all [B][T][d]; gains float32
+    [d], gate, scale and shift float32 [B][d] (rows any multiple of 4 elements apart).  y may be x, out may be f."""
+    dev = _attn_device(x, stream)
+    shape = x.shape
+    if len(shape) != 3:
+        raise ValueError(f"x must be [B][T][d], got {list(shape)}")
+    B, T, d = shape
+    xt = x.dtype
+    ft = xt if f is None else f.dtype
+    ot = xt if out is None else out.dtype
+    if xt not in _ATTN_DTYPES or ft not in _ATTN_DTYPES or ot not in _ATTN_DTYPES:
+        raise ValueError("x, f and out must be float32 or bfloat16")
+    f32 = torch.float32
+    gp, gs = _modulation("gate", gate, dev, (B, d))
+    sp, ss = _modulation("scale", scale, dev, (B, d))
+    hp, hs = _modulation("shift", shift, dev, (B, d))
+    _check(load_library().rm_block_norm(
+        B, T, d, _ATTN_DTYPES[xt], _ATTN_DTYPES[ft], _ATTN_DTYPES[ot], _rows("x", x, xt, dev, shape),
+        None if f is None else _rows("f", f, ft, dev, shape), norm_post, _vector("gain_post", gain_post, f32, dev, (d,)),
+        gp, gs, x_scale, f_scale, None if y is None else _rows("y", y, xt, dev, shape),
+        _vector("gain_pre", gain_pre, f32, dev, (d,)), sp, ss, hp, hs, eps,
+        None if out is None else _rows("out", out, ot, dev, shape), _stream(stream)))
 
 
 def rm_profile_kernel_events(kernel: int, ev_begin: Optional[int], ev_end: Optional[int]) -> None:
