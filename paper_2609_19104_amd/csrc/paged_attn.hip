@@ -1,4 +1,7 @@
-// Attention of one new token over a paged cache (rm_paged_attention).
+// Attention of one new token over a paged cache (rm_paged_attention): the kernel that walks the pages, and the join of
+// what several of its waves have of one token's head.
+#include <algorithm>
+
 #include "rm_attn.h"
 #include "rm_serve.h"
 
@@ -6,76 +9,536 @@ namespace rm_serve {
 
 namespace {
 
-template <bool BF>
-__device__ __forceinline__ float at(const char *p, int i) {
-    if constexpr (BF) return static_cast<float>(reinterpret_cast<const __bf16 *>(p)[i]);
-    else return reinterpret_cast<const float *>(p)[i];
+using rm_attn::divide;
+using rm_attn::kRaise;
+
+// A unit is one token, one key head and up to QR query heads of it; its keys are tiles of KT.  All tiles of all units in a
+// row, token by token, are divided evenly among the waves, whatever the lengths are: each wave reads the positions, finds
+// the unit where its share begins and goes on from unit to unit, the next tiles' keys, values, queries and table entries
+// always under way.  A unit that lies in one wave is written by it; what several waves have of one is joined afterwards.
+template <bool BF, int DH>
+struct Shape {
+    static constexpr int ES = BF ? 2 : 4, ROWB = DH * ES, CPR = ROWB / 16;
+    static constexpr int RPI = 64 / CPR;                          // rows of a load instruction (1 KB)
+    static constexpr int KT = ROWB <= 512 ? 8192 / ROWB : 16;     // keys of a tile
+    static constexpr int NI = KT / RPI;                           // load instructions of a tile's keys or values
+    static constexpr int TILEB = KT * ROWB;
+};
+template <bool BF, int DH, int QR>
+constexpr int lds_bytes() { return 4 * Shape<BF, DH>::TILEB + QR * Shape<BF, DH>::ROWB + 512; }
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N < 63 ? N : 63) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// A load of 4 bytes a lane into LDS at lds + 4 lane (as rm_dma::dma16).
+__device__ __forceinline__ void dma4(const void *g, uint32_t lds) {
+    uint32_t keep;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep)
+                 : "v"(g), "s"(lds)
+                 : "memory");
 }
 
-// One workgroup a token and query head, its waves taking keys by turns; a lane holds up to four of the columns.
-template <bool BF>
-__global__ __launch_bounds__(256) void paged_kernel(PagedArgs a) {
-    __shared__ float so[4][256], sm[4], sl[4];
-    const int n = blockIdx.x / a.Hq, h = blockIdx.x - n * a.Hq, hk = h / a.G;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int s = a.seq ? a.seq[n] : n, pos = a.pos[n];
-    const int64_t cap = static_cast<int64_t>(a.per) * a.page;
-    int end = s < 0 || s >= a.seqs || pos < 0 ? 0 : static_cast<int>(min(static_cast<int64_t>(pos) + 1, cap));
-    const int lo = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
-    const int32_t *table = a.table + static_cast<int64_t>(end > 0 ? s : 0) * a.per;
-    const char *q = a.q + n * a.q_t + h * a.q_h;
-    const float slope = a.slopes ? a.slopes[h] * rm_attn::kLog2e : 0.0f;
-    float qv[4], o[4] = {0, 0, 0, 0}, m = -INFINITY, l = 0.0f;
-    for (int i = 0; i < 4; ++i) qv[i] = lane + 64 * i < a.D ? at<BF>(q, lane + 64 * i) : 0.0f;
-    for (int j = lo + wave; j < end; j += 4) {
-        const int p = table[j / a.page];
-        if (p < 0 || p >= a.n_pages) continue;
-        const char *k = a.k + p * a.k_p + (j % a.page) * a.k_t + hk * a.k_h;
-        const char *v = a.v + p * a.v_p + (j % a.page) * a.v_t + hk * a.v_h;
-        float x = 0.0f;
-        for (int i = 0; i < 4; ++i)
-            if (lane + 64 * i < a.D) x = fmaf(qv[i], at<BF>(k, lane + 64 * i), x);
-        for (int w = 32; w >= 1; w >>= 1) x += __shfl_xor(x, w);
-        x *= a.scale;
-        if (a.cap != 0.0f) x = a.cap * tanhf(x);
-        x -= slope * static_cast<float>(pos - j);
-        if (x > m) {
-            const float f = m == -INFINITY ? 0.0f : exp2f(m - x);
-            l *= f;
-            for (int i = 0; i < 4; ++i) o[i] *= f;
-            m = x;
+// A whole number that is the same in every lane, read by way of the scalar cache: not among the loads that the waits count.
+__device__ __forceinline__ int32_t scalar(const int32_t *p, int i) {
+    typedef const __attribute__((address_space(4))) int32_t *constant;
+    return *reinterpret_cast<constant>(reinterpret_cast<uintptr_t>(p) + static_cast<uintptr_t>(i) * 4);
+}
+
+// Joined over the lanes whose numbers are the same modulo 16.
+__device__ __forceinline__ float rows_max(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return rm_attn::xor32_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return rm_attn::xor32_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
+    const int lo = __shfl(static_cast<int>(x), lane), hi = __shfl(static_cast<int>(x >> 32), lane);
+    return static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo));
+}
+
+// The keys [lo, end) that a token at position p of table s sees.
+__device__ __forceinline__ void seen(const PagedArgs &a, int p, int s, int &lo, int &end) {
+    const int cap = a.per * a.page;
+    end = p >= 0 && s >= 0 && s < a.seqs ? min(p, cap - 1) + 1 : 0;
+    lo = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
+    if (lo >= end) lo = end = 0;
+}
+template <int KT>
+__device__ __forceinline__ int tiles(int lo, int end) {  // (one for a token that sees nothing: its zeros are written)
+    return max(1, (end + KT - 1) / KT - lo / KT);
+}
+
+template <bool BF, int DH, int QR>
+__global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
+    typedef Shape<BF, DH> S;
+    constexpr int ES = S::ES, ROWB = S::ROWB, CPR = S::CPR, RPI = S::RPI, KT = S::KT, NI = S::NI, TILEB = S::TILEB;
+    constexpr int RT = QR > 16 ? 2 : 1;         // tiles of 16 query heads
+    constexpr int NS = KT / 16, QF = ROWB / 64, DB = DH / 16, NQ = QR / RPI;
+    constexpr uint64_t kFull = KT == 64 ? ~0ull : (1ull << KT) - 1;
+    static_assert(NQ >= 1 && NI >= 1, "load instructions");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[lds_bytes<BF, DH, QR>()];
+    uint8_t *const lds_q = lds + 4 * TILEB;
+    int32_t *const lds_t = reinterpret_cast<int32_t *>(lds_q + QR * ROWB);
+    const uint32_t at_k = rm_dma::lds_addr(lds), at_q = rm_dma::lds_addr(lds_q);
+    const uint32_t at_t = at_q + QR * ROWB;
+    const int lane = threadIdx.x, m16 = lane & 15, h4 = lane >> 4;
+    const int w = blockIdx.x;
+
+    // ---------------------------------------------------------------- this wave's share
+    auto weight = [&](int n) {
+        int lo, end;
+        seen(a, a.pos[n], a.seq ? a.seq[n] : n, lo, end);
+        return tiles<KT>(lo, end);
+    };
+    int total = 0;
+    for (int n = lane; n < a.N; n += 64) total += weight(n);
+    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
+    total = __builtin_amdgcn_readfirstlane(total) * a.units;
+    const int share = max((total + a.waves - 1) / a.waves, a.least);
+    const int64_t begin64 = static_cast<int64_t>(w) * share;
+    if (begin64 >= total) {
+        if (!a.by_unit && lane == 0) a.info[w] = make_int2(0, 0);
+        return;
+    }
+    const int begin = static_cast<int>(begin64);
+    int left = min(share, total - begin);  // tiles of the share that have not been staged
+    int n = 0, before = 0;                 // the token where it begins, and the tiles (of a unit) before it
+    for (int n0 = 0; n0 < a.N; n0 += 64) {
+        const int mine = n0 + lane < a.N ? weight(n0 + lane) : 0;
+        int upto = mine;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o);
+            if (lane >= o) upto += v;
         }
-        const float w = m == -INFINITY ? (x == -INFINITY ? 0.0f : x) : exp2f(x - m);
-        l += w;
-        for (int i = 0; i < 4; ++i)
-            if (lane + 64 * i < a.D) o[i] = w == 0.0f && x == -INFINITY ? o[i] : fmaf(w, at<BF>(v, lane + 64 * i), o[i]);
+        const uint64_t past = __ballot((before + upto) * a.units > begin);
+        if (past != 0) {
+            const int l = __builtin_ctzll(past);
+            n = n0 + l;
+            before += __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l);
+            break;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
     }
-    for (int i = 0; i < 4; ++i) so[wave][lane + 64 * i] = o[i];
-    if (lane == 0) sm[wave] = m, sl[wave] = l;
+
+    // ---------------------------------------------------------------- tiles
+    struct Tile {
+        int n, u, lo, end, t, t0, t1;  // token, unit of it, its keys and tiles
+        int pos, seq;
+        int base;                      // the unit's first tile among all
+    };
+    auto enter = [&](Tile &c, int p, int s) __attribute__((always_inline)) {  // c.n's keys
+        c.pos = p, c.seq = s;
+        seen(a, p, s, c.lo, c.end);
+        c.t0 = c.lo / KT;
+        c.t1 = c.t0 + tiles<KT>(c.lo, c.end);
+        if (c.end == 0) c.seq = 0;
+    };
+    auto place_of = [&](int i, int &p, int &s) __attribute__((always_inline)) {
+        i = min(i, a.N - 1);
+        p = scalar(a.pos, i);
+        s = a.seq ? scalar(a.seq, i) : i;
+    };
+    int next_p, next_s;  // the next token's
+    auto advance = [&](Tile &c) __attribute__((always_inline)) {
+        if (++c.t < c.t1) return;
+        c.base += c.t1 - c.t0;
+        if (++c.u < a.units) {
+            c.t = c.t0;
+            return;
+        }
+        c.u = 0;
+        ++c.n;
+        enter(c, next_p, next_s);
+        place_of(c.n + 1, next_p, next_s);
+        c.t = c.t0;
+    };
+
+    const int lrow = lane / CPR;
+    auto swz_k = [](int row) { return CPR == 8 ? (row >> 1) & 7 : row & 15; };
+    auto swz_v = [](int row) {
+        if constexpr (BF) return CPR == 8 ? 2 * ((row >> 1) & 3) : 2 * (row & 7);
+        else return 4 * ((row >> 2) & 3);
+    };
+    const uint32_t last_chunk = a.D * ES / 16 - 1;
+    const uint32_t chunk_k = lane % CPR ^ swz_k(lrow), chunk_v = lane % CPR ^ swz_v(lrow);
+    auto fetch_table = [&](const Tile &c, int slot) __attribute__((always_inline)) {
+        const int j = min(c.t * KT + (lane & (KT - 1)), max(c.end - 1, 0));
+        dma4(a.table + static_cast<int64_t>(c.seq) * a.per + divide(j, a.by_page),
+             __builtin_amdgcn_readfirstlane(at_t + slot * 256));
+    };
+    // Stages a tile whose table entries have come into a buffer, its unit's queries too if it is the first one here; says
+    // which of its keys are seen.  The others' rows are the cache's first one.
+    auto stage = [&](const Tile &c, int slot, int buf, bool queries) __attribute__((always_inline)) -> uint64_t {
+        const int j = c.t * KT + (lane & (KT - 1)), jj = min(j, max(c.end - 1, 0));
+        const int pg = lds_t[slot * 64 + lane];
+        const bool ok = j >= c.lo && j < c.end && static_cast<uint32_t>(pg) < static_cast<uint32_t>(a.n_pages);
+        const int in_page = jj - divide(jj, a.by_page) * a.page;
+        const int64_t ko = ok ? pg * a.k_p + in_page * a.k_t : 0, vo = ok ? pg * a.v_p + in_page * a.v_t : 0;
+        const int hk = divide(c.u, a.by_q_tiles), qt = c.u - hk * a.q_tiles;
+        if (queries) {
+            const int h0 = hk * a.G + qt * QR, most = min(QR, a.G - qt * QR) - 1;
+            const char *q = a.q + c.n * a.q_t;
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                const uint32_t ch = min(chunk_k ^ static_cast<uint32_t>(swz_k(i * RPI)), last_chunk);
+                rm_dma::dma16(q + (h0 + min(i * RPI + lrow, most)) * a.q_h + ch * 16,
+                              __builtin_amdgcn_readfirstlane(at_q + i * 1024));
+            }
+        }
+        const char *k = a.k + hk * a.k_h, *v = a.v + hk * a.v_h;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const uint32_t ch = min(chunk_k ^ static_cast<uint32_t>(swz_k(i * RPI)), last_chunk);
+            rm_dma::dma16(k + from_lane(ko, i * RPI + lrow) + ch * 16,
+                          __builtin_amdgcn_readfirstlane(at_k + buf * 2 * TILEB + i * 1024));
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const uint32_t ch = min(chunk_v ^ static_cast<uint32_t>(swz_v(i * RPI)), last_chunk);
+            rm_dma::dma16(v + from_lane(vo, i * RPI + lrow) + ch * 16,
+                          __builtin_amdgcn_readfirstlane(at_k + buf * 2 * TILEB + TILEB + i * 1024));
+        }
+        return __ballot(ok) & kFull;
+    };
+
+    typedef typename std::conditional<BF, rm_bf16x8, rm_f32x4>::type Frag;
+    // Chunk 4 c + h4 of row m16, by c mod 4 (the rest are offsets).
+    uint32_t k_at[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) k_at[c] = m16 * ROWB + (((4 * c + h4) ^ swz_k(m16)) & (CPR - 1)) * 16;
+    auto read_chunk = [&](const uint8_t *rows, int c) __attribute__((always_inline)) {
+        Frag f = *reinterpret_cast<const Frag *>(rows + k_at[c & 3] + (c >> 2) * 256);
+        // Columns past the head's are its last ones again, which must not meet each other.
+        return static_cast<uint32_t>(4 * c + h4) <= last_chunk ? f : Frag{};
+    };
+
+    Tile cur;
+    cur.n = n;
+    {
+        int p, s;
+        place_of(n, p, s);
+        place_of(n + 1, next_p, next_s);
+        enter(cur, p, s);
+        const int in = begin - before * a.units, each = cur.t1 - cur.t0;
+        cur.u = in / each;
+        cur.t = cur.t0 + (in - cur.u * each);
+        cur.base = begin - (cur.t - cur.t0);
+    }
+    fetch_table(cur, 0);
+    wait_loads<0>();
+    Tile nxt = cur;
+    --left;
+    if (left > 0) advance(nxt);
+    fetch_table(nxt, 1);
+    uint64_t vis = stage(cur, 0, 0, true), vis_next = 0;
+    bool fresh = true;  // cur is the first tile of a unit here
+
+    Frag qf[RT][QF];
+    rm_f32x4 o[RT][DB];
+    float m[RT], l[RT], slope[RT];
+    int2 end_info = make_int2(0, 0);
+    for (int turn = 0;; turn ^= 1) {
+        const bool more = left > 0, next_fresh = more && (nxt.u != cur.u || nxt.n != cur.n);
+        wait_loads<2 * NI>();  // the next tile's table entries, and this one's queries
+        if (fresh) {
+            const int hk = divide(cur.u, a.by_q_tiles), head = hk * a.G, g0 = (cur.u - hk * a.q_tiles) * QR;
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const uint8_t *rows = lds_q + r * 16 * ROWB;
+#pragma unroll
+                for (int c = 0; c < QF; ++c) {
+                    // (QR = 8: rows 8 .. 15 are 0 .. 7 again, in the places that those have)
+                    if constexpr (QR == 8) {
+                        const int row = m16 & 7;
+                        Frag f = *reinterpret_cast<const Frag *>(
+                            lds_q + row * ROWB + ((((4 * (c & 3) + h4) ^ swz_k(row)) & (CPR - 1)) * 16) + (c >> 2) * 256);
+                        qf[r][c] = static_cast<uint32_t>(4 * c + h4) <= last_chunk ? f : Frag{};
+                    } else {
+                        qf[r][c] = read_chunk(rows, c);
+                    }
+                }
+                m[r] = -INFINITY;
+                l[r] = 0.0f;
+                slope[r] = a.slopes ? a.slopes[head + min(g0 + r * 16 + m16, a.G - 1)] * rm_attn::kLog2e : 0.0f;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[r][d] = rm_f32x4{};
+            }
+        }
+        Tile after = nxt;
+        const int buf = turn * 2 * TILEB;
+        if (more) {
+            wait_lds();  // the queries, and the tile before this one: their places are free
+            if (left > 1) advance(after);
+            // (Its entries go where this tile's were.)
+            fetch_table(after, turn);
+            vis_next = stage(nxt, turn ^ 1, turn ^ 1, next_fresh);
+            if (next_fresh) wait_loads<3 * NI + 1 + NQ>();
+            else wait_loads<3 * NI + 1>();
+        } else {
+            wait_loads<NI>();
+        }
+
+        // ---------------------------------------------------------------- S^T = K Q^T
+        const uint8_t *const kt = lds + buf, *const vt = kt + TILEB;
+        rm_f32x4 s[RT][NS];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < NS; ++i) s[r][i] = rm_f32x4{};
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int c = 0; c < QF; ++c) {
+                const Frag kf = read_chunk(kt + i * 16 * ROWB, c);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    if constexpr (BF) {
+                        s[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][c], s[r][i], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[r][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[r][c][e], s[r][i], 0, 0, 0);
+                    }
+                }
+            }
+
+        // ---------------------------------------------------------------- softmax
+        const int j0 = cur.t * KT + 4 * h4;
+        const uint64_t bits = vis >> (4 * h4);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x = s[r][i][e] * a.scale;
+                    if (a.cap != 0.0f) x = a.cap * (BF ? rm_attn::tanh_relative(x) : tanhf(x));
+                    if (a.slopes) x = fmaf(-slope[r], static_cast<float>(cur.pos - (j0 + 16 * i + e)), x);
+                    if (vis != kFull) x = (bits >> (16 * i + e)) & 1 ? x : -INFINITY;
+                    s[r][i][e] = x;
+                    top = fmaxf(top, x);
+                }
+            top = rows_max(top);
+            const bool raise = top > m[r] + kRaise;  // (false for top = -inf)
+            if (__any(raise)) {
+                const float mn = raise ? top : m[r];
+                const float f = raise ? __builtin_amdgcn_exp2f(m[r] - mn) : 1.0f;
+                m[r] = mn;
+                l[r] *= f;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[r][d] *= f;
+            }
+            const float ref = m[r] == -INFINITY ? 0.0f : m[r];
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[r][i][e] = __builtin_amdgcn_exp2f(s[r][i][e] - ref);
+                    l[r] += s[r][i][e];
+                }
+        }
+
+        // ---------------------------------------------------------------- O^T += V^T P^T
+        if (more) {
+            if (next_fresh) wait_loads<2 * NI + 1 + NQ>();
+            else wait_loads<2 * NI + 1>();
+        } else {
+            wait_loads<0>();
+        }
+        if (vis != kFull) {  // values of keys that are not seen: 0 times an infinity or NaN is not 0
+#pragma unroll
+            for (int i = 0; i < TILEB / 1024; ++i) {
+                const int at = i * 64 + lane;
+                if (!((vis >> (at / CPR)) & 1)) *reinterpret_cast<rm_u32x4 *>(lds + buf + TILEB + at * 16) = rm_u32x4{0, 0, 0, 0};
+            }
+            wait_lds();
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            if constexpr (BF) {
+                typedef __attribute__((address_space(3))) rm_s16x4 lds_s16x4;
+                rm_s16x4 p[RT];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const rm_bf16x4 b = {static_cast<__bf16>(s[r][i][0]), static_cast<__bf16>(s[r][i][1]),
+                                         static_cast<__bf16>(s[r][i][2]), static_cast<__bf16>(s[r][i][3])};
+                    p[r] = __builtin_bit_cast(rm_s16x4, b);
+                }
+                const int row = 4 * h4 + (m16 >> 2);
+                const uint8_t *v = vt + (16 * i + row) * ROWB + (m16 & 3) * 8;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const rm_s16x4 f = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_s16x4 *)(v + (((2 * d) & 15) ^ swz_v(row)) * 16 + (d >> 3) * 256));
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+                        o[r][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(f, p[r], o[r][d], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int row = 16 * i + 4 * h4 + e;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        const float f = *reinterpret_cast<const float *>(
+                            vt + row * ROWB + (((4 * d) & 15) ^ (4 * h4)) * 16 + (d >> 2) * 256 + m16 * 4);
+#pragma unroll
+                        for (int r = 0; r < RT; ++r)
+                            o[r][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(f, s[r][i][e], o[r][d], 0, 0, 0);
+                    }
+                }
+            }
+        }
+
+        // ---------------------------------------------------------------- the unit's end, or the share's
+        if (!more || next_fresh) {
+            const bool starts = cur.base >= begin, ends = cur.t + 1 == cur.t1;
+            const int unit = cur.n * a.units + cur.u;
+            const int hk = divide(cur.u, a.by_q_tiles), qt = cur.u - hk * a.q_tiles;
+            if (starts) {
+                const int parts = (cur.base + (cur.t1 - cur.t0) - 1) / share - w + 1;
+                if (a.by_unit && lane == 0) a.info[unit] = make_int2(w, parts);
+                if (!ends) end_info = make_int2(unit, parts);
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float sum = rows_sum(l[r]);
+                const int g = qt * QR + r * 16 + m16;
+                if (r * 16 + m16 >= QR || g >= a.G) continue;
+                if (starts && ends) {
+                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    char *dst = a.o + cur.n * a.o_t + static_cast<int64_t>(hk * a.G + g) * a.o_h;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        const int c = 16 * d + 4 * h4;
+                        if (c >= a.D) continue;
+                        const rm_f32x4 y = o[r][d] * inv;
+                        if constexpr (BF)
+                            *reinterpret_cast<rm_bf16x4 *>(dst + c * 2) =
+                                rm_bf16x4{static_cast<__bf16>(y[0]), static_cast<__bf16>(y[1]), static_cast<__bf16>(y[2]),
+                                          static_cast<__bf16>(y[3])};
+                        else
+                            *reinterpret_cast<rm_f32x4 *>(dst + c * 4) = y;
+                    }
+                } else {
+                    const int64_t row = (2 * static_cast<int64_t>(w) + starts) * QR + r * 16 + m16;
+                    if (h4 == 0) a.part_ml[row] = make_float2(m[r], sum);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        const int c = 16 * d + 4 * h4;
+                        if (c < a.D) *reinterpret_cast<rm_f32x4 *>(a.part_o + row * a.D + c) = o[r][d];
+                    }
+                }
+            }
+        }
+        if (!more) break;
+        cur = nxt;
+        nxt = after;
+        vis = vis_next;
+        fresh = next_fresh;
+        --left;
+    }
+    if (!a.by_unit && lane == 0) a.info[w] = end_info;
+}
+
+// One workgroup an entry and query head: the parts that waves w .. w + parts - 1 left of a unit, added in a fixed order.
+template <bool BF, int LPR, int QR>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
+    constexpr int GR = 256 / LPR;
+    __shared__ float red[4], sums[GR];
+    __shared__ rm_f32x4 part[GR][LPR];
+    const int e = blockIdx.x / a.rows, r = blockIdx.x - e * a.rows;
+    const int2 info = a.info[e];
+    const int parts = info.y, unit = a.by_unit ? e : info.x, w = a.by_unit ? info.x : e;
+    if (parts < 2) return;
+    const int n = unit / a.units, u = unit - n * a.units, hk = u / a.q_tiles, g = (u - hk * a.q_tiles) * QR + r;
+    if (g >= a.G) return;
+    auto row = [&](int p) { return (2 * static_cast<int64_t>(w + p) + (p == 0)) * QR + r; };
+    const int tid = threadIdx.x, lane = tid % LPR, grp = tid / LPR;
+    float top = -INFINITY;
+    for (int p = tid; p < parts; p += 256) top = fmaxf(top, a.part_ml[row(p)].x);
+    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if ((tid & 63) == 0) red[tid >> 6] = top;
     __syncthreads();
-    const float top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-    float total = 0.0f, r = 0.0f;
-    const int c = threadIdx.x;
-    for (int w = 0; w < 4; ++w) {
-        if (sl[w] == 0.0f) continue;
-        const float f = exp2f(sm[w] - top);
-        total += sl[w] * f;
-        r += so[w][c] * f;
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float ref = top == -INFINITY ? 0.0f : top;
+    const int c = min(lane * 4, a.D - 4);
+    rm_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    float l = 0.0f;
+#pragma unroll 4
+    for (int p = grp; p < parts; p += GR) {
+        const float2 ml = a.part_ml[row(p)];
+        const rm_f32x4 v = *reinterpret_cast<const rm_f32x4 *>(a.part_o + row(p) * a.D + c);
+        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+        l += ml.y * f;
+        o += v * f;
     }
-    r = total == 0.0f ? 0.0f : r / total;
-    if (c >= a.D) return;
-    char *dst = a.o + n * a.o_t + h * a.o_h;
-    if constexpr (BF) reinterpret_cast<__bf16 *>(dst)[c] = static_cast<__bf16>(r);
-    else reinterpret_cast<float *>(dst)[c] = r;
+    part[grp][lane] = o;
+    if (lane == 0) sums[grp] = l;
+    __syncthreads();
+    if (grp != 0 || lane * 4 >= a.D) return;
+    float sum = 0.0f;
+    o = rm_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < GR; ++i) {
+        sum += sums[i];
+        o += part[i][lane];
+    }
+    o *= sum == 0.0f ? 0.0f : 1.0f / sum;
+    char *dst = a.o + n * a.o_t + static_cast<int64_t>(hk * a.G + g) * a.o_h;
+    if constexpr (BF)
+        *reinterpret_cast<rm_bf16x4 *>(dst + c * 2) =
+            rm_bf16x4{static_cast<__bf16>(o[0]), static_cast<__bf16>(o[1]), static_cast<__bf16>(o[2]), static_cast<__bf16>(o[3])};
+    else
+        *reinterpret_cast<rm_f32x4 *>(dst + c * 4) = o;
+}
+
+template <bool BF, int DH, int QR>
+hipError_t go(const PagedPlan &p, const PagedArgs &a, hipStream_t st) {
+    paged_kernel<BF, DH, QR><<<dim3(static_cast<unsigned>(a.waves)), 64, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !p.join) return e;
+    const unsigned entries = static_cast<unsigned>(a.by_unit ? a.N * a.units : a.waves);
+    paged_join_kernel<BF, DH / 4, QR><<<dim3(entries * static_cast<unsigned>(a.rows)), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+template <bool BF, int DH>
+hipError_t by_heads(const PagedPlan &p, const PagedArgs &a, hipStream_t st) {
+    return p.qr == 8 ? go<BF, DH, 8>(p, a, st) : p.qr == 16 ? go<BF, DH, 16>(p, a, st) : go<BF, DH, 32>(p, a, st);
+}
+template <bool BF>
+hipError_t by_width(const PagedPlan &p, const PagedArgs &a, hipStream_t st) {
+    return p.dh == 64 ? by_heads<BF, 64>(p, a, st) : p.dh == 128 ? by_heads<BF, 128>(p, a, st) : by_heads<BF, 256>(p, a, st);
+}
+
+template <bool BF, int DH>
+void shape_of(PagedPlan &p) {
+    const int bytes = p.qr == 8    ? lds_bytes<BF, DH, 8>()
+                      : p.qr == 16 ? lds_bytes<BF, DH, 16>()
+                                   : lds_bytes<BF, DH, 32>();
+    p.kt = Shape<BF, DH>::KT;
+    p.per_cu = std::min(4, 160 * 1024 / bytes);
 }
 
 }  // namespace
 
-hipError_t launch_paged(const PagedArgs &a, bool bf16, hipStream_t st) {
-    const dim3 grid(static_cast<unsigned>(a.N) * a.Hq);
-    if (bf16) paged_kernel<true><<<grid, 256, 0, st>>>(a);
-    else paged_kernel<false><<<grid, 256, 0, st>>>(a);
-    return hipGetLastError();
+void paged_shape(bool bf16, int D, int G, PagedPlan *p) {
+    p->dh = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+    p->qr = G <= 8 ? 8 : G <= 16 ? 16 : 32;
+    if (bf16) p->dh == 64 ? shape_of<true, 64>(*p) : p->dh == 128 ? shape_of<true, 128>(*p) : shape_of<true, 256>(*p);
+    else p->dh == 64 ? shape_of<false, 64>(*p) : p->dh == 128 ? shape_of<false, 128>(*p) : shape_of<false, 256>(*p);
+}
+
+hipError_t launch_paged(const PagedPlan &p, const PagedArgs &a, bool bf16, hipStream_t st) {
+    return bf16 ? by_width<true>(p, a, st) : by_width<false>(p, a, st);
 }
 
 }  // namespace rm_serve

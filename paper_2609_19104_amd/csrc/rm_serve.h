@@ -1,7 +1,7 @@
 // Arguments of the serving-step kernels (page_slots.hip, paged_attn.hip, block_norm.hip).
 #pragma once
 
-#include "rm_internal.h"
+#include "rm_attn_plan.h"
 
 namespace rm_serve {
 
@@ -22,10 +22,26 @@ struct PagedArgs {
     const int32_t *table = nullptr, *seq = nullptr, *pos = nullptr;
     const float *slopes = nullptr;
     int N = 0, seqs = 0, page = 0, n_pages = 0, per = 0, window = 0;
-    int D = 0, Hq = 0, Hk = 0, G = 0;
+    rm_attn::Divisor by_page, by_q_tiles;
+    int D = 0, G = 0;
+    // Units of a token: key heads times blocks of query heads; query heads of a block at most.
+    int units = 0, q_tiles = 0, rows = 0;
+    // Waves, the least tiles of one, and where the parts of divided units are told: [N units] or [waves].
+    int waves = 0, least = 0, by_unit = 0;
     float scale = 0.0f, cap = 0.0f;  // scores in powers of two; with a cap: scale = score scale / cap
+    float *part_o = nullptr;         // [waves][2][rows of a block][D]
+    float2 *part_ml = nullptr;       // [waves][2][rows of a block]
+    int2 *info = nullptr;
 };
-hipError_t launch_paged(const PagedArgs &a, bool bf16, hipStream_t st);
+struct PagedPlan {
+    int dh = 0, qr = 0;          // columns of a row in LDS, query heads of a block
+    int kt = 0, per_cu = 0;      // keys of a tile, waves of a compute unit
+    int waves = 0, units = 0, q_tiles = 0, by_unit = 0;
+    bool join = false;
+    size_t off_ml = 0, off_info = 0, total = 0;
+};
+void paged_shape(bool bf16, int D, int G, PagedPlan *p);  // dh, qr, kt and per_cu
+hipError_t launch_paged(const PagedPlan &p, const PagedArgs &a, bool bf16, hipStream_t st);
 
 struct NormArgs {
     const char *x = nullptr, *f = nullptr;

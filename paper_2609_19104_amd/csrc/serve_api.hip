@@ -32,6 +32,32 @@ rm_status check_pages(int page, int n_pages, int max_pages) {
     return RM_OK;
 }
 
+constexpr int kLeastTiles = 2;
+
+rm_status paged_plan(const rm_attn_shape *s, int n_tok, int page, int max_pages, rm_serve::PagedPlan *p) {
+    rm_status r = check_attn_shape(s);
+    if (r == RM_OK) r = check_pages(page, 1, max_pages);
+    if (r != RM_OK) return r;
+    if (n_tok <= 0) return api_fail(RM_ERR_INVALID_ARG, "n_tok=%d must be positive", n_tok);
+    if (static_cast<int64_t>(n_tok) * s->n_q_heads >= kMaxGroups)
+        return api_fail(RM_ERR_SHAPE, "n_tok x n_q_heads = %d x %d is not below 2^24", n_tok, s->n_q_heads);
+    const int G = s->n_q_heads / s->n_kv_heads;
+    rm_serve::paged_shape(s->dtype == RM_BF16, s->head_dim, G, p);
+    p->q_tiles = static_cast<int>(ceil_div(G, p->qr));
+    p->units = s->n_kv_heads * p->q_tiles;
+    const int64_t units = static_cast<int64_t>(n_tok) * p->units;
+    const int64_t most = units * (ceil_div(static_cast<int64_t>(max_pages) * page, p->kt) + 1);  // tiles, at most
+    if (most > INT32_MAX) return api_fail(RM_ERR_SHAPE, "%lld tiles of keys are more than 2^31 - 1", static_cast<long long>(most));
+    p->waves = static_cast<int>(std::min<int64_t>(256 * p->per_cu, ceil_div(most, kLeastTiles)));
+    p->by_unit = units <= p->waves;
+    p->join = p->waves > 1;
+    const size_t rows = static_cast<size_t>(p->waves) * 2 * p->qr;
+    p->off_ml = align_up(rows * s->head_dim * 4, 256);
+    p->off_info = align_up(p->off_ml + rows * 8, 256);
+    p->total = align_up(p->off_info + static_cast<size_t>(p->by_unit ? units : p->waves) * 8, 256);
+    return RM_OK;
+}
+
 }  // namespace
 
 RM_EXPORT rm_status rm_page_slots(int32_t n_seqs, int32_t max_tok, int32_t page, int32_t n_pages, int32_t max_pages,
@@ -77,11 +103,10 @@ RM_EXPORT rm_status rm_page_slots(int32_t n_seqs, int32_t max_tok, int32_t page,
 RM_EXPORT rm_status rm_paged_attention_workspace_size(const rm_attn_shape *s, int32_t n_tok, int32_t page,
                                                       int32_t max_pages, size_t *bytes) {
     if (!bytes) return api_fail(RM_ERR_INVALID_ARG, "bytes is NULL");
-    rm_status r = check_attn_shape(s);
-    if (r == RM_OK) r = check_pages(page, 1, max_pages);
+    rm_serve::PagedPlan p;
+    const rm_status r = paged_plan(s, n_tok, page, max_pages, &p);
     if (r != RM_OK) return r;
-    if (n_tok <= 0) return api_fail(RM_ERR_INVALID_ARG, "n_tok=%d must be positive", n_tok);
-    *bytes = 0;
+    *bytes = p.total;
     return api_ok();
 }
 
@@ -90,11 +115,11 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
                                        const rm_heads *v, const rm_heads *out, const int32_t *table,
                                        const int32_t *seq, const int32_t *pos, int32_t window, const float *slopes,
                                        void *ws, size_t ws_bytes, void *stream) {
-    rm_status r = check_attn_shape(s);
+    rm_serve::PagedPlan p;
+    rm_status r = paged_plan(s, n_tok, page, max_pages, &p);
     if (r == RM_OK) r = check_pages(page, n_pages, max_pages);
     if (r != RM_OK) return r;
-    if (n_tok <= 0 || n_seqs <= 0)
-        return api_fail(RM_ERR_INVALID_ARG, "n_tok=%d and n_seqs=%d must be positive", n_tok, n_seqs);
+    if (n_seqs <= 0) return api_fail(RM_ERR_INVALID_ARG, "n_seqs=%d must be positive", n_seqs);
     if (!seq && n_seqs < n_tok)
         return api_fail(RM_ERR_SHAPE, "n_seqs=%d tables are fewer than the n_tok=%d tokens (no seq given)", n_seqs, n_tok);
     if (window < 0) return api_fail(RM_ERR_INVALID_ARG, "window=%d must not be negative", window);
@@ -110,12 +135,15 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
     if (!table || !pos) return api_fail(RM_ERR_INVALID_ARG, "table or pos is NULL");
     if (!aligned(table, 4) || !aligned(pos, 4) || !aligned(seq, 4) || !aligned(slopes, 4))
         return api_fail(RM_ERR_ALIGN, "table, seq, pos and slopes must be 4-byte aligned");
-    if (static_cast<int64_t>(n_tok) * s->n_q_heads >= kMaxGroups)
-        return api_fail(RM_ERR_SHAPE, "n_tok x n_q_heads = %d x %d is not below 2^24", n_tok, s->n_q_heads);
     const size_t n4 = static_cast<size_t>(n_tok) * 4;
     const Extent in[7] = {x[0], x[1], x[2], {table, static_cast<size_t>(n_seqs) * max_pages * 4}, {seq, seq ? n4 : 0},
                           {pos, n4}, {slopes, slopes ? static_cast<size_t>(s->n_q_heads) * 4 : 0}};
-    r = check_apart(in, 7, &x[3], 1);
+    if (!ws) return api_fail(RM_ERR_INVALID_ARG, "workspace is NULL");
+    if (!aligned(ws, 256)) return api_fail(RM_ERR_ALIGN, "workspace must be 256-byte aligned");
+    if (ws_bytes < p.total)
+        return api_fail(RM_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu required", ws_bytes, p.total);
+    const Extent written[2] = {x[3], {ws, p.total}};
+    r = check_apart(in, 7, written, 2);
     if (r != RM_OK) return r;
     rm_serve::PagedArgs a;
     a.q = static_cast<const char *>(q->data), a.k = static_cast<const char *>(k->data);
@@ -125,7 +153,13 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
     a.v_p = st[2][0], a.v_t = st[2][1], a.v_h = st[2][2];
     a.table = table, a.seq = seq, a.pos = pos, a.slopes = slopes;
     a.N = n_tok, a.seqs = n_seqs, a.page = page, a.n_pages = n_pages, a.per = max_pages, a.window = window;
-    a.D = D, a.Hq = s->n_q_heads, a.Hk = s->n_kv_heads, a.G = a.Hq / a.Hk;
+    a.D = D, a.G = s->n_q_heads / s->n_kv_heads;
+    a.units = p.units, a.q_tiles = p.q_tiles, a.rows = std::min(a.G, p.qr);
+    a.by_page = rm_attn::divisor(page), a.by_q_tiles = rm_attn::divisor(p.q_tiles);
+    a.waves = p.waves, a.least = kLeastTiles, a.by_unit = p.by_unit;
+    a.part_o = static_cast<float *>(ws);
+    a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.off_ml);
+    a.info = reinterpret_cast<int2 *>(static_cast<char *>(ws) + p.off_info);
     const float log2e = 1.4426950408889634f;
     if (s->softcap > 0.0f) {
         a.cap = s->softcap * log2e;
@@ -133,8 +167,7 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
     } else {
         a.scale = s->scale * log2e;
     }
-    (void)ws, (void)ws_bytes;
-    const hipError_t e = rm_serve::launch_paged(a, s->dtype == RM_BF16, static_cast<hipStream_t>(stream));
+    const hipError_t e = rm_serve::launch_paged(p, a, s->dtype == RM_BF16, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return api_fail(RM_ERR_HIP, "paged attention launch: %s", hipGetErrorString(e));
     return api_ok();
 }

@@ -63,7 +63,7 @@ def test_page_slots_refuses(lib, kw, expected):
 
 
 def _paged(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), N=3, seqs=3, page=16, n_pages=10, per=4, q=None, k=None, v=None,
-           out=None, table=5 * MB, seq=None, pos=6 * MB, window=0, slopes=None, ws=None, ws_bytes=0):
+           out=None, table=5 * MB, seq=None, pos=6 * MB, window=0, slopes=None, ws=64 * MB, ws_bytes=64 * MB):
     q, out = q or H(1 * MB, 0, 512, 64), out or H(4 * MB, 0, 512, 64)
     k, v = k or H(2 * MB, page * 128, 128, 64), v or H(3 * MB, page * 128, 128, 64)
     return lib.rm_paged_attention(ctypes.byref(rm.AttnShape(*shape)), N, seqs, page, n_pages, per, q, k, v, out, table, seq,
@@ -86,6 +86,7 @@ def _paged(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), N=3, seqs=3, page=16, n_page
     (dict(n_pages=0), rm.RM_ERR_INVALID_ARG),
     (dict(per=0), rm.RM_ERR_INVALID_ARG),
     (dict(per=1 << 26), rm.RM_ERR_SHAPE),
+    (dict(N=1 << 15, seqs=1 << 15, per=1 << 18), rm.RM_ERR_SHAPE),  # more tiles than a whole number counts
     (dict(n_pages=1 << 27), rm.RM_ERR_SHAPE),
     (dict(window=-1), rm.RM_ERR_INVALID_ARG),
     (dict(q=H(None, 0, 512, 64)), rm.RM_ERR_INVALID_ARG),
@@ -107,6 +108,12 @@ def _paged(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), N=3, seqs=3, page=16, n_page
     (dict(pos=4 * MB + 64), rm.RM_ERR_INVALID_ARG),
     (dict(seq=4 * MB + 128), rm.RM_ERR_INVALID_ARG),
     (dict(slopes=4 * MB + 128), rm.RM_ERR_INVALID_ARG),
+    (dict(ws=None), rm.RM_ERR_INVALID_ARG),
+    (dict(ws=64 * MB + 128), rm.RM_ERR_ALIGN),
+    (dict(ws_bytes=100), rm.RM_ERR_WORKSPACE),
+    (dict(ws=4 * MB), rm.RM_ERR_INVALID_ARG),                       # over out
+    (dict(ws=3 * MB - 256), rm.RM_ERR_INVALID_ARG),                 # over v
+    (dict(ws=5 * MB - 256), rm.RM_ERR_INVALID_ARG),                 # over the table
 ])
 def test_paged_attention_refuses(lib, kw, expected):
     assert _paged(lib, **kw) == expected
