@@ -1,4 +1,6 @@
 // A paged cache's tables and the cache row of every new token, from the requests' lengths (rm_page_slots).
+#include <algorithm>
+
 #include "rm_serve.h"
 
 namespace rm_serve {
@@ -11,19 +13,27 @@ constexpr int kThreads = 1024;
 constexpr uint32_t kMost = 1u << 30;
 __device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) { return min(a + b, kMost); }
 
+__device__ __forceinline__ int divide(int n, rm_attn::Divisor d) {  // n < 2^30
+    return d.mul == 0 ? n : static_cast<int>(__umulhi(static_cast<uint32_t>(n), d.mul) >> d.shift);
+}
+
 // Running sums of two values over the workgroup's threads, their own included; all gets the sums of everyone.
 __device__ __forceinline__ uint2 scan(uint2 v, uint2 &all, uint2 (&wave_sum)[kThreads / 64]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t x = __shfl_up(v.x, o), y = __shfl_up(v.y, o);
         if (lane >= o) v = make_uint2(add(v.x, x), add(v.y, y));
+    }
+    if (waves == 1) {
+        all = make_uint2(__shfl(v.x, 63), __shfl(v.y, 63));
+        return v;
     }
     __syncthreads();
     if (lane == 63) wave_sum[wave] = v;
     __syncthreads();
     all = make_uint2(0, 0);
     uint2 before = all;
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < waves; ++w) {
         if (w == wave) before = all;
         all = make_uint2(add(all.x, wave_sum[w].x), add(all.y, wave_sum[w].y));
     }
@@ -41,28 +51,41 @@ __device__ __forceinline__ int find(const uint32_t *ends, int n, uint32_t x) {
     return lo;
 }
 
-// One workgroup; requests in chunks of one a thread.
-__global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
+// The row of position p in a request's table (-1: none).
+__device__ __forceinline__ int row_of(const SlotArgs &a, const int32_t *table, int p) {
+    const int i = divide(p, a.by_page), pg = table[i];
+    return pg >= 0 && pg < a.n_pages ? pg * a.page + p - i * a.page : -1;
+}
+
+// One workgroup, which keeps the order of the requests; it takes them in chunks of one a thread.  Bound by its round trips:
+// lengths, then tables and free list, then the stores.  fill: it writes the tokens too.
+__global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fill) {
     __shared__ uint2 wave_sum[kThreads / 64];
     __shared__ uint32_t ends[kThreads], wants[kThreads];
     __shared__ int32_t held[kThreads], begins[kThreads];
-    const int tid = threadIdx.x;
-    const int64_t room = static_cast<int64_t>(a.per) * a.page;
+    const int tid = threadIdx.x, threads = blockDim.x;
+    const int room = a.per * a.page;
+    const bool once = a.B <= threads;  // one chunk: everything is read once
+    auto pages = [&](int tokens) { return tokens > 0 ? static_cast<uint32_t>(divide(tokens - 1, a.by_page) + 1) : 0u; };
+    int n = 0, old = 0;
+    auto fetch = [&](int b) {
+        n = b < a.B ? a.n_new[b] : 0;
+        old = b < a.B ? min(max(a.len[b], 0), room) : 0;
+    };
+    fetch(tid);
     const uint32_t n_free = min(max(a.n_free[0], 0), a.n_pages);
-    auto length = [&](int b) { return static_cast<int>(min(static_cast<int64_t>(max(a.len[b], 0)), room)); };
-    auto pages = [&](int64_t tokens) { return static_cast<uint32_t>((tokens + a.page - 1) / a.page); };
 
     // Ended requests give their pages back.
     uint32_t back = n_free;
-    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-        const int b = b0 + tid;
-        uint2 mine = make_uint2(0, 0), all;
-        if (b < a.B && a.n_new[b] < 0) mine.x = pages(length(b));
-        const uint2 upto = scan(mine, all, wave_sum);
+    for (int b0 = 0; b0 < a.B; b0 += threads) {
+        if (b0 > 0) fetch(b0 + tid);
+        if (!__syncthreads_or(n < 0)) continue;
+        uint2 all;
+        const uint2 upto = scan(make_uint2(n < 0 ? pages(old) : 0, 0), all, wave_sum);
         ends[tid] = upto.x;
         __syncthreads();
-        for (uint32_t k = tid; k < all.x; k += kThreads) {
-            const int r = find(ends, kThreads, k);
+        for (uint32_t k = tid; k < all.x; k += threads) {
+            const int r = find(ends, threads, k);
             const uint32_t i = k - (r > 0 ? ends[r - 1] : 0), to = add(back, k);
             if (to < static_cast<uint32_t>(a.n_pages))
                 a.free_pages[to] = a.table[static_cast<int64_t>(b0 + r) * a.per + i];
@@ -70,61 +93,86 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
         back = add(back, all.x);
         __syncthreads();
     }
-    const uint32_t avail = min(back, static_cast<uint32_t>(a.n_pages));
+    const uint32_t avail = min(back, static_cast<uint32_t>(a.n_pages)), max_tok = a.max_tok;
 
     uint32_t tokens = 0, wanted = 0, taken = 0, refused = 0;  // (taken, refused: of this thread's requests)
-    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+    for (int b0 = 0; b0 < a.B; b0 += threads) {
         const int b = b0 + tid;
+        if (!once) fetch(b);
         const bool is = b < a.B;
-        const int n = is ? a.n_new[b] : 0, old = is ? length(b) : 0;
-        uint2 mine = make_uint2(static_cast<uint32_t>(min(max(n, 0), static_cast<int>(kMost))), 0), all;
-        // The tokens' ends first: they decide which requests fit.
-        uint2 upto = scan(mine, all, wave_sum);
-        const uint32_t end = add(tokens, upto.x), n_all = all.x;
-        const bool fits = n >= 0 && static_cast<int64_t>(old) + n <= room && (n == 0 || end <= static_cast<uint32_t>(a.max_tok));
         const uint32_t have = pages(old);
-        mine.x = fits ? pages(static_cast<int64_t>(old) + n) - have : 0;
-        upto = scan(mine, all, wave_sum);
-        const bool served = fits && (mine.x == 0 || add(wanted, upto.x) <= avail);
-        ends[tid] = end;
-        wants[tid] = upto.x;
-        held[tid] = have;
-        begins[tid] = served ? old : -1;
-        if (served) taken += mine.x;
+        bool fits = n >= 0 && n <= room - old;
+        uint2 mine = make_uint2(static_cast<uint32_t>(min(max(n, 0), static_cast<int>(kMost))), fits ? pages(old + n) - have : 0);
+        uint2 all, upto = scan(mine, all, wave_sum);
+        const uint32_t end = add(tokens, upto.x), n_all = all.x;
+        if (add(tokens, n_all) > max_tok) {  // tokens past the batch's room want no pages
+            fits = fits && (n == 0 || end <= max_tok);
+            if (!fits) mine.y = 0;
+            upto.y = scan(mine, all, wave_sum).y;
+        }
+        const bool served = fits && (mine.y == 0 || add(wanted, upto.y) <= avail);
+        const uint32_t first_want = add(wanted, upto.y - mine.y);  // (exact where it is served)
+        const int start = served ? old : -1;
+        if (served) taken += mine.y;
         if (is) {
             if (n >= 0 && !served) ++refused;
             a.len_out[b] = n < 0 ? 0 : served ? old + n : old;
-            a.start[b] = served ? old : -1;
+            a.start[b] = start;
             a.first[b + 1] = static_cast<int32_t>(end);
             if (b == 0) a.first[0] = 0;
         }
-        __syncthreads();
-        for (uint32_t k = tid; k < all.x; k += kThreads) {
-            const int r = find(wants, kThreads, k);
-            const uint32_t at = add(wanted, k);
-            if (begins[r] < 0 || at >= avail) continue;
-            const uint32_t i = held[r] + k - (r > 0 ? wants[r - 1] : 0);
-            a.table[static_cast<int64_t>(b0 + r) * a.per + i] = a.free_pages[avail - 1 - at];
-        }
-        __syncthreads();
-        const uint32_t last = min(add(tokens, n_all), static_cast<uint32_t>(a.max_tok));
-        for (uint32_t t = tokens + tid; t < last; t += kThreads) {
-            const int r = find(ends, kThreads, t);
-            const int p = begins[r] < 0 ? -1 : static_cast<int>(begins[r] + (t - (r > 0 ? ends[r - 1] : tokens)));
-            int row = -1;
-            if (p >= 0) {
-                const int pg = a.table[static_cast<int64_t>(b0 + r) * a.per + p / a.page];
-                if (pg >= 0 && pg < a.n_pages) row = pg * a.page + p % a.page;
+        int32_t *const table = a.table + static_cast<int64_t>(is ? b : 0) * a.per;
+        if (!__syncthreads_or(n > 1)) {
+            // One token of every request at most: each thread has its own token and its page.
+            if (served && n == 1) {
+                int pg;
+                if (mine.y != 0) {
+                    pg = a.free_pages[avail - 1 - first_want];
+                    table[have] = pg;
+                } else {
+                    pg = table[divide(old, a.by_page)];
+                }
+                if (fill) {
+                    const int in_page = old - divide(old, a.by_page) * a.page;
+                    a.slot[end - 1] = pg >= 0 && pg < a.n_pages ? pg * a.page + in_page : -1;
+                }
             }
-            a.seq[t] = b0 + r;
-            a.pos[t] = p;
-            a.slot[t] = row;
+            if (fill && n == 1 && end <= max_tok) {
+                a.seq[end - 1] = b;
+                a.pos[end - 1] = start;
+                if (!served) a.slot[end - 1] = -1;
+            }
+        } else {
+            ends[tid] = end;
+            wants[tid] = upto.y;
+            held[tid] = have;
+            begins[tid] = start;
+            __syncthreads();
+            for (uint32_t k = tid; k < all.y; k += threads) {
+                const int r = find(wants, threads, k);
+                const uint32_t at = add(wanted, k);
+                if (begins[r] < 0 || at >= avail) continue;
+                const uint32_t i = held[r] + k - (r > 0 ? wants[r - 1] : 0);
+                a.table[static_cast<int64_t>(b0 + r) * a.per + i] = a.free_pages[avail - 1 - at];
+            }
+            if (fill) {
+                __syncthreads();
+                const uint32_t last = min(add(tokens, n_all), max_tok);
+                for (uint32_t t = tokens + tid; t < last; t += threads) {
+                    const int r = find(ends, threads, t);
+                    const int p = begins[r] < 0 ? -1 : static_cast<int>(begins[r] + (t - (r > 0 ? ends[r - 1] : tokens)));
+                    a.seq[t] = b0 + r;
+                    a.pos[t] = p;
+                    a.slot[t] = p < 0 ? -1 : row_of(a, a.table + static_cast<int64_t>(b0 + r) * a.per, p);
+                }
+            }
         }
         tokens = add(tokens, n_all);
-        wanted = add(wanted, all.x);
-        __syncthreads();
+        wanted = add(wanted, all.y);
+        if (!once) __syncthreads();
     }
-    for (uint32_t t = tokens + tid; t < static_cast<uint32_t>(a.max_tok); t += kThreads) a.seq[t] = a.pos[t] = a.slot[t] = -1;
+    if (fill)
+        for (uint32_t t = tokens + tid; t < max_tok; t += threads) a.seq[t] = a.pos[t] = a.slot[t] = -1;
     uint2 all;
     scan(make_uint2(taken, refused), all, wave_sum);
     if (tid == 0) {
@@ -133,10 +181,55 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
     }
 }
 
+constexpr int kFillThreads = 256, kFillTokens = 1024;
+
+// The tokens of a batch that one workgroup would be long about, after the kernel above: a workgroup takes kFillTokens of
+// them.  It finds its first token's request by whole workgroups of comparisons, the others' from there on in LDS.
+__global__ __launch_bounds__(kFillThreads) void fill_kernel(SlotArgs a) {
+    __shared__ uint32_t ends[kFillTokens];
+    __shared__ int32_t begins[kFillTokens];
+    const int tid = threadIdx.x;
+    const uint32_t t0 = blockIdx.x * kFillTokens;
+    const int32_t *const end_of = a.first + 1;
+    int lo = 0, n = a.B + 1;  // the first request that ends above t0 is in [lo, lo + n), a.B if none does
+    while (n > 1) {
+        const int step = (n + kFillThreads - 1) / kFillThreads, i = lo + (tid + 1) * step - 1;
+        const bool below = (tid + 1) * step <= n && i < a.B && static_cast<uint32_t>(end_of[i]) <= t0;
+        const int done = __syncthreads_count(below) * step;
+        lo += done;
+        n = min(n - done, step);
+    }
+    const int count = min(kFillTokens, a.B - lo);  // requests in LDS
+    for (int i = tid; i < count; i += kFillThreads) {
+        ends[i] = end_of[lo + i];
+        begins[i] = a.start[lo + i];
+    }
+    const uint32_t base = lo < a.B ? a.first[lo] : 0;
+    __syncthreads();
+    for (uint32_t t = t0 + tid; t < min(t0 + kFillTokens, static_cast<uint32_t>(a.max_tok)); t += kFillThreads) {
+        int r = find(ends, count, t), b = lo + r, start = -1;
+        uint32_t from = 0;
+        if (r < count) {
+            start = begins[r];
+            from = r > 0 ? ends[r - 1] : base;
+        } else {  // behind those (requests without tokens are many here), or behind the last
+            b += find(reinterpret_cast<const uint32_t *>(end_of) + b, a.B - b, t);
+            if (b < a.B) start = a.start[b], from = a.first[b];
+        }
+        const int p = start < 0 ? -1 : static_cast<int>(start + (t - from));
+        a.seq[t] = b < a.B ? b : -1;
+        a.pos[t] = p;
+        a.slot[t] = p < 0 ? -1 : row_of(a, a.table + static_cast<int64_t>(b) * a.per, p);
+    }
+}
+
 }  // namespace
 
 hipError_t launch_page_slots(const SlotArgs &a, hipStream_t st) {
-    page_slots_kernel<<<1, kThreads, 0, st>>>(a);
+    const bool fill = a.max_tok <= a.most_fill;
+    const int threads = std::min(kThreads, (std::max(a.B, std::min(a.max_tok, fill ? kThreads : 0)) + 63) / 64 * 64);
+    page_slots_kernel<<<1, threads, 0, st>>>(a, fill);
+    if (!fill) fill_kernel<<<(a.max_tok + kFillTokens - 1) / kFillTokens, kFillThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 

@@ -7,6 +7,8 @@ namespace rm_serve {
 
 struct SlotArgs {
     int B = 0, max_tok = 0, page = 0, n_pages = 0, per = 0;  // per: table entries of a request
+    int most_fill = 4096;
+    rm_attn::Divisor by_page;
     const int32_t *n_new = nullptr, *len = nullptr, *n_free = nullptr;
     int32_t *table = nullptr, *free_pages = nullptr;
     int32_t *len_out = nullptr, *n_free_out = nullptr, *refused = nullptr;
@@ -49,7 +51,7 @@ struct NormArgs {
     const float *gain_post = nullptr, *gate = nullptr, *gain_pre = nullptr, *scale = nullptr, *shift = nullptr;
     int64_t gate_b = 0, scale_b = 0, shift_b = 0;  // elements from sample to sample
     int64_t rows = 0;
-    int T = 0, d = 0, norm_post = 0;
+    int T = 0, d = 0, norm_post = 0, many = 2048;
     float x_scale = 1.0f, f_scale = 1.0f, eps = 0.0f;
 };
 hipError_t launch_block_norm(const NormArgs &a, bool x_bf16, bool f_bf16, bool out_bf16, hipStream_t st);

@@ -92,6 +92,7 @@ RM_EXPORT rm_status rm_page_slots(int32_t n_seqs, int32_t max_tok, int32_t page,
     if (o != RM_OK) return o;
     rm_serve::SlotArgs a;
     a.B = n_seqs, a.max_tok = max_tok, a.page = page, a.n_pages = n_pages, a.per = max_pages;
+    a.by_page = rm_attn::divisor(page);
     a.n_new = n_new, a.len = len, a.n_free = n_free, a.table = table, a.free_pages = free_pages;
     a.len_out = len_out, a.n_free_out = n_free_out, a.refused = refused;
     a.first = first, a.start = start, a.seq = seq, a.pos = pos, a.slot = slot;
