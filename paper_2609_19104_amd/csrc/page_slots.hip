@@ -8,6 +8,7 @@ namespace rm_serve {
 namespace {
 
 constexpr int kThreads = 1024;
+constexpr int kAtOnce = 4;  // pages of a thread whose loads are in flight together
 // Running sums stop here, above every number of tokens or pages that a call takes; a sum that stops at its limit may
 // still be taken in any order.
 constexpr uint32_t kMost = 1u << 30;
@@ -84,11 +85,19 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
         const uint2 upto = scan(make_uint2(n < 0 ? pages(old) : 0, 0), all, wave_sum);
         ends[tid] = upto.x;
         __syncthreads();
-        for (uint32_t k = tid; k < all.x; k += threads) {
-            const int r = find(ends, threads, k);
-            const uint32_t i = k - (r > 0 ? ends[r - 1] : 0), to = add(back, k);
-            if (to < static_cast<uint32_t>(a.n_pages))
-                a.free_pages[to] = a.table[static_cast<int64_t>(b0 + r) * a.per + i];
+        for (uint32_t k0 = tid; k0 < all.x; k0 += kAtOnce * threads) {
+            int32_t pg[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const uint32_t k = min(k0 + j * threads, all.x - 1);
+                const int r = find(ends, threads, k);
+                pg[j] = a.table[static_cast<int64_t>(b0 + r) * a.per + (k - (r > 0 ? ends[r - 1] : 0))];
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const uint32_t k = k0 + j * threads, to = add(back, k);
+                if (k < all.x && to < static_cast<uint32_t>(a.n_pages)) a.free_pages[to] = pg[j];
+            }
         }
         back = add(back, all.x);
         __syncthreads();
@@ -148,12 +157,21 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
             held[tid] = have;
             begins[tid] = start;
             __syncthreads();
-            for (uint32_t k = tid; k < all.y; k += threads) {
-                const int r = find(wants, threads, k);
-                const uint32_t at = add(wanted, k);
-                if (begins[r] < 0 || at >= avail) continue;
-                const uint32_t i = held[r] + k - (r > 0 ? wants[r - 1] : 0);
-                a.table[static_cast<int64_t>(b0 + r) * a.per + i] = a.free_pages[avail - 1 - at];
+            // (Pages from avail - wanted on are the served requests' and perhaps a refused one's.)
+            const uint32_t some = min(all.y, avail - min(avail, wanted));
+            for (uint32_t k0 = tid; k0 < some; k0 += kAtOnce * threads) {
+                int32_t pg[kAtOnce];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    pg[j] = a.free_pages[avail - 1 - wanted - min(k0 + j * threads, some - 1)];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    const uint32_t k = k0 + j * threads;
+                    if (k >= some) break;
+                    const int r = find(wants, threads, k);
+                    if (begins[r] >= 0)
+                        a.table[static_cast<int64_t>(b0 + r) * a.per + held[r] + k - (r > 0 ? wants[r - 1] : 0)] = pg[j];
+                }
             }
             if (fill) {
                 __syncthreads();
@@ -181,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
     }
 }
 
-constexpr int kFillThreads = 256, kFillTokens = 1024;
+constexpr int kFillThreads = 256, kFillTokens = 512;
 
 // The tokens of a batch that one workgroup would be long about, after the kernel above: a workgroup takes kFillTokens of
 // them.  It finds its first token's request by whole workgroups of comparisons, the others' from there on in LDS.
@@ -227,7 +245,7 @@ __global__ __launch_bounds__(kFillThreads) void fill_kernel(SlotArgs a) {
 
 hipError_t launch_page_slots(const SlotArgs &a, hipStream_t st) {
     const bool fill = a.max_tok <= a.most_fill;
-    const int threads = std::min(kThreads, (std::max(a.B, std::min(a.max_tok, fill ? kThreads : 0)) + 63) / 64 * 64);
+    const int threads = std::min(kThreads, (std::max(a.B, std::min(a.max_tok, kThreads)) + 63) / 64 * 64);
     page_slots_kernel<<<1, threads, 0, st>>>(a, fill);
     if (!fill) fill_kernel<<<(a.max_tok + kFillTokens - 1) / kFillTokens, kFillThreads, 0, st>>>(a);
     return hipGetLastError();

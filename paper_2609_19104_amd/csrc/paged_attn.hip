@@ -12,10 +12,11 @@ namespace {
 using rm_attn::divide;
 using rm_attn::kRaise;
 
-// A unit is one token, one key head and up to QR query heads of it; its keys are tiles of KT.  All tiles of all units in a
-// row, token by token, are divided evenly among the waves, whatever the lengths are: each wave reads the positions, finds
-// the unit where its share begins and goes on from unit to unit, the next tiles' keys, values, queries and table entries
-// always under way.  A unit that lies in one wave is written by it; what several waves have of one is joined afterwards.
+// A unit is one key head and up to QR of its query heads; a wave has one.  A token's keys are tiles of KT; the tiles of all
+// tokens, one token after the other, are divided evenly among groups of waves, one wave a unit, whatever the lengths are:
+// each wave reads the positions, finds the token where its group's share begins and goes on from token to token, the next
+// tiles' keys, values, queries and table entries always under way.  So the waves of a group read the heads of the same rows
+// at the same time.  A token whose tiles lie in one group's share is written by it; what several have is joined afterwards.
 template <bool BF, int DH>
 struct Shape {
     static constexpr int ES = BF ? 2 : 4, ROWB = DH * ES, CPR = ROWB / 16;
@@ -24,6 +25,7 @@ struct Shape {
     static constexpr int NI = KT / RPI;                           // load instructions of a tile's keys or values
     static constexpr int TILEB = KT * ROWB;
 };
+constexpr int room(int columns) { return columns <= 64 ? 64 : columns <= 128 ? 128 : 256; }
 template <bool BF, int DH, int QR>
 constexpr int lds_bytes() { return 4 * Shape<BF, DH>::TILEB + QR * Shape<BF, DH>::ROWB + 512; }
 
@@ -32,6 +34,35 @@ __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N < 63 ? N : 63) : "memory");
 }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Four loads of 16 bytes a lane, to LDS at lds, lds + 1024 and so on, each from its own base in scalar registers and an
+// offset a lane (as rm_attn::dma16_pair).  nt: keys and values are read once, and pass by the caches' other lines.
+__device__ __forceinline__ void dma16_four(const char *const (&base)[4], const uint32_t (&off)[4], uint32_t lds) {
+    uint32_t keep;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %9\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5 nt\n\t"
+        "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %6 nt\n\t"
+        "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %7 nt\n\t"
+        "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %8 nt\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(keep)
+        : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base[0]), "s"(base[1]), "s"(base[2]), "s"(base[3]),
+          "s"(lds)
+        : "memory", "scc");
+}
+// The same with an address a lane.
+__device__ __forceinline__ void dma16_four(const char *const (&at)[4], uint32_t lds) {
+    uint32_t keep;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt\n\t"
+        "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off nt\n\t"
+        "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, off nt\n\t"
+        "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, off nt\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(keep)
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(lds)
+        : "memory", "scc");
+}
 
 // A load of 4 bytes a lane into LDS at lds + 4 lane (as rm_dma::dma16).
 __device__ __forceinline__ void dma4(const void *g, uint32_t lds) {
@@ -63,6 +94,12 @@ __device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
     return static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo));
 }
 
+__device__ __forceinline__ int64_t at_lane(int64_t x, int lane) {  // (in scalar registers)
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(x), lane);
+    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(x >> 32), lane);
+    return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+
 // The keys [lo, end) that a token at position p of table s sees.
 __device__ __forceinline__ void seen(const PagedArgs &a, int p, int s, int &lo, int &end) {
     const int cap = a.per * a.page;
@@ -75,12 +112,14 @@ __device__ __forceinline__ int tiles(int lo, int end) {  // (one for a token tha
     return max(1, (end + KT - 1) / KT - lo / KT);
 }
 
-template <bool BF, int DH, int QR>
+// Rows have room for DH columns in LDS; the products take DC of them.
+template <bool BF, int DC, int QR>
 __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
+    constexpr int DH = room(DC);
     typedef Shape<BF, DH> S;
     constexpr int ES = S::ES, ROWB = S::ROWB, CPR = S::CPR, RPI = S::RPI, KT = S::KT, NI = S::NI, TILEB = S::TILEB;
     constexpr int RT = QR > 16 ? 2 : 1;         // tiles of 16 query heads
-    constexpr int NS = KT / 16, QF = ROWB / 64, DB = DH / 16, NQ = QR / RPI;
+    constexpr int NS = KT / 16, QF = DC * ES / 64, DB = DC / 16, NQ = QR / RPI;
     constexpr uint64_t kFull = KT == 64 ? ~0ull : (1ull << KT) - 1;
     static_assert(NQ >= 1 && NI >= 1, "load instructions");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[lds_bytes<BF, DH, QR>()];
@@ -89,39 +128,74 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     const uint32_t at_k = rm_dma::lds_addr(lds), at_q = rm_dma::lds_addr(lds_q);
     const uint32_t at_t = at_q + QR * ROWB;
     const int lane = threadIdx.x, m16 = lane & 15, h4 = lane >> 4;
-    const int w = blockIdx.x;
+    const int grp = divide(blockIdx.x, a.by_units), unit = blockIdx.x - grp * a.units;
+    const int hk = divide(unit, a.by_q_tiles), g0 = (unit - hk * a.q_tiles) * QR;  // the unit's key and first query head
+    const int heads = min(QR, a.G - g0);
 
-    // ---------------------------------------------------------------- this wave's share
-    auto weight = [&](int n) {
-        int lo, end;
-        seen(a, a.pos[n], a.seq ? a.seq[n] : n, lo, end);
-        return tiles<KT>(lo, end);
+    // ---------------------------------------------------------------- this group's share
+    // Tokens in blocks of 64 times per, a lane's following each other: their positions, tables and tiles in registers.
+    constexpr int MOST = 8;
+    const int per = min(MOST, (a.N + 63) >> 6);
+    int tp[MOST], ts[MOST], tw[MOST];
+    auto fetch = [&](int n0) __attribute__((always_inline)) {
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) {
+            tp[i] = -1, ts[i] = 0;
+            const int n = n0 + lane * per + i;
+            if (i < per && n < a.N) {
+                tp[i] = a.pos[n];
+                ts[i] = a.seq ? a.seq[n] : n;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) {
+            int lo, end;
+            seen(a, tp[i], ts[i], lo, end);
+            tw[i] = i < per && n0 + lane * per + i < a.N ? tiles<KT>(lo, end) : 0;
+            sum += tw[i];
+        }
+        return sum;
     };
-    int total = 0;
-    for (int n = lane; n < a.N; n += 64) total += weight(n);
+    int total = 0, mine = 0;
+    for (int n0 = 0; n0 < a.N; n0 += 64 * per) {
+        mine = fetch(n0);
+        total += mine;
+    }
     for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
-    total = __builtin_amdgcn_readfirstlane(total) * a.units;
-    const int share = max((total + a.waves - 1) / a.waves, a.least);
-    const int64_t begin64 = static_cast<int64_t>(w) * share;
+    total = __builtin_amdgcn_readfirstlane(total);
+    const int share = max((total + a.groups - 1) / a.groups, a.least);
+    const int64_t begin64 = static_cast<int64_t>(grp) * share;
     if (begin64 >= total) {
-        if (!a.by_unit && lane == 0) a.info[w] = make_int2(0, 0);
+        if (!a.by_token && unit == 0 && lane == 0) a.info[grp] = make_int2(0, 0);
         return;
     }
     const int begin = static_cast<int>(begin64);
     int left = min(share, total - begin);  // tiles of the share that have not been staged
-    int n = 0, before = 0;                 // the token where it begins, and the tiles (of a unit) before it
-    for (int n0 = 0; n0 < a.N; n0 += 64) {
-        const int mine = n0 + lane < a.N ? weight(n0 + lane) : 0;
+    // The token where it begins, the tiles before it, its position and table.
+    int n = 0, before = 0, here_p = -1, here_s = 0;
+    for (int n0 = 0; n0 < a.N; n0 += 64 * per) {
+        if (a.N > 64 * MOST) mine = fetch(n0);
         int upto = mine;
         for (int o = 1; o < 64; o <<= 1) {
             const int v = __shfl_up(upto, o);
             if (lane >= o) upto += v;
         }
-        const uint64_t past = __ballot((before + upto) * a.units > begin);
+        const uint64_t past = __ballot(before + upto > begin);
         if (past != 0) {
             const int l = __builtin_ctzll(past);
-            n = n0 + l;
             before += __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l);
+            n = n0 + l * per;
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < MOST; ++i) {
+                const int each = __builtin_amdgcn_readlane(tw[i], l);
+                if (found) continue;
+                found = before + each > begin;
+                here_p = __builtin_amdgcn_readlane(tp[i], l);
+                here_s = __builtin_amdgcn_readlane(ts[i], l);
+                if (!found) before += each, ++n;
+            }
             break;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
@@ -129,35 +203,29 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
 
     // ---------------------------------------------------------------- tiles
     struct Tile {
-        int n, u, lo, end, t, t0, t1;  // token, unit of it, its keys and tiles
+        int n, lo, end, t, t0, t1;  // token, its keys and tiles
         int pos, seq;
-        int base;                      // the unit's first tile among all
+        int base;                   // the token's first tile among all
     };
     auto enter = [&](Tile &c, int p, int s) __attribute__((always_inline)) {  // c.n's keys
         c.pos = p, c.seq = s;
         seen(a, p, s, c.lo, c.end);
-        c.t0 = c.lo / KT;
+        c.t = c.t0 = c.lo / KT;
         c.t1 = c.t0 + tiles<KT>(c.lo, c.end);
         if (c.end == 0) c.seq = 0;
     };
-    auto place_of = [&](int i, int &p, int &s) __attribute__((always_inline)) {
-        i = min(i, a.N - 1);
-        p = scalar(a.pos, i);
-        s = a.seq ? scalar(a.seq, i) : i;
-    };
     int next_p, next_s;  // the next token's
+    auto look_at = [&](int i) __attribute__((always_inline)) {
+        i = min(i, a.N - 1);
+        next_p = scalar(a.pos, i);
+        next_s = a.seq ? scalar(a.seq, i) : i;
+    };
     auto advance = [&](Tile &c) __attribute__((always_inline)) {
         if (++c.t < c.t1) return;
         c.base += c.t1 - c.t0;
-        if (++c.u < a.units) {
-            c.t = c.t0;
-            return;
-        }
-        c.u = 0;
         ++c.n;
         enter(c, next_p, next_s);
-        place_of(c.n + 1, next_p, next_s);
-        c.t = c.t0;
+        look_at(c.n + 1);
     };
 
     const int lrow = lane / CPR;
@@ -178,33 +246,51 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     auto stage = [&](const Tile &c, int slot, int buf, bool queries) __attribute__((always_inline)) -> uint64_t {
         const int j = c.t * KT + (lane & (KT - 1)), jj = min(j, max(c.end - 1, 0));
         const int pg = lds_t[slot * 64 + lane];
-        const bool ok = j >= c.lo && j < c.end && static_cast<uint32_t>(pg) < static_cast<uint32_t>(a.n_pages);
-        const int in_page = jj - divide(jj, a.by_page) * a.page;
-        const int64_t ko = ok ? pg * a.k_p + in_page * a.k_t : 0, vo = ok ? pg * a.v_p + in_page * a.v_t : 0;
-        const int hk = divide(c.u, a.by_q_tiles), qt = c.u - hk * a.q_tiles;
+        const bool is = static_cast<uint32_t>(pg) < static_cast<uint32_t>(a.n_pages), ok = is && j >= c.lo && j < c.end;
+        // (Where a load instruction's rows are of one page, those behind the last key are that page's next rows.)
+        const int at = a.whole ? j : jj;
+        const int64_t p = is ? pg : 0, in_page = at - divide(at, a.by_page) * a.page;
+        const int64_t ko = p * a.k_p + in_page * a.k_t, vo = p * a.v_p + in_page * a.v_t;
         if (queries) {
-            const int h0 = hk * a.G + qt * QR, most = min(QR, a.G - qt * QR) - 1;
             const char *q = a.q + c.n * a.q_t;
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
                 const uint32_t ch = min(chunk_k ^ static_cast<uint32_t>(swz_k(i * RPI)), last_chunk);
-                rm_dma::dma16(q + (h0 + min(i * RPI + lrow, most)) * a.q_h + ch * 16,
+                rm_dma::dma16(q + (hk * a.G + g0 + min(i * RPI + lrow, heads - 1)) * a.q_h + ch * 16,
                               __builtin_amdgcn_readfirstlane(at_q + i * 1024));
             }
         }
-        const char *k = a.k + hk * a.k_h, *v = a.v + hk * a.v_h;
+        auto rows = [&](const char *base, int64_t from, int64_t step, bool values, uint32_t to) __attribute__((always_inline)) {
+            auto chunk = [&](int i) {
+                const uint32_t x = values ? chunk_v ^ static_cast<uint32_t>(swz_v(i * RPI))
+                                          : chunk_k ^ static_cast<uint32_t>(swz_k(i * RPI));
+                return min(x, last_chunk) * 16;
+            };
+            if (a.whole) {  // the rows of an instruction follow each other
+                const uint32_t own = lrow * static_cast<uint32_t>(step);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const uint32_t ch = min(chunk_k ^ static_cast<uint32_t>(swz_k(i * RPI)), last_chunk);
-            rm_dma::dma16(k + from_lane(ko, i * RPI + lrow) + ch * 16,
-                          __builtin_amdgcn_readfirstlane(at_k + buf * 2 * TILEB + i * 1024));
-        }
+                for (int i0 = 0; i0 < NI; i0 += 4) {
+                    const char *b[4];
+                    uint32_t off[4];
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const uint32_t ch = min(chunk_v ^ static_cast<uint32_t>(swz_v(i * RPI)), last_chunk);
-            rm_dma::dma16(v + from_lane(vo, i * RPI + lrow) + ch * 16,
-                          __builtin_amdgcn_readfirstlane(at_k + buf * 2 * TILEB + TILEB + i * 1024));
-        }
+                    for (int i = 0; i < 4; ++i) {
+                        b[i] = base + at_lane(from, (i0 + i) * RPI);
+                        off[i] = own + chunk(i0 + i);
+                    }
+                    dma16_four(b, off, __builtin_amdgcn_readfirstlane(to + i0 * 1024));
+                }
+            } else {
+#pragma unroll
+                for (int i0 = 0; i0 < NI; i0 += 4) {
+                    const char *b[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) b[i] = base + from_lane(from, (i0 + i) * RPI + lrow) + chunk(i0 + i);
+                    dma16_four(b, __builtin_amdgcn_readfirstlane(to + i0 * 1024));
+                }
+            }
+        };
+        rows(a.k + hk * a.k_h, ko, a.k_t, false, at_k + buf * 2 * TILEB);
+        rows(a.v + hk * a.v_h, vo, a.v_t, true, at_k + buf * 2 * TILEB + TILEB);
         return __ballot(ok) & kFull;
     };
 
@@ -221,16 +307,10 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
 
     Tile cur;
     cur.n = n;
-    {
-        int p, s;
-        place_of(n, p, s);
-        place_of(n + 1, next_p, next_s);
-        enter(cur, p, s);
-        const int in = begin - before * a.units, each = cur.t1 - cur.t0;
-        cur.u = in / each;
-        cur.t = cur.t0 + (in - cur.u * each);
-        cur.base = begin - (cur.t - cur.t0);
-    }
+    look_at(n + 1);
+    enter(cur, here_p, here_s);
+    cur.base = before;
+    cur.t += begin - before;
     fetch_table(cur, 0);
     wait_loads<0>();
     Tile nxt = cur;
@@ -238,17 +318,19 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     if (left > 0) advance(nxt);
     fetch_table(nxt, 1);
     uint64_t vis = stage(cur, 0, 0, true), vis_next = 0;
-    bool fresh = true;  // cur is the first tile of a unit here
+    bool fresh = true;  // cur is the first tile of a token here
 
     Frag qf[RT][QF];
     rm_f32x4 o[RT][DB];
     float m[RT], l[RT], slope[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+        slope[r] = a.slopes ? a.slopes[hk * a.G + g0 + min(r * 16 + m16, heads - 1)] * rm_attn::kLog2e : 0.0f;
     int2 end_info = make_int2(0, 0);
     for (int turn = 0;; turn ^= 1) {
-        const bool more = left > 0, next_fresh = more && (nxt.u != cur.u || nxt.n != cur.n);
+        const bool more = left > 0, next_fresh = more && nxt.n != cur.n;
         wait_loads<2 * NI>();  // the next tile's table entries, and this one's queries
         if (fresh) {
-            const int hk = divide(cur.u, a.by_q_tiles), head = hk * a.G, g0 = (cur.u - hk * a.q_tiles) * QR;
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 const uint8_t *rows = lds_q + r * 16 * ROWB;
@@ -266,7 +348,6 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
                 }
                 m[r] = -INFINITY;
                 l[r] = 0.0f;
-                slope[r] = a.slopes ? a.slopes[head + min(g0 + r * 16 + m16, a.G - 1)] * rm_attn::kLog2e : 0.0f;
 #pragma unroll
                 for (int d = 0; d < DB; ++d) o[r][d] = rm_f32x4{};
             }
@@ -398,24 +479,22 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             }
         }
 
-        // ---------------------------------------------------------------- the unit's end, or the share's
+        // ---------------------------------------------------------------- the token's end, or the share's
         if (!more || next_fresh) {
             const bool starts = cur.base >= begin, ends = cur.t + 1 == cur.t1;
-            const int unit = cur.n * a.units + cur.u;
-            const int hk = divide(cur.u, a.by_q_tiles), qt = cur.u - hk * a.q_tiles;
             if (starts) {
-                const int parts = (cur.base + (cur.t1 - cur.t0) - 1) / share - w + 1;
-                if (a.by_unit && lane == 0) a.info[unit] = make_int2(w, parts);
-                if (!ends) end_info = make_int2(unit, parts);
+                const int parts = (cur.base + (cur.t1 - cur.t0) - 1) / share - grp + 1;
+                if (a.by_token && unit == 0 && lane == 0) a.info[cur.n] = make_int2(grp, parts);
+                if (!ends) end_info = make_int2(cur.n, parts);
             }
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 const float sum = rows_sum(l[r]);
-                const int g = qt * QR + r * 16 + m16;
-                if (r * 16 + m16 >= QR || g >= a.G) continue;
+                const int g = r * 16 + m16;
+                if (g >= heads) continue;
                 if (starts && ends) {
                     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    char *dst = a.o + cur.n * a.o_t + static_cast<int64_t>(hk * a.G + g) * a.o_h;
+                    char *dst = a.o + cur.n * a.o_t + static_cast<int64_t>(hk * a.G + g0 + g) * a.o_h;
 #pragma unroll
                     for (int d = 0; d < DB; ++d) {
                         const int c = 16 * d + 4 * h4;
@@ -429,7 +508,7 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
                             *reinterpret_cast<rm_f32x4 *>(dst + c * 4) = y;
                     }
                 } else {
-                    const int64_t row = (2 * static_cast<int64_t>(w) + starts) * QR + r * 16 + m16;
+                    const int64_t row = ((2 * static_cast<int64_t>(grp) + starts) * a.units + unit) * QR + g;
                     if (h4 == 0) a.part_ml[row] = make_float2(m[r], sum);
 #pragma unroll
                     for (int d = 0; d < DB; ++d) {
@@ -446,41 +525,63 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         fresh = next_fresh;
         --left;
     }
-    if (!a.by_unit && lane == 0) a.info[w] = end_info;
+    if (!a.by_token && unit == 0 && lane == 0) a.info[grp] = end_info;
 }
 
-// One workgroup an entry and query head: the parts that waves w .. w + parts - 1 left of a unit, added in a fixed order.
+// One workgroup an entry, unit and query head of it: the parts that groups of waves left of a token, in a fixed order.
 template <bool BF, int LPR, int QR>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
     constexpr int GR = 256 / LPR;
-    __shared__ float red[4], sums[GR];
+    __shared__ float tops[GR], sums[GR];
     __shared__ rm_f32x4 part[GR][LPR];
-    const int e = blockIdx.x / a.rows, r = blockIdx.x - e * a.rows;
+    const int each = a.units * a.rows, e = blockIdx.x / each, ur = blockIdx.x - e * each;
+    const int u = ur / a.rows, r = ur - u * a.rows;
     const int2 info = a.info[e];
-    const int parts = info.y, unit = a.by_unit ? e : info.x, w = a.by_unit ? info.x : e;
+    const int parts = info.y, n = a.by_token ? e : info.x, first = a.by_token ? info.x : e;
     if (parts < 2) return;
-    const int n = unit / a.units, u = unit - n * a.units, hk = u / a.q_tiles, g = (u - hk * a.q_tiles) * QR + r;
+    const int hk = u / a.q_tiles, g = (u - hk * a.q_tiles) * QR + r;
     if (g >= a.G) return;
-    auto row = [&](int p) { return (2 * static_cast<int64_t>(w + p) + (p == 0)) * QR + r; };
+    auto row = [&](int p) { return ((2 * static_cast<int64_t>(first + p) + (p == 0)) * a.units + u) * QR + r; };
     const int tid = threadIdx.x, lane = tid % LPR, grp = tid / LPR;
-    float top = -INFINITY;
-    for (int p = tid; p < parts; p += 256) top = fmaxf(top, a.part_ml[row(p)].x);
-    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if ((tid & 63) == 0) red[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float ref = top == -INFINITY ? 0.0f : top;
     const int c = min(lane * 4, a.D - 4);
     rm_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    float l = 0.0f;
-#pragma unroll 4
-    for (int p = grp; p < parts; p += GR) {
-        const float2 ml = a.part_ml[row(p)];
-        const rm_f32x4 v = *reinterpret_cast<const rm_f32x4 *>(a.part_o + row(p) * a.D + c);
-        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-        l += ml.y * f;
-        o += v * f;
+    float m = -INFINITY, l = 0.0f;
+    for (int p0 = grp; p0 < parts; p0 += 4 * GR) {
+        float2 ml[4];
+        rm_f32x4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t at = row(min(p0 + i * GR, parts - 1));
+            ml[i] = a.part_ml[at];
+            v[i] = *reinterpret_cast<const rm_f32x4 *>(a.part_o + at * a.D + c);
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (p0 + i * GR >= parts) ml[i] = make_float2(-INFINITY, 0.0f);
+            top = fmaxf(top, ml[i].x);
+        }
+        const float ref = top == -INFINITY ? 0.0f : top;
+        float f = __builtin_amdgcn_exp2f(m - ref);
+        l *= f;
+        o *= f;
+        m = top;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (ml[i].y == 0.0f) continue;  // (no key with a weight: its sums are zeros)
+            f = __builtin_amdgcn_exp2f(ml[i].x - ref);
+            l += ml[i].y * f;
+            o += v[i] * f;
+        }
     }
+    if (lane == 0) tops[grp] = m;
+    __syncthreads();
+    float top = tops[0];
+#pragma unroll
+    for (int i = 1; i < GR; ++i) top = fmaxf(top, tops[i]);
+    const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+    o *= f;
+    l *= f;
     part[grp][lane] = o;
     if (lane == 0) sums[grp] = l;
     __syncthreads();
@@ -501,22 +602,26 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
         *reinterpret_cast<rm_f32x4 *>(dst + c * 4) = o;
 }
 
-template <bool BF, int DH, int QR>
+template <bool BF, int DC, int QR>
 hipError_t go(const PagedPlan &p, const PagedArgs &a, hipStream_t st) {
-    paged_kernel<BF, DH, QR><<<dim3(static_cast<unsigned>(a.waves)), 64, 0, st>>>(a);
+    paged_kernel<BF, DC, QR><<<dim3(static_cast<unsigned>(a.groups) * a.units), 64, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.join) return e;
-    const unsigned entries = static_cast<unsigned>(a.by_unit ? a.N * a.units : a.waves);
-    paged_join_kernel<BF, DH / 4, QR><<<dim3(entries * static_cast<unsigned>(a.rows)), 256, 0, st>>>(a);
+    const unsigned entries = static_cast<unsigned>(std::min(a.N, a.groups));
+    paged_join_kernel<BF, room(DC) / 4, QR><<<dim3(entries * a.units * a.rows), 256, 0, st>>>(a);
     return hipGetLastError();
 }
-template <bool BF, int DH>
+template <bool BF, int DC>
 hipError_t by_heads(const PagedPlan &p, const PagedArgs &a, hipStream_t st) {
-    return p.qr == 8 ? go<BF, DH, 8>(p, a, st) : p.qr == 16 ? go<BF, DH, 16>(p, a, st) : go<BF, DH, 32>(p, a, st);
+    return p.qr == 8 ? go<BF, DC, 8>(p, a, st) : p.qr == 16 ? go<BF, DC, 16>(p, a, st) : go<BF, DC, 32>(p, a, st);
 }
+// The least of 64, 96, 128, 192 and 256 columns that hold the head.
 template <bool BF>
 hipError_t by_width(const PagedPlan &p, const PagedArgs &a, hipStream_t st) {
-    return p.dh == 64 ? by_heads<BF, 64>(p, a, st) : p.dh == 128 ? by_heads<BF, 128>(p, a, st) : by_heads<BF, 256>(p, a, st);
+    if (a.D <= 64) return by_heads<BF, 64>(p, a, st);
+    if (a.D <= 96) return by_heads<BF, 96>(p, a, st);
+    if (a.D <= 128) return by_heads<BF, 128>(p, a, st);
+    return a.D <= 192 ? by_heads<BF, 192>(p, a, st) : by_heads<BF, 256>(p, a, st);
 }
 
 template <bool BF, int DH>
@@ -525,16 +630,17 @@ void shape_of(PagedPlan &p) {
                       : p.qr == 16 ? lds_bytes<BF, DH, 16>()
                                    : lds_bytes<BF, DH, 32>();
     p.kt = Shape<BF, DH>::KT;
+    p.rpi = Shape<BF, DH>::RPI;
     p.per_cu = std::min(4, 160 * 1024 / bytes);
 }
 
 }  // namespace
 
 void paged_shape(bool bf16, int D, int G, PagedPlan *p) {
-    p->dh = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+    const int dh = room(D);
     p->qr = G <= 8 ? 8 : G <= 16 ? 16 : 32;
-    if (bf16) p->dh == 64 ? shape_of<true, 64>(*p) : p->dh == 128 ? shape_of<true, 128>(*p) : shape_of<true, 256>(*p);
-    else p->dh == 64 ? shape_of<false, 64>(*p) : p->dh == 128 ? shape_of<false, 128>(*p) : shape_of<false, 256>(*p);
+    if (bf16) dh == 64 ? shape_of<true, 64>(*p) : dh == 128 ? shape_of<true, 128>(*p) : shape_of<true, 256>(*p);
+    else dh == 64 ? shape_of<false, 64>(*p) : dh == 128 ? shape_of<false, 128>(*p) : shape_of<false, 256>(*p);
 }
 
 hipError_t launch_paged(const PagedPlan &p, const PagedArgs &a, bool bf16, hipStream_t st) {

@@ -45,16 +45,15 @@ rm_status paged_plan(const rm_attn_shape *s, int n_tok, int page, int max_pages,
     rm_serve::paged_shape(s->dtype == RM_BF16, s->head_dim, G, p);
     p->q_tiles = static_cast<int>(ceil_div(G, p->qr));
     p->units = s->n_kv_heads * p->q_tiles;
-    const int64_t units = static_cast<int64_t>(n_tok) * p->units;
-    const int64_t most = units * (ceil_div(static_cast<int64_t>(max_pages) * page, p->kt) + 1);  // tiles, at most
+    const int64_t most = n_tok * (ceil_div(static_cast<int64_t>(max_pages) * page, p->kt) + 1);  // tiles, at most
     if (most > INT32_MAX) return api_fail(RM_ERR_SHAPE, "%lld tiles of keys are more than 2^31 - 1", static_cast<long long>(most));
-    p->waves = static_cast<int>(std::min<int64_t>(256 * p->per_cu, ceil_div(most, kLeastTiles)));
-    p->by_unit = units <= p->waves;
-    p->join = p->waves > 1;
-    const size_t rows = static_cast<size_t>(p->waves) * 2 * p->qr;
+    p->groups = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(256 * p->per_cu / p->units, ceil_div(most, kLeastTiles))));
+    p->by_token = n_tok <= p->groups;
+    p->join = p->groups > 1;
+    const size_t rows = static_cast<size_t>(p->groups) * 2 * p->units * p->qr;
     p->off_ml = align_up(rows * s->head_dim * 4, 256);
     p->off_info = align_up(p->off_ml + rows * 8, 256);
-    p->total = align_up(p->off_info + static_cast<size_t>(p->by_unit ? units : p->waves) * 8, 256);
+    p->total = align_up(p->off_info + static_cast<size_t>(std::min(n_tok, p->groups)) * 8, 256);
     return RM_OK;
 }
 
@@ -157,7 +156,9 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
     a.D = D, a.G = s->n_q_heads / s->n_kv_heads;
     a.units = p.units, a.q_tiles = p.q_tiles, a.rows = std::min(a.G, p.qr);
     a.by_page = rm_attn::divisor(page), a.by_q_tiles = rm_attn::divisor(p.q_tiles);
-    a.waves = p.waves, a.least = kLeastTiles, a.by_unit = p.by_unit;
+    a.by_units = rm_attn::divisor(p.units);
+    a.groups = p.groups, a.least = kLeastTiles, a.by_token = p.by_token;
+    a.whole = page % p.rpi == 0 && a.k_t < 1 << 28 && a.v_t < 1 << 28;
     a.part_o = static_cast<float *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.off_ml);
     a.info = reinterpret_cast<int2 *>(static_cast<char *>(ws) + p.off_info);

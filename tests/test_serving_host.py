@@ -86,7 +86,7 @@ def _paged(lib, *, shape=(8, 2, 64, 1, 0.125, 0.0), N=3, seqs=3, page=16, n_page
     (dict(n_pages=0), rm.RM_ERR_INVALID_ARG),
     (dict(per=0), rm.RM_ERR_INVALID_ARG),
     (dict(per=1 << 26), rm.RM_ERR_SHAPE),
-    (dict(N=1 << 15, seqs=1 << 15, per=1 << 18), rm.RM_ERR_SHAPE),  # more tiles than a whole number counts
+    (dict(N=1 << 17, seqs=1 << 17, per=1 << 22), rm.RM_ERR_SHAPE),  # more tiles than a whole number counts
     (dict(n_pages=1 << 27), rm.RM_ERR_SHAPE),
     (dict(window=-1), rm.RM_ERR_INVALID_ARG),
     (dict(q=H(None, 0, 512, 64)), rm.RM_ERR_INVALID_ARG),
