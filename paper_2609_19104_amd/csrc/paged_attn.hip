@@ -73,6 +73,22 @@ __device__ __forceinline__ void dma4(const void *g, uint32_t lds) {
                  : "memory");
 }
 
+// The value, as if it became known here only: what is made of it then stays where it is used, instead of taking registers
+// and time in front of the loop.
+__device__ __forceinline__ int here(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// The kernel's arguments, to be read when they are used: kept from the start, they would take the scalar registers of the
+// loop.
+typedef const __attribute__((address_space(4))) PagedArgs *Arguments;
+__device__ __forceinline__ Arguments again() {
+    auto p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return (Arguments)p;
+}
+
 // A whole number that is the same in every lane, read by way of the scalar cache: not among the loads that the waits count.
 __device__ __forceinline__ int32_t scalar(const int32_t *p, int i) {
     typedef const __attribute__((address_space(4))) int32_t *constant;
@@ -94,34 +110,44 @@ __device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
     return static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo));
 }
 
-__device__ __forceinline__ int64_t at_lane(int64_t x, int lane) {  // (in scalar registers)
-    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(x), lane);
-    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(x >> 32), lane);
-    return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+// The sum of a value over the lanes up to the own one, in data-parallel steps along the rows of 16 lanes and across them.
+__device__ __forceinline__ int running_sum(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+    return v;
 }
 
 // The keys [lo, end) that a token at position p of table s sees.
-__device__ __forceinline__ void seen(const PagedArgs &a, int p, int s, int &lo, int &end) {
+template <class A>
+__device__ __forceinline__ void seen(const A &a, int p, int s, int &lo, int &end) {
     const int cap = a.per * a.page;
-    end = p >= 0 && s >= 0 && s < a.seqs ? min(p, cap - 1) + 1 : 0;
-    lo = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
-    if (lo >= end) lo = end = 0;
+    const bool is = (p >= 0) & (static_cast<uint32_t>(s) < static_cast<uint32_t>(a.seqs));
+    end = is ? min(p, cap - 1) + 1 : 0;
+    const bool cut = (a.window > 0) & (p >= a.window);
+    lo = cut ? p - a.window + 1 : 0;
+    const bool any = lo < end;
+    lo = any ? lo : 0;
+    end = any ? end : 0;
 }
 template <int KT>
 __device__ __forceinline__ int tiles(int lo, int end) {  // (one for a token that sees nothing: its zeros are written)
     return max(1, (end + KT - 1) / KT - lo / KT);
 }
 
-// Rows have room for DH columns in LDS; the products take DC of them.
-template <bool BF, int DC, int QR>
+// Rows have room for DH columns in LDS; the products take DC of them.  WHOLE: the rows of a load instruction are of one page.
+template <bool BF, bool WHOLE, int DC, int QR>
 __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     constexpr int DH = room(DC);
     typedef Shape<BF, DH> S;
     constexpr int ES = S::ES, ROWB = S::ROWB, CPR = S::CPR, RPI = S::RPI, KT = S::KT, NI = S::NI, TILEB = S::TILEB;
     constexpr int RT = QR > 16 ? 2 : 1;         // tiles of 16 query heads
     constexpr int NS = KT / 16, QF = DC * ES / 64, DB = DC / 16, NQ = QR / RPI;
-    constexpr uint64_t kFull = KT == 64 ? ~0ull : (1ull << KT) - 1;
-    static_assert(NQ >= 1 && NI >= 1, "load instructions");
+    constexpr uint64_t kFull = ~0ull >> (64 - KT);
+    static_assert(NQ >= 1 && NI % 4 == 0 && DC / 16 % (NI / 4) == 0, "load instructions");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[lds_bytes<BF, DH, QR>()];
     uint8_t *const lds_q = lds + 4 * TILEB;
     int32_t *const lds_t = reinterpret_cast<int32_t *>(lds_q + QR * ROWB);
@@ -133,72 +159,85 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     const int heads = min(QR, a.G - g0);
 
     // ---------------------------------------------------------------- this group's share
-    // Tokens in blocks of 64 times per, a lane's following each other: their positions, tables and tiles in registers.
-    constexpr int MOST = 8;
-    const int per = min(MOST, (a.N + 63) >> 6);
-    int tp[MOST], ts[MOST], tw[MOST];
-    auto fetch = [&](int n0) __attribute__((always_inline)) {
-        int sum = 0;
-#pragma unroll
-        for (int i = 0; i < MOST; ++i) {
-            tp[i] = -1, ts[i] = 0;
-            const int n = n0 + lane * per + i;
-            if (i < per && n < a.N) {
-                tp[i] = a.pos[n];
-                ts[i] = a.seq ? a.seq[n] : n;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < MOST; ++i) {
-            int lo, end;
-            seen(a, tp[i], ts[i], lo, end);
-            tw[i] = i < per && n0 + lane * per + i < a.N ? tiles<KT>(lo, end) : 0;
-            sum += tw[i];
-        }
-        return sum;
+    int share, begin, left;       // tiles of a share, the first one's number, tiles that have not been staged
+    int n, before;                // the token where it begins, and the tiles before it,
+    int here_p, here_s, next_p, next_s;  // its position and table, and the next token's
+    const int32_t *const seqs = a.seq ? a.seq : a.pos;  // (something to load from either way)
+    auto look_at = [&](int i) __attribute__((always_inline)) {
+        const Arguments b = again();
+        const int32_t *pos = b->pos, *seq = b->seq;
+        i = min(i, b->N - 1);
+        next_p = scalar(pos, i);
+        next_s = seq ? scalar(seq, i) : i;
     };
-    int total = 0, mine = 0;
-    for (int n0 = 0; n0 < a.N; n0 += 64 * per) {
-        mine = fetch(n0);
-        total += mine;
-    }
-    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
-    total = __builtin_amdgcn_readfirstlane(total);
-    const int share = max((total + a.groups - 1) / a.groups, a.least);
-    const int64_t begin64 = static_cast<int64_t>(grp) * share;
-    if (begin64 >= total) {
-        if (!a.by_token && unit == 0 && lane == 0) a.info[grp] = make_int2(0, 0);
-        return;
-    }
-    const int begin = static_cast<int>(begin64);
-    int left = min(share, total - begin);  // tiles of the share that have not been staged
-    // The token where it begins, the tiles before it, its position and table.
-    int n = 0, before = 0, here_p = -1, here_s = 0;
-    for (int n0 = 0; n0 < a.N; n0 += 64 * per) {
-        if (a.N > 64 * MOST) mine = fetch(n0);
-        int upto = mine;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(upto, o);
-            if (lane >= o) upto += v;
-        }
-        const uint64_t past = __ballot(before + upto > begin);
-        if (past != 0) {
-            const int l = __builtin_ctzll(past);
-            before += __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l);
-            n = n0 + l * per;
-            bool found = false;
+    auto divided = [&](int total) __attribute__((always_inline)) {  // false: there is nothing for this group
+        share = max(divide(total + a.groups - 1, a.by_groups), a.least);
+        const int64_t first = static_cast<int64_t>(grp) * share;
+        begin = static_cast<int>(min(first, static_cast<int64_t>(total)));
+        left = min(share, total - begin);
+        if (left <= 0 && !a.by_token && unit == 0 && lane == 0) a.info[grp] = make_int2(0, 0);
+        return left > 0;
+    };
+    if (__builtin_expect(a.N <= 64, true)) {  // a token a lane
+        const int i = min(lane, a.N - 1), p = a.pos[i], t = a.seq ? seqs[i] : i;
+        int lo, end;
+        seen(a, p, t, lo, end);
+        const int mine = lane < a.N ? tiles<KT>(lo, end) : 0, upto = running_sum(mine);
+        if (!divided(__builtin_amdgcn_readlane(upto, 63))) return;
+        n = __builtin_ctzll(__ballot(upto > begin) | 1ull << 63);
+        before = __builtin_amdgcn_readlane(upto, n) - __builtin_amdgcn_readlane(mine, n);
+        here_p = __builtin_amdgcn_readlane(p, n), here_s = __builtin_amdgcn_readlane(t, n);
+        next_p = __builtin_amdgcn_readlane(p, min(n + 1, 63)), next_s = __builtin_amdgcn_readlane(t, min(n + 1, 63));
+    } else {  // blocks of 512 tokens, a lane's eight following each other
+        constexpr int PER = 8;
+        int tw[PER], mine = 0, total = 0;
+        auto fetch = [&](int n0) __attribute__((always_inline)) {
+            int tp[PER], ts[PER];
 #pragma unroll
-            for (int i = 0; i < MOST; ++i) {
-                const int each = __builtin_amdgcn_readlane(tw[i], l);
-                if (found) continue;
-                found = before + each > begin;
-                here_p = __builtin_amdgcn_readlane(tp[i], l);
-                here_s = __builtin_amdgcn_readlane(ts[i], l);
-                if (!found) before += each, ++n;
+            for (int i = 0; i < PER; ++i) {
+                const int at = min(n0 + lane * PER + i, a.N - 1);
+                tp[i] = a.pos[at];
+                ts[i] = seqs[at];
             }
-            break;
+            mine = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                int lo, end;
+                seen(a, tp[i], a.seq ? ts[i] : n0 + lane * PER + i, lo, end);
+                tw[i] = n0 + lane * PER + i < a.N ? tiles<KT>(lo, end) : 0;
+                mine += tw[i];
+            }
+        };
+#pragma unroll 1
+        for (int n0 = 0; n0 < a.N; n0 += 64 * PER) {
+            fetch(n0);
+            total += mine;
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
+        if (!divided(__builtin_amdgcn_readlane(running_sum(total), 63))) return;
+        n = a.N - 1, before = 0;
+#pragma unroll 1
+        for (int n0 = 0; n0 < a.N; n0 += 64 * PER) {
+            if (a.N > 64 * PER) fetch(n0);
+            const int upto = running_sum(mine);
+            const uint64_t past = __ballot(before + upto > begin);
+            if (past != 0) {
+                const int l = __builtin_ctzll(past);
+                before += __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l);
+                n = n0 + l * PER;
+                bool found = false;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int each = __builtin_amdgcn_readlane(tw[i], l);
+                    found = found || before + each > begin;
+                    if (!found) before += each, ++n;
+                }
+                break;
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
+        }
+        look_at(n);
+        here_p = next_p, here_s = next_s;
+        look_at(n + 1);
     }
 
     // ---------------------------------------------------------------- tiles
@@ -209,16 +248,10 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     };
     auto enter = [&](Tile &c, int p, int s) __attribute__((always_inline)) {  // c.n's keys
         c.pos = p, c.seq = s;
-        seen(a, p, s, c.lo, c.end);
+        seen(*again(), p, s, c.lo, c.end);
         c.t = c.t0 = c.lo / KT;
         c.t1 = c.t0 + tiles<KT>(c.lo, c.end);
         if (c.end == 0) c.seq = 0;
-    };
-    int next_p, next_s;  // the next token's
-    auto look_at = [&](int i) __attribute__((always_inline)) {
-        i = min(i, a.N - 1);
-        next_p = scalar(a.pos, i);
-        next_s = a.seq ? scalar(a.seq, i) : i;
     };
     auto advance = [&](Tile &c) __attribute__((always_inline)) {
         if (++c.t < c.t1) return;
@@ -238,60 +271,67 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     const uint32_t chunk_k = lane % CPR ^ swz_k(lrow), chunk_v = lane % CPR ^ swz_v(lrow);
     auto fetch_table = [&](const Tile &c, int slot) __attribute__((always_inline)) {
         const int j = min(c.t * KT + (lane & (KT - 1)), max(c.end - 1, 0));
-        dma4(a.table + static_cast<int64_t>(c.seq) * a.per + divide(j, a.by_page),
+        const Arguments b = again();
+        dma4(b->table + static_cast<int64_t>(c.seq) * b->per + divide(j, a.by_page),
              __builtin_amdgcn_readfirstlane(at_t + slot * 256));
     };
-    // Stages a tile whose table entries have come into a buffer, its unit's queries too if it is the first one here; says
-    // which of its keys are seen.  The others' rows are the cache's first one.
-    auto stage = [&](const Tile &c, int slot, int buf, bool queries) __attribute__((always_inline)) -> uint64_t {
+    // Of a tile whose table entries have come: where the lane's key and value are (from the head's first row on), and which
+    // keys are seen.  A page that is none is taken for the first one.
+    // WHOLE: in units of 16 bytes, of which a cache has fewer than 2^32.
+    typedef typename std::conditional<WHOLE, uint32_t, int64_t>::type Offset;
+    const uint32_t k_p16 = static_cast<uint32_t>(a.k_p >> 4), k_t16 = static_cast<uint32_t>(a.k_t >> 4);
+    const uint32_t v_p16 = static_cast<uint32_t>(a.v_p >> 4), v_t16 = static_cast<uint32_t>(a.v_t >> 4);
+    struct Place {
+        Offset k, v;
+        uint64_t vis;
+    };
+    auto place = [&](const Tile &c, int slot) __attribute__((always_inline)) {
         const int j = c.t * KT + (lane & (KT - 1)), jj = min(j, max(c.end - 1, 0));
         const int pg = lds_t[slot * 64 + lane];
         const bool is = static_cast<uint32_t>(pg) < static_cast<uint32_t>(a.n_pages), ok = is && j >= c.lo && j < c.end;
-        // (Where a load instruction's rows are of one page, those behind the last key are that page's next rows.)
-        const int at = a.whole ? j : jj;
-        const int64_t p = is ? pg : 0, in_page = at - divide(at, a.by_page) * a.page;
-        const int64_t ko = p * a.k_p + in_page * a.k_t, vo = p * a.v_p + in_page * a.v_t;
-        if (queries) {
-            const char *q = a.q + c.n * a.q_t;
+        // (WHOLE: rows behind the last key are its page's next ones, as far as the load instruction that has it goes.)
+        const int at = WHOLE ? j : jj;
+        const Offset p = is ? pg : 0, in_page = at - divide(at, a.by_page) * a.page;
+        if constexpr (WHOLE)
+            return Place{p * k_p16 + in_page * k_t16, p * v_p16 + in_page * v_t16, __ballot(ok) & kFull};
+        else
+            return Place{p * a.k_p + in_page * a.k_t, p * a.v_p + in_page * a.v_t, __ballot(ok) & kFull};
+    };
+    auto stage_queries = [&](const Tile &c) __attribute__((always_inline)) {
+        const Arguments b = again();
+        const char *q = b->q + c.n * b->q_t;
+        const int own = here(lane), orow = own / CPR;
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) {
-                const uint32_t ch = min(chunk_k ^ static_cast<uint32_t>(swz_k(i * RPI)), last_chunk);
-                rm_dma::dma16(q + (hk * a.G + g0 + min(i * RPI + lrow, heads - 1)) * a.q_h + ch * 16,
-                              __builtin_amdgcn_readfirstlane(at_q + i * 1024));
-            }
+        for (int i = 0; i < NQ; ++i) {
+            const uint32_t ch = min(static_cast<uint32_t>(own % CPR ^ swz_k(orow) ^ swz_k(i * RPI)), last_chunk);
+            rm_dma::dma16(q + (hk * b->G + g0 + min(i * RPI + orow, heads - 1)) * b->q_h + ch * 16,
+                          __builtin_amdgcn_readfirstlane(at_q + i * 1024));
         }
-        auto rows = [&](const char *base, int64_t from, int64_t step, bool values, uint32_t to) __attribute__((always_inline)) {
-            auto chunk = [&](int i) {
-                const uint32_t x = values ? chunk_v ^ static_cast<uint32_t>(swz_v(i * RPI))
-                                          : chunk_k ^ static_cast<uint32_t>(swz_k(i * RPI));
-                return min(x, last_chunk) * 16;
-            };
-            if (a.whole) {  // the rows of an instruction follow each other
-                const uint32_t own = lrow * static_cast<uint32_t>(step);
-#pragma unroll
-                for (int i0 = 0; i0 < NI; i0 += 4) {
-                    const char *b[4];
-                    uint32_t off[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        b[i] = base + at_lane(from, (i0 + i) * RPI);
-                        off[i] = own + chunk(i0 + i);
-                    }
-                    dma16_four(b, off, __builtin_amdgcn_readfirstlane(to + i0 * 1024));
-                }
-            } else {
-#pragma unroll
-                for (int i0 = 0; i0 < NI; i0 += 4) {
-                    const char *b[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) b[i] = base + from_lane(from, (i0 + i) * RPI + lrow) + chunk(i0 + i);
-                    dma16_four(b, __builtin_amdgcn_readfirstlane(to + i0 * 1024));
-                }
-            }
+    };
+    const char *const k_head = a.k + hk * a.k_h, *const v_head = a.v + hk * a.v_h;
+    // Load instructions i0 .. i0 + 3 of a tile's keys or values into a buffer.
+    auto stage = [&](const Place &at, bool values, int i0, int buf) __attribute__((always_inline)) {
+        const char *const base = values ? v_head : k_head, *b[4];
+        const Offset from = values ? at.v : at.k;
+        const uint32_t to = __builtin_amdgcn_readfirstlane(at_k + (buf * 2 + values) * TILEB + i0 * 1024);
+        auto chunk = [&](int i) {
+            const uint32_t x = values ? chunk_v ^ static_cast<uint32_t>(swz_v(i * RPI))
+                                      : chunk_k ^ static_cast<uint32_t>(swz_k(i * RPI));
+            return min(x, last_chunk) * 16;
         };
-        rows(a.k + hk * a.k_h, ko, a.k_t, false, at_k + buf * 2 * TILEB);
-        rows(a.v + hk * a.v_h, vo, a.v_t, true, at_k + buf * 2 * TILEB + TILEB);
-        return __ballot(ok) & kFull;
+        if constexpr (WHOLE) {  // the rows of an instruction follow each other
+            uint32_t off[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                b[i] = base + (static_cast<uint64_t>(__builtin_amdgcn_readlane(from, (i0 + i) * RPI)) << 4);
+                off[i] = (lrow * (values ? v_t16 : k_t16) << 4) + chunk(i0 + i);
+            }
+            dma16_four(b, off, to);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[i] = base + from_lane(from, (i0 + i) * RPI + lrow) + chunk(i0 + i);
+            dma16_four(b, to);
+        }
     };
 
     typedef typename std::conditional<BF, rm_bf16x8, rm_f32x4>::type Frag;
@@ -305,19 +345,14 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         return static_cast<uint32_t>(4 * c + h4) <= last_chunk ? f : Frag{};
     };
 
-    Tile cur;
-    cur.n = n;
-    look_at(n + 1);
-    enter(cur, here_p, here_s);
-    cur.base = before;
-    cur.t += begin - before;
-    fetch_table(cur, 0);
-    wait_loads<0>();
-    Tile nxt = cur;
-    --left;
-    if (left > 0) advance(nxt);
-    fetch_table(nxt, 1);
-    uint64_t vis = stage(cur, 0, 0, true), vis_next = 0;
+    Tile cur, nxt;
+    nxt.n = n;
+    enter(nxt, here_p, here_s);
+    nxt.base = before;
+    nxt.t += begin - before;
+    cur = nxt;
+    fetch_table(nxt, 0);
+    uint64_t vis = 0;
     bool fresh = true;  // cur is the first tile of a token here
 
     Frag qf[RT][QF];
@@ -327,10 +362,17 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     for (int r = 0; r < RT; ++r)
         slope[r] = a.slopes ? a.slopes[hk * a.G + g0 + min(r * 16 + m16, heads - 1)] * rm_attn::kLog2e : 0.0f;
     int2 end_info = make_int2(0, 0);
+    // A step stages a tile and takes the products of the one before it; the first has none before it.  The load
+    // instructions go out between the products, since a wave that issues several in a row waits for the load unit.
+    bool first = true;
+    Place next = {0, 0, 0};
     for (int turn = 0;; turn ^= 1) {
-        const bool more = left > 0, next_fresh = more && nxt.n != cur.n;
-        wait_loads<2 * NI>();  // the next tile's table entries, and this one's queries
-        if (fresh) {
+        const bool more = left > 0, next_fresh = more && (first || nxt.n != cur.n);
+        if (first) wait_loads<0>();
+        else wait_loads<NI>();  // the next tile's table entries, this one's queries and keys
+        const int buf = (turn ^ 1) * 2 * TILEB;
+        const uint8_t *const kt = lds + buf, *const vt = kt + TILEB;
+        if (!first && fresh) {
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 const uint8_t *rows = lds_q + r * 16 * ROWB;
@@ -352,61 +394,95 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
                 for (int d = 0; d < DB; ++d) o[r][d] = rm_f32x4{};
             }
         }
-        Tile after = nxt;
-        const int buf = turn * 2 * TILEB;
-        if (more) {
-            wait_lds();  // the queries, and the tile before this one: their places are free
-            if (left > 1) advance(after);
-            // (Its entries go where this tile's were.)
-            fetch_table(after, turn);
-            vis_next = stage(nxt, turn ^ 1, turn ^ 1, next_fresh);
-            if (next_fresh) wait_loads<3 * NI + 1 + NQ>();
-            else wait_loads<3 * NI + 1>();
-        } else {
-            wait_loads<NI>();
-        }
-
         // ---------------------------------------------------------------- S^T = K Q^T
-        const uint8_t *const kt = lds + buf, *const vt = kt + TILEB;
+        // All reads first: one after the other with its product, each would cost the whole way to LDS and back.
+        Frag kf[QF][NS];
+        if (!first) {
+#pragma unroll
+            for (int c = 0; c < QF; ++c)
+#pragma unroll
+                for (int i = 0; i < NS; ++i) kf[c][i] = read_chunk(kt + i * 16 * ROWB, c);
+        }
+        Tile after = nxt;
+        if (more) {
+            if (left > 1) advance(after);
+            next = place(nxt, turn);
+            wait_lds();  // the queries, the table entries and the values of the tile before this one: their places are free
+            fetch_table(after, turn ^ 1);
+            if (next_fresh) stage_queries(nxt);
+        }
+        constexpr int CH = NS == 1 ? 2 : 1, GS = NI / 4;  // (two chains of sums where there is one tile of 16 keys)
+        rm_f32x4 part[CH][RT][NS];
+#pragma unroll
+        for (int h = 0; h < CH; ++h)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < NS; ++i) part[h][r][i] = rm_f32x4{};
+#pragma unroll
+        for (int g = 0; g < GS; ++g) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) stage(next, false, 4 * g, turn);
+            if (first) continue;
+#pragma unroll
+            for (int c = g * QF / GS; c < (g + 1) * QF / GS; ++c)
+#pragma unroll
+                for (int i = 0; i < NS; ++i)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        rm_f32x4 &x = part[c % CH][r][i];
+                        if constexpr (BF) {
+                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[c][i], qf[r][c], x, 0, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                x = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][i][e], qf[r][c][e], x, 0, 0, 0);
+                        }
+                    }
+        }
+        if (first) {
+#pragma unroll
+            for (int g = 0; g < GS; ++g) stage(next, true, 4 * g, turn);
+            cur = nxt, nxt = after, vis = next.vis, first = false;
+            --left;
+            continue;
+        }
         rm_f32x4 s[RT][NS];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int i = 0; i < NS; ++i) s[r][i] = rm_f32x4{};
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-#pragma unroll
-            for (int c = 0; c < QF; ++c) {
-                const Frag kf = read_chunk(kt + i * 16 * ROWB, c);
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    if constexpr (BF) {
-                        s[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][c], s[r][i], 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            s[r][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[r][c][e], s[r][i], 0, 0, 0);
-                    }
-                }
+            for (int i = 0; i < NS; ++i) {
+                s[r][i] = part[0][r][i];
+                if constexpr (CH > 1) s[r][i] += part[CH - 1][r][i];
             }
 
         // ---------------------------------------------------------------- softmax
-        const int j0 = cur.t * KT + 4 * h4;
-        const uint64_t bits = vis >> (4 * h4);
+        auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < NS; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[r][i][e] = f(s[r][i][e], r, 16 * i + e);
+        };
+        each([&](float x, int, int) { return x * a.scale; });
+        if (__builtin_expect(a.cap != 0.0f, false))
+            each([&](float x, int, int) { return a.cap * (BF ? rm_attn::tanh_relative(x) : tanhf(x)); });
+        if (__builtin_expect(a.slopes != nullptr, false)) {
+            const int d0 = cur.pos - (cur.t * KT + 4 * here(h4));
+            each([&](float x, int r, int j) { return fmaf(-slope[r], static_cast<float>(d0 - j), x); });
+        }
+        if (__builtin_expect(vis != kFull, false)) {
+            const uint64_t bits = vis >> (4 * here(h4));
+            each([&](float x, int, int j) { return (bits >> j) & 1 ? x : -INFINITY; });
+        }
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < NS; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x = s[r][i][e] * a.scale;
-                    if (a.cap != 0.0f) x = a.cap * (BF ? rm_attn::tanh_relative(x) : tanhf(x));
-                    if (a.slopes) x = fmaf(-slope[r], static_cast<float>(cur.pos - (j0 + 16 * i + e)), x);
-                    if (vis != kFull) x = (bits >> (16 * i + e)) & 1 ? x : -INFINITY;
-                    s[r][i][e] = x;
-                    top = fmaxf(top, x);
-                }
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, s[r][i][e]);
             top = rows_max(top);
             const bool raise = top > m[r] + kRaise;  // (false for top = -inf)
             if (__any(raise)) {
@@ -428,77 +504,89 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         }
 
         // ---------------------------------------------------------------- O^T += V^T P^T
-        if (more) {
-            if (next_fresh) wait_loads<2 * NI + 1 + NQ>();
-            else wait_loads<2 * NI + 1>();
-        } else {
-            wait_loads<0>();
-        }
-        if (vis != kFull) {  // values of keys that are not seen: 0 times an infinity or NaN is not 0
+        if (!more) wait_loads<0>();
+        else if (next_fresh) wait_loads<NI + 1 + NQ>();
+        else wait_loads<NI + 1>();
+        if (__builtin_expect(vis != kFull, false)) {  // values of keys that are not seen: 0 times an infinity or NaN is not 0
+            const int own = here(lane);
 #pragma unroll
             for (int i = 0; i < TILEB / 1024; ++i) {
-                const int at = i * 64 + lane;
+                const int at = i * 64 + own;
                 if (!((vis >> (at / CPR)) & 1)) *reinterpret_cast<rm_u32x4 *>(lds + buf + TILEB + at * 16) = rm_u32x4{0, 0, 0, 0};
             }
             wait_lds();
         }
+        if constexpr (BF) {
+            typedef __attribute__((address_space(3))) rm_s16x4 lds_s16x4;
+            const int row = 4 * h4 + (m16 >> 2);
+            const uint8_t *v = vt + row * ROWB + (m16 & 3) * 8;
+            rm_s16x4 vf[NS][DB];
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            if constexpr (BF) {
-                typedef __attribute__((address_space(3))) rm_s16x4 lds_s16x4;
-                rm_s16x4 p[RT];
+            for (int i = 0; i < NS; ++i)
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    vf[i][d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_s16x4 *)(v + 16 * i * ROWB + (((2 * d) & 15) ^ swz_v(row)) * 16 + (d >> 3) * 256));
+#pragma unroll
+            for (int x = 0; x < NS * DB; ++x) {
+                const int i = x / DB, d = x % DB;
+                if (x % (NS * DB / GS) == 0) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (more) stage(next, true, 4 * (x / (NS * DB / GS)), turn);
+                }
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
-                    const rm_bf16x4 b = {static_cast<__bf16>(s[r][i][0]), static_cast<__bf16>(s[r][i][1]),
+                    const rm_bf16x4 p = {static_cast<__bf16>(s[r][i][0]), static_cast<__bf16>(s[r][i][1]),
                                          static_cast<__bf16>(s[r][i][2]), static_cast<__bf16>(s[r][i][3])};
-                    p[r] = __builtin_bit_cast(rm_s16x4, b);
+                    o[r][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf[i][d], __builtin_bit_cast(rm_s16x4, p), o[r][d], 0,
+                                                                        0, 0);
                 }
-                const int row = 4 * h4 + (m16 >> 2);
-                const uint8_t *v = vt + (16 * i + row) * ROWB + (m16 & 3) * 8;
+            }
+        } else {
 #pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const rm_s16x4 f = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_s16x4 *)(v + (((2 * d) & 15) ^ swz_v(row)) * 16 + (d >> 3) * 256));
+            for (int i = 0; i < NS; ++i) {
+                float vf[4][DB];
 #pragma unroll
-                    for (int r = 0; r < RT; ++r)
-                        o[r][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(f, p[r], o[r][d], 0, 0, 0);
-                }
-            } else {
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int d = 0; d < DB; ++d)
+                        vf[e][d] = *reinterpret_cast<const float *>(
+                            vt + (16 * i + 4 * h4 + e) * ROWB + (((4 * d) & 15) ^ (4 * h4)) * 16 + (d >> 2) * 256 + m16 * 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int row = 16 * i + 4 * h4 + e;
+                    __builtin_amdgcn_sched_barrier(0);
+                    if ((4 * i + e) % (4 * NS / GS) == 0 && more) stage(next, true, 4 * ((4 * i + e) / (4 * NS / GS)), turn);
 #pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        const float f = *reinterpret_cast<const float *>(
-                            vt + row * ROWB + (((4 * d) & 15) ^ (4 * h4)) * 16 + (d >> 2) * 256 + m16 * 4);
+                    for (int r = 0; r < RT; ++r)
 #pragma unroll
-                        for (int r = 0; r < RT; ++r)
-                            o[r][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(f, s[r][i][e], o[r][d], 0, 0, 0);
-                    }
+                        for (int d = 0; d < DB; ++d)
+                            o[r][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e][d], s[r][i][e], o[r][d], 0, 0, 0);
                 }
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
 
         // ---------------------------------------------------------------- the token's end, or the share's
         if (!more || next_fresh) {
+            const Arguments b = again();
             const bool starts = cur.base >= begin, ends = cur.t + 1 == cur.t1;
             if (starts) {
                 const int parts = (cur.base + (cur.t1 - cur.t0) - 1) / share - grp + 1;
-                if (a.by_token && unit == 0 && lane == 0) a.info[cur.n] = make_int2(grp, parts);
+                if (b->by_token && unit == 0 && lane == 0) b->info[cur.n] = make_int2(grp, parts);
                 if (!ends) end_info = make_int2(cur.n, parts);
             }
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 const float sum = rows_sum(l[r]);
-                const int g = r * 16 + m16;
+                const int own = here(lane), g = r * 16 + (own & 15), c0 = 4 * (own >> 4);
                 if (g >= heads) continue;
                 if (starts && ends) {
                     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    char *dst = a.o + cur.n * a.o_t + static_cast<int64_t>(hk * a.G + g0 + g) * a.o_h;
+                    char *dst = b->o + cur.n * b->o_t + static_cast<int64_t>(hk * b->G + g0 + g) * b->o_h;
 #pragma unroll
                     for (int d = 0; d < DB; ++d) {
-                        const int c = 16 * d + 4 * h4;
-                        if (c >= a.D) continue;
+                        const int c = 16 * d + c0;
+                        if (c >= b->D) continue;
                         const rm_f32x4 y = o[r][d] * inv;
                         if constexpr (BF)
                             *reinterpret_cast<rm_bf16x4 *>(dst + c * 2) =
@@ -508,12 +596,12 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
                             *reinterpret_cast<rm_f32x4 *>(dst + c * 4) = y;
                     }
                 } else {
-                    const int64_t row = ((2 * static_cast<int64_t>(grp) + starts) * a.units + unit) * QR + g;
-                    if (h4 == 0) a.part_ml[row] = make_float2(m[r], sum);
+                    const int64_t row = ((2 * static_cast<int64_t>(grp) + starts) * b->units + unit) * QR + g;
+                    if (c0 == 0) b->part_ml[row] = make_float2(m[r], sum);
 #pragma unroll
                     for (int d = 0; d < DB; ++d) {
-                        const int c = 16 * d + 4 * h4;
-                        if (c < a.D) *reinterpret_cast<rm_f32x4 *>(a.part_o + row * a.D + c) = o[r][d];
+                        const int c = 16 * d + c0;
+                        if (c < b->D) *reinterpret_cast<rm_f32x4 *>(b->part_o + row * b->D + c) = o[r][d];
                     }
                 }
             }
@@ -521,44 +609,46 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         if (!more) break;
         cur = nxt;
         nxt = after;
-        vis = vis_next;
+        vis = next.vis;
         fresh = next_fresh;
         --left;
     }
-    if (!a.by_token && unit == 0 && lane == 0) a.info[grp] = end_info;
+    const Arguments b = again();
+    if (!b->by_token && unit == 0 && lane == 0) b->info[grp] = end_info;
 }
 
-// One workgroup an entry, unit and query head of it: the parts that groups of waves left of a token, in a fixed order.
+// The parts that groups of waves left of a token, joined in a fixed order: `share` lane groups (a power of two) divide the
+// parts of one query head, and a workgroup takes as many heads of an entry and unit as it has such.  Bound by three round
+// trips (the entry, the parts, the store).
 template <bool BF, int LPR, int QR>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int share, int blocks) {
     constexpr int GR = 256 / LPR;
     __shared__ float tops[GR], sums[GR];
     __shared__ rm_f32x4 part[GR][LPR];
-    const int each = a.units * a.rows, e = blockIdx.x / each, ur = blockIdx.x - e * each;
-    const int u = ur / a.rows, r = ur - u * a.rows;
+    const int eu = blockIdx.x / blocks, block = blockIdx.x - eu * blocks, e = divide(eu, a.by_units), u = eu - e * a.units;
     const int2 info = a.info[e];
     const int parts = info.y, n = a.by_token ? e : info.x, first = a.by_token ? info.x : e;
     if (parts < 2) return;
-    const int hk = u / a.q_tiles, g = (u - hk * a.q_tiles) * QR + r;
-    if (g >= a.G) return;
+    const int tid = threadIdx.x, lane = tid % LPR, grp = tid / LPR, sub = grp & (share - 1);
+    const int r = block * (GR / share) + grp / share, hk = divide(u, a.by_q_tiles), g = (u - hk * a.q_tiles) * QR + r;
+    const bool is = r < QR && g < a.G;
     auto row = [&](int p) { return ((2 * static_cast<int64_t>(first + p) + (p == 0)) * a.units + u) * QR + r; };
-    const int tid = threadIdx.x, lane = tid % LPR, grp = tid / LPR;
     const int c = min(lane * 4, a.D - 4);
     rm_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
-    for (int p0 = grp; p0 < parts; p0 += 4 * GR) {
+    for (int p0 = is ? sub : parts; p0 < parts; p0 += 4 * share) {
         float2 ml[4];
         rm_f32x4 v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t at = row(min(p0 + i * GR, parts - 1));
+            const int64_t at = row(min(p0 + i * share, parts - 1));
             ml[i] = a.part_ml[at];
             v[i] = *reinterpret_cast<const rm_f32x4 *>(a.part_o + at * a.D + c);
         }
         float top = m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (p0 + i * GR >= parts) ml[i] = make_float2(-INFINITY, 0.0f);
+            if (p0 + i * share >= parts) ml[i] = make_float2(-INFINITY, 0.0f);
             top = fmaxf(top, ml[i].x);
         }
         const float ref = top == -INFINITY ? 0.0f : top;
@@ -574,26 +664,25 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
             o += v[i] * f;
         }
     }
-    if (lane == 0) tops[grp] = m;
-    __syncthreads();
-    float top = tops[0];
-#pragma unroll
-    for (int i = 1; i < GR; ++i) top = fmaxf(top, tops[i]);
-    const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
-    o *= f;
-    l *= f;
-    part[grp][lane] = o;
-    if (lane == 0) sums[grp] = l;
-    __syncthreads();
-    if (grp != 0 || lane * 4 >= a.D) return;
-    float sum = 0.0f;
-    o = rm_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < GR; ++i) {
-        sum += sums[i];
-        o += part[i][lane];
+    if (share > 1) {
+        if (lane == 0) tops[grp] = m;
+        __syncthreads();
+        float top = m;
+        for (int i = 0; i < share; ++i) top = fmaxf(top, tops[grp - sub + i]);
+        const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+        part[grp][lane] = o * f;
+        if (lane == 0) sums[grp] = l * f;
+        __syncthreads();
+        if (sub != 0) return;
+        l = 0.0f;
+        o = rm_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < share; ++i) {
+            l += sums[grp + i];
+            o += part[grp + i][lane];
+        }
     }
-    o *= sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (!is || lane * 4 >= a.D) return;
+    o *= l == 0.0f ? 0.0f : 1.0f / l;
     char *dst = a.o + n * a.o_t + static_cast<int64_t>(hk * a.G + g) * a.o_h;
     if constexpr (BF)
         *reinterpret_cast<rm_bf16x4 *>(dst + c * 2) =
@@ -604,11 +693,19 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
 
 template <bool BF, int DC, int QR>
 hipError_t go(const PagedPlan &p, const PagedArgs &a, hipStream_t st) {
-    paged_kernel<BF, DC, QR><<<dim3(static_cast<unsigned>(a.groups) * a.units), 64, 0, st>>>(a);
+    const dim3 grid(static_cast<unsigned>(a.groups) * a.units);
+    if (p.whole) paged_kernel<BF, true, DC, QR><<<grid, 64, 0, st>>>(a);
+    else paged_kernel<BF, false, DC, QR><<<grid, 64, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.join) return e;
-    const unsigned entries = static_cast<unsigned>(std::min(a.N, a.groups));
-    paged_join_kernel<BF, room(DC) / 4, QR><<<dim3(entries * a.units * a.rows), 256, 0, st>>>(a);
+    // A token has groups / N parts and two more where it begins and ends, if all are as long; a lane group takes four at a
+    // time.
+    constexpr int LPR = room(DC) / 4, GR = 256 / LPR;
+    const int entries = std::min(a.N, a.groups), parts = a.groups / entries + 2;
+    int share = 1;
+    while (share < GR && share * 4 < parts) share *= 2;
+    const int blocks = (a.rows * share + GR - 1) / GR;
+    paged_join_kernel<BF, LPR, QR><<<dim3(static_cast<unsigned>(entries) * a.units * blocks), 256, 0, st>>>(a, share, blocks);
     return hipGetLastError();
 }
 template <bool BF, int DC>

@@ -24,13 +24,12 @@ struct PagedArgs {
     const int32_t *table = nullptr, *seq = nullptr, *pos = nullptr;
     const float *slopes = nullptr;
     int N = 0, seqs = 0, page = 0, n_pages = 0, per = 0, window = 0;
-    rm_attn::Divisor by_page, by_q_tiles, by_units;
+    rm_attn::Divisor by_page, by_q_tiles, by_units, by_groups;
     int D = 0, G = 0;
     // Units of a token: key heads times blocks of query heads; query heads of a block at most.
     int units = 0, q_tiles = 0, rows = 0;
     // Groups of waves, the least tiles of one, and where the parts of divided tokens are told: [N] or [groups].
     int groups = 0, least = 0, by_token = 0;
-    int whole = 0;                   // the rows of a load instruction are of one page
     float scale = 0.0f, cap = 0.0f;  // scores in powers of two; with a cap: scale = score scale / cap
     float *part_o = nullptr;         // [groups][2][units][rows of a block][D]
     float2 *part_ml = nullptr;       // [groups][2][units][rows of a block]
@@ -40,7 +39,7 @@ struct PagedPlan {
     int qr = 0, kt = 0;          // query heads of a block, keys of a tile
     int rpi = 0, per_cu = 0;     // rows of a load instruction, waves of a compute unit
     int groups = 0, units = 0, q_tiles = 0, by_token = 0;
-    bool join = false;
+    bool join = false, whole = false;  // whole: the rows of a load instruction are of one page
     size_t off_ml = 0, off_info = 0, total = 0;
 };
 void paged_shape(bool bf16, int D, int G, PagedPlan *p);  // qr, kt, rpi and per_cu

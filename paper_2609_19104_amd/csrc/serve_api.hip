@@ -32,7 +32,7 @@ rm_status check_pages(int page, int n_pages, int max_pages) {
     return RM_OK;
 }
 
-constexpr int kLeastTiles = 2;
+constexpr int kLeastTiles = 1;
 
 rm_status paged_plan(const rm_attn_shape *s, int n_tok, int page, int max_pages, rm_serve::PagedPlan *p) {
     rm_status r = check_attn_shape(s);
@@ -46,8 +46,9 @@ rm_status paged_plan(const rm_attn_shape *s, int n_tok, int page, int max_pages,
     p->q_tiles = static_cast<int>(ceil_div(G, p->qr));
     p->units = s->n_kv_heads * p->q_tiles;
     const int64_t most = n_tok * (ceil_div(static_cast<int64_t>(max_pages) * page, p->kt) + 1);  // tiles, at most
-    if (most > INT32_MAX) return api_fail(RM_ERR_SHAPE, "%lld tiles of keys are more than 2^31 - 1", static_cast<long long>(most));
-    p->groups = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(256 * p->per_cu / p->units, ceil_div(most, kLeastTiles))));
+    if (most >= (1 << 30) - 2048)
+        return api_fail(RM_ERR_SHAPE, "%lld tiles of keys are not below 2^30 - 2048", static_cast<long long>(most));
+    p->groups = most <= 4 ? 1 : static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(256 * p->per_cu / p->units, ceil_div(most, kLeastTiles))));
     p->by_token = n_tok <= p->groups;
     p->join = p->groups > 1;
     const size_t rows = static_cast<size_t>(p->groups) * 2 * p->units * p->qr;
@@ -156,9 +157,11 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
     a.D = D, a.G = s->n_q_heads / s->n_kv_heads;
     a.units = p.units, a.q_tiles = p.q_tiles, a.rows = std::min(a.G, p.qr);
     a.by_page = rm_attn::divisor(page), a.by_q_tiles = rm_attn::divisor(p.q_tiles);
-    a.by_units = rm_attn::divisor(p.units);
+    a.by_units = rm_attn::divisor(p.units), a.by_groups = rm_attn::divisor(p.groups);
     a.groups = p.groups, a.least = kLeastTiles, a.by_token = p.by_token;
-    a.whole = page % p.rpi == 0 && a.k_t < 1 << 28 && a.v_t < 1 << 28;
+    // (An instruction's rows from its first one in 32 bits, and rows of the cache in 32 bits of 16 bytes each.)
+    const size_t wide = size_t{16} << 32;
+    p.whole = page % p.rpi == 0 && a.k_t < 1 << 28 && a.v_t < 1 << 28 && x[1].n < wide && x[2].n < wide;
     a.part_o = static_cast<float *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.off_ml);
     a.info = reinterpret_cast<int2 *>(static_cast<char *>(ws) + p.off_info);
