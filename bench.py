@@ -54,7 +54,9 @@ HBM_PEAK_GBS = 8000.0  # MI355X HBM3E, 8 TB/s
 BF16_PEAK_TFLOPS = 2500.0  # MI355X dense bf16 matrix cores (no sparsity)
 PROFILES = os.path.join(ROOT, "profiles")
 CSRC = os.path.join(ROOT, "paper_2609_19104_amd", "csrc")
-ATTENTION_SOURCES = ("attn_", "rm_attn", "qk_norm_rope", "rm_rope")  # how their names begin
+# How the names of the attention side's and the serving step's files begin.
+ATTENTION_SOURCES = ("attn_", "rm_attn", "qk_norm_rope", "rm_rope", "rm_checks", "rm_serve", "serve_api", "page_slots",
+                     "paged_attn", "block_norm")
 COLD_BYTES = 1 << 30   # weight copies rotated through per timed run
 
 
@@ -823,7 +825,8 @@ def _code_only(text: str) -> str:
 
 def kernel_source_digest() -> str:
     """sha256 over the HIP sources' code (names and code without comments, files sorted): identifies the kernels
-    a counter run measured.  The attention side's files are left out: no counted kernel is compiled from them."""
+    a counter run measured.  The attention side's and the serving step's files are left out: no counted kernel is
+    compiled from them."""
     import hashlib
     h = hashlib.sha256()
     for name in sorted(os.listdir(CSRC)):

@@ -638,9 +638,11 @@ def _vector(name: str, t: Optional[torch.Tensor], dtype, index: int, shape) -> O
     """Pointer of an optional contiguous tensor of a dtype, device and shape."""
     if t is None:
         return None
-    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape
-            and t.is_contiguous()):
-        return t.data_ptr()
+    try:  # the usual case first
+        if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     _need_cuda(name, t, (dtype,))
     raise ValueError(f"{name} must be {dtype} {list(shape)} on device {index}, got {list(t.shape)} on {t.device}")
 
@@ -863,24 +865,20 @@ def rm_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
         _stream(stream)))
 
 
-def _rows(name: str, t: torch.Tensor, dtype, index: int, shape) -> int:
-    """Pointer of a contiguous activation tensor."""
-    if t.shape == shape and t.dtype is dtype and t.get_device() == index and t.is_contiguous():
-        return t.data_ptr()
-    _need_cuda(name, t, (dtype,), len(shape))
-    raise ValueError(f"{name} must be {list(shape)} on device {index}, got {list(t.shape)} on {t.device}")
-
-
 def _modulation(name: str, t: Optional[torch.Tensor], index: int, shape) -> Tuple[Optional[int], int]:
     """Pointer and row stride of a float32 [B][d] tensor whose rows are contiguous."""
     if t is None:
         return None, 0
+    try:
+        row, c = t.stride()
+        if c == 1 and t.dtype is torch.float32 and t.shape == shape and t.get_device() == index:
+            return t.data_ptr(), row
+    except (AttributeError, ValueError):
+        pass
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.shape != shape or t.dtype is not torch.float32 or t.get_device() != index or t.stride(1) != 1:
-        raise ValueError(f"{name} must be float32 {list(shape)} on device {index} with contiguous rows, got {t.dtype} "
-                         f"{list(t.shape)} on {t.device}")
-    return t.data_ptr(), t.stride(0)
+    raise ValueError(f"{name} must be float32 {list(shape)} on device {index} with contiguous rows, got {t.dtype} "
+                     f"{list(t.shape)} on {t.device}")
 
 
 def rm_block_norm(x: torch.Tensor, f: Optional[torch.Tensor], y: Optional[torch.Tensor], out: Optional[torch.Tensor],
@@ -900,16 +898,15 @@ def rm_block_norm(x: torch.Tensor, f: Optional[torch.Tensor], y: Optional[torch.
     ot = xt if out is None else out.dtype
     if xt not in _ATTN_DTYPES or ft not in _ATTN_DTYPES or ot not in _ATTN_DTYPES:
         raise ValueError("x, f and out must be float32 or bfloat16")
-    f32 = torch.float32
-    gp, gs = _modulation("gate", gate, dev, (B, d))
-    sp, ss = _modulation("scale", scale, dev, (B, d))
-    hp, hs = _modulation("shift", shift, dev, (B, d))
+    f32, row, mod = torch.float32, (d,), (B, d)
+    gp, gs = _modulation("gate", gate, dev, mod)
+    sp, ss = _modulation("scale", scale, dev, mod)
+    hp, hs = _modulation("shift", shift, dev, mod)
     _check(load_library().rm_block_norm(
-        B, T, d, _ATTN_DTYPES[xt], _ATTN_DTYPES[ft], _ATTN_DTYPES[ot], _rows("x", x, xt, dev, shape),
-        None if f is None else _rows("f", f, ft, dev, shape), norm_post, _vector("gain_post", gain_post, f32, dev, (d,)),
-        gp, gs, x_scale, f_scale, None if y is None else _rows("y", y, xt, dev, shape),
-        _vector("gain_pre", gain_pre, f32, dev, (d,)), sp, ss, hp, hs, eps,
-        None if out is None else _rows("out", out, ot, dev, shape), _stream(stream)))
+        B, T, d, _ATTN_DTYPES[xt], _ATTN_DTYPES[ft], _ATTN_DTYPES[ot], _vector("x", x, xt, dev, shape),
+        _vector("f", f, ft, dev, shape), norm_post, _vector("gain_post", gain_post, f32, dev, row), gp, gs, x_scale, f_scale,
+        _vector("y", y, xt, dev, shape), _vector("gain_pre", gain_pre, f32, dev, row), sp, ss, hp, hs, eps,
+        _vector("out", out, ot, dev, shape), _stream(stream)))
 
 
 def rm_profile_kernel_events(kernel: int, ev_begin: Optional[int], ev_end: Optional[int]) -> None:

@@ -5,22 +5,26 @@ namespace rm_serve {
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x8 __attribute__((ext_vector_type(8), aligned(16)));
+template <int V>
+using Floats = float __attribute__((ext_vector_type(V), aligned(16)));
 
-// Eight elements as they lie in memory.
-template <bool BF>
-using Raw = typename std::conditional<BF, bf16x8, f32x8>::type;
+// V elements as they lie in memory.
+template <bool BF, int V>
+using Raw = typename std::conditional<BF, __bf16 __attribute__((ext_vector_type(V))), Floats<V>>::type;
 
-template <bool BF>
-__device__ __forceinline__ Raw<BF> load(const char *p, int64_t i) {
-    return *reinterpret_cast<const Raw<BF> *>(p + i * (BF ? 2 : 4));
+// Nontemporal: a row is read once and not written again, and passes by the caches' other lines.
+template <bool BF, int V>
+__device__ __forceinline__ Raw<BF, V> load(const char *p, int64_t i) {
+    return __builtin_nontemporal_load(reinterpret_cast<const Raw<BF, V> *>(p + i * (BF ? 2 : 4)));
 }
-template <bool BF>
-__device__ __forceinline__ void store(char *p, int64_t i, f32x8 v) {
-    *reinterpret_cast<Raw<BF> *>(p + i * (BF ? 2 : 4)) = __builtin_convertvector(v, Raw<BF>);
+template <bool BF, int V>
+__device__ __forceinline__ void store(char *p, int64_t i, Floats<V> v) {
+    __builtin_nontemporal_store(__builtin_convertvector(v, Raw<BF, V>), reinterpret_cast<Raw<BF, V> *>(p + i * (BF ? 2 : 4)));
 }
-__device__ __forceinline__ f32x8 load(const float *p, int c) { return *reinterpret_cast<const f32x8 *>(p + c); }
+template <int V>
+__device__ __forceinline__ Floats<V> load(const float *p, int c) {
+    return *reinterpret_cast<const Floats<V> *>(p + c);
+}
 
 // A row's sum over its TPR threads.
 template <int TPR>
@@ -35,29 +39,31 @@ __device__ __forceinline__ float sum_row(float s, float *red) {
     return s;
 }
 
-// TPR threads hold a row in registers, N chunks of 8 columns each, so that x and f are read once, all at the start.
+// TPR threads hold a row in registers, N chunks of V columns each, so that x and f are read once, all at the start.  A
+// chunk is 16 bytes of the widest of the three, so that a wave's loads of it are consecutive.
 template <bool XB, bool FB, bool OB, int TPR, int N>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(NormArgs a) {
-    constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;  // of a workgroup
+__global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void block_norm_kernel(NormArgs a) {
+    constexpr int V = XB && FB && OB ? 8 : 4, ROWS = TPR < 128 ? 256 / TPR : 1;  // rows of a workgroup
+    typedef Floats<V> Vec;
     __shared__ float red[2][16];
     const int t = threadIdx.x % TPR;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
-    if (row >= a.rows) return;  // (the whole wave)
+    if (row >= a.rows) return;  // (the whole wave, and with more than one wave to a row the whole workgroup)
     const int b = static_cast<int>(row) / a.T;
     const int64_t base = row * a.d;
-    Raw<XB> x[N];
-    Raw<FB> f[N];
-    f32x8 u[N];
+    Raw<XB, V> x[N];
+    Raw<FB, V> f[N];
+    Vec u[N];
     // Columns past the row's end are its last ones again, and count as zeros.
     int c[N];
     bool has[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        c[i] = (t + i * TPR) * 8;
+        c[i] = (t + i * TPR) * V;
         has[i] = c[i] < a.d;
-        c[i] = min(c[i], a.d - 8);
-        x[i] = load<XB>(a.x, base + c[i]);
-        if (a.f) f[i] = load<FB>(a.f, base + c[i]);
+        c[i] = min(c[i], a.d - V);
+        x[i] = load<XB, V>(a.x, base + c[i]);
+        if (a.f) f[i] = load<FB, V>(a.f, base + c[i]);
     }
     if (a.f) {
         float rf = a.f_scale;
@@ -67,26 +73,26 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(NormA
             for (int i = 0; i < N; ++i) {
                 float p = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p = fmaf(static_cast<float>(f[i][e]), static_cast<float>(f[i][e]), p);
+                for (int e = 0; e < V; ++e) p = fmaf(static_cast<float>(f[i][e]), static_cast<float>(f[i][e]), p);
                 s += has[i] ? p : 0.0f;
             }
             rf *= rm_rnorm_from_ssq(sum_row<TPR>(s, red[0]), a.d, a.eps);
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            f32x8 v = __builtin_convertvector(f[i], f32x8) * rf;
-            if (a.gain_post) v *= load(a.gain_post, c[i]);
-            if (a.gate) v *= load(a.gate + b * a.gate_b, c[i]);
-            u[i] = __builtin_convertvector(x[i], f32x8) * a.x_scale + v;
+            Vec v = __builtin_convertvector(f[i], Vec) * rf;
+            if (a.gain_post) v *= load<V>(a.gain_post, c[i]);
+            if (a.gate) v *= load<V>(a.gate + b * a.gate_b, c[i]);
+            u[i] = __builtin_convertvector(x[i], Vec) * a.x_scale + v;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) u[i] = __builtin_convertvector(x[i], f32x8) * a.x_scale;
+        for (int i = 0; i < N; ++i) u[i] = __builtin_convertvector(x[i], Vec) * a.x_scale;
     }
     if (a.y) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (has[i]) store<XB>(a.y, base + c[i], u[i]);
+            if (has[i]) store<XB, V>(a.y, base + c[i], u[i]);
     }
     if (!a.out) return;
     float s = 0.0f;
@@ -94,34 +100,37 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(NormA
     for (int i = 0; i < N; ++i) {
         float p = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p = fmaf(u[i][e], u[i][e], p);
+        for (int e = 0; e < V; ++e) p = fmaf(u[i][e], u[i][e], p);
         s += has[i] ? p : 0.0f;
     }
     const float ru = rm_rnorm_from_ssq(sum_row<TPR>(s, red[1]), a.d, a.eps);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        f32x8 v = u[i] * ru;
-        if (a.gain_pre) v *= load(a.gain_pre, c[i]);
-        if (a.scale) v *= 1.0f + load(a.scale + b * a.scale_b, c[i]);
-        if (a.shift) v += load(a.shift + b * a.shift_b, c[i]);
-        if (has[i]) store<OB>(a.out, base + c[i], v);
+        Vec v = u[i] * ru;
+        if (a.gain_pre) v *= load<V>(a.gain_pre, c[i]);
+        if (a.scale) v *= 1.0f + load<V>(a.scale + b * a.scale_b, c[i]);
+        if (a.shift) v += load<V>(a.shift + b * a.shift_b, c[i]);
+        if (has[i]) store<OB, V>(a.out, base + c[i], v);
     }
 }
 
+template <bool XB, bool FB, bool OB, int TPR, int COLUMNS>
+hipError_t go(const NormArgs &a, hipStream_t st) {
+    constexpr int V = XB && FB && OB ? 8 : 4, ROWS = TPR < 128 ? 256 / TPR : 1;
+    const dim3 grid(static_cast<unsigned>((a.rows + ROWS - 1) / ROWS));
+    block_norm_kernel<XB, FB, OB, TPR, COLUMNS / V><<<grid, TPR < 128 ? 256 : TPR, 0, st>>>(a);
+    return hipGetLastError();
+}
+// Eight columns a thread while 256 threads hold the row with that, then more.
 template <bool XB, bool FB, bool OB>
 hipError_t by_row(const NormArgs &a, hipStream_t st) {
-    const int chunks = a.d / 8;
-    const auto rows = static_cast<unsigned>(a.rows);
-    const dim3 fours((rows + 3) / 4), ones(rows);
-    if (chunks <= 64) block_norm_kernel<XB, FB, OB, 64, 1><<<fours, 256, 0, st>>>(a);
-    else if (a.rows >= a.many && chunks <= 128) block_norm_kernel<XB, FB, OB, 64, 2><<<fours, 256, 0, st>>>(a);
-    else if (a.rows >= a.many && chunks <= 256) block_norm_kernel<XB, FB, OB, 64, 4><<<fours, 256, 0, st>>>(a);
-    else if (chunks <= 256) block_norm_kernel<XB, FB, OB, 256, 1><<<ones, 256, 0, st>>>(a);
-    else if (chunks <= 512) block_norm_kernel<XB, FB, OB, 256, 2><<<ones, 256, 0, st>>>(a);
-    else if (chunks <= 1024) block_norm_kernel<XB, FB, OB, 256, 4><<<ones, 256, 0, st>>>(a);
-    else if (chunks <= 2048) block_norm_kernel<XB, FB, OB, 1024, 2><<<ones, 1024, 0, st>>>(a);
-    else block_norm_kernel<XB, FB, OB, 1024, 4><<<ones, 1024, 0, st>>>(a);
-    return hipGetLastError();
+    if (a.d <= 512) return go<XB, FB, OB, 64, 8>(a, st);
+    if (a.d <= 1024) return go<XB, FB, OB, 128, 8>(a, st);
+    if (a.d <= 2048) return go<XB, FB, OB, 256, 8>(a, st);
+    if (a.d <= 4096) return go<XB, FB, OB, 256, 16>(a, st);
+    if (a.d <= 8192) return go<XB, FB, OB, 256, 32>(a, st);
+    if (a.d <= 16384) return go<XB, FB, OB, 1024, 16>(a, st);
+    return go<XB, FB, OB, 1024, 32>(a, st);
 }
 template <bool XB, bool FB>
 hipError_t by_out(const NormArgs &a, bool ob, hipStream_t st) {

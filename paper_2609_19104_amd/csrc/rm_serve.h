@@ -51,7 +51,7 @@ struct NormArgs {
     const float *gain_post = nullptr, *gate = nullptr, *gain_pre = nullptr, *scale = nullptr, *shift = nullptr;
     int64_t gate_b = 0, scale_b = 0, shift_b = 0;  // elements from sample to sample
     int64_t rows = 0;
-    int T = 0, d = 0, norm_post = 0, many = 2048;
+    int T = 0, d = 0, norm_post = 0;
     float x_scale = 1.0f, f_scale = 1.0f, eps = 0.0f;
 };
 hipError_t launch_block_norm(const NormArgs &a, bool x_bf16, bool f_bf16, bool out_bf16, hipStream_t st);
