@@ -175,7 +175,7 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         const int64_t first = static_cast<int64_t>(grp) * share;
         begin = static_cast<int>(min(first, static_cast<int64_t>(total)));
         left = min(share, total - begin);
-        if (left <= 0 && !a.by_token && unit == 0 && lane == 0) a.info[grp] = make_int2(0, 0);
+        if (left <= 0 && a.info && !a.by_token && unit == 0 && lane == 0) a.info[grp] = make_int2(0, 0);
         return left > 0;
     };
     if (__builtin_expect(a.N <= 64, true)) {  // a token a lane
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     auto advance = [&](Tile &c) __attribute__((always_inline)) {
         if (++c.t < c.t1) return;
         c.base += c.t1 - c.t0;
-        ++c.n;
+        c.n = min(c.n + 1, a.N - 1);
         enter(c, next_p, next_s);
         look_at(c.n + 1);
     };
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             const bool starts = cur.base >= begin, ends = cur.t + 1 == cur.t1;
             if (starts) {
                 const int parts = (cur.base + (cur.t1 - cur.t0) - 1) / share - grp + 1;
-                if (b->by_token && unit == 0 && lane == 0) b->info[cur.n] = make_int2(grp, parts);
+                if (b->info && b->by_token && unit == 0 && lane == 0) b->info[cur.n] = make_int2(grp, parts);
                 if (!ends) end_info = make_int2(cur.n, parts);
             }
 #pragma unroll
@@ -614,7 +614,7 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         --left;
     }
     const Arguments b = again();
-    if (!b->by_token && unit == 0 && lane == 0) b->info[grp] = end_info;
+    if (b->info && !b->by_token && unit == 0 && lane == 0) b->info[grp] = end_info;
 }
 
 // The parts that groups of waves left of a token, joined in a fixed order: `share` lane groups (a power of two) divide the

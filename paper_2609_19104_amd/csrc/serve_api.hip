@@ -51,6 +51,7 @@ rm_status paged_plan(const rm_attn_shape *s, int n_tok, int page, int max_pages,
     p->groups = most <= 4 ? 1 : static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(256 * p->per_cu / p->units, ceil_div(most, kLeastTiles))));
     p->by_token = n_tok <= p->groups;
     p->join = p->groups > 1;
+    if (!p->join) return RM_OK;  // every token is one wave's
     const size_t rows = static_cast<size_t>(p->groups) * 2 * p->units * p->qr;
     p->off_ml = align_up(rows * s->head_dim * 4, 256);
     p->off_info = align_up(p->off_ml + rows * 8, 256);
@@ -139,10 +140,12 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
     const size_t n4 = static_cast<size_t>(n_tok) * 4;
     const Extent in[7] = {x[0], x[1], x[2], {table, static_cast<size_t>(n_seqs) * max_pages * 4}, {seq, seq ? n4 : 0},
                           {pos, n4}, {slopes, slopes ? static_cast<size_t>(s->n_q_heads) * 4 : 0}};
-    if (!ws) return api_fail(RM_ERR_INVALID_ARG, "workspace is NULL");
-    if (!aligned(ws, 256)) return api_fail(RM_ERR_ALIGN, "workspace must be 256-byte aligned");
-    if (ws_bytes < p.total)
-        return api_fail(RM_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu required", ws_bytes, p.total);
+    if (p.total > 0) {
+        if (!ws) return api_fail(RM_ERR_INVALID_ARG, "workspace is NULL");
+        if (!aligned(ws, 256)) return api_fail(RM_ERR_ALIGN, "workspace must be 256-byte aligned");
+        if (ws_bytes < p.total)
+            return api_fail(RM_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu required", ws_bytes, p.total);
+    }
     const Extent written[2] = {x[3], {ws, p.total}};
     r = check_apart(in, 7, written, 2);
     if (r != RM_OK) return r;
@@ -162,9 +165,11 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
     // (An instruction's rows from its first one in 32 bits, and rows of the cache in 32 bits of 16 bytes each.)
     const size_t wide = size_t{16} << 32;
     p.whole = page % p.rpi == 0 && a.k_t < 1 << 28 && a.v_t < 1 << 28 && x[1].n < wide && x[2].n < wide;
-    a.part_o = static_cast<float *>(ws);
-    a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.off_ml);
-    a.info = reinterpret_cast<int2 *>(static_cast<char *>(ws) + p.off_info);
+    if (p.total > 0) {
+        a.part_o = static_cast<float *>(ws);
+        a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.off_ml);
+        a.info = reinterpret_cast<int2 *>(static_cast<char *>(ws) + p.off_info);
+    }
     const float log2e = 1.4426950408889634f;
     if (s->softcap > 0.0f) {
         a.cap = s->softcap * log2e;

@@ -383,6 +383,38 @@ def test_paged_offsets_past_32_bits():
     check_paged(q, k[used], v[used], compact, pos, out=out, heads=[0, 7, 15])
 
 
+def test_paged_offsets_past_36_bits():
+    """Pages 40 GiB apart: more than 2^32 pieces of 16 bytes."""
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("needs 150 GiB of free memory")
+    g = gen(15)
+    page, Hk, D = 16, 2, 64
+    apart = (40 << 30) // 2
+    room = torch.empty((2 * apart + page * Hk * D * 2,), dtype=BF, device="cuda")
+    k = room.as_strided((3, page, Hk, D), (apart, Hk * D, D, 1))
+    v = room.as_strided((3, page, Hk, D), (apart, Hk * D, D, 1), page * Hk * D)
+    near_k, near_v = randn(g, (3, page, Hk, D), BF), randn(g, (3, page, Hk, D), BF)
+    k.copy_(near_k)
+    v.copy_(near_v)
+    table, pos, q = ints([[2, 0, 1], [1, 2, 0]]), ints([40, 17]), randn(g, (2, 8, D), BF, 2.0)
+    out = run_paged(q, k, v, table, pos)
+    check_paged(q, near_k, near_v, table, pos, out=out)
+    assert torch.equal(out, run_paged(q, near_k, near_v, table, pos))
+    del room, k, v
+    torch.cuda.empty_cache()
+
+
+def test_paged_batches_of_one_wave():
+    """So few keys that no token is divided: no workspace."""
+    g = gen(16)
+    for N, D, Hq, Hk, dtype in ((1, 64, 8, 1, BF), (1, 128, 80, 2, F32), (2, 72, 4, 4, BF)):
+        k, v, table = cache(g, N, 2, 16, Hk, D, dtype)
+        q = randn(g, (N, Hq, D), dtype, 2.0)
+        assert rm.paged_attention_workspace(q, k, table).numel() == 0 or N * 2 * 16 > 32
+        for p in (0, 13, 31):
+            check_paged(q, k, v, table, ints([p - i for i in range(N)]))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_paged_is_the_same_on_every_call(dtype):
     """Repeated calls, with other things in the workspace, on another stream, and captured and replayed on new positions."""

@@ -125,6 +125,7 @@ def test_paged_attention_workspace_refuses(lib):
     s = ctypes.byref(rm.AttnShape(8, 2, 64, 1, 0.125, 0.0))
     assert lib.rm_paged_attention_workspace_size(s, 3, 16, 4, ctypes.byref(n)) == rm.RM_OK
     assert n.value % 256 == 0
+    assert lib.rm_paged_attention_workspace_size(s, 1, 16, 8, ctypes.byref(n)) == rm.RM_OK and n.value == 0  # one wave's
     assert lib.rm_paged_attention_workspace_size(s, 3, 16, 4, None) == rm.RM_ERR_INVALID_ARG
     assert lib.rm_paged_attention_workspace_size(None, 3, 16, 4, ctypes.byref(n)) == rm.RM_ERR_INVALID_ARG
     assert lib.rm_paged_attention_workspace_size(s, 0, 16, 4, ctypes.byref(n)) == rm.RM_ERR_INVALID_ARG
