@@ -18,26 +18,36 @@ __device__ __forceinline__ int divide(int n, rm_attn::Divisor d) {  // n < 2^30
     return d.mul == 0 ? n : static_cast<int>(__umulhi(static_cast<uint32_t>(n), d.mul) >> d.shift);
 }
 
+// v added to by the lane CTRL of a data-parallel step says, in the rows of lanes of MASK.
+template <int CTRL, int MASK>
+__device__ __forceinline__ uint2 step(uint2 v) {
+    return make_uint2(add(v.x, __builtin_amdgcn_update_dpp(0, static_cast<int>(v.x), CTRL, MASK, 0xf, false)),
+                      add(v.y, __builtin_amdgcn_update_dpp(0, static_cast<int>(v.y), CTRL, MASK, 0xf, false)));
+}
+__device__ __forceinline__ uint2 scan16(uint2 v) {  // along the rows of 16 lanes
+    return step<0x118, 0xf>(step<0x114, 0xf>(step<0x112, 0xf>(step<0x111, 0xf>(v))));
+}
+__device__ __forceinline__ uint2 of_lane(uint2 v, int lane) {
+    return make_uint2(__builtin_amdgcn_readlane(v.x, lane), __builtin_amdgcn_readlane(v.y, lane));
+}
+
 // Running sums of two values over the workgroup's threads, their own included; all gets the sums of everyone.
 __device__ __forceinline__ uint2 scan(uint2 v, uint2 &all, uint2 (&wave_sum)[kThreads / 64]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = __shfl_up(v.x, o), y = __shfl_up(v.y, o);
-        if (lane >= o) v = make_uint2(add(v.x, x), add(v.y, y));
-    }
+    static_assert(kThreads == 1024, "a row of lanes has the sums of 16 waves");
+    const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    v = step<0x143, 0xc>(step<0x142, 0xa>(scan16(v)));
     if (waves == 1) {
-        all = make_uint2(__shfl(v.x, 63), __shfl(v.y, 63));
+        all = of_lane(v, 63);
         return v;
     }
     __syncthreads();
     if (lane == 63) wave_sum[wave] = v;
     __syncthreads();
-    all = make_uint2(0, 0);
-    uint2 before = all;
-    for (int w = 0; w < waves; ++w) {
-        if (w == wave) before = all;
-        all = make_uint2(add(all.x, wave_sum[w].x), add(all.y, wave_sum[w].y));
-    }
+    const uint2 sums = scan16(lane < waves ? wave_sum[lane] : make_uint2(0, 0));
+    all = of_lane(sums, waves - 1);
+    if (wave == 0) return v;
+    const uint2 before = of_lane(sums, wave - 1);
     return make_uint2(add(v.x, before.x), add(v.y, before.y));
 }
 

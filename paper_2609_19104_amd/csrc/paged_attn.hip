@@ -620,9 +620,10 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
 // The parts that groups of waves left of a token, joined in a fixed order: `share` lane groups (a power of two) divide the
 // parts of one query head, and a workgroup takes as many heads of an entry and unit as it has such.  Bound by three round
 // trips (the entry, the parts, the store).
+constexpr int kJoinAtOnce = 8;  // parts of a lane group whose loads are in flight together
 template <bool BF, int LPR, int QR>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int share, int blocks) {
-    constexpr int GR = 256 / LPR;
+    constexpr int GR = 256 / LPR, AT = kJoinAtOnce;
     __shared__ float tops[GR], sums[GR];
     __shared__ rm_f32x4 part[GR][LPR];
     const int eu = blockIdx.x / blocks, block = blockIdx.x - eu * blocks, e = divide(eu, a.by_units), u = eu - e * a.units;
@@ -636,19 +637,22 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int share,
     const int c = min(lane * 4, a.D - 4);
     rm_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
-    for (int p0 = is ? sub : parts; p0 < parts; p0 += 4 * share) {
-        float2 ml[4];
-        rm_f32x4 v[4];
+    for (int p0 = is ? sub : parts; p0 < parts; p0 += AT * share) {
+        float2 ml[AT];
+        rm_f32x4 v[AT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t at = row(min(p0 + i * share, parts - 1));
-            ml[i] = a.part_ml[at];
-            v[i] = *reinterpret_cast<const rm_f32x4 *>(a.part_o + at * a.D + c);
+        for (int i = 0; i < AT; ++i) {
+            ml[i] = make_float2(-INFINITY, 0.0f);
+            v[i] = rm_f32x4{};
+            if (p0 + i * share < parts) {
+                const int64_t at = row(p0 + i * share);
+                ml[i] = a.part_ml[at];
+                v[i] = *reinterpret_cast<const rm_f32x4 *>(a.part_o + at * a.D + c);
+            }
         }
         float top = m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (p0 + i * share >= parts) ml[i] = make_float2(-INFINITY, 0.0f);
+        for (int i = 0; i < AT; ++i) {
             top = fmaxf(top, ml[i].x);
         }
         const float ref = top == -INFINITY ? 0.0f : top;
@@ -657,7 +661,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int share,
         o *= f;
         m = top;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < AT; ++i) {
             if (ml[i].y == 0.0f) continue;  // (no key with a weight: its sums are zeros)
             f = __builtin_amdgcn_exp2f(ml[i].x - ref);
             l += ml[i].y * f;
@@ -698,8 +702,8 @@ hipError_t go(const PagedPlan &p, const PagedArgs &a, hipStream_t st) {
     else paged_kernel<BF, false, DC, QR><<<grid, 64, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.join) return e;
-    // A token has groups / N parts and two more where it begins and ends, if all are as long; a lane group takes four at a
-    // time.
+    // A token has groups / N parts and two more where it begins and ends, if all are as long; lane groups
+    // share them until one has at most four.
     constexpr int LPR = room(DC) / 4, GR = 256 / LPR;
     const int entries = std::min(a.N, a.groups), parts = a.groups / entries + 2;
     int share = 1;
