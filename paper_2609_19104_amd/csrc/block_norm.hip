@@ -39,8 +39,14 @@ __device__ __forceinline__ float sum_row(float s, float *red) {
     return s;
 }
 
-// TPR threads hold a row in registers, N chunks of V columns each, so that x and f are read once, all at the start.  A
-// chunk is 16 bytes of the widest of the three, so that a wave's loads of it are consecutive.
+// TPR threads hold a row in registers, N chunks of V columns each, so that x and f are read once, all at the start, and
+// both sums of squares and the norms are float32.  A chunk is 16 bytes of the widest of the three types, so that a wave's
+// loads of it are consecutive.  out is made of u before u is rounded for y: two roundings fewer than from y.
+//
+// Bound by memory: 16384 rows of 2048 columns, float32 x and y, bf16 f and out, gains, gate, scale and shift: 77 us, 5.2 TB/s
+// (a copy: 4.9).  On the way there: three passes over a row 282; a wave a row in registers, eight columns a chunk, 99.5, as
+// its float32 loads leave every other 16 bytes to the next one; 256 threads a row 94; past the caches 90.  850 rows 5.9 us
+// and 51 of 1024 columns 3.4, in a graph: a launch and two trips to memory.
 template <bool XB, bool FB, bool OB, int TPR, int N>
 __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void block_norm_kernel(NormArgs a) {
     constexpr int V = XB && FB && OB ? 8 : 4, ROWS = TPR < 128 ? 256 / TPR : 1;  // rows of a workgroup

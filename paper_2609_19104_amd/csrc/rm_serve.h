@@ -7,7 +7,7 @@ namespace rm_serve {
 
 struct SlotArgs {
     int B = 0, max_tok = 0, page = 0, n_pages = 0, per = 0;  // per: table entries of a request
-    int most_fill = 4096;
+    int most_fill = 4096;  // tokens that the first kernel writes
     rm_attn::Divisor by_page;
     const int32_t *n_new = nullptr, *len = nullptr, *n_free = nullptr;
     int32_t *table = nullptr, *free_pages = nullptr;
@@ -28,8 +28,8 @@ struct PagedArgs {
     int D = 0, G = 0;
     // Units of a token: key heads times blocks of query heads; query heads of a block at most.
     int units = 0, q_tiles = 0, rows = 0;
-    // Groups of waves, the least tiles of one, and where the parts of divided tokens are told: [N] or [groups].
-    int groups = 0, least = 0, by_token = 0;
+    // Groups of waves, and where the parts of divided tokens are told: [N] or [groups].
+    int groups = 0, by_token = 0;
     float scale = 0.0f, cap = 0.0f;  // scores in powers of two; with a cap: scale = score scale / cap
     float *part_o = nullptr;         // [groups][2][units][rows of a block][D]
     float2 *part_ml = nullptr;       // [groups][2][units][rows of a block]

@@ -32,7 +32,9 @@ rm_status check_pages(int page, int n_pages, int max_pages) {
     return RM_OK;
 }
 
-constexpr int kLeastTiles = 1;
+// Up to this many tiles one group has them all and no join follows (one token on 128 keys of 64 columns 6.2 us, in three groups
+// 8.6).  Above, a tile a group pays (one token on 1024 keys, 8 heads of 64 columns: a tile each 8.2, two each 10.4, four 14).
+constexpr int64_t kOneGroup = 4;
 
 rm_status paged_plan(const rm_attn_shape *s, int n_tok, int page, int max_pages, rm_serve::PagedPlan *p) {
     rm_status r = check_attn_shape(s);
@@ -48,7 +50,9 @@ rm_status paged_plan(const rm_attn_shape *s, int n_tok, int page, int max_pages,
     const int64_t most = n_tok * (ceil_div(static_cast<int64_t>(max_pages) * page, p->kt) + 1);  // tiles, at most
     if (most >= (1 << 30) - 2048)
         return api_fail(RM_ERR_SHAPE, "%lld tiles of keys are not below 2^30 - 2048", static_cast<long long>(most));
-    p->groups = most <= 4 ? 1 : static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(256 * p->per_cu / p->units, ceil_div(most, kLeastTiles))));
+    // As many groups as fill 256 compute units once.
+    const int64_t fill = std::max(1, 256 * p->per_cu / p->units);
+    p->groups = most <= kOneGroup ? 1 : static_cast<int>(std::min(fill, most));
     p->by_token = n_tok <= p->groups;
     p->join = p->groups > 1;
     if (!p->join) return RM_OK;  // every token is one wave's
@@ -161,7 +165,7 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
     a.units = p.units, a.q_tiles = p.q_tiles, a.rows = std::min(a.G, p.qr);
     a.by_page = rm_attn::divisor(page), a.by_q_tiles = rm_attn::divisor(p.q_tiles);
     a.by_units = rm_attn::divisor(p.units), a.by_groups = rm_attn::divisor(p.groups);
-    a.groups = p.groups, a.least = kLeastTiles, a.by_token = p.by_token;
+    a.groups = p.groups, a.by_token = p.by_token;
     // (An instruction's rows from its first one in 32 bits, and rows of the cache in 32 bits of 16 bytes each.)
     const size_t wide = size_t{16} << 32;
     p.whole = page % p.rpi == 0 && a.k_t < 1 << 28 && a.v_t < 1 << 28 && x[1].n < wide && x[2].n < wide;
