@@ -413,14 +413,6 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             }
         }
         // ---------------------------------------------------------------- S^T = K Q^T
-        // All reads first: one after the other with its product, each would cost the whole way to LDS and back.
-        Frag kf[QF][NS];
-        if (!first) {
-#pragma unroll
-            for (int c = 0; c < QF; ++c)
-#pragma unroll
-                for (int i = 0; i < NS; ++i) kf[c][i] = read_chunk(kt + i * 16 * ROWB, c);
-        }
         Tile after = nxt;
         if (more) {
             if (left > 1) advance(after);
@@ -437,24 +429,37 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int i = 0; i < NS; ++i) part[h][r][i] = rm_f32x4{};
+        // In as many groups as the loads: a group's reads from LDS, four load instructions, its products, so that a read's way
+        // to LDS and back passes while the load unit is busy, and few fragments take registers.
 #pragma unroll
         for (int g = 0; g < GS; ++g) {
+            constexpr int PER = (QF + GS - 1) / GS;
+            const int c0 = g * QF / GS, c1 = (g + 1) * QF / GS;
+            Frag kf[PER][NS];
+            __builtin_amdgcn_sched_barrier(0);
+            if (!first) {
+#pragma unroll
+                for (int c = c0; c < c1; ++c)
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) kf[c - c0][i] = read_chunk(kt + i * 16 * ROWB, c);
+            }
             __builtin_amdgcn_sched_barrier(0);
             if (more) stage(next, false, 4 * g, turn);
             if (first) continue;
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int c = g * QF / GS; c < (g + 1) * QF / GS; ++c)
+            for (int c = c0; c < c1; ++c)
 #pragma unroll
                 for (int i = 0; i < NS; ++i)
 #pragma unroll
                     for (int r = 0; r < RT; ++r) {
                         rm_f32x4 &x = part[c % CH][r][i];
                         if constexpr (BF) {
-                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[c][i], qf[r][c], x, 0, 0, 0);
+                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[c - c0][i], qf[r][c], x, 0, 0, 0);
                         } else {
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                x = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][i][e], qf[r][c][e], x, 0, 0, 0);
+                                x = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c - c0][i][e], qf[r][c][e], x, 0, 0, 0);
                         }
                     }
         }
@@ -536,50 +541,59 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         }
         if constexpr (BF) {
             typedef __attribute__((address_space(3))) rm_s16x4 lds_s16x4;
+            constexpr int PER = NS * DB / GS;
             const int row = 4 * h4 + (m16 >> 2);
             const uint8_t *v = vt + row * ROWB + (m16 & 3) * 8;
-            rm_s16x4 vf[NS][DB];
 #pragma unroll
-            for (int i = 0; i < NS; ++i)
+            for (int g = 0; g < GS; ++g) {
+                rm_s16x4 vf[PER];
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    vf[i][d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                for (int x = 0; x < PER; ++x) {
+                    const int i = (g * PER + x) / DB, d = (g * PER + x) % DB;
+                    vf[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                         (lds_s16x4 *)(v + 16 * i * ROWB + (((2 * d) & 15) ^ swz_v(row)) * 16 + (d >> 3) * 256));
-#pragma unroll
-            for (int x = 0; x < NS * DB; ++x) {
-                const int i = x / DB, d = x % DB;
-                if (x % (NS * DB / GS) == 0) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (more) stage(next, true, 4 * (x / (NS * DB / GS)), turn);
                 }
+                __builtin_amdgcn_sched_barrier(0);
+                if (more) stage(next, true, 4 * g, turn);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    const rm_bf16x4 p = {static_cast<__bf16>(s[r][i][0]), static_cast<__bf16>(s[r][i][1]),
-                                         static_cast<__bf16>(s[r][i][2]), static_cast<__bf16>(s[r][i][3])};
-                    o[r][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf[i][d], __builtin_bit_cast(rm_s16x4, p), o[r][d], 0,
-                                                                        0, 0);
+                for (int x = 0; x < PER; ++x) {
+                    const int i = (g * PER + x) / DB, d = (g * PER + x) % DB;
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        const rm_bf16x4 p = {static_cast<__bf16>(s[r][i][0]), static_cast<__bf16>(s[r][i][1]),
+                                             static_cast<__bf16>(s[r][i][2]), static_cast<__bf16>(s[r][i][3])};
+                        o[r][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf[x], __builtin_bit_cast(rm_s16x4, p), o[r][d],
+                                                                            0, 0, 0);
+                    }
                 }
             }
         } else {
+            constexpr int PER = 4 * NS / GS;  // fours of keys, one of each lane row
 #pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                float vf[4][DB];
+            for (int g = 0; g < GS; ++g) {
+                float vf[PER][DB];
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int x = 0; x < PER; ++x) {
+                    const int row = 16 * ((g * PER + x) / 4) + 4 * h4 + (g * PER + x) % 4;
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
-                        vf[e][d] = *reinterpret_cast<const float *>(
-                            vt + (16 * i + 4 * h4 + e) * ROWB + (((4 * d) & 15) ^ (4 * h4)) * 16 + (d >> 2) * 256 + m16 * 4);
+                        vf[x][d] = *reinterpret_cast<const float *>(vt + row * ROWB + (((4 * d) & 15) ^ (4 * h4)) * 16 +
+                                                                    (d >> 2) * 256 + m16 * 4);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (more) stage(next, true, 4 * g, turn);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    if ((4 * i + e) % (4 * NS / GS) == 0 && more) stage(next, true, 4 * ((4 * i + e) / (4 * NS / GS)), turn);
+                for (int x = 0; x < PER; ++x)
 #pragma unroll
                     for (int r = 0; r < RT; ++r)
 #pragma unroll
                         for (int d = 0; d < DB; ++d)
-                            o[r][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e][d], s[r][i][e], o[r][d], 0, 0, 0);
-                }
+                            o[r][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                                vf[x][d], s[r][(g * PER + x) / 4][(g * PER + x) % 4], o[r][d], 0, 0, 0);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
