@@ -175,9 +175,12 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:  # the current stream's handle itself, without a Stream object around it
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return _raw_stream(_current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -649,10 +652,13 @@ def _vector(name: str, t: Optional[torch.Tensor], dtype, index: int, shape) -> O
 
 def _attn_device(t: torch.Tensor, stream) -> int:
     """The tensors' device, which has to be the current one (the kernels are launched there), as the stream's has."""
-    index = t.get_device() if isinstance(t, torch.Tensor) else -1
+    try:
+        index = t.get_device()
+    except AttributeError:
+        index = -1
     if index < 0:
         raise ValueError("tensors must be on a HIP device")
-    if index != torch._C._cuda_getDevice():
+    if index != _current_device():
         raise ValueError(f"tensors are on {t.device}, which is not the current device")
     if stream is not None and getattr(stream, "device_index", index) != index:
         raise ValueError(f"the stream is of another device than the tensors, which are on {t.device}")
@@ -865,10 +871,8 @@ def rm_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
         _stream(stream)))
 
 
-def _modulation(name: str, t: Optional[torch.Tensor], index: int, shape) -> Tuple[Optional[int], int]:
+def _modulation(name: str, t: torch.Tensor, index: int, shape) -> Tuple[int, int]:
     """Pointer and row stride of a float32 [B][d] tensor whose rows are contiguous."""
-    if t is None:
-        return None, 0
     try:
         row, c = t.stride()
         if c == 1 and t.dtype is torch.float32 and t.shape == shape and t.get_device() == index:
@@ -896,17 +900,27 @@ def rm_block_norm(x: torch.Tensor, f: Optional[torch.Tensor], y: Optional[torch.
     xt = x.dtype
     ft = xt if f is None else f.dtype
     ot = xt if out is None else out.dtype
-    if xt not in _ATTN_DTYPES or ft not in _ATTN_DTYPES or ot not in _ATTN_DTYPES:
-        raise ValueError("x, f and out must be float32 or bfloat16")
-    f32, row, mod = torch.float32, (d,), (B, d)
-    gp, gs = _modulation("gate", gate, dev, mod)
-    sp, ss = _modulation("scale", scale, dev, mod)
-    hp, hs = _modulation("shift", shift, dev, mod)
+    try:
+        xd, fd, od = _ATTN_DTYPES[xt], _ATTN_DTYPES[ft], _ATTN_DTYPES[ot]
+    except KeyError:
+        raise ValueError("x, f and out must be float32 or bfloat16") from None
+    f32 = torch.float32
+    gp = sp = hp = g1 = g2 = None
+    gs = ss = hs = 0
+    if gate is not None:
+        gp, gs = _modulation("gate", gate, dev, (B, d))
+    if scale is not None:
+        sp, ss = _modulation("scale", scale, dev, (B, d))
+    if shift is not None:
+        hp, hs = _modulation("shift", shift, dev, (B, d))
+    if gain_post is not None:
+        g1 = _vector("gain_post", gain_post, f32, dev, (d,))
+    if gain_pre is not None:
+        g2 = _vector("gain_pre", gain_pre, f32, dev, (d,))
     _check(load_library().rm_block_norm(
-        B, T, d, _ATTN_DTYPES[xt], _ATTN_DTYPES[ft], _ATTN_DTYPES[ot], _vector("x", x, xt, dev, shape),
-        _vector("f", f, ft, dev, shape), norm_post, _vector("gain_post", gain_post, f32, dev, row), gp, gs, x_scale, f_scale,
-        _vector("y", y, xt, dev, shape), _vector("gain_pre", gain_pre, f32, dev, row), sp, ss, hp, hs, eps,
-        _vector("out", out, ot, dev, shape), _stream(stream)))
+        B, T, d, xd, fd, od, _vector("x", x, xt, dev, shape), _vector("f", f, ft, dev, shape), norm_post, g1, gp, gs, x_scale,
+        f_scale, _vector("y", y, xt, dev, shape), g2, sp, ss, hp, hs, eps, _vector("out", out, ot, dev, shape),
+        _stream(stream)))
 
 
 def rm_profile_kernel_events(kernel: int, ev_begin: Optional[int], ev_end: Optional[int]) -> None:
