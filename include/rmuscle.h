@@ -448,7 +448,9 @@ rm_status rm_page_slots(int32_t n_seqs, int32_t max_tok, int32_t page, int32_t n
  *   ws, ws_bytes: at least rm_paged_attention_workspace_size bytes (which may be 0: ws may then be NULL), 256-byte
  *             aligned; scratch as for rm_workspace_size.
  * Several new tokens of one request are several n with its seq and rising pos; its keys are read for each of them, so a
- * long chunk of a prompt is better served by rm_span_attention on keys in a row.  n_tok * n_q_heads < 2^24.
+ * long chunk of a prompt is better served by rm_span_attention on keys in a row.  n_tok * n_q_heads < 2^24 and
+ * n_tok * (max_pages * page / 16 + 1) < 2^30 - 2048.  Repeated calls give bitwise equal outputs; how a token's keys are
+ * divided, and with it the order of its sums, depends on the whole batch's positions.
  * Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN, RM_ERR_WORKSPACE, RM_ERR_HIP. */
 rm_status rm_paged_attention_workspace_size(const rm_attn_shape *s, int32_t n_tok, int32_t page, int32_t max_pages,
                                             size_t *bytes);

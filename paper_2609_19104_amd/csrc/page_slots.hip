@@ -125,7 +125,9 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
         const bool is = b < a.B;
         const uint32_t have = pages(old);
         bool fits = n >= 0 && n <= room - old;
-        uint2 mine = make_uint2(static_cast<uint32_t>(min(max(n, 0), static_cast<int>(kMost))), fits ? pages(old + n) - have : 0);
+        uint2 mine;
+        mine.x = static_cast<uint32_t>(min(max(n, 0), static_cast<int>(kMost)));
+        mine.y = fits ? pages(old + n) - have : 0;
         uint2 all, upto = scan(mine, all, wave_sum);
         const uint32_t end = add(tokens, upto.x), n_all = all.x;
         if (add(tokens, n_all) > max_tok) {  // tokens past the batch's room want no pages

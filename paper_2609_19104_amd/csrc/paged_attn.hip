@@ -3,10 +3,10 @@
 //
 // One pass over the keys with a running maximum and sum, as in rm_attn.h, but for rows that share their keys only with the
 // few query heads of a key head: every byte of the cache is read once, and reading is what bounds it.  What that took, us for
-// 64 tokens of 32 heads on 8 on up to 8192 keys (1.21 GB) / 4 of 32 on 4 on 131072 (1.07 GB), bf16, heads of 128 columns:
+// 64 tokens of 32 heads on 8 on up to 8192 keys (1.18 GB) / 4 of 32 on 4 on 131072 (1.06 GB), bf16, heads of 128 columns:
 // a workgroup a query head 4998 / 67790; the kernel below with a wave a share of (token, head, key) 248 / 209; loads past the
 // caches' other lines 191 / 180; waves of a group on the same rows at the same time, and what else is told below, 189 / 172:
-// 6.4 and 6.2 TB/s (a read of one large buffer: 5.9).  Smaller calls are bound by round trips: launch, positions, table,
+// 6.3 and 6.2 TB/s (a read of one large buffer: 5.9).  Smaller calls are bound by round trips: launch, positions, table,
 // keys, the parts' join: one token on 850 keys 11.3, on 8192 14.5.
 #include <algorithm>
 
@@ -87,9 +87,9 @@ __device__ __forceinline__ void dma4(const void *g, uint32_t lds) {
 
 // Matrix-core layout (16x16 tiles): S^T = K Q^T, so a lane holds scores of query head lane % 16, keys 4 (lane / 16) + {0..3} of
 // 16; O^T = V^T P^T takes them as they are, V's fragments read in the same order of keys.  A group of 8 heads fills half of
-// a tile, which costs nothing in bf16 (the products take a sixth of the time that a tile's bytes do); in float32 the products
-// are a third of a step of 2.1 us, which bounds calls of that type (37 tokens of 6 heads on 3, 72 columns, 1111 keys each:
-// 24 us, 71 MB).  Fragments of QR = 8 heads are kept in half the LDS, so that four waves fit.
+// a tile, which costs nothing in bf16 (the products take a sixth of the time that a tile's bytes do); in float32 they are a third
+// of a step of 2.1 us, and issuing the loads half of it (37 tokens of 6 heads on 3, 72 columns, up to 1111 keys each: 24 us
+// for 63 MB).  Fragments of QR = 8 heads are kept in half the LDS, so that four waves fit.
 
 // The value, as if it became known here only: what is made of it then stays where it is used, instead of taking registers
 // and time in front of the loop.
@@ -535,7 +535,8 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
 #pragma unroll
             for (int i = 0; i < TILEB / 1024; ++i) {
                 const int at = i * 64 + own;
-                if (!((vis >> (at / CPR)) & 1)) *reinterpret_cast<rm_u32x4 *>(lds + buf + TILEB + at * 16) = rm_u32x4{0, 0, 0, 0};
+                if (!((vis >> (at / CPR)) & 1))
+                    *reinterpret_cast<rm_u32x4 *>(lds + buf + TILEB + at * 16) = rm_u32x4{0, 0, 0, 0};
             }
             wait_lds();
         }
@@ -603,7 +604,8 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             const Arguments b = again();
             const bool starts = cur.base >= begin, ends = cur.t + 1 == cur.t1;
             if (starts) {
-                const int parts = (cur.base + (cur.t1 - cur.t0) - 1) / share - grp + 1;
+                // (No more than there are groups, whatever else may write the positions meanwhile.)
+                const int parts = min((cur.base + (cur.t1 - cur.t0) - 1) / share, b->groups - 1) - grp + 1;
                 if (b->info && b->by_token && unit == 0 && lane == 0) b->info[cur.n] = make_int2(grp, parts);
                 if (!ends) end_info = make_int2(cur.n, parts);
             }
@@ -721,8 +723,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int share,
     o *= l == 0.0f ? 0.0f : 1.0f / l;
     char *dst = a.o + n * a.o_t + static_cast<int64_t>(hk * a.G + g) * a.o_h;
     if constexpr (BF)
-        *reinterpret_cast<rm_bf16x4 *>(dst + c * 2) =
-            rm_bf16x4{static_cast<__bf16>(o[0]), static_cast<__bf16>(o[1]), static_cast<__bf16>(o[2]), static_cast<__bf16>(o[3])};
+        *reinterpret_cast<rm_bf16x4 *>(dst + c * 2) = rm_bf16x4{static_cast<__bf16>(o[0]), static_cast<__bf16>(o[1]),
+                                                                static_cast<__bf16>(o[2]), static_cast<__bf16>(o[3])};
     else
         *reinterpret_cast<rm_f32x4 *>(dst + c * 4) = o;
 }

@@ -79,8 +79,9 @@ RM_EXPORT rm_status rm_page_slots(int32_t n_seqs, int32_t max_tok, int32_t page,
     if (n_pages >= 1 << 30) return api_fail(RM_ERR_SHAPE, "n_pages=%d is not below 2^30", n_pages);
     const size_t b4 = static_cast<size_t>(n_seqs) * 4, t4 = static_cast<size_t>(max_tok) * 4;
     const Extent in[3] = {{n_new, b4}, {len, b4}, {n_free, 4}};
-    const Extent out[10] = {{len_out, b4}, {n_free_out, 4}, {table, b4 * max_pages}, {free_pages, static_cast<size_t>(n_pages) * 4},
-                            {first, b4 + 4}, {start, b4}, {seq, t4}, {pos, t4}, {slot, t4}, {refused, refused ? 4u : 0u}};
+    const size_t p4 = static_cast<size_t>(n_pages) * 4;
+    const Extent out[10] = {{len_out, b4}, {n_free_out, 4}, {table, b4 * max_pages}, {free_pages, p4}, {first, b4 + 4},
+                            {start, b4}, {seq, t4}, {pos, t4}, {slot, t4}, {refused, refused ? 4u : 0u}};
     for (const Extent &e : in)
         if (!e.p) return api_fail(RM_ERR_INVALID_ARG, "n_new, len or n_free is NULL");
     for (const Extent &e : out)
@@ -224,8 +225,10 @@ RM_EXPORT rm_status rm_block_norm(int32_t B, int32_t T, int32_t d, int32_t x_dty
         if (!mod[i].p) continue;
         if (B > 1) {
             if (mod[i].stride < 0 || mod[i].stride > INT64_MAX / 16 / B)
-                return api_fail(RM_ERR_SHAPE, "%s: a stride of %lld elements", mod[i].name, static_cast<long long>(mod[i].stride));
-            if (mod[i].stride % 4 != 0) return api_fail(RM_ERR_ALIGN, "%s: its stride must be a multiple of 16 bytes", mod[i].name);
+                return api_fail(RM_ERR_SHAPE, "%s: a stride of %lld elements", mod[i].name,
+                                static_cast<long long>(mod[i].stride));
+            if (mod[i].stride % 4 != 0)
+                return api_fail(RM_ERR_ALIGN, "%s: its stride must be a multiple of 16 bytes", mod[i].name);
             stride[i] = mod[i].stride;
         }
         in[4 + i] = {mod[i].p, static_cast<size_t>(stride[i]) * (B - 1) * 4 + d4};

@@ -140,7 +140,8 @@ def test_slots_in_a_graph():
     r = serving.page_slots(length, [0] * B, table, free, n_free, page, 1000)
     length, table, free, n_free = r.length, r.table, r.free_pages, r.n_free
     t = dict(n_new=ints([1] * B), length=ints(length), table=ints(table), free_pages=ints(free), n_free=ints([n_free]))
-    o = {k: torch.zeros((n,), dtype=torch.int32, device="cuda") for k, n in dict(first=B + 1, start=B, seq=B, pos=B, slot=B).items()}
+    sizes = dict(first=B + 1, start=B, seq=B, pos=B, slot=B)
+    o = {k: torch.zeros((n,), dtype=torch.int32, device="cuda") for k, n in sizes.items()}
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
         graph = torch.cuda.CUDAGraph()
@@ -326,7 +327,8 @@ def test_scores_without_end(dtype, D):
     out = run_paged(q, k, v, table, pos)
     k2 = k.clone()
     k2[page, 3, 0, :] = 0
-    ref = serving.paged_attention(f64(q), f64(k2), f64(v), table.cpu().numpy(), None, pos.cpu().numpy(), 0, np.float32(D ** -0.5))[0]
+    ref = serving.paged_attention(f64(q), f64(k2), f64(v), table.cpu().numpy(), None, pos.cpu().numpy(), 0,
+                                  np.float32(D ** -0.5))[0]
     kk, vv = f64(k2)[table.cpu()[0]].reshape(-1, 2, D)[:61, 0], f64(v)[table.cpu()[0]].reshape(-1, 2, D)[:61, 0]
     seen = np.ones((1, 61), bool)
     seen[0, 19] = False
@@ -465,7 +467,8 @@ def test_paged_refuses_a_small_workspace_and_other_devices():
     pos = ints([9000, 9000])
     if n > 0:
         with pytest.raises(rm.RmError) as e:
-            rm.rm_paged_attention(q, k, v, table, pos, torch.empty_like(q), torch.empty(n - 1, dtype=torch.uint8, device="cuda"))
+            rm.rm_paged_attention(q, k, v, table, pos, torch.empty_like(q),
+                                  torch.empty(n - 1, dtype=torch.uint8, device="cuda"))
         assert e.value.status == rm.RM_ERR_WORKSPACE
     with pytest.raises(ValueError):
         rm.rm_paged_attention(q, k.cpu(), v, table, pos, torch.empty_like(q), None)

@@ -187,7 +187,8 @@ def test_the_binding_refuses_cpu_tensors():
     i = torch.zeros(4, dtype=torch.int32)
     x = torch.zeros(2, 4, 8)
     with pytest.raises(ValueError):
-        rm.rm_page_slots(i, i, torch.zeros((4, 2), dtype=torch.int32), i, i[:1], torch.zeros(5, dtype=torch.int32), i, i, i, i, 4)
+        rm.rm_page_slots(i, i, torch.zeros((4, 2), dtype=torch.int32), i, i[:1], torch.zeros(5, dtype=torch.int32), i, i, i,
+                         i, 4)
     with pytest.raises(ValueError):
         rm.rm_paged_attention(x, x[None], x[None], torch.zeros((2, 1), dtype=torch.int32), i[:2], torch.zeros_like(x), None)
     with pytest.raises(ValueError):
