@@ -358,9 +358,12 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) k_at[c] = m16 * ROWB + (((4 * c + h4) ^ swz_k(m16)) & (CPR - 1)) * 16;
     auto read_chunk = [&](const uint8_t *rows, int c) __attribute__((always_inline)) {
-        Frag f = *reinterpret_cast<const Frag *>(rows + k_at[c & 3] + (c >> 2) * 256);
-        // Columns past the head's are its last ones again, which must not meet each other.
-        return static_cast<uint32_t>(4 * c + h4) <= last_chunk ? f : Frag{};
+        return *reinterpret_cast<const Frag *>(rows + k_at[c & 3] + (c >> 2) * 256);
+    };
+    // Columns past the head's are its last ones again, which must not meet each other.
+    const bool narrow = last_chunk + 1 < DC * ES / 16;
+    auto own_columns = [&](Frag &f, int c) __attribute__((always_inline)) {
+        f = static_cast<uint32_t>(4 * c + h4) <= last_chunk ? f : Frag{};
     };
 
     Tile cur, nxt;
@@ -379,6 +382,7 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
 #pragma unroll
     for (int r = 0; r < RT; ++r)
         slope[r] = a.slopes ? a.slopes[hk * a.G + g0 + min(r * 16 + m16, heads - 1)] * rm_attn::kLog2e : 0.0f;
+    const float sc = a.cap != 0.0f || a.slopes ? 1.0f : a.scale;
     int2 end_info = make_int2(0, 0);
     // A step stages a tile and takes the products of the one before it; the first has none before it.  The load
     // instructions go out between the products, since a wave that issues several in a row waits for the load unit.
@@ -401,10 +405,11 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
                         const int row = m16 & 7;
                         Frag f = *reinterpret_cast<const Frag *>(
                             lds_q + row * ROWB + ((((4 * (c & 3) + h4) ^ swz_k(row)) & (CPR - 1)) * 16) + (c >> 2) * 256);
-                        qf[r][c] = static_cast<uint32_t>(4 * c + h4) <= last_chunk ? f : Frag{};
+                        qf[r][c] = f;
                     } else {
                         qf[r][c] = read_chunk(rows, c);
                     }
+                    own_columns(qf[r][c], c);
                 }
                 m[r] = -INFINITY;
                 l[r] = 0.0f;
@@ -446,6 +451,12 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             __builtin_amdgcn_sched_barrier(0);
             if (more) stage(next, false, 4 * g, turn);
             if (first) continue;
+            if (narrow) {
+#pragma unroll
+                for (int c = c0; c < c1; ++c)
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) own_columns(kf[c - c0][i], c);
+            }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int c = c0; c < c1; ++c)
@@ -488,12 +499,13 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[r][i][e] = f(s[r][i][e], r, 16 * i + e);
         };
-        each([&](float x, int, int) { return x * a.scale; });
+        // Scores in powers of two are sc times these: plain products, or with a cap or a bias the scores themselves.
         if (__builtin_expect(a.cap != 0.0f, false))
-            each([&](float x, int, int) { return a.cap * (BF ? rm_attn::tanh_relative(x) : tanhf(x)); });
+            each([&](float x, int, int) { return a.cap * (BF ? rm_attn::tanh_relative(x * a.scale) : tanhf(x * a.scale)); });
         if (__builtin_expect(a.slopes != nullptr, false)) {
             const int d0 = cur.pos - (cur.t * KT + 4 * here(h4));
-            each([&](float x, int r, int j) { return fmaf(-slope[r], static_cast<float>(d0 - j), x); });
+            const float in = a.cap != 0.0f ? 1.0f : a.scale;
+            each([&](float x, int r, int j) { return fmaf(x, in, -slope[r] * static_cast<float>(d0 - j)); });
         }
         if (__builtin_expect(vis != kFull, false)) {
             const uint64_t bits = vis >> (4 * here(h4));
@@ -506,7 +518,7 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             for (int i = 0; i < NS; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, s[r][i][e]);
-            top = rows_max(top);
+            top = rows_max(top) * sc;
             const bool raise = top > m[r] + kRaise;  // (false for top = -inf)
             if (__any(raise)) {
                 const float mn = raise ? top : m[r];
@@ -521,7 +533,9 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             for (int i = 0; i < NS; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[r][i][e] = __builtin_amdgcn_exp2f(s[r][i][e] - ref);
+                    // (float32 rounds the score first, as the maximum was: the largest weight is 1 exactly)
+                    const float x = s[r][i][e];
+                    s[r][i][e] = __builtin_amdgcn_exp2f(BF ? fmaf(x, sc, -ref) : rm_attn::scaled(x, sc) - ref);
                     l[r] += s[r][i][e];
                 }
         }
