@@ -55,8 +55,8 @@ BF16_PEAK_TFLOPS = 2500.0  # MI355X dense bf16 matrix cores (no sparsity)
 PROFILES = os.path.join(ROOT, "profiles")
 CSRC = os.path.join(ROOT, "paper_2609_19104_amd", "csrc")
 # How the names of the attention side's and the serving step's files begin.
-ATTENTION_SOURCES = ("attn_", "rm_attn", "qk_norm_rope", "rm_rope", "rm_checks", "rm_serve", "serve_api", "page_slots",
-                     "paged_attn", "block_norm")
+ATTENTION_SOURCES = ("attn_", "rm_attn", "qk_norm_rope", "rm_rope", "rm_checks", "rm_serve", "rm_paged", "serve_api",
+                     "page_slots", "paged_attn", "block_norm")
 COLD_BYTES = 1 << 30   # weight copies rotated through per timed run
 
 

@@ -30,7 +30,7 @@ HIPCC_FLAGS = [
 # The attention kernels' accumulators stay in the registers that ordinary instructions take: the softmax reads and rescales
 # them, and in accumulation registers each such use is a move there and back.
 EXTRA_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-               for name in ("attn_bf16.hip", "attn_bf16_cap.hip", "attn_f32.hip", "paged_attn.hip")}
+               for name in ("attn_bf16.hip", "attn_bf16_cap.hip", "attn_f32.hip", "paged_attn_bf16.hip", "paged_attn_f32.hip")}
 
 
 def hipcc() -> str:

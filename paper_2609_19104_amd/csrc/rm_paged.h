@@ -1,5 +1,5 @@
-// Attention of one new token over a paged cache (rm_paged_attention): the kernel that walks the pages, and the join of
-// what several of its waves have of one token's head.
+// Attention of one new token over a paged cache (rm_paged_attention; bf16 in paged_attn_bf16.hip, float32 in
+// paged_attn_f32.hip): the kernel that walks the pages, and the join of what several of its waves have of one token's head.
 //
 // One pass over the keys with a running maximum and sum, as in rm_attn.h, but for rows that share their keys only with the
 // few query heads of a key head: every byte of the cache is read once, and reading is what bounds it.  What that took, us for
@@ -8,6 +8,8 @@
 // caches' other lines 191 / 180; waves of a group on the same rows at the same time, and what else is told below, 189 / 172:
 // 6.3 and 6.2 TB/s (a read of one large buffer: 5.9).  Smaller calls are bound by round trips: launch, positions, table,
 // keys, the parts' join: one token on 850 keys 11.3, on 8192 14.5.
+#pragma once
+
 #include <algorithm>
 
 #include "rm_attn.h"
@@ -782,18 +784,14 @@ void shape_of(PagedPlan &p) {
     p.rpi = Shape<BF, DH>::RPI;
     p.per_cu = std::min(4, 160 * 1024 / bytes);
 }
+template <bool BF>
+void shape_of(int D, int G, PagedPlan &p) {
+    p.qr = G <= 8 ? 8 : G <= 16 ? 16 : 32;
+    if (room(D) == 64) shape_of<BF, 64>(p);
+    else if (room(D) == 128) shape_of<BF, 128>(p);
+    else shape_of<BF, 256>(p);
+}
 
 }  // namespace
-
-void paged_shape(bool bf16, int D, int G, PagedPlan *p) {
-    const int dh = room(D);
-    p->qr = G <= 8 ? 8 : G <= 16 ? 16 : 32;
-    if (bf16) dh == 64 ? shape_of<true, 64>(*p) : dh == 128 ? shape_of<true, 128>(*p) : shape_of<true, 256>(*p);
-    else dh == 64 ? shape_of<false, 64>(*p) : dh == 128 ? shape_of<false, 128>(*p) : shape_of<false, 256>(*p);
-}
-
-hipError_t launch_paged(const PagedPlan &p, const PagedArgs &a, bool bf16, hipStream_t st) {
-    return bf16 ? by_width<true>(p, a, st) : by_width<false>(p, a, st);
-}
 
 }  // namespace rm_serve

@@ -1,4 +1,4 @@
-// Arguments of the serving-step kernels (page_slots.hip, paged_attn.hip, block_norm.hip).
+// Arguments of the serving-step kernels (page_slots.hip, rm_paged.h, block_norm.hip).
 #pragma once
 
 #include "rm_attn_plan.h"
@@ -42,8 +42,10 @@ struct PagedPlan {
     bool join = false, whole = false;  // whole: the rows of a load instruction are of one page
     size_t off_ml = 0, off_info = 0, total = 0;
 };
-void paged_shape(bool bf16, int D, int G, PagedPlan *p);  // qr, kt, rpi and per_cu
-hipError_t launch_paged(const PagedPlan &p, const PagedArgs &a, bool bf16, hipStream_t st);
+void paged_shape_bf16(int D, int G, PagedPlan *p);  // qr, kt, rpi and per_cu
+void paged_shape_f32(int D, int G, PagedPlan *p);
+hipError_t launch_paged_bf16(const PagedPlan &p, const PagedArgs &a, hipStream_t st);
+hipError_t launch_paged_f32(const PagedPlan &p, const PagedArgs &a, hipStream_t st);
 
 struct NormArgs {
     const char *x = nullptr, *f = nullptr;

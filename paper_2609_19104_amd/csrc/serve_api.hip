@@ -44,7 +44,7 @@ rm_status paged_plan(const rm_attn_shape *s, int n_tok, int page, int max_pages,
     if (static_cast<int64_t>(n_tok) * s->n_q_heads >= kMaxGroups)
         return api_fail(RM_ERR_SHAPE, "n_tok x n_q_heads = %d x %d is not below 2^24", n_tok, s->n_q_heads);
     const int G = s->n_q_heads / s->n_kv_heads;
-    rm_serve::paged_shape(s->dtype == RM_BF16, s->head_dim, G, p);
+    s->dtype == RM_BF16 ? rm_serve::paged_shape_bf16(s->head_dim, G, p) : rm_serve::paged_shape_f32(s->head_dim, G, p);
     p->q_tiles = static_cast<int>(ceil_div(G, p->qr));
     p->units = s->n_kv_heads * p->q_tiles;
     const int64_t most = n_tok * (ceil_div(static_cast<int64_t>(max_pages) * page, p->kt) + 1);  // tiles, at most
@@ -182,7 +182,8 @@ RM_EXPORT rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, in
     } else {
         a.scale = s->scale * log2e;
     }
-    const hipError_t e = rm_serve::launch_paged(p, a, s->dtype == RM_BF16, static_cast<hipStream_t>(stream));
+    const auto hs = static_cast<hipStream_t>(stream);
+    const hipError_t e = s->dtype == RM_BF16 ? rm_serve::launch_paged_bf16(p, a, hs) : rm_serve::launch_paged_f32(p, a, hs);
     if (e != hipSuccess) return api_fail(RM_ERR_HIP, "paged attention launch: %s", hipGetErrorString(e));
     return api_ok();
 }
