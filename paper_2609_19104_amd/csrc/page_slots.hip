@@ -8,7 +8,7 @@ namespace rm_serve {
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kAtOnce = 4;  // pages of a thread whose loads are in flight together
+constexpr int kAtOnce = 4;  // pages or tokens of a thread whose loads are in flight together
 // Running sums stop here, above every number of tokens or pages that a call takes; a sum that stops at its limit may
 // still be taken in any order.
 constexpr uint32_t kMost = 1u << 30;
@@ -18,21 +18,29 @@ __device__ __forceinline__ int divide(int n, rm_attn::Divisor d) {  // n < 2^30
     return d.mul == 0 ? n : static_cast<int>(__umulhi(static_cast<uint32_t>(n), d.mul) >> d.shift);
 }
 
+struct Sums {
+    uint32_t x, y, z;
+};
+__device__ __forceinline__ Sums add(Sums a, Sums b) { return {add(a.x, b.x), add(a.y, b.y), add(a.z, b.z)}; }
+
 // v added to by the lane CTRL of a data-parallel step says, in the rows of lanes of MASK.
 template <int CTRL, int MASK>
-__device__ __forceinline__ uint2 step(uint2 v) {
-    return make_uint2(add(v.x, __builtin_amdgcn_update_dpp(0, static_cast<int>(v.x), CTRL, MASK, 0xf, false)),
-                      add(v.y, __builtin_amdgcn_update_dpp(0, static_cast<int>(v.y), CTRL, MASK, 0xf, false)));
+__device__ __forceinline__ Sums step(Sums v) {
+    auto moved = [](uint32_t x) -> uint32_t {
+        return __builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, MASK, 0xf, false);
+    };
+    return add(v, {moved(v.x), moved(v.y), moved(v.z)});
 }
-__device__ __forceinline__ uint2 scan16(uint2 v) {  // along the rows of 16 lanes
+__device__ __forceinline__ Sums scan16(Sums v) {  // along the rows of 16 lanes
     return step<0x118, 0xf>(step<0x114, 0xf>(step<0x112, 0xf>(step<0x111, 0xf>(v))));
 }
-__device__ __forceinline__ uint2 of_lane(uint2 v, int lane) {
-    return make_uint2(__builtin_amdgcn_readlane(v.x, lane), __builtin_amdgcn_readlane(v.y, lane));
+__device__ __forceinline__ Sums of_lane(Sums v, int lane) {
+    return {static_cast<uint32_t>(__builtin_amdgcn_readlane(v.x, lane)), static_cast<uint32_t>(__builtin_amdgcn_readlane(v.y, lane)),
+            static_cast<uint32_t>(__builtin_amdgcn_readlane(v.z, lane))};
 }
 
-// Running sums of two values over the workgroup's threads, their own included; all gets the sums of everyone.
-__device__ __forceinline__ uint2 scan(uint2 v, uint2 &all, uint2 (&wave_sum)[kThreads / 64]) {
+// Running sums of three values over the workgroup's threads, their own included; all gets the sums of everyone.
+__device__ __forceinline__ Sums scan(Sums v, Sums &all, Sums (&wave_sum)[kThreads / 64]) {
     static_assert(kThreads == 1024, "a row of lanes has the sums of 16 waves");
     const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -44,22 +52,29 @@ __device__ __forceinline__ uint2 scan(uint2 v, uint2 &all, uint2 (&wave_sum)[kTh
     __syncthreads();
     if (lane == 63) wave_sum[wave] = v;
     __syncthreads();
-    const uint2 sums = scan16(lane < waves ? wave_sum[lane] : make_uint2(0, 0));
+    const Sums sums = scan16(lane < waves ? wave_sum[lane] : Sums{0, 0, 0});
     all = of_lane(sums, waves - 1);
-    if (wave == 0) return v;
-    const uint2 before = of_lane(sums, wave - 1);
-    return make_uint2(add(v.x, before.x), add(v.y, before.y));
+    return wave == 0 ? v : add(v, of_lane(sums, wave - 1));
 }
 
-// The first of n rising ends that is above x (n if none is).
+// The first of n rising ends that is above x (n if none is), for several x side by side: one after the other, each would
+// cost ten trips to LDS.
+template <int K>
+__device__ __forceinline__ void find(const uint32_t *ends, int n, const uint32_t (&x)[K], int (&r)[K]) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) r[i] = 0;
+    for (int step = n > 0 ? 1 << (31 - __builtin_clz(n)) : 0; step >= 1; step >>= 1)
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const int at = r[i] + step;
+            if (ends[min(at, n) - 1] <= x[i] && at <= n) r[i] = at;
+        }
+}
 __device__ __forceinline__ int find(const uint32_t *ends, int n, uint32_t x) {
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (ends[mid] > x) hi = mid;
-        else lo = mid + 1;
-    }
-    return lo;
+    const uint32_t one[1] = {x};
+    int r[1];
+    find(ends, n, one, r);
+    return r[0];
 }
 
 // The row of position p in a request's table (-1: none).
@@ -71,12 +86,14 @@ __device__ __forceinline__ int row_of(const SlotArgs &a, const int32_t *table, i
 // One workgroup, since every page taken depends on all requests before: running sums over the requests, a thread each
 // (chunks of them where they are more than threads), give each its tokens' and pages' numbers; then threads take single
 // pages and tokens, whose request is the first with an end above their number.  Bound by round trips, not by its few bytes:
-// lengths, tables and free list, the stores; 64 requests of a token each take 3.0 us in a graph, an empty kernel 1.6.
+// lengths, tables and free list, the stores; 64 requests of a token each take 2.7 us in a graph, an empty kernel 1.6.  A page
+// that one request gives back and another takes in the same step is read from the ended request's table, since through the
+// free list it would wait for a store and a barrier; with one scan for all three sums, 256 requests went from 14.4 to 13.1 us.
 // fill: it writes the tokens too, up to most_fill of them (a thousand threads write 4 KB at a time: 131072 tokens took 79 us
-// here, 5 in the kernel below and 7 for the rest; 17152 20, then 4.8 and 10.9).
+// here, 5 in the kernel below and 8 for the rest; 17152 20, then 5 and 10).
 __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fill) {
-    __shared__ uint2 wave_sum[kThreads / 64];
-    __shared__ uint32_t ends[kThreads], wants[kThreads];
+    __shared__ Sums wave_sum[kThreads / 64];
+    __shared__ uint32_t ends[kThreads], wants[kThreads], backs[kThreads];
     __shared__ int32_t held[kThreads], begins[kThreads];
     const int tid = threadIdx.x, threads = blockDim.x;
     const int room = a.per * a.page;
@@ -88,53 +105,47 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
         old = b < a.B ? min(max(a.len[b], 0), room) : 0;
     };
     fetch(tid);
-    const uint32_t n_free = min(max(a.n_free[0], 0), a.n_pages);
+    const uint32_t n_free = min(max(a.n_free[0], 0), a.n_pages), n_pages = a.n_pages, max_tok = a.max_tok;
+    // Where page number k lies that the ended requests of the chunk at b0 give back, r the one that has it.
+    auto given = [&](int b0, uint32_t k, int r) {
+        return a.table + static_cast<int64_t>(b0 + r) * a.per + (k - (r > 0 ? backs[r - 1] : 0));
+    };
 
-    // Ended requests give their pages back.
+    // Ended requests give their pages back before anyone takes pages: with several chunks in a pass of its own.
     uint32_t back = n_free;
-    for (int b0 = 0; b0 < a.B; b0 += threads) {
+    for (int b0 = once ? a.B : 0; b0 < a.B; b0 += threads) {
         if (b0 > 0) fetch(b0 + tid);
-        if (!__syncthreads_or(n < 0)) continue;
-        uint2 all;
-        const uint2 upto = scan(make_uint2(n < 0 ? pages(old) : 0, 0), all, wave_sum);
-        ends[tid] = upto.x;
+        Sums all;
+        backs[tid] = scan({0, 0, n < 0 ? pages(old) : 0}, all, wave_sum).z;
         __syncthreads();
-        for (uint32_t k0 = tid; k0 < all.x; k0 += kAtOnce * threads) {
-            int32_t pg[kAtOnce];
-#pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                const uint32_t k = min(k0 + j * threads, all.x - 1);
-                const int r = find(ends, threads, k);
-                pg[j] = a.table[static_cast<int64_t>(b0 + r) * a.per + (k - (r > 0 ? ends[r - 1] : 0))];
-            }
-#pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                const uint32_t k = k0 + j * threads, to = add(back, k);
-                if (k < all.x && to < static_cast<uint32_t>(a.n_pages)) a.free_pages[to] = pg[j];
-            }
+        for (uint32_t k = tid; k < all.z; k += threads) {
+            const uint32_t to = add(back, k);
+            if (to < n_pages) a.free_pages[to] = *given(b0, k, find(backs, threads, k));
         }
-        back = add(back, all.x);
+        back = add(back, all.z);
         __syncthreads();
     }
-    const uint32_t avail = min(back, static_cast<uint32_t>(a.n_pages)), max_tok = a.max_tok;
 
-    uint32_t tokens = 0, wanted = 0, taken = 0, refused = 0;  // (taken, refused: of this thread's requests)
+    uint32_t tokens = 0, wanted = 0, taken = 0, refused = 0, avail = 0;  // (taken, refused: of this thread's requests)
     for (int b0 = 0; b0 < a.B; b0 += threads) {
         const int b = b0 + tid;
         if (!once) fetch(b);
         const bool is = b < a.B;
         const uint32_t have = pages(old);
         bool fits = n >= 0 && n <= room - old;
-        uint2 mine;
+        Sums mine, all;
         mine.x = static_cast<uint32_t>(min(max(n, 0), static_cast<int>(kMost)));
         mine.y = fits ? pages(old + n) - have : 0;
-        uint2 all, upto = scan(mine, all, wave_sum);
+        mine.z = once && n < 0 ? have : 0;
+        Sums upto = scan(mine, all, wave_sum);
         const uint32_t end = add(tokens, upto.x), n_all = all.x;
         if (add(tokens, n_all) > max_tok) {  // tokens past the batch's room want no pages
             fits = fits && (n == 0 || end <= max_tok);
             if (!fits) mine.y = 0;
             upto.y = scan(mine, all, wave_sum).y;
         }
+        const uint32_t n_back = all.z;
+        avail = min(add(back, n_back), n_pages);
         const bool served = fits && (mine.y == 0 || add(wanted, upto.y) <= avail);
         const uint32_t first_want = add(wanted, upto.y - mine.y);  // (exact where it is served)
         const int start = served ? old : -1;
@@ -146,59 +157,75 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
             a.first[b + 1] = static_cast<int32_t>(end);
             if (b == 0) a.first[0] = 0;
         }
+        ends[tid] = end;
+        wants[tid] = upto.y;
+        backs[tid] = upto.z;
+        held[tid] = have;
+        begins[tid] = start;
+        const bool ones = !__syncthreads_or(n > 1);  // one token of every request at most
+        // Where the page lies that is taken as number k of all: at the top of the free list, or if this step's ended requests
+        // give it back, still in their tables.
+        auto page_of = [&](uint32_t k) {
+            const uint32_t i = avail - 1 - k;
+            return i < back || n_back == 0 ? a.free_pages + i : given(b0, i - back, find(backs, threads, i - back));
+        };
+        // Pages given back go to the free list, pages taken (from avail - wanted on they are the served requests' and perhaps
+        // a refused one's) into the tables: all loads of a turn, then its stores.
+        const uint32_t some = ones ? 0 : min(all.y, avail - min(avail, wanted));
+        int pg_own = -1;
         int32_t *const table = a.table + static_cast<int64_t>(is ? b : 0) * a.per;
-        if (!__syncthreads_or(n > 1)) {
-            // One token of every request at most: each thread has its own token and its page.
-            if (served && n == 1) {
-                int pg;
-                if (mine.y != 0) {
-                    pg = a.free_pages[avail - 1 - first_want];
-                    table[have] = pg;
-                } else {
-                    pg = table[divide(old, a.by_page)];
-                }
-                if (fill) {
-                    const int in_page = old - divide(old, a.by_page) * a.page;
-                    a.slot[end - 1] = pg >= 0 && pg < a.n_pages ? pg * a.page + in_page : -1;
+        if (ones && served && n == 1) {
+            pg_own = mine.y != 0 ? *page_of(first_want) : table[divide(old, a.by_page)];
+        }
+        for (uint32_t k0 = tid; k0 < max(n_back, some); k0 += kAtOnce * threads) {
+            int32_t from_ended[kAtOnce], from_free[kAtOnce];
+            uint32_t k[kAtOnce];
+            int r[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) k[j] = k0 + j * threads;
+            if (k0 < n_back) find(backs, threads, k, r);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                from_ended[j] = k[j] < n_back ? *given(b0, k[j], r[j]) : 0;
+                from_free[j] = k[j] < some ? *page_of(wanted + k[j]) : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const uint32_t to = add(back, k[j]);
+                if (k[j] < n_back && to < n_pages) a.free_pages[to] = from_ended[j];
+                if (k[j] < some) {
+                    const int q = find(wants, threads, k[j]);
+                    if (begins[q] >= 0)
+                        a.table[static_cast<int64_t>(b0 + q) * a.per + held[q] + k[j] - (q > 0 ? wants[q - 1] : 0)] = from_free[j];
                 }
             }
+        }
+        if (ones) {  // each thread has its own token
+            if (served && n == 1 && mine.y != 0) table[have] = pg_own;
             if (fill && n == 1 && end <= max_tok) {
+                const int in_page = old - divide(old, a.by_page) * a.page;
                 a.seq[end - 1] = b;
                 a.pos[end - 1] = start;
-                if (!served) a.slot[end - 1] = -1;
+                a.slot[end - 1] = pg_own >= 0 && pg_own < a.n_pages ? pg_own * a.page + in_page : -1;
             }
-        } else {
-            ends[tid] = end;
-            wants[tid] = upto.y;
-            held[tid] = have;
-            begins[tid] = start;
+        } else if (fill) {
             __syncthreads();
-            // (Pages from avail - wanted on are the served requests' and perhaps a refused one's.)
-            const uint32_t some = min(all.y, avail - min(avail, wanted));
-            for (uint32_t k0 = tid; k0 < some; k0 += kAtOnce * threads) {
-                int32_t pg[kAtOnce];
+            const uint32_t last = min(add(tokens, n_all), max_tok);
+            for (uint32_t t0 = tokens + tid; t0 < last; t0 += kAtOnce * threads) {
+                uint32_t t[kAtOnce];
+                int r[kAtOnce], p[kAtOnce], row[kAtOnce];
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j)
-                    pg[j] = a.free_pages[avail - 1 - wanted - min(k0 + j * threads, some - 1)];
+                for (int j = 0; j < kAtOnce; ++j) t[j] = t0 + j * threads;
+                find(ends, threads, t, r);
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) {
-                    const uint32_t k = k0 + j * threads;
-                    if (k >= some) break;
-                    const int r = find(wants, threads, k);
-                    if (begins[r] >= 0)
-                        a.table[static_cast<int64_t>(b0 + r) * a.per + held[r] + k - (r > 0 ? wants[r - 1] : 0)] = pg[j];
+                    const int q = min(r[j], threads - 1);
+                    p[j] = t[j] >= last || begins[q] < 0 ? -1 : static_cast<int>(begins[q] + (t[j] - (q > 0 ? ends[q - 1] : tokens)));
+                    row[j] = p[j] < 0 ? -1 : row_of(a, a.table + static_cast<int64_t>(b0 + q) * a.per, p[j]);
                 }
-            }
-            if (fill) {
-                __syncthreads();
-                const uint32_t last = min(add(tokens, n_all), max_tok);
-                for (uint32_t t = tokens + tid; t < last; t += threads) {
-                    const int r = find(ends, threads, t);
-                    const int p = begins[r] < 0 ? -1 : static_cast<int>(begins[r] + (t - (r > 0 ? ends[r - 1] : tokens)));
-                    a.seq[t] = b0 + r;
-                    a.pos[t] = p;
-                    a.slot[t] = p < 0 ? -1 : row_of(a, a.table + static_cast<int64_t>(b0 + r) * a.per, p);
-                }
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (t[j] < last) a.seq[t[j]] = b0 + r[j], a.pos[t[j]] = p[j], a.slot[t[j]] = row[j];
             }
         }
         tokens = add(tokens, n_all);
@@ -207,8 +234,8 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
     }
     if (fill)
         for (uint32_t t = tokens + tid; t < max_tok; t += threads) a.seq[t] = a.pos[t] = a.slot[t] = -1;
-    uint2 all;
-    scan(make_uint2(taken, refused), all, wave_sum);
+    Sums all;
+    scan({taken, refused, 0}, all, wave_sum);
     if (tid == 0) {
         a.n_free_out[0] = static_cast<int32_t>(avail - all.x);
         if (a.refused) a.refused[0] = static_cast<int32_t>(all.y);
@@ -241,21 +268,34 @@ __global__ __launch_bounds__(kFillThreads) void fill_kernel(SlotArgs a) {
     }
     const uint32_t base = lo < a.B ? a.first[lo] : 0;
     __syncthreads();
-    for (uint32_t t = t0 + tid; t < min(t0 + kFillTokens, static_cast<uint32_t>(a.max_tok)); t += kFillThreads) {
-        int r = find(ends, count, t), b = lo + r, start = -1;
+    constexpr int K = kFillTokens / kFillThreads;
+    uint32_t t[K];
+    int r[K], b[K], p[K], row[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) t[j] = t0 + tid + j * kFillThreads;
+    find(ends, count, t, r);
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        int start = -1;
         uint32_t from = 0;
-        if (r < count) {
-            start = begins[r];
-            from = r > 0 ? ends[r - 1] : base;
+        b[j] = lo + r[j];
+        if (r[j] < count) {
+            start = begins[r[j]];
+            from = r[j] > 0 ? ends[r[j] - 1] : base;
         } else {  // behind those (requests without tokens are many here), or behind the last
-            b += find(reinterpret_cast<const uint32_t *>(end_of) + b, a.B - b, t);
-            if (b < a.B) start = a.start[b], from = a.first[b];
+            b[j] += find(reinterpret_cast<const uint32_t *>(end_of) + b[j], a.B - b[j], t[j]);
+            if (b[j] < a.B) start = a.start[b[j]], from = a.first[b[j]];
         }
-        const int p = start < 0 ? -1 : static_cast<int>(start + (t - from));
-        a.seq[t] = b < a.B ? b : -1;
-        a.pos[t] = p;
-        a.slot[t] = p < 0 ? -1 : row_of(a, a.table + static_cast<int64_t>(b) * a.per, p);
+        p[j] = start < 0 || t[j] >= static_cast<uint32_t>(a.max_tok) ? -1 : static_cast<int>(start + (t[j] - from));
+        row[j] = p[j] < 0 ? -1 : row_of(a, a.table + static_cast<int64_t>(b[j]) * a.per, p[j]);
     }
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+        if (t[j] < static_cast<uint32_t>(a.max_tok)) {
+            a.seq[t[j]] = b[j] < a.B ? b[j] : -1;
+            a.pos[t[j]] = p[j];
+            a.slot[t[j]] = row[j];
+        }
 }
 
 }  // namespace
