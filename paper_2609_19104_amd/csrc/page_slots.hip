@@ -88,16 +88,24 @@ __device__ __forceinline__ int row_of(const SlotArgs &a, const int32_t *table, i
 // pages and tokens, whose request is the first with an end above their number.  Bound by round trips, not by its few bytes:
 // lengths, tables and free list, the stores; 64 requests of a token each take 2.7 us in a graph, an empty kernel 1.6.  A page
 // that one request gives back and another takes in the same step is read from the ended request's table, since through the
-// free list it would wait for a store and a barrier; with one scan for all three sums, 256 requests went from 14.4 to 13.1 us.
-// fill: it writes the tokens too, up to most_fill of them (a thousand threads write 4 KB at a time: 131072 tokens took 79 us
-// here, 5 in the kernel below and 8 for the rest; 17152 20, then 5 and 10).
-__global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fill) {
+// free list it would wait for a store and a barrier.
+// fill: it writes the tokens too, where they are few (a thousand threads write 4 KB at a time: 131072 tokens took 79 us here,
+// 17152 20).
+//
+// MANY: the same by many workgroups, for more tokens of no more requests than a workgroup has threads.  Each makes all
+// running sums; the first page_blocks of them move pages, the others write tokens, whose new pages they take from where they
+// lie, not from the tables.  So nobody reads what another writes: of the free list what was free, of the tables what a
+// request had; lengths and count, where they are updated in place, are left to finish_kernel.  256 requests with 8 thousand
+// tokens 5.2 us (one workgroup for the pages and, after it, many for the tokens 13.1), 1024 with 66 thousand 5.4 (10.3).
+template <bool MANY>
+__global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fill, int page_blocks) {
     __shared__ Sums wave_sum[kThreads / 64];
     __shared__ uint32_t ends[kThreads], wants[kThreads], backs[kThreads];
     __shared__ int32_t held[kThreads], begins[kThreads];
     const int tid = threadIdx.x, threads = blockDim.x;
     const int room = a.per * a.page;
-    const bool once = a.B <= threads;  // one chunk: everything is read once
+    const bool once = MANY || a.B <= threads;  // one chunk: everything is read once
+    const bool tells = !MANY || blockIdx.x == 0;
     auto pages = [&](int tokens) { return tokens > 0 ? static_cast<uint32_t>(divide(tokens - 1, a.by_page) + 1) : 0u; };
     int n = 0, old = 0;
     auto fetch = [&](int b) {
@@ -150,9 +158,9 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
         const uint32_t first_want = add(wanted, upto.y - mine.y);  // (exact where it is served)
         const int start = served ? old : -1;
         if (served) taken += mine.y;
-        if (is) {
-            if (n >= 0 && !served) ++refused;
-            a.len_out[b] = n < 0 ? 0 : served ? old + n : old;
+        if (is && n >= 0 && !served) ++refused;
+        if (is && tells) {
+            if (!MANY || !a.in_place) a.len_out[b] = n < 0 ? 0 : served ? old + n : old;
             a.start[b] = start;
             a.first[b + 1] = static_cast<int32_t>(end);
             if (b == 0) a.first[0] = 0;
@@ -162,7 +170,7 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
         backs[tid] = upto.z;
         held[tid] = have;
         begins[tid] = start;
-        const bool ones = !__syncthreads_or(n > 1);  // one token of every request at most
+        const bool ones = !__syncthreads_or(n > 1) && !MANY;  // one token of every request at most
         // Where the page lies that is taken as number k of all: at the top of the free list, or if this step's ended requests
         // give it back, still in their tables.
         auto page_of = [&](uint32_t k) {
@@ -177,20 +185,23 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
         if (ones && served && n == 1) {
             pg_own = mine.y != 0 ? *page_of(first_want) : table[divide(old, a.by_page)];
         }
-        for (uint32_t k0 = tid; k0 < max(n_back, some); k0 += kAtOnce * threads) {
-            int32_t from_ended[kAtOnce], from_free[kAtOnce];
-            uint32_t k[kAtOnce];
-            int r[kAtOnce];
+        constexpr int AT = MANY ? 1 : kAtOnce;
+        const uint32_t movers = MANY ? page_blocks * threads : threads;
+        for (uint32_t k0 = MANY ? blockIdx.x * threads + tid : tid; k0 < max(n_back, some); k0 += AT * movers) {
+            if (MANY && static_cast<int>(blockIdx.x) >= page_blocks) break;
+            int32_t from_ended[AT], from_free[AT];
+            uint32_t k[AT];
+            int r[AT];
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) k[j] = k0 + j * threads;
+            for (int j = 0; j < AT; ++j) k[j] = k0 + j * movers;
             if (k0 < n_back) find(backs, threads, k, r);
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
+            for (int j = 0; j < AT; ++j) {
                 from_ended[j] = k[j] < n_back ? *given(b0, k[j], r[j]) : 0;
                 from_free[j] = k[j] < some ? *page_of(wanted + k[j]) : 0;
             }
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
+            for (int j = 0; j < AT; ++j) {
                 const uint32_t to = add(back, k[j]);
                 if (k[j] < n_back && to < n_pages) a.free_pages[to] = from_ended[j];
                 if (k[j] < some) {
@@ -200,7 +211,26 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
                 }
             }
         }
-        if (ones) {  // each thread has its own token
+        if constexpr (MANY) {
+            const uint32_t last = min(n_all, max_tok), writers = (gridDim.x - page_blocks) * threads;
+            if (static_cast<int>(blockIdx.x) >= page_blocks)
+                for (uint32_t t = (blockIdx.x - page_blocks) * threads + tid; t < max_tok; t += writers) {
+                    int r = -1, p = -1, row = -1;
+                    if (t < last) {
+                        r = find(ends, threads, t);
+                        if (begins[r] >= 0) {
+                            p = static_cast<int>(begins[r] + (t - (r > 0 ? ends[r - 1] : 0)));
+                            const uint32_t i = divide(p, a.by_page), own = held[r];
+                            const int pg = i < own ? a.table[static_cast<int64_t>(r) * a.per + i]
+                                                   : *page_of((r > 0 ? wants[r - 1] : 0) + i - own);
+                            if (pg >= 0 && pg < a.n_pages) row = pg * a.page + p - static_cast<int>(i) * a.page;
+                        }
+                    }
+                    a.seq[t] = r;
+                    a.pos[t] = p;
+                    a.slot[t] = row;
+                }
+        } else if (ones) {  // each thread has its own token
             if (served && n == 1 && mine.y != 0) table[have] = pg_own;
             if (fill && n == 1 && end <= max_tok) {
                 const int in_page = old - divide(old, a.by_page) * a.page;
@@ -232,19 +262,37 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a, int fi
         wanted = add(wanted, all.y);
         if (!once) __syncthreads();
     }
-    if (fill)
+    if (!MANY && fill)
         for (uint32_t t = tokens + tid; t < max_tok; t += threads) a.seq[t] = a.pos[t] = a.slot[t] = -1;
+    if (!tells) return;
     Sums all;
     scan({taken, refused, 0}, all, wave_sum);
     if (tid == 0) {
-        a.n_free_out[0] = static_cast<int32_t>(avail - all.x);
+        if (!MANY || !a.in_place) a.n_free_out[0] = static_cast<int32_t>(avail - all.x);
         if (a.refused) a.refused[0] = static_cast<int32_t>(all.y);
     }
 }
 
+// The lengths and the count, from where the requests start and what they were, after workgroups that all read the old ones.
+__global__ __launch_bounds__(kThreads) void finish_kernel(SlotArgs a) {
+    __shared__ Sums wave_sum[kThreads / 64];
+    const int b = threadIdx.x;
+    const uint32_t n_free = min(max(a.n_free[0], 0), a.n_pages);
+    auto pages = [&](int tokens) { return tokens > 0 ? static_cast<uint32_t>(divide(tokens - 1, a.by_page) + 1) : 0u; };
+    Sums mine = {0, 0, 0}, all;
+    if (b < a.B) {
+        const int n = a.n_new[b], old = min(max(a.len[b], 0), a.per * a.page), start = a.start[b];
+        a.len_out[b] = n < 0 ? 0 : start >= 0 ? start + n : old;
+        if (n < 0) mine.x = pages(old);
+        else if (start >= 0) mine.y = pages(start + n) - pages(start);
+    }
+    scan(mine, all, wave_sum);
+    if (b == 0) a.n_free_out[0] = static_cast<int32_t>(min(add(n_free, all.x), static_cast<uint32_t>(a.n_pages)) - all.y);
+}
+
 constexpr int kFillThreads = 256, kFillTokens = 512;
 
-// The tokens of a batch that one workgroup would be long about, after the kernel above: a workgroup takes kFillTokens of
+// The tokens of more requests than a workgroup has threads, after the kernel above by one: a workgroup takes kFillTokens of
 // them.  It finds its first token's request by whole workgroups of comparisons (two rounds for up to 65536 requests, where
 // halving takes sixteen), the others' from there on in LDS.  131072 tokens take 5.4 us, as few take: trips to memory.
 __global__ __launch_bounds__(kFillThreads) void fill_kernel(SlotArgs a) {
@@ -300,10 +348,26 @@ __global__ __launch_bounds__(kFillThreads) void fill_kernel(SlotArgs a) {
 
 }  // namespace
 
+// One workgroup for a token each (64 requests of which some end 4.7 us, by many workgroups 5.1) and for few tokens.  Else many,
+// from 257 tokens on (a prompt of 500 6.6 and 4.0, 256 requests of 4 tokens 10.6 and 5.3, of one 6.9 and 5.3); where lengths and
+// count are updated in place from 4097 on: that takes a second launch, which costs the host 2 us, so that many are faster only
+// in graphs and with prompts (64 requests of 32 tokens 7.7 and 5.4; 256 of one, with room for 2048, 4.6 and 5.9).
 hipError_t launch_page_slots(const SlotArgs &a, hipStream_t st) {
-    const bool fill = a.max_tok <= a.most_fill;
-    const int threads = std::min(kThreads, (std::max(a.B, std::min(a.max_tok, kThreads)) + 63) / 64 * 64);
-    page_slots_kernel<<<1, threads, 0, st>>>(a, fill);
+    const bool fill = a.max_tok <= (a.in_place || a.B > kThreads ? 4096 : std::max(256, a.B));
+    const int wide = (a.B + 63) / 64 * 64;
+    if (!fill && a.B <= kThreads) {
+        const int threads = std::max(256, wide);
+        // A thread for each page that the tokens take and for one in 16 of the tables', as ended requests may give back
+        // (with threads for the first only, 16 of 256 requests ending, 512 pages at most each, 7.0 us).
+        const int64_t pages = a.max_tok / a.page + a.B + static_cast<int64_t>(a.B) * a.per / 16;
+        const int movers = static_cast<int>(std::min<int64_t>(64, pages / threads + 1));
+        const int writers = std::min((a.max_tok + threads - 1) / threads, 256 * 2048 / threads);
+        page_slots_kernel<true><<<movers + writers, threads, 0, st>>>(a, 0, movers);
+        if (a.in_place) finish_kernel<<<1, wide, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    const int threads = std::min(kThreads, std::max(wide, (std::min(a.max_tok, kThreads) + 63) / 64 * 64));
+    page_slots_kernel<false><<<1, threads, 0, st>>>(a, fill, 0);
     if (!fill) fill_kernel<<<(a.max_tok + kFillTokens - 1) / kFillTokens, kFillThreads, 0, st>>>(a);
     return hipGetLastError();
 }

@@ -7,7 +7,7 @@ namespace rm_serve {
 
 struct SlotArgs {
     int B = 0, max_tok = 0, page = 0, n_pages = 0, per = 0;  // per: table entries of a request
-    int most_fill = 4096;  // tokens that the first kernel writes
+    bool in_place = false;  // len_out is len, or n_free_out is n_free
     rm_attn::Divisor by_page;
     const int32_t *n_new = nullptr, *len = nullptr, *n_free = nullptr;
     int32_t *table = nullptr, *free_pages = nullptr;

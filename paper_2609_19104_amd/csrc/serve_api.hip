@@ -102,6 +102,7 @@ RM_EXPORT rm_status rm_page_slots(int32_t n_seqs, int32_t max_tok, int32_t page,
     a.n_new = n_new, a.len = len, a.n_free = n_free, a.table = table, a.free_pages = free_pages;
     a.len_out = len_out, a.n_free_out = n_free_out, a.refused = refused;
     a.first = first, a.start = start, a.seq = seq, a.pos = pos, a.slot = slot;
+    a.in_place = len_out == len || n_free_out == n_free;
     const hipError_t e = rm_serve::launch_page_slots(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return api_fail(RM_ERR_HIP, "page slots launch: %s", hipGetErrorString(e));
     return api_ok();

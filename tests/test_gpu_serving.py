@@ -161,6 +161,64 @@ def test_slots_in_a_graph():
         length, table, free, n_free = r.length, r.table, r.free_pages, r.n_free
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,page,per,tokens,room", [
+    (1, 16, 40, 257, 257), (1, 1, 9000, 8000, 8500), (3, 7, 30, 200, 700), (64, 16, 12, 30, 4097), (255, 3, 50, 60, 20000),
+    (256, 24, 8, 40, 6000), (1000, 16, 4, 12, 9001), (1024, 8, 5, 9, 4100), (1024, 256, 2, 130, 100000),
+])
+def test_slots_by_many_workgroups(B, page, per, tokens, room, in_place):
+    """Many tokens of up to 1024 requests: ended ones, scarce pages, too little room, requests that do not fit."""
+    rng = np.random.default_rng(B + room)
+    for scarce in (1.0, 0.3):
+        n_pages = max(2, int(B * per * scarce))
+        length, table, free, n_free = [0] * B, rng.integers(-3, n_pages + 3, (B, per)), rng.permutation(n_pages), n_pages
+        for step in range(5):
+            n_new = rng.integers(0, tokens + 1, B)
+            n_new[rng.random(B) < 0.25] = -1
+            n_new[rng.random(B) < 0.2] = 1
+            n_new[rng.random(B) < 0.02] = per * page + 1
+            if step == 0:
+                n_new[0] = tokens
+            r = check_slots(n_new, length, table, free, n_free, page, room, in_place=in_place)
+            length, table, free, n_free = r.length, r.table, r.free_pages, r.n_free
+
+
+def test_slots_by_many_workgroups_in_a_graph():
+    """Prompts captured once and replayed, with the lengths, the count, both or neither updated in place."""
+    rng = np.random.default_rng(6)
+    B, page, per, room = 90, 8, 16, 5000
+    n_pages = B * per // 3
+    for length_out, n_free_out in ((None, None), (B, None), (None, 1), (B, 1)):
+        length, table, free, n_free = [0] * B, np.full((B, per), -1), rng.permutation(n_pages), n_pages
+        t = dict(n_new=ints([0] * B), length=ints(length), table=ints(table), free_pages=ints(free), n_free=ints([n_free]))
+        sizes = dict(first=B + 1, start=B, seq=room, pos=room, slot=room)
+        o = {k: torch.zeros((n,), dtype=torch.int32, device="cuda") for k, n in sizes.items()}
+        told = [None if n is None else torch.zeros((n,), dtype=torch.int32, device="cuda") for n in (length_out, n_free_out)]
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                rm.rm_page_slots(t["n_new"], t["length"], t["table"], t["free_pages"], t["n_free"], o["first"], o["start"],
+                                 o["seq"], o["pos"], o["slot"], page, length_out=told[0], n_free_out=told[1])
+        for step in range(6):
+            n_new = rng.integers(0, 60, B)
+            n_new[rng.random(B) < 0.3] = -1
+            t["n_new"].copy_(ints(n_new))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            r = serving.page_slots(n_new, length, table, free, n_free, page, room)
+            for name, want in (("first", r.first), ("start", r.start), ("seq", r.seq), ("pos", r.pos), ("slot", r.slot)):
+                np.testing.assert_array_equal(o[name].cpu().numpy(), np.asarray(want), err_msg=f"{name}, step {step}")
+            for name, own, want in (("length", told[0], r.length), ("n_free", told[1], [r.n_free])):
+                np.testing.assert_array_equal((t[name] if own is None else own).cpu().numpy(), np.asarray(want))
+                if own is not None:
+                    t[name].copy_(own)
+            np.testing.assert_array_equal(t["table"].cpu().numpy(), np.asarray(r.table))
+            np.testing.assert_array_equal(t["free_pages"].cpu().numpy(), np.asarray(r.free_pages))
+            length, table, free, n_free = r.length, r.table, r.free_pages, r.n_free
+
+
 # ----------------------------------------------------------------------------------------------------------
 # Paged attention
 # ----------------------------------------------------------------------------------------------------------
