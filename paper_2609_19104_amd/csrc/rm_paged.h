@@ -263,11 +263,11 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
     // ---------------------------------------------------------------- tiles
     struct Tile {
         int n, lo, end, t, t0, t1;  // token, its keys and tiles
-        int pos, seq;
+        int seq;
         int base;                   // the token's first tile among all
     };
     auto enter = [&](Tile &c, int p, int s) __attribute__((always_inline)) {  // c.n's keys
-        c.pos = p, c.seq = s;
+        c.seq = s;
         seen(*again(), p, s, c.lo, c.end);
         c.t = c.t0 = c.lo / KT;
         c.t1 = c.t0 + tiles<KT>(c.lo, c.end);
@@ -505,7 +505,8 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         if (__builtin_expect(a.cap != 0.0f, false))
             each([&](float x, int, int) { return a.cap * (BF ? rm_attn::tanh_relative(x * a.scale) : tanhf(x * a.scale)); });
         if (__builtin_expect(a.slopes != nullptr, false)) {
-            const int d0 = cur.pos - (cur.t * KT + 4 * here(h4));
+            // (Counted from the last seen key: the same weights, and a position far behind the table costs them no digits.)
+            const int d0 = cur.end - 1 - (cur.t * KT + 4 * here(h4));
             const float in = a.cap != 0.0f ? 1.0f : a.scale;
             each([&](float x, int r, int j) { return fmaf(x, in, -slope[r] * static_cast<float>(d0 - j)); });
         }
@@ -579,6 +580,8 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
                     const int i = (g * PER + x) / DB, d = (g * PER + x) % DB;
 #pragma unroll
                     for (int r = 0; r < RT; ++r) {
+                        // Weights in bf16, as the matrix cores take them: half a step of each, 2^-8; their sum is of the
+                        // unrounded ones.
                         const rm_bf16x4 p = {static_cast<__bf16>(s[r][i][0]), static_cast<__bf16>(s[r][i][1]),
                                              static_cast<__bf16>(s[r][i][2]), static_cast<__bf16>(s[r][i][3])};
                         o[r][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf[x], __builtin_bit_cast(rm_s16x4, p), o[r][d],

@@ -300,6 +300,21 @@ def test_paged_cap_bias_window(dtype, cap, bias, window, D):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_paged_bias_far_behind_the_table(dtype, cap):
+    """Positions far behind the table's last key add the same to a head's scores, slope times the rest of the distance, and
+    so leave its weights as they are at the last key's position."""
+    g = gen(17)
+    N, Hq, Hk, D, page, per = 6, 8, 2, 64, 16, 7
+    k, v, table = cache(g, N, per, page, Hk, D, dtype)
+    q = randn(g, (N, Hq, D), dtype, 2.0)
+    slopes = (torch.rand((Hq,), generator=g) * 0.3 + 0.05).cuda()
+    far = run_paged(q, k, v, table, ints([page * per, 1 << 20, (1 << 24) + 1, 1 << 28, (1 << 30) + 7, (1 << 31) - 1]),
+                    slopes=slopes, cap=cap)
+    check_paged(q, k, v, table, ints([page * per - 1] * N), slopes=slopes, cap=cap, out=far)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("D,Hq,Hk,N,length", [(64, 8, 1, 1, 20000), (128, 8, 2, 3, 9000), (256, 8, 1, 1, 5000),
                                               (72, 4, 4, 2, 3001), (128, 40, 1, 2, 4000)])
 def test_long_caches(dtype, D, Hq, Hk, N, length):
