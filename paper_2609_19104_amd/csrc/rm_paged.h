@@ -130,6 +130,22 @@ __device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
     return static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo));
 }
 
+// Weights as the matrix cores take them, in two bf16 parts: what truncation leaves, and the rest, of which at most half a step
+// is lost, 2^-8 of a value below 2^-7 of the weight.  In one part the loss was up to 2^-8 of each weight, as much as the
+// rounding of the output (error of 64 bf16 tokens against 64 bits 2.0e-3, now 1.7e-3, what the output's rounding leaves).  The
+// rest of a weight that is not 0 is not 0 either (at least 2^-100, or as much as such a small weight): times an infinite value
+// it would be NaN.  The second product costs 64 tokens 0.5 of 199 us in a graph, 64 of 20 heads to a key head 0.5 of 26.4
+// (with matrix instructions of 16 keys 1.0 and 2.7).
+__device__ __forceinline__ void in_two(rm_f32x4 w, rm_s16x4 &high, rm_s16x4 &rest) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t bits = __float_as_uint(w[e]);
+        const float r = fmaxf(w[e] - __uint_as_float(bits & 0xffff0000u), fminf(w[e], 0x1p-100f));
+        high[e] = static_cast<short>(bits >> 16);
+        rest[e] = __builtin_bit_cast(short, static_cast<__bf16>(r));
+    }
+}
+
 // The sum of a value over the lanes up to the own one, in data-parallel steps along the rows of 16 lanes and across them.
 __device__ __forceinline__ int running_sum(int v) {
     v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
@@ -559,35 +575,54 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         }
         if constexpr (BF) {
             typedef __attribute__((address_space(3))) rm_s16x4 lds_s16x4;
-            constexpr int PER = NS * DB / GS;
+            // A matrix instruction takes 32 keys: two fours of a lane, once with the weights' first parts and once with their
+            // rests, or where a tile has 16 keys, the one four with both at once.
+            constexpr int PAIRS = (NS + 1) / 2, PER = PAIRS * DB / GS;
             const int row = 4 * h4 + (m16 >> 2);
             const uint8_t *v = vt + row * ROWB + (m16 & 3) * 8;
+            auto both = [](rm_s16x4 x, rm_s16x4 y) __attribute__((always_inline)) {
+                return __builtin_bit_cast(rm_bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+            };
+            rm_bf16x8 w[NS == 1 ? 1 : 2][RT][PAIRS];
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    rm_s16x4 high[2], rest[2];
+                    in_two(s[r][2 * i], high[0], rest[0]);
+                    if constexpr (NS == 1) {
+                        w[0][r][i] = both(high[0], rest[0]);
+                    } else {
+                        in_two(s[r][2 * i + 1], high[1], rest[1]);
+                        w[0][r][i] = both(high[0], high[1]);
+                        w[1][r][i] = both(rest[0], rest[1]);
+                    }
+                }
 #pragma unroll
             for (int g = 0; g < GS; ++g) {
-                rm_s16x4 vf[PER];
+                rm_s16x4 vf[PER][2];
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int x = 0; x < PER; ++x) {
                     const int i = (g * PER + x) / DB, d = (g * PER + x) % DB;
-                    vf[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_s16x4 *)(v + 16 * i * ROWB + (((2 * d) & 15) ^ swz_v(row)) * 16 + (d >> 3) * 256));
+#pragma unroll
+                    for (int j = 0; j < (NS == 1 ? 1 : 2); ++j)
+                        vf[x][j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (lds_s16x4 *)(v + 16 * (2 * i + j) * ROWB + (((2 * d) & 15) ^ swz_v(row)) * 16 + (d >> 3) * 256));
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (more) stage(next, true, 4 * g, turn);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < PER; ++x) {
-                    const int i = (g * PER + x) / DB, d = (g * PER + x) % DB;
+                for (int part = 0; part < (NS == 1 ? 1 : 2); ++part)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        // Weights in bf16, as the matrix cores take them: half a step of each, 2^-8; their sum is of the
-                        // unrounded ones.
-                        const rm_bf16x4 p = {static_cast<__bf16>(s[r][i][0]), static_cast<__bf16>(s[r][i][1]),
-                                             static_cast<__bf16>(s[r][i][2]), static_cast<__bf16>(s[r][i][3])};
-                        o[r][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf[x], __builtin_bit_cast(rm_s16x4, p), o[r][d],
-                                                                            0, 0, 0);
+                    for (int x = 0; x < PER; ++x) {
+                        const int i = (g * PER + x) / DB, d = (g * PER + x) % DB;
+#pragma unroll
+                        for (int r = 0; r < RT; ++r)
+                            o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(vf[x][0], vf[x][NS == 1 ? 0 : 1]),
+                                                                              w[part][r][i], o[r][d], 0, 0, 0);
                     }
-                }
             }
         } else {
             constexpr int PER = 4 * NS / GS;  // fours of keys, one of each lane row
