@@ -427,7 +427,7 @@ rm_status rm_prefix_attention(const rm_attn_shape *s, int32_t n_groups, int32_t 
  *             names a page outside [0, n_pages).  rm_qk_norm_rope drops the key and value of such a slot, and
  *             rm_paged_attention gives 0 for such a position.
  * 1 <= n_seqs <= 2^20, 1 <= max_tok < 2^30, n_pages < 2^30, n_pages * page < 2^31, max_pages * page < 2^30.  The outputs
- * must not overlap each other or the inputs.  Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_ALIGN (4 bytes). */
+ * must not overlap each other or the inputs.  Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_ALIGN (4 bytes), RM_ERR_HIP. */
 rm_status rm_page_slots(int32_t n_seqs, int32_t max_tok, int32_t page, int32_t n_pages, int32_t max_pages,
                         const int32_t *n_new, const int32_t *len, const int32_t *n_free, int32_t *table,
                         int32_t *free_pages, int32_t *len_out, int32_t *n_free_out, int32_t *refused, int32_t *first,
@@ -470,7 +470,7 @@ rm_status rm_paged_attention(const rm_attn_shape *s, int32_t n_tok, int32_t n_se
  *             scale_stride and shift_stride elements apart (parts of one projection's rows will do).
  * d a multiple of 8 of at most 32768, B * T < 2^24; all pointers and strides multiples of 16 bytes.  y may be x, and out may
  * be f of the same type; any other overlap of an output is refused.  Sums and norms are float32.
- * Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN. */
+ * Errors: RM_ERR_INVALID_ARG, RM_ERR_SHAPE, RM_ERR_DTYPE, RM_ERR_ALIGN, RM_ERR_HIP. */
 rm_status rm_block_norm(int32_t B, int32_t T, int32_t d, int32_t x_dtype, int32_t f_dtype, int32_t out_dtype,
                         const void *x, const void *f, int32_t norm_post, const float *gain_post, const float *gate,
                         int64_t gate_stride, float x_scale, float f_scale, void *y, const float *gain_pre,

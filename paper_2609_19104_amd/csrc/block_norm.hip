@@ -1,4 +1,6 @@
 // Norm of a block's output, gate, residual, and the next block's norm and modulation in one pass (rm_block_norm).
+#include <algorithm>
+
 #include "rm_serve.h"
 
 namespace rm_serve {
@@ -53,7 +55,7 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void block_norm_kernel(NormA
     typedef Floats<V> Vec;
     __shared__ float red[2][16];
     const int t = threadIdx.x % TPR;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
+    const int64_t row = a.row0 + static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
     if (row >= a.rows) return;  // (the whole wave, and with more than one wave to a row the whole workgroup)
     const int b = static_cast<int>(row) / a.T;
     const int64_t base = row * a.d;
@@ -122,10 +124,16 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void block_norm_kernel(NormA
 
 template <bool XB, bool FB, bool OB, int TPR, int COLUMNS>
 hipError_t go(const NormArgs &a, hipStream_t st) {
-    constexpr int V = XB && FB && OB ? 8 : 4, ROWS = TPR < 128 ? 256 / TPR : 1;
-    const dim3 grid(static_cast<unsigned>((a.rows + ROWS - 1) / ROWS));
-    block_norm_kernel<XB, FB, OB, TPR, COLUMNS / V><<<grid, TPR < 128 ? 256 : TPR, 0, st>>>(a);
-    return hipGetLastError();
+    constexpr int V = XB && FB && OB ? 8 : 4, ROWS = TPR < 128 ? 256 / TPR : 1, THREADS = TPR < 128 ? 256 : TPR;
+    // A launch holds below 2^32 threads: of rows above 8192 columns 2^22 - 1.
+    constexpr int64_t most = INT64_C(0xffffffff) / THREADS * ROWS;
+    for (NormArgs part = a; part.row0 < a.rows; part.row0 += most) {
+        const int64_t rows = std::min(a.rows - part.row0, most);
+        block_norm_kernel<XB, FB, OB, TPR, COLUMNS / V><<<static_cast<unsigned>((rows + ROWS - 1) / ROWS), THREADS, 0, st>>>(part);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 // Eight columns a thread while 256 threads hold the row with that, then more.
 template <bool XB, bool FB, bool OB>

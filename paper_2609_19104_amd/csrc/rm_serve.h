@@ -52,7 +52,7 @@ struct NormArgs {
     char *y = nullptr, *out = nullptr;
     const float *gain_post = nullptr, *gate = nullptr, *gain_pre = nullptr, *scale = nullptr, *shift = nullptr;
     int64_t gate_b = 0, scale_b = 0, shift_b = 0;  // elements from sample to sample
-    int64_t rows = 0;
+    int64_t rows = 0, row0 = 0;  // row0: a launch's first
     int T = 0, d = 0, norm_post = 0;
     float x_scale = 1.0f, f_scale = 1.0f, eps = 0.0f;
 };

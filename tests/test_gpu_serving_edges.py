@@ -8,6 +8,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2609_19104_amd as rm
 from oracle import serving
 
 pytestmark = pytest.mark.gpu
@@ -71,3 +72,27 @@ def test_small_weights_of_infinite_values(low):
     assert (out[..., 9] == float("inf")).all() and (out[..., 20] == -float("inf")).all()
     keep = [c for c in range(D) if c not in (9, 20)]
     assert out[..., keep].isfinite().all()
+
+
+# ----------------------------------------------------------------------------------------------------------
+# Block norm
+# ----------------------------------------------------------------------------------------------------------
+
+def test_block_norm_of_more_rows_than_a_launch_holds():
+    """2^22 + 6 rows of 8200 columns, 1024 threads each: past 2^32 threads.  Every number is a whole one that bf16 holds."""
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("needs 160 GiB of free memory")
+    d, T = 8200, (1 << 21) + 3
+    value = (torch.arange(2 * T, device="cuda") % 241).to(BF).view(2, T, 1)
+    x, f = torch.empty((2, T, d), dtype=BF, device="cuda"), torch.ones((2, T, d), dtype=BF, device="cuda")
+    x.copy_(value.expand_as(x))
+    gate = (torch.arange(2 * d, device="cuda").view(2, d) % 13).float()
+    rm.rm_block_norm(x, f, x, None, gate=gate)
+    torch.cuda.synchronize()
+    step = 1 << 17
+    for b in range(2):
+        for t in range(0, T, step):
+            want = value[b, t:t + step] + gate[b].to(BF)
+            assert torch.equal(x[b, t:t + step], want), (b, t)
+    del x, f, want
+    torch.cuda.empty_cache()
