@@ -444,7 +444,7 @@ rm_status rm_page_slots(int32_t n_seqs, int32_t max_tok, int32_t page, int32_t n
  *   table:    int32 [n_seqs][max_pages]; keys on a page outside [0, n_pages) are not seen.
  *   seq:      int32 [n_tok] or NULL (token n is of request n, n_seqs >= n_tok); outside [0, n_seqs): sees nothing.
  *   pos:      int32 [n_tok]; negative: sees nothing; positions from max_pages * page on see the table's last key too.
- *   window:   0: no window.  slopes: float32 [n_q_heads] or NULL: no bias.
+ *   window:   0: no window.  slopes: float32 [n_q_heads], of either sign, or NULL: no bias.
  *   ws, ws_bytes: at least rm_paged_attention_workspace_size bytes (which may be 0: ws may then be NULL), 256-byte
  *             aligned; scratch as for rm_workspace_size.
  * Several new tokens of one request are several n with its seq and rising pos; its keys are read for each of them, so a

@@ -520,11 +520,27 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
         // Scores in powers of two are sc times these: plain products, or with a cap or a bias the scores themselves.
         if (__builtin_expect(a.cap != 0.0f, false))
             each([&](float x, int, int) { return a.cap * (BF ? rm_attn::tanh_relative(x * a.scale) : tanhf(x * a.scale)); });
+        // A bias is counted from the key that a token may see where it is highest (the last one, for a negative slope the first):
+        // the same weights, and a position far behind the table costs them no digits.  Slope times distance may still be far
+        // larger than what tells the weights apart, so it is rounded only after `off` is taken from it, about what it is here:
+        // the running maximum, or for a token's first tile the bias of its first key.  (Beyond 2^24 the maximum's own rounding
+        // would count; there the nearest key has the weight.)
+        float off[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) off[r] = 0.0f;
         if (__builtin_expect(a.slopes != nullptr, false)) {
-            // (Counted from the last seen key: the same weights, and a position far behind the table costs them no digits.)
-            const int d0 = cur.end - 1 - (cur.t * KT + 4 * here(h4));
             const float in = a.cap != 0.0f ? 1.0f : a.scale;
-            each([&](float x, int r, int j) { return fmaf(x, in, -slope[r] * static_cast<float>(d0 - j)); });
+            int from[RT];  // distance of the tile's first key
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                from[r] = (slope[r] < 0.0f ? cur.lo : cur.end - 1) - cur.t * KT;
+                const float about = m[r] == -INFINITY ? -slope[r] * static_cast<float>(from[r]) : m[r];
+                off[r] = fabsf(about) < 0x1p24f ? about : 0.0f;
+            }
+            const int own = 4 * here(h4);
+            each([&](float x, int r, int j) {
+                return fmaf(x, in, fmaf(-slope[r], static_cast<float>(from[r] - own - j), -off[r]));
+            });
         }
         if (__builtin_expect(vis != kFull, false)) {
             const uint64_t bits = vis >> (4 * here(h4));
@@ -537,7 +553,7 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             for (int i = 0; i < NS; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, s[r][i][e]);
-            top = rows_max(top) * sc;
+            top = rows_max(top) * sc + off[r];
             const bool raise = top > m[r] + kRaise;  // (false for top = -inf)
             if (__any(raise)) {
                 const float mn = raise ? top : m[r];
@@ -547,7 +563,7 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
 #pragma unroll
                 for (int d = 0; d < DB; ++d) o[r][d] *= f;
             }
-            const float ref = m[r] == -INFINITY ? 0.0f : m[r];
+            const float ref = (m[r] == -INFINITY ? 0.0f : m[r]) - off[r];
 #pragma unroll
             for (int i = 0; i < NS; ++i)
 #pragma unroll

@@ -19,14 +19,16 @@ if not torch.cuda.is_available():
 from test_gpu_serving import BF, F32, U, U32, cache, f64, gen, ints, randn, run_paged  # noqa: E402
 
 
-def paged_within(out, q, k, v, table, pos, e, spare, seq=None, window=0, slopes=None, scale=None, cap=0.0, heads=None):
-    """out against the oracle, e(big) the bound of a score's error, big the score's size sum |q||k| scale."""
+def paged_within(out, q, k, v, table, pos, e, spare, seq=None, window=0, slopes=None, scale=None, cap=0.0, heads=None,
+                 counted=None):
+    """out against the oracle, e(big) the bound of a score's error, big the score's size sum |q||k| scale; counted: keys whose
+    weights are not too small to change the sums."""
     D = q.shape[2]
     s = np.float32(D ** -0.5 if scale is None else scale)
     ref, mag, big = serving.paged_attention(f64(q), f64(k), f64(v), table.cpu().numpy(),
                                             None if seq is None else seq.cpu().numpy(), pos.cpu().numpy(), window, s, cap,
                                             f64(slopes), heads)
-    longest = min(int(pos.max()) + 1, table.shape[1] * k.shape[1])
+    longest = min(int(pos.max()) + 1, table.shape[1] * k.shape[1]) if counted is None else counted
     x = e(big[..., None])
     rest = 2 * x * (1 + x) + (2.0 ** -15 if q.dtype == BF else 0.0) + (longest + 32) * U32
     got, at = f64(out), slice(None) if heads is None else heads
@@ -96,3 +98,72 @@ def test_block_norm_of_more_rows_than_a_launch_holds():
             assert torch.equal(x[b, t:t + step], want), (b, t)
     del x, f, want
     torch.cuda.empty_cache()
+
+
+# ----------------------------------------------------------------------------------------------------------
+# Bias by distance
+# ----------------------------------------------------------------------------------------------------------
+
+def biased_error(D):
+    """A key's exponent is its score and slope times its distance, less that of the key where the weights lie.  Of keys with a
+    weight these differ by no more than the scores do and the 40 powers of two below which weights do not count, and the slope in
+    powers of two, their difference and their sum are rounded once each: 4 roundings of the score's size and 60, whatever
+    the distances.  (At the least slope used, 0.07, that is 0.1 powers of two a key, 500 keys are in reach.)"""
+    return lambda big: (D + 8) * U32 * big + 4 * U32 * (big + 60.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D,window", [(64, 0), (128, 100000), (256, 0)])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_negative_slopes_on_long_caches(dtype, D, window, cap):
+    """A bias that rises with the distance puts the weight on the first keys, 140 thousand from the last."""
+    g = gen(42, D, window)
+    N, Hq, Hk, page, length = 2, 4, 1, 64, 140000
+    k, v, table = cache(g, N, -(-length // page), page, Hk, D, dtype)
+    q, pos = randn(g, (N, Hq, D), dtype), ints([length - 1, length - 20000])
+    slopes = torch.tensor([-0.5, -0.07, 0.5, -3.0], device="cuda")
+    out = run_paged(q, k, v, table, pos, window=window, slopes=slopes, cap=cap)
+    paged_within(out, q, k, v, table, pos, lambda big: biased_error(D)(big) + 16 * U32 * (big if cap else 0.0), 2.0 ** -10,
+                 window=window, slopes=slopes, cap=cap, counted=1000)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("slope", [-0.5, 0.5])
+def test_bias_where_the_nearest_pages_are_none(dtype, slope):
+    """The weight lies far from both ends of what a token might see: the pages up to there, or from there on, are none."""
+    g = gen(43, slope > 0)
+    N, Hq, Hk, D, page, per = 2, 4, 2, 64, 64, 3000
+    k, v, _ = cache(g, 1, 40, page, Hk, D, dtype)
+    table = torch.full((N, per), -1, dtype=torch.int32)
+    table[:, 1500:1520] = torch.randperm(40, generator=g).view(2, 20).to(torch.int32)
+    table, q, pos = table.cuda(), randn(g, (N, Hq, D), dtype), ints([per * page - 1, per * page - 777])
+    slopes = torch.full((Hq,), slope, device="cuda")
+    out = run_paged(q, k, v, table, pos, slopes=slopes)
+    paged_within(out, q, k, v, table, pos, biased_error(D), 2.0 ** -10, slopes=slopes, counted=1000)
+
+
+def test_negative_slopes_past_2_24_keys():
+    """Distances that float32 does not hold, on a table that names a few pages over and over."""
+    g = gen(44)
+    Hq, Hk, D, page, per = 2, 1, 8, 256, 1 << 18
+    k, v, _ = cache(g, 1, 37, page, Hk, D, F32)
+    table = torch.randint(0, 37, (1, per), generator=g).to(torch.int32).cuda()
+    q, slopes = randn(g, (1, Hq, D), F32), torch.tensor([-0.5, -0.25], device="cuda")
+    out = run_paged(q, k, v, table, ints([per * page - 2]), slopes=slopes)
+    # (From the thousandth key on, scores of about 3 are lowered by 250 and more.)
+    paged_within(out, q, k, v, table, ints([999]), biased_error(D), 2.0 ** -10, slopes=slopes)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 256])
+def test_slopes_that_leave_one_key(dtype, D):
+    """Slopes so large that slope times distance passes float32: the nearest key's value, or the farthest one's."""
+    g = gen(45, D)
+    page = 16
+    k, v, table = cache(g, 3, 300, page, 1, D, dtype)
+    q, pos = randn(g, (3, 4, D), dtype), ints([0, 40, 4700])
+    out = run_paged(q, k, v, table, pos, slopes=torch.tensor([1e38, -1e38, 1e30, -1e30], device="cuda"))
+    for n, p in enumerate(pos.tolist()):
+        near, far = v[table[n, p // page].item(), p % page, 0], v[table[n, 0].item(), 0, 0]
+        for h, want in enumerate((near, far, near, far)):
+            assert torch.equal(out[n, h], want), (n, h)
