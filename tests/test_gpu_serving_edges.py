@@ -34,6 +34,8 @@ def paged_within(out, q, k, v, table, pos, e, spare, seq=None, window=0, slopes=
     got, at = f64(out), slice(None) if heads is None else heads
     assert rest[:, at].max() <= spare
     tol = (U[q.dtype] * np.abs(ref) + (1 + U[q.dtype]) * rest * mag + 1e-30)[:, at]
+    seen = mag[:, at] > 0  # (a bound that most values lie within says nothing)
+    assert (4 * tol[seen] < np.abs(ref[:, at])[seen]).mean() > 0.5
     err = np.abs(got - ref)[:, at]
     assert np.isfinite(got).all()
     assert (err <= tol).all(), f"error {float((err / tol).max()):.3f} times the bound"
@@ -167,3 +169,28 @@ def test_slopes_that_leave_one_key(dtype, D):
         near, far = v[table[n, p // page].item(), p % page, 0], v[table[n, 0].item(), 0, 0]
         for h, want in enumerate((near, far, near, far)):
             assert torch.equal(out[n, h], want), (n, h)
+
+
+# ----------------------------------------------------------------------------------------------------------
+# Caps
+# ----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("cap", [0.5, 5.0, 30.0, 256.0, 257.0, 1e4, 1e6, 1e8, 1e30])
+@pytest.mark.parametrize("bias,window", [(False, 0), (True, 77)])
+def test_caps_of_every_size(dtype, D, cap, bias, window):
+    """A capped score is off by 16 roundings of its own value (the polynomial or the exponential 7, the product with the cap and
+    the score over the cap one each; float32's tanhf 5), whatever the cap: no term of the cap's size."""
+    g = gen(46, D, int(min(cap, 1e9)), bias)
+    N, Hq, Hk, page, per = 5, 6, 2, 16, 20
+    k, v, table = cache(g, N, per, page, Hk, D, dtype)
+    q, pos = randn(g, (N, Hq, D), dtype), ints([3, 60, 100, 300, 319])
+    slopes = torch.tensor([0.5, 0.1, 0.0, 0.03, -0.01, 0.2], device="cuda") if bias else None
+    out = run_paged(q, k, v, table, pos, window=window, slopes=slopes, cap=cap)
+
+    def error(big):
+        e = biased_error(D)(big) if bias else (D + 8) * U32 * big
+        return e + 16 * U32 * np.minimum(cap, big)
+
+    paged_within(out, q, k, v, table, pos, error, 2.0 ** -10, window=window, slopes=slopes, cap=cap)
