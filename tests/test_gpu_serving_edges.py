@@ -194,3 +194,46 @@ def test_caps_of_every_size(dtype, D, cap, bias, window):
         return e + 16 * U32 * np.minimum(cap, big)
 
     paged_within(out, q, k, v, table, pos, error, 2.0 ** -10, window=window, slopes=slopes, cap=cap)
+
+
+# ----------------------------------------------------------------------------------------------------------
+# Batches of more tokens than a wave looks through at once (512)
+# ----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("N", [511, 512, 513, 1024, 1025, 1300, 2049])
+@pytest.mark.parametrize("D,Hq,Hk", [(64, 4, 1), (128, 8, 4), (72, 6, 6)])
+@pytest.mark.parametrize("numbered", [False, True])
+def test_long_batches(dtype, N, D, Hq, Hk, numbered):
+    """Shares of a group that begin in every block of 512 tokens, tokens that see nothing on both sides of their borders, more
+    tokens than groups and fewer."""
+    g = gen(47, N, D, numbered)
+    page, per = 8, 14
+    k, v, table = cache(g, N, per, page, Hk, D, dtype)
+    pos = (torch.rand((N,), generator=g) ** 2 * per * page).to(torch.int32)
+    pos[::11] = -1
+    for border in range(512, N + 1, 512):
+        pos[border - 9:border + 14] = -3
+        pos[border - 2:border] = per * page - 1
+    pos[N - 1] = 77
+    seq = torch.randperm(N, generator=g).to(torch.int32).cuda() if numbered else None
+    q, pos = randn(g, (N, Hq, D), dtype), pos.cuda()
+    out = run_paged(q, k, v, table, pos, seq=seq)
+    paged_within(out, q, k, v, table, pos, lambda big: (D + 8) * U32 * big, 2.0 ** -10, seq=seq, heads=[0, Hq - 1])
+    assert (out[pos < 0] == 0).all() and out.isfinite().all()
+
+
+@pytest.mark.parametrize("N", [600, 1500])
+def test_long_batches_with_one_long_cache(N):
+    """The keys of nearly all groups are one token's, in the first, the second and the last block."""
+    g = gen(48, N)
+    D, page, per, Hq, Hk = 64, 16, 600, 4, 2
+    k, v, _ = cache(g, 1, per, page, Hk, D, BF)
+    table = torch.stack([torch.randperm(per, generator=g) for _ in range(4)]).to(torch.int32).cuda()
+    seq = torch.randint(0, 4, (N,), generator=g).to(torch.int32).cuda()
+    for at in (3, 513, N - 1):
+        pos = (torch.rand((N,), generator=g) * 20).to(torch.int32) - 2
+        pos[at] = per * page - 1
+        q, pos = randn(g, (N, Hq, D), BF), pos.cuda()
+        out = run_paged(q, k, v, table, pos, seq=seq)
+        paged_within(out, q, k, v, table, pos, lambda big: (D + 8) * U32 * big, 2.0 ** -10, seq=seq, heads=[0, 3])
