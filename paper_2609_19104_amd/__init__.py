@@ -175,7 +175,13 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+def _no_gpu(*_) -> int:
+    raise RuntimeError("this build of torch has no GPU support")
+
+
+# (A torch without a GPU has neither; what needs none, such as workspace sizes, works there.)
+_current_device = getattr(torch._C, "_cuda_getDevice", _no_gpu)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _no_gpu)
 
 
 def _stream(stream) -> Optional[int]:
