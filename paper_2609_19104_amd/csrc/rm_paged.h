@@ -5,9 +5,9 @@
 // few query heads of a key head: every byte of the cache is read once, and reading is what bounds it.  What that took, us for
 // 64 tokens of 32 heads on 8 on up to 8192 keys (1.18 GB) / 4 of 32 on 4 on 131072 (1.06 GB), bf16, heads of 128 columns:
 // a workgroup a query head 4998 / 67790; the kernel below with a wave a share of (token, head, key) 248 / 209; loads past the
-// caches' other lines 191 / 180; waves of a group on the same rows at the same time, and what else is told below, 189 / 172:
-// 6.3 and 6.2 TB/s (a read of one large buffer: 5.9).  Smaller calls are bound by round trips: launch, positions, table,
-// keys, the parts' join: one token on 850 keys 11.3, on 8192 14.5.
+// caches' other lines 191 / 180; waves of a group on the same rows at the same time, and what else is told below, 189 / 173:
+// 6.2 and 6.1 TB/s (a read of one large buffer: 5.9).  Smaller calls are bound by round trips: launch, positions, table,
+// keys, the parts' join: one token on 850 keys 11.3, on 8192 14.7.
 #pragma once
 
 #include <algorithm>
@@ -90,8 +90,9 @@ __device__ __forceinline__ void dma4(const void *g, uint32_t lds) {
 // Matrix-core layout (16x16 tiles): S^T = K Q^T, so a lane holds scores of query head lane % 16, keys 4 (lane / 16) + {0..3} of
 // 16; O^T = V^T P^T takes them as they are, V's fragments read in the same order of keys.  A group of 8 heads fills half of
 // a tile, which costs nothing in bf16 (the products take a sixth of the time that a tile's bytes do); in float32 they are a third
-// of a step of 2.1 us, and issuing the loads half of it (37 tokens of 6 heads on 3, 72 columns, up to 1111 keys each: 24 us
-// for 63 MB).  Fragments of QR = 8 heads are kept in half the LDS, so that four waves fit.
+// of a step of 2.1 us, and issuing the loads half of it (37 tokens of 6 heads on 3, 72 columns, up to 1111 keys each: 25 us
+// for 63 MB; a row has room for 128 columns in LDS, so that 14 of its 32 lanes fetch the last 16 bytes again).  Fragments of
+// QR = 8 heads are kept in half the LDS, so that four waves fit.
 
 // The value, as if it became known here only: what is made of it then stays where it is used, instead of taking registers
 // and time in front of the loop.

@@ -32,8 +32,9 @@ rm_status check_pages(int page, int n_pages, int max_pages) {
     return RM_OK;
 }
 
-// Up to this many tiles one group has them all and no join follows (one token on 128 keys of 64 columns 6.2 us, in three groups
-// 8.6).  Above, a tile a group pays (one token on 1024 keys, 8 heads of 64 columns: a tile each 8.2, two each 10.4, four 14).
+// Up to this many tiles one group has them all and no join follows (one token on 128 keys, 8 heads of 64 columns on 1, 6.2 us
+// in a graph, in three groups 8.6).  Above, a tile a group pays (one token on 1024 keys, 8 heads of 64 columns on 8: a tile each
+// 8.2, two each 10.4, four 14).  All before the weights' second part, which adds 0.1 to 0.2.
 constexpr int64_t kOneGroup = 4;
 
 rm_status paged_plan(const rm_attn_shape *s, int n_tok, int page, int max_pages, rm_serve::PagedPlan *p) {

@@ -1,9 +1,10 @@
-"""GPU tests of the serving-step calls where their bounds are tight: weights of bf16 attention to 2^-15.
+"""GPU tests of the serving-step calls where their bounds are tight: weights of bf16 attention, biases far from their zero, caps
+of every size, batches past 512 tokens; and block norms past one launch.
 
 Bound (u32 = 2^-24, u = the output type's half step): as in test_gpu_serving.py, with the weights in two bf16 parts: the
 first by truncation, which leaves a rest below 2^-7 of the weight, the second the rest rounded by at most 2^-8 of it, so a
 weight is off by 2^-15.  A bound is worth its name while it leaves little beside the output's own rounding: of every case the
-rest is at most `spare` of the softmax average of |v|."""
+rest is at most `spare` of the softmax average of |v|, and most values are four bounds from 0 or more."""
 import numpy as np
 import pytest
 import torch
