@@ -523,9 +523,9 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             each([&](float x, int, int) { return a.cap * (BF ? rm_attn::tanh_relative(x * a.scale) : tanhf(x * a.scale)); });
         // A bias is counted from the key that a token may see where it is highest (the last one, for a negative slope the first):
         // the same weights, and a position far behind the table costs them no digits.  Slope times distance may still be far
-        // larger than what tells the weights apart, so it is rounded only after `off` is taken from it, about what it is here:
-        // the running maximum, or for a token's first tile the bias of its first key.  (Beyond 2^24 the maximum's own rounding
-        // would count; there the nearest key has the weight.)
+        // larger than what tells the weights apart, so it is rounded only after `off` is taken from it, about what it is where
+        // it counts: the running maximum, or the highest bias of the tile, if that is more (a token's first tile, or the first
+        // after missing pages).  Beyond 2^24 the maximum's own rounding would count; there the nearest key has the weight.
         float off[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) off[r] = 0.0f;
@@ -534,8 +534,10 @@ __global__ __launch_bounds__(64, 1) void paged_kernel(PagedArgs a) {
             int from[RT];  // distance of the tile's first key
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                from[r] = (slope[r] < 0.0f ? cur.lo : cur.end - 1) - cur.t * KT;
-                const float about = m[r] == -INFINITY ? -slope[r] * static_cast<float>(from[r]) : m[r];
+                const bool rises = slope[r] < 0.0f;  // (with the distance)
+                from[r] = (rises ? cur.lo : cur.end - 1) - cur.t * KT;
+                const int nearest = rises ? min(from[r], 0) : max(from[r] - (KT - 1), 0);
+                const float about = fmaxf(m[r], -slope[r] * static_cast<float>(nearest));
                 off[r] = fabsf(about) < 0x1p24f ? about : 0.0f;
             }
             const int own = 4 * here(h4);

@@ -145,6 +145,39 @@ def test_bias_where_the_nearest_pages_are_none(dtype, slope):
     paged_within(out, q, k, v, table, pos, biased_error(D), 2.0 ** -10, slopes=slopes, counted=1000)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("slope,D", [(0.5, 64), (-0.5, 128), (0.07, 256), (12.0, 64)])
+def test_bias_on_both_sides_of_missing_pages(dtype, slope, D):
+    """The first pages and the last ones are kept, those between are none: the running maximum of one side says nothing of the
+    other."""
+    g = gen(49, D, slope > 0)
+    N, Hq, Hk, page, per = 2, 4, 2, 64, 3000
+    k, v, _ = cache(g, 1, 40, page, Hk, D, dtype)
+    table = torch.full((N, per), -1, dtype=torch.int32)
+    kept = torch.randperm(40, generator=g).view(2, 20).to(torch.int32)
+    table[:, :3], table[:, 1400], table[:, per - 9:] = kept[:, :3], kept[:, 3], kept[:, 4:13]
+    table, q, pos = table.cuda(), randn(g, (N, Hq, D), dtype), ints([per * page - 1, per * page - 77])
+    slopes = torch.full((Hq,), slope, device="cuda")
+    out = run_paged(q, k, v, table, pos, slopes=slopes)
+    paged_within(out, q, k, v, table, pos, biased_error(D), 2.0 ** -10, slopes=slopes, counted=1000)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("reach", [1.0, 0.05])
+def test_one_wave_on_both_sides_of_missing_pages(dtype, reach):
+    """So many heads that a wave has all keys of its head, from the first pages over the gap to the last few keys, one tile."""
+    g = gen(50, int(reach * 100))
+    H, D, page, per = 600, 8, 64, 3000
+    k, v, _ = cache(g, 1, 20, page, H, D, dtype)
+    table = torch.full((2, per), -1, dtype=torch.int32)
+    table[:, :3], table[:, 1400], table[:, per - 1] = torch.arange(3), 3, torch.arange(4, 6)
+    table, q, pos = table.cuda(), randn(g, (2, H, D), dtype), ints([per * page - 40, per * page - 61])
+    assert rm.paged_attention_workspace(q, k, table).numel() == 0  # no head is divided
+    slopes = (reach * torch.tensor([0.5, -0.5, 0.31, -4.0, 12.0, 1.7])).repeat(100).cuda()
+    out = run_paged(q, k, v, table, pos, slopes=slopes)
+    paged_within(out, q, k, v, table, pos, biased_error(D), 2.0 ** -10, slopes=slopes, heads=list(range(12)), counted=1000)
+
+
 def test_negative_slopes_past_2_24_keys():
     """Distances that float32 does not hold, on a table that names a few pages over and over."""
     g = gen(44)
